@@ -1,0 +1,60 @@
+/*
+ * fnn_net.h -- the operators of the network that ends in the maps of fnn.h, on one AMD Instinct MI355X (gfx950).
+ *
+ * The Speedy MASt3R paper (arXiv 2503.10017) speeds up the matching (fnn.h) and the network before it: attention that
+ * never writes the score matrix ("FlashMatch", section 3.4.1) and layers fused with what follows them ("GraphFusion", section
+ * 3.4.2).  This header has the operators of a pre-norm transformer block over image tokens and of the matching head (section
+ * 3.2.4: layers that end in one descriptor per pixel), with their gradients:
+ *
+ *   fnn_layer_norm   y = (x - mean) / sqrt(var + eps) * weight + bias          and fnn_layer_norm_backward
+ *   fnn_linear       y = act(x w^T + bias) + residual                         and fnn_linear_backward
+ *   fnn_attention    softmax(scale q k^T) v over packed sequences             and fnn_attention_backward
+ *
+ * Conventions: those of fnn.h (status codes; device pointers; caller-owned buffers and workspaces, the latter 256-byte
+ * aligned; asynchronous on `stream`; argument errors before anything is enqueued; capturable in a HIP graph; no state between calls), and
+ *  - A matrix is an fnn_map: n rows of d elements, row_stride >= d elements apart (the stride of fewer than two rows is not looked at);
+ *    outputs are passed the same way and written through `data`.  Rows may start anywhere that their element type may (2 or 4 bytes);
+ *    rows on 16-byte boundaries are faster.  A matrix of no elements needs no pointer.  Elements between the rows are neither read for
+ *    their value nor written.  All matrices of a call have one dtype, unless said otherwise.
+ *  - Outputs must not overlap inputs or each other; the exceptions are named.
+ *  - Results do not depend on the order in which workgroups run: the same call gives the same bits.
+ *  - Sums, products, statistics and activations are fp32; outputs are rounded once, to nearest even, to their type.  Infinities and NaN in the inputs
+ *    reach the outputs that depend on them, and no others.
+ */
+#ifndef FNN_NET_H
+#define FNN_NET_H
+
+#include "fnn.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define FNN_MAX_NORM_WIDTH 16384
+
+/*
+ * Layer norm over the rows of x (n rows of d <= FNN_MAX_NORM_WIDTH elements, any dtype):
+ *   mean = sum_k x[k] / d,  rstd = 1 / sqrt(sum_k (x[k] - mean)^2 / d + eps),  y[k] = (x[k] - mean) * rstd * weight[k] + bias[k]
+ * weight and bias (device, d elements of weight_dtype, which is x's dtype or FNN_F32) may each be NULL: 1 and 0.
+ * mean and rstd (device float[n]) may be NULL; the gradient takes them.  y may be x itself (same rows).  No workspace.
+ * Errors: FNN_E_NULL, FNN_E_SHAPE (n > 2^31 - 64, d < 1 or too large, strides, x and y of different size), FNN_E_DTYPE, FNN_E_RANGE (eps
+ * negative or not a number).
+ */
+int32_t fnn_layer_norm(const fnn_map* x, const void* weight, const void* bias, int32_t weight_dtype, float eps,
+                       const fnn_map* y, float* mean, float* rstd, void* stream);
+
+/*
+ * Its gradient.  With h = (x - mean) * rstd and g = dy * weight:
+ *   dx = rstd * (g - sum_k g / d - h * sum_k (g h) / d),  dweight = sum over the rows of dy * h,  dbias = sum over the rows of dy
+ * mean and rstd are those of fnn_layer_norm.  dx, dweight and dbias (the latter two of weight_dtype, d elements) may each be
+ * NULL: not wanted.  dx may be dy or x itself (same rows).
+ */
+size_t fnn_layer_norm_backward_workspace_bytes(int64_t n, int32_t d);
+int32_t fnn_layer_norm_backward(const fnn_map* dy, const fnn_map* x, const float* mean, const float* rstd, const void* weight,
+                                int32_t weight_dtype, const fnn_map* dx, void* dweight, void* dbias,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* FNN_NET_H */

@@ -1,7 +1,7 @@
 """MI355X-native fast reciprocal nearest-neighbour matching (the FastNN stage of Speedy MASt3R).
 
-The work is done by hand-written HIP kernels behind the C ABI in ``include/fnn.h``
-(``lib/libfnn.so``); this package only marshals torch tensors into that ABI.  There is
+The work is done by hand-written HIP kernels behind the C ABI in ``include/fnn.h`` and, for the operators of the network
+before the matching, ``include/fnn_net.h`` (``lib/libfnn.so``); this package only marshals torch tensors into that ABI.  There is
 no CPU or eager fallback: calls raise if the library is missing.
 """
 from . import binding  # noqa: F401
@@ -24,4 +24,9 @@ from .binding import (  # noqa: F401
     fnn_workspace_bytes_opts,
     library_path,
     load_library,
+)
+from .net import (  # noqa: F401
+    fnn_layer_norm,
+    fnn_layer_norm_backward,
+    fnn_layer_norm_backward_workspace_bytes,
 )

@@ -81,6 +81,12 @@ def load_library():
     lib.fnn_trace_kind_name.argtypes = [i32]
     lib.fnn_measure_ceiling.restype = i32
     lib.fnn_measure_ceiling.argtypes = [i32, i32, vp, sz, vp, vp]
+    lib.fnn_layer_norm.restype = i32
+    lib.fnn_layer_norm.argtypes = [vp, vp, vp, i32, ctypes.c_float, vp, vp, vp, vp]
+    lib.fnn_layer_norm_backward_workspace_bytes.restype = sz
+    lib.fnn_layer_norm_backward_workspace_bytes.argtypes = [i64, i32]
+    lib.fnn_layer_norm_backward.restype = i32
+    lib.fnn_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 

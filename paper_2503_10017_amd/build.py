@@ -11,19 +11,23 @@ LIB_DIR = os.path.join(_HERE, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libfnn.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
 
-SOURCES = ["prep.hip", "search.hip", "coarse.hip", "recip.hip", "walk.hip", "tail.hip", "dense.hip", "dense_coarse.hip", "blocked.hip", "pixels.hip", "api.hip", "trace.hip", "ceiling.hip"]
+SOURCES = ["prep.hip", "search.hip", "coarse.hip", "recip.hip", "walk.hip", "tail.hip", "dense.hip", "dense_coarse.hip", "blocked.hip", "pixels.hip", "api.hip", "trace.hip", "ceiling.hip",
+           "layer_norm.hip", "net_api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    "-fno-honor-nans",  # inputs are finite by contract; keeps max/compare chains free of NaN quieting
     "-Wno-unused-command-line-argument",
 ]
+# The matching path: inputs are finite by contract; keeps max/compare chains free of NaN quieting.
+MATCHING_FLAGS = ["-fno-honor-nans"]
+# The network's operators carry infinities and NaN from the inputs to the outputs that depend on them.
+NETWORK_SOURCES = {"layer_norm.hip", "net_api.hip"}
 
 
 def _compile(src: str) -> str:
     obj = os.path.join(OBJ_DIR, os.path.splitext(src)[0] + ".o")
-    cmd = ["hipcc", *HIPCC_FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = ["hipcc", *HIPCC_FLAGS, *([] if src in NETWORK_SOURCES else MATCHING_FLAGS), "-c", os.path.join(CSRC, src), "-o", obj]
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{res.stdout}\n{res.stderr}")

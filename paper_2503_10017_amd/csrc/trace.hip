@@ -104,6 +104,12 @@ const char* fnn_trace_kind_name(int32_t kind) {
         case TK_DENSE_SAMPLE: return "dense_sample_kernel";
         case TK_DENSE_ALIKE: return "dense_alike_kernel";
         case TK_RECIP_TAIL: return "recip_tail_kernel";
+        case TK_LAYER_NORM: return "layer_norm_kernel";
+        case TK_LAYER_NORM_BACKWARD: return "layer_norm_backward_kernels";
+        case TK_LINEAR: return "linear_kernels";
+        case TK_LINEAR_BACKWARD: return "linear_backward_kernels";
+        case TK_ATTENTION: return "attention_kernels";
+        case TK_ATTENTION_BACKWARD: return "attention_backward_kernels";
         default: return "unknown";
     }
 }

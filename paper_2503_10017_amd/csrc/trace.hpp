@@ -30,7 +30,13 @@ enum TraceKind : int {
     TK_DENSE_SAMPLE = 19,
     TK_DENSE_ALIKE = 20,
     TK_RECIP_TAIL = 21,
-    TK_COUNT = 22
+    TK_LAYER_NORM = 22,
+    TK_LAYER_NORM_BACKWARD = 23,
+    TK_LINEAR = 24,
+    TK_LINEAR_BACKWARD = 25,
+    TK_ATTENTION = 26,
+    TK_ATTENTION_BACKWARD = 27,
+    TK_COUNT = 28
 };
 
 // Returns false when no trace is open or it is full; otherwise hands out the next event pair.

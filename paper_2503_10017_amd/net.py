@@ -1,0 +1,96 @@
+"""ctypes binding of the network's operators in libfnn.so (include/fnn_net.h): argument marshalling only.
+
+Every function has the name and meaning of the C entry point it wraps; torch supplies device memory and the current stream.
+Tensors are taken with the strides that they have, as long as the elements of a row are contiguous.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from .binding import _DTYPES, FnnError, _pack_map, _ptr, _stream_ptr, _workspace, load_library
+
+
+def _matrix(t: Optional[torch.Tensor], what: str):
+    """A struct fnn_map of a 2-D device tensor (None: NULL)."""
+    if t is None:
+        return None
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what} must be a 2-D device tensor")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {t.dtype} of {what}")
+    n, d = t.shape
+    row_stride, element_stride = t.stride()
+    if d > 1 and element_stride != 1:
+        raise ValueError(f"the rows of {what} must be contiguous")
+    return _pack_map(t.data_ptr(), n, d, _DTYPES[t.dtype], row_stride if n > 1 else max(d, row_stride))
+
+
+def _vector(t: Optional[torch.Tensor], count: int, dtype, what: str):
+    """The address of a contiguous device tensor of `count` elements of `dtype` (None: NULL)."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous device tensor of {count} elements")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be of {dtype}")
+    return t.data_ptr()
+
+
+def _check(status: int, where: str):
+    if status != 0:
+        raise FnnError(status, where)
+
+
+def _weight_dtype(x, weight, bias):
+    of = weight if weight is not None else bias
+    return x.dtype if of is None else of.dtype
+
+
+def fnn_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   out: Optional[torch.Tensor] = None, want_stats: bool = False, stream=None):
+    """Layer norm over the rows of x [n][d]; weight and bias [d] of x's dtype or fp32.  Returns (y, mean, rstd), the latter two
+    float32 [n] for the gradient, or None without ``want_stats``."""
+    lib = load_library()
+    xm = _matrix(x, "x")
+    n, d = x.shape
+    wt = _weight_dtype(x, weight, bias)
+    if out is None:
+        out = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    mean = rstd = None
+    if want_stats:
+        mean = torch.empty(n, dtype=torch.float32, device=x.device)
+        rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    _check(lib.fnn_layer_norm(xm, _vector(weight, d, wt, "weight"), _vector(bias, d, wt, "bias"), _DTYPES.get(wt, -1), eps,
+                              _matrix(out, "out"), _ptr(mean), _ptr(rstd), _stream_ptr(stream, x.device)), "fnn_layer_norm")
+    return out, mean, rstd
+
+
+def fnn_layer_norm_backward_workspace_bytes(n: int, d: int) -> int:
+    return int(load_library().fnn_layer_norm_backward_workspace_bytes(n, d))
+
+
+def fnn_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                            weight: Optional[torch.Tensor] = None, want_x: bool = True, want_weight: bool = True,
+                            out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradient of fnn_layer_norm; returns (dx, dweight, dbias), the latter two of weight's dtype (x's without a weight), None
+    where not wanted."""
+    lib = load_library()
+    n, d = x.shape
+    wt = x.dtype if weight is None else weight.dtype
+    dx = out
+    if dx is None and want_x:
+        dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
+    dweight = dbias = None
+    if want_weight:
+        dweight = torch.empty(d, dtype=wt, device=x.device)
+        dbias = torch.empty(d, dtype=wt, device=x.device)
+        if workspace is None:
+            workspace = _workspace(lib.fnn_layer_norm_backward_workspace_bytes(n, d), x.device)
+    _check(lib.fnn_layer_norm_backward(_matrix(dy, "dy"), _matrix(x, "x"), _vector(mean, n, torch.float32, "mean"),
+                                       _vector(rstd, n, torch.float32, "rstd"), _vector(weight, d, wt, "weight"),
+                                       _DTYPES.get(wt, -1), _matrix(dx, "dx"), _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                       0 if workspace is None else workspace.numel(), _stream_ptr(stream, x.device)),
+           "fnn_layer_norm_backward")
+    return dx, dweight, dbias

@@ -1,0 +1,63 @@
+"""Host-only checks of the network operators' C ABI: fnn_net.h's functions are exported and bad arguments are refused before
+the device is touched (no GPU needed)."""
+import math
+import os
+import subprocess
+
+import pytest
+
+import paper_2503_10017_amd as fnn
+from paper_2503_10017_amd import binding
+from test_abi import ROOT, declared_functions, lib  # noqa: F401
+
+OK, NULL, SHAPE, DTYPE, RANGE, WORKSPACE, HIP, UNSUPPORTED = range(8)
+
+
+def matrix(n=4, d=64, dtype=1, stride=None, data=0x10000):
+    return binding._pack_map(data, n, d, dtype, d if stride is None else stride)
+
+
+def test_every_declared_symbol_is_exported(lib):  # noqa: F811
+    names = set(declared_functions("fnn_net.h"))
+    assert {"fnn_layer_norm", "fnn_layer_norm_backward", "fnn_layer_norm_backward_workspace_bytes"} <= names
+    for name in names:
+        assert hasattr(lib, name) and hasattr(fnn, name), name
+
+
+def test_header_is_plain_c(tmp_path):
+    source = tmp_path / "use.c"
+    source.write_text('#include "fnn_net.h"\nint main(void) { return 0; }\n')
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-I", os.path.join(ROOT, "include"), "-c", str(source), "-o", str(tmp_path / "use.o")], check=True)
+
+
+def test_layer_norm_refusals(lib):  # noqa: F811
+    def call(x=matrix(), y=matrix(data=0x20000), weight=0x3000, bias=0x4000, weight_dtype=1, eps=1e-6):
+        return lib.fnn_layer_norm(x, weight, bias, weight_dtype, eps, y, None, None, None)
+
+    assert call(x=None) == NULL and call(y=None) == NULL
+    assert call(x=matrix(data=0)) == NULL and call(y=matrix(data=0)) == NULL
+    for bad in (matrix(n=-1), matrix(n=2 ** 31), matrix(d=0), matrix(d=-4, stride=64), matrix(d=16385), matrix(stride=63), matrix(stride=2 ** 62), matrix(n=5), matrix(d=32)):
+        assert call(x=bad) == SHAPE and call(y=bad) == SHAPE
+    assert call(x=matrix(dtype=3)) == DTYPE and call(y=matrix(dtype=2)) == DTYPE
+    assert call(weight_dtype=2) == DTYPE and call(weight_dtype=7) == DTYPE
+    for eps in (-1e-9, math.nan, math.inf):
+        assert call(eps=eps) == RANGE
+    assert call(x=matrix(n=0, data=0), y=matrix(n=0, data=0)) == OK
+    assert call(x=matrix(n=0, data=0, stride=0), y=matrix(n=0, data=0)) == OK
+
+
+def test_layer_norm_backward_refusals(lib):  # noqa: F811
+    need = fnn.fnn_layer_norm_backward_workspace_bytes(4, 64)
+    assert need > 0
+    for n, d in ((-1, 64), (4, 0), (4, 16385), (2 ** 31, 8)):
+        assert fnn.fnn_layer_norm_backward_workspace_bytes(n, d) == 0
+
+    def call(dy=matrix(), x=matrix(), mean=0x5000, rstd=0x6000, weight_dtype=1, dx=matrix(data=0x20000), dweight=0x7000, ws=0x100000, ws_bytes=need):
+        return lib.fnn_layer_norm_backward(dy, x, mean, rstd, 0x3000, weight_dtype, dx, dweight, None, ws, ws_bytes, None)
+
+    assert call(dy=None) == NULL and call(x=None) == NULL and call(mean=None) == NULL and call(rstd=None) == NULL
+    for bad in (matrix(n=3), matrix(d=32), matrix(stride=1)):
+        assert call(dy=bad) == SHAPE and call(x=bad) == SHAPE and call(dx=bad) == SHAPE
+    assert call(dy=matrix(dtype=0)) == DTYPE and call(dx=matrix(dtype=2)) == DTYPE and call(weight_dtype=2) == DTYPE
+    assert call(ws=None) == WORKSPACE and call(ws=0x100010) == WORKSPACE and call(ws_bytes=need - 1) == WORKSPACE
+    assert call(dx=None, dweight=None) == OK     # nothing wanted
