@@ -54,6 +54,39 @@ int32_t fnn_layer_norm_backward(const fnn_map* dy, const fnn_map* x, const float
                                 int32_t weight_dtype, const fnn_map* dx, void* dweight, void* dbias,
                                 void* workspace, size_t workspace_bytes, void* stream);
 
+/* Activations of fnn_linear. */
+typedef enum {
+    FNN_ACT_NONE = 0,
+    FNN_ACT_RELU = 1,  /* max(p, 0) */
+    FNN_ACT_GELU = 2,  /* p Phi(p), Phi the integral of the normal density */
+    FNN_ACT_SILU = 3   /* p / (1 + exp(-p)) */
+} fnn_act;
+
+/*
+ * A linear layer: p = x w^T + bias, y = act(p) + residual, for x [rows][inner], w [outer][inner], y, pre and residual
+ * [rows][outer] and bias [outer], all of one dtype.  bias, residual and pre may be NULL; pre receives p, which the gradient
+ * takes.  Sizes of 0 are fine (inner == 0: p = bias).  16-bit types multiply on the 16-bit matrix instructions, FNN_F32 on the
+ * fp32 ones; sums are fp32.  y may be the residual itself (same rows).
+ * The workspace is for few tiles with a long `inner`, whose products are split and joined in a fixed order;
+ * fnn_linear_workspace_bytes may return 0, and returns 0 for invalid sizes.
+ * Errors: FNN_E_NULL, FNN_E_SHAPE, FNN_E_DTYPE, FNN_E_RANGE (act), FNN_E_WORKSPACE.
+ */
+size_t fnn_linear_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype);
+int32_t fnn_linear(const fnn_map* x, const fnn_map* w, const void* bias, int32_t act, const fnn_map* residual,
+                   const fnn_map* y, const fnn_map* pre, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Its gradient.  With q = dy * act'(pre) (act == FNN_ACT_NONE: q = dy, and pre is not looked at):
+ *   dx = q w,  dw = q^T x,  dbias = sum over the rows of q
+ * dx [rows][inner], dw [outer][inner] and dbias [outer] are of x's dtype and may each be NULL: not wanted.  The residual's gradient is dy itself.
+ * In 16-bit types q is rounded to that type before the products, as their matrix instructions take it; dbias sums the
+ * unrounded values.  FNN_ACT_RELU's slope at 0 is 0.
+ */
+size_t fnn_linear_backward_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t act);
+int32_t fnn_linear_backward(const fnn_map* dy, const fnn_map* x, const fnn_map* w, const fnn_map* pre, int32_t act,
+                            const fnn_map* dx, const fnn_map* dw, void* dbias, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
 #ifdef __cplusplus
 }
 #endif

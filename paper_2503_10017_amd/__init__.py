@@ -29,4 +29,8 @@ from .net import (  # noqa: F401
     fnn_layer_norm,
     fnn_layer_norm_backward,
     fnn_layer_norm_backward_workspace_bytes,
+    fnn_linear,
+    fnn_linear_backward,
+    fnn_linear_backward_workspace_bytes,
+    fnn_linear_workspace_bytes,
 )

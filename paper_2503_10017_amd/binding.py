@@ -87,6 +87,14 @@ def load_library():
     lib.fnn_layer_norm_backward_workspace_bytes.argtypes = [i64, i32]
     lib.fnn_layer_norm_backward.restype = i32
     lib.fnn_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.fnn_linear_workspace_bytes.restype = sz
+    lib.fnn_linear_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.fnn_linear.restype = i32
+    lib.fnn_linear.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.fnn_linear_backward_workspace_bytes.restype = sz
+    lib.fnn_linear_backward_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    lib.fnn_linear_backward.restype = i32
+    lib.fnn_linear_backward.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 

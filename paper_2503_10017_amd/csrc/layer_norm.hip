@@ -187,24 +187,6 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_kerne
     }
 }
 
-// The columns' sums over the workgroups: 32 columns a workgroup, 32 threads over the partial rows of each.
-template <int WT>
-__global__ __launch_bounds__(1024) void layer_norm_columns_kernel(const float* partial, int64_t groups, int32_t d, void* dweight, void* dbias) {
-    typedef typename Elem<WT>::T W;
-    __shared__ float part[32][33];
-    const int column = blockIdx.x * 32 + (threadIdx.x & 31), strand = threadIdx.x >> 5;
-    float sum = 0.f;
-    if (column < 2 * d)
-        for (int64_t g = strand; g < groups; g += 32) sum += partial[g * 2 * d + column];
-    part[strand][threadIdx.x & 31] = sum;
-    __syncthreads();
-    if (strand == 0 && column < 2 * d) {
-        for (int i = 1; i < 32; ++i) sum += part[i][threadIdx.x];
-        W* out = (W*)(column < d ? dweight : dbias);
-        if (out) out[column < d ? column : column - d] = (W)sum;
-    }
-}
-
 // Calls f(LANES, CHUNKS) with the narrowest shape that holds a row of d elements: one wave a row as long as its registers do.
 template <int DT, typename F>
 hipError_t with_shape(int d, F f) {
@@ -265,8 +247,7 @@ hipError_t launch_layer_norm_backward(const NormBackArgs& a, int dtype, int weig
                           dim3((unsigned)groups), dim3(norm_threads(lanes.value)), 0, s, a);
         });
         if (e != hipSuccess || !a.partial) return e;
-        return launch(TK_LAYER_NORM_BACKWARD, layer_norm_columns_kernel<wt.value>, dim3((unsigned)((2 * a.d + 31) / 32)), dim3(1024), 0, s,
-                      (const float*)a.partial, groups, a.d, a.dweight, a.dbias);
+        return launch_column_sums(a.partial, groups, 2 * (int64_t)a.d, a.d, a.dweight, a.dbias, weight_dtype, TK_LAYER_NORM_BACKWARD, s);
     });
 }
 

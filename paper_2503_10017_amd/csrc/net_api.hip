@@ -6,6 +6,7 @@
 
 #include "fnn_kernels.hpp"
 #include "net_kernels.hpp"
+#include "trace.hpp"
 
 using namespace fnn;
 
@@ -34,6 +35,34 @@ int32_t done(hipError_t e) { return e == hipSuccess ? FNN_OK : FNN_E_HIP; }
         const int32_t status_ = (call);       \
         if (status_ != FNN_OK) return status_; \
     } while (0)
+
+size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Sizes that the linear layers take: every dimension an int32, so that tiles and columns are.
+bool linear_sizes(int64_t rows, int64_t inner, int64_t outer) {
+    return rows >= 0 && rows <= MAX_SLOTS && inner >= 0 && inner <= MAX_SLOTS && outer >= 0 && outer <= MAX_SLOTS;
+}
+bool same_shape(const fnn_map* m, int64_t n, int64_t d) { return m->n == n && m->d == d; }
+
+// The workspace of the linear gradient: q, the shares of dbias, and one area that the two products use in turn.
+struct LinearBackLayout {
+    size_t q, sums, partial, total;  // offsets
+    int64_t q_stride;
+};
+LinearBackLayout linear_back_layout(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t act) {
+    LinearBackLayout L;
+    const size_t es = dtype == FNN_F32 ? 4 : 2;
+    L.q_stride = (outer + 7) / 8 * 8;
+    size_t at = 0;
+    L.q = at;
+    if (act != FNN_ACT_NONE) at += aligned((size_t)rows * L.q_stride * es);
+    L.sums = at;
+    at += aligned((size_t)slope_strips(rows, outer) * outer * sizeof(float));
+    L.partial = at;
+    const size_t x = gemm_workspace(rows, inner, outer, dtype, 0, 1), w = gemm_workspace(outer, inner, rows, dtype, 1, 1);
+    L.total = at + aligned(x > w ? x : w);
+    return L;
+}
 
 }  // namespace
 
@@ -102,6 +131,124 @@ int32_t fnn_layer_norm_backward(const fnn_map* dy, const fnn_map* x, const float
     a.dx_stride = dx ? stride_of(dx) : 0;
     a.d = x->d;
     return done(launch_layer_norm_backward(a, x->dtype, weight_dtype, (hipStream_t)stream));
+}
+
+size_t fnn_linear_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
+    if (!linear_sizes(rows, inner, outer) || !valid_type(dtype)) return 0;
+    return gemm_workspace(rows, outer, inner, dtype, 0, 0);
+}
+
+int32_t fnn_linear(const fnn_map* x, const fnn_map* w, const void* bias, int32_t act, const fnn_map* residual,
+                   const fnn_map* y, const fnn_map* pre, void* workspace, size_t workspace_bytes, void* stream) {
+    FNN_CHECK(check_matrix(x));
+    FNN_CHECK(check_matrix(w));
+    FNN_CHECK(check_matrix(y));
+    if (residual) FNN_CHECK(check_matrix(residual));
+    if (pre) FNN_CHECK(check_matrix(pre));
+    const int64_t rows = x->n, inner = x->d, outer = w->n;
+    if (w->d != inner || !same_shape(y, rows, outer) || (residual && !same_shape(residual, rows, outer)) || (pre && !same_shape(pre, rows, outer)))
+        return FNN_E_SHAPE;
+    if (w->dtype != x->dtype || y->dtype != x->dtype || (residual && residual->dtype != x->dtype) || (pre && pre->dtype != x->dtype))
+        return FNN_E_DTYPE;
+    if (act < FNN_ACT_NONE || act > FNN_ACT_SILU) return FNN_E_RANGE;
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, fnn_linear_workspace_bytes(rows, inner, outer, x->dtype)));
+    GemmArgs a;
+    memset(&a, 0, sizeof(a));
+    a.a = x->data;
+    a.b = w->data;
+    a.lda = stride_of(x);
+    a.ldb = stride_of(w);
+    a.m = rows;
+    a.n = (int32_t)outer;
+    a.k = (int32_t)inner;
+    a.y = const_cast<void*>(y->data);
+    a.bias = bias;
+    a.residual = residual ? residual->data : nullptr;
+    a.pre = pre ? const_cast<void*>(pre->data) : nullptr;
+    a.ldy = stride_of(y);
+    a.ldr = residual ? stride_of(residual) : 0;
+    a.ldp = pre ? stride_of(pre) : 0;
+    a.act = act;
+    a.partial = (float*)workspace;
+    return done(launch_gemm(a, x->dtype, 0, 0, TK_LINEAR, (hipStream_t)stream));
+}
+
+size_t fnn_linear_backward_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t act) {
+    if (!linear_sizes(rows, inner, outer) || !valid_type(dtype) || act < FNN_ACT_NONE || act > FNN_ACT_SILU) return 0;
+    return linear_back_layout(rows, inner, outer, dtype, act).total;
+}
+
+int32_t fnn_linear_backward(const fnn_map* dy, const fnn_map* x, const fnn_map* w, const fnn_map* pre, int32_t act,
+                            const fnn_map* dx, const fnn_map* dw, void* dbias, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+    FNN_CHECK(check_matrix(dy));
+    FNN_CHECK(check_matrix(x));
+    FNN_CHECK(check_matrix(w));
+    if (act < FNN_ACT_NONE || act > FNN_ACT_SILU) return FNN_E_RANGE;
+    const bool slope = act != FNN_ACT_NONE;
+    if (slope) FNN_CHECK(check_matrix(pre));
+    if (dx) FNN_CHECK(check_matrix(dx));
+    if (dw) FNN_CHECK(check_matrix(dw));
+    const int64_t rows = x->n, inner = x->d, outer = w->n;
+    if (w->d != inner || !same_shape(dy, rows, outer) || (slope && !same_shape(pre, rows, outer)) || (dx && !same_shape(dx, rows, inner)) ||
+        (dw && !same_shape(dw, outer, inner)))
+        return FNN_E_SHAPE;
+    if (w->dtype != x->dtype || dy->dtype != x->dtype || (slope && pre->dtype != x->dtype) || (dx && dx->dtype != x->dtype) || (dw && dw->dtype != x->dtype))
+        return FNN_E_DTYPE;
+    if (!dx && !dw && !dbias) return FNN_OK;
+    const LinearBackLayout L = linear_back_layout(rows, inner, outer, x->dtype, act);
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, L.total));
+    const hipStream_t s = (hipStream_t)stream;
+    char* ws = (char*)workspace;
+
+    const void* q = dy->data;
+    int64_t q_stride = stride_of(dy);
+    if (outer > 0 && ((slope && (dx || dw) && rows > 0) || dbias)) {
+        SlopeArgs a;
+        memset(&a, 0, sizeof(a));
+        a.dy = dy->data;
+        a.pre = slope ? pre->data : nullptr;
+        a.p = slope && (dx || dw) ? ws + L.q : nullptr;
+        a.partial = dbias ? (float*)(ws + L.sums) : nullptr;
+        a.m = rows;
+        a.dy_stride = stride_of(dy);
+        a.pre_stride = slope ? stride_of(pre) : 0;
+        a.p_stride = L.q_stride;
+        a.n = (int32_t)outer;
+        a.act = act;
+        if (launch_slope(a, x->dtype, s) != hipSuccess) return FNN_E_HIP;
+        if (dbias && launch_column_sums(a.partial, slope_strips(rows, outer), outer, outer, dbias, nullptr, x->dtype, TK_LINEAR_BACKWARD, s) != hipSuccess)
+            return FNN_E_HIP;
+        if (slope) q = ws + L.q, q_stride = L.q_stride;
+    }
+    GemmArgs a;
+    memset(&a, 0, sizeof(a));
+    a.partial = (float*)(ws + L.partial);
+    if (dx) {
+        a.a = q;
+        a.lda = q_stride;
+        a.b = w->data;
+        a.ldb = stride_of(w);
+        a.m = rows;
+        a.n = (int32_t)inner;
+        a.k = (int32_t)outer;
+        a.y = const_cast<void*>(dx->data);
+        a.ldy = stride_of(dx);
+        if (launch_gemm(a, x->dtype, 0, 1, TK_LINEAR_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+    }
+    if (dw) {
+        a.a = q;
+        a.lda = q_stride;
+        a.b = x->data;
+        a.ldb = stride_of(x);
+        a.m = outer;
+        a.n = (int32_t)inner;
+        a.k = (int32_t)rows;
+        a.y = const_cast<void*>(dw->data);
+        a.ldy = stride_of(dw);
+        if (launch_gemm(a, x->dtype, 1, 1, TK_LINEAR_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+    }
+    return FNN_OK;
 }
 
 }  // extern "C"

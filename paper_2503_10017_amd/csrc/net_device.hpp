@@ -68,4 +68,162 @@ __device__ __forceinline__ float wave_sum(float x) {
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// ---- activations and their slopes ----
+// 16-bit outputs take exp and the reciprocal from the hardware (2 units in the last place of fp32) and erfc from Abramowitz and Stegun, formula
+// 7.1.26 (its error, 1.5e-7, is far below half a step of the output); fp32 outputs take the library's functions.
+
+enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
+
+template <bool FAST>
+__device__ __forceinline__ float exp_of(float x) {
+    if constexpr (FAST) return __builtin_amdgcn_exp2f(x * 1.44269504f);
+    else return expf(x);
+}
+template <bool FAST>
+__device__ __forceinline__ float over(float a, float b) {
+    if constexpr (FAST) return a * __builtin_amdgcn_rcpf(b);
+    else return a / b;
+}
+// Phi(x), the integral of the normal density up to x; exp(-x^2 / 2) comes along.
+template <bool FAST>
+__device__ __forceinline__ float normal_integral(float x, float& gauss) {
+    gauss = exp_of<FAST>(-0.5f * x * x);
+    if constexpr (FAST) {
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(x), 0.3275911f * 0.70710678f, 1.f));
+        float p = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
+        p = __builtin_fmaf(t, p, 1.421413741f);
+        p = __builtin_fmaf(t, p, -0.284496736f);
+        p = __builtin_fmaf(t, p, 0.254829592f);
+        const float tail = 0.5f * p * t * gauss;  // Phi(-|x|)
+        return x < 0.f ? tail : 1.f - tail;
+    } else {
+        return 0.5f * erfcf(-0.70710678118654752f * x);
+    }
+}
+// x = act(x), for N values; the choice is the same in every lane and made once.
+template <bool FAST, int N>
+__device__ __forceinline__ void activate(float (&x)[N], int act) {
+    if (act == ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = x[e] < 0.f ? 0.f : x[e];
+    } else if (act == ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            float gauss;
+            x[e] *= normal_integral<FAST>(x[e], gauss);
+        }
+    } else if (act == ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = over<FAST>(x[e], 1.f + exp_of<FAST>(-x[e]));
+    }
+}
+// p *= act'(x)
+template <bool FAST, int N>
+__device__ __forceinline__ void times_slope(float (&p)[N], const float (&x)[N], int act) {
+    if (act == ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) p[e] = x[e] > 0.f ? p[e] : x[e] <= 0.f ? 0.f : x[e];  // a NaN stays one
+    } else if (act == ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            float gauss;
+            const float phi = normal_integral<FAST>(x[e], gauss);
+            p[e] *= __builtin_fmaf(x[e] * 0.39894228f, gauss, phi);
+        }
+    } else if (act == ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float s = over<FAST>(1.f, 1.f + exp_of<FAST>(-x[e]));
+            p[e] *= s * __builtin_fmaf(x[e], 1.f - s, 1.f);
+        }
+    }
+}
+
+// ---- matrix instructions: 32 x 32 results over a run of 16 bytes per lane, two lane halves ----
+// mma32(a, b): result register v of lane (c = lane & 31, h = lane >> 5) belongs to row 8 (v / 4) + 4 h + v % 4 of a and row c of b.
+template <int DT>
+__device__ __forceinline__ f32x16 mma32(uint4 a, uint4 b, f32x16 acc) {
+    if constexpr (DT == CT_F16) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
+    } else if constexpr (DT == CT_BF16) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+    } else {
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+    }
+}
+// The same for 16 x 16: lane (r = lane & 15, q = lane >> 4) holds 16 bytes of row r at run q; result register v belongs to row 4 q + v of a and
+// row r of b.
+template <int DT>
+__device__ __forceinline__ f32x4 mma16(uint4 a, uint4 b, f32x4 acc) {
+    if constexpr (DT == CT_F16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
+    } else if constexpr (DT == CT_BF16) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+    } else {
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+    }
+}
+// A lane's 16 results of mma32, rearranged: out[p] = the 8 consecutive rows 16 p + 8 h .. + 7 of a (p = 0, 1).
+__device__ __forceinline__ void rows_of_eight(const f32x16& acc, float (&out)[2][8]) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[8 * p + e]), __float_as_uint(acc[8 * p + 4 + e]), false, false);
+            out[p][e] = __uint_as_float(sw[0]);
+            out[p][4 + e] = __uint_as_float(sw[1]);
+        }
+}
+
+// 16 bytes from p, of which the first `count` elements exist; the rest are zero.  p as in load_elems.
+template <int DT>
+__device__ __forceinline__ uint4 load_run(const typename Elem<DT>::T* p, int count) {
+    uint4 v = {0u, 0u, 0u, 0u};
+    if (count >= Elem<DT>::N) {
+        __builtin_memcpy(&v, p, 16);
+    } else if (count > 0) {
+        typename Elem<DT>::T raw[Elem<DT>::N];
+#pragma unroll
+        for (int e = 0; e < Elem<DT>::N; ++e) raw[e] = e < count ? p[e] : (typename Elem<DT>::T)0.f;
+        __builtin_memcpy(&v, raw, 16);
+    }
+    return v;
+}
+
+// ---- direct loads from a buffer to LDS ----
+// A buffer of `bytes` bytes from base (both the same in every lane): what lies behind it reads as zero.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ i32x4 buffer_of(const void* base, uint32_t bytes) {
+    const uint64_t at = (uint64_t)base;
+    i32x4 b;
+    b[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)at);
+    b[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32) & 0xFFFF);
+    b[2] = __builtin_amdgcn_readfirstlane((int)bytes);
+    b[3] = 0x00020000;
+    return b;
+}
+__device__ __forceinline__ uint32_t lds_address(const char* lds) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)lds;
+}
+// 16 bytes per lane from `offset` in the buffer to LDS at `to` + 16 * lane (`to` the same in every lane).  Written in assembly because the compiler
+// makes every later LDS read wait for a load to LDS that it knows of, whichever part of LDS it reads; whoever reads what this brings
+// waits for it (vmcnt) first, and then meets the other waves at a barrier.
+__device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(buffer) : "m0", "memory");
+}
+__device__ __forceinline__ void lds_loads_arrived() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
+// ---- transposing reads of 16-bit tiles in LDS ----
+// Of every 16 lanes, lanes 4 r .. 4 r + 3 name the 16 elements of row r (r = 0 .. 3), four each; lane t gets column t of the four rows.
+typedef short i16x4v __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint2 read_transposed(const char* lds) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4v*)lds));
+}
+
 }  // namespace fnn

@@ -37,4 +37,39 @@ struct NormBackArgs {
 int64_t layer_norm_backward_groups(int64_t n, int32_t d);
 hipError_t launch_layer_norm_backward(const NormBackArgs& a, int dtype, int weight_dtype, hipStream_t s);
 
+// C[m][n] = sum over k of A(m, k) B(n, k), then y = act(C + bias) + residual.
+struct GemmArgs {
+    const void* a;
+    const void* b;
+    int64_t lda, ldb;  // elements between rows
+    int64_t m;
+    int32_t n, k;
+    void* y;
+    const void* bias;
+    const void* residual;
+    void* pre;         // C + bias is stored too
+    int64_t ldy, ldr, ldp;
+    int32_t act;
+    float* partial;    // [splits][tiles_m * rows of a tile][tiles_n * columns of a tile]
+    int32_t tiles_m, tiles_n, splits;
+};
+// Bytes of `partial` that a product of these sizes wants (0: none): a function of the sizes and layouts alone.
+size_t gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, int layout_a, int layout_b);
+hipError_t launch_gemm(GemmArgs a, int dtype, int layout_a, int layout_b, int trace_kind, hipStream_t s);
+
+// p = dy * act'(pre), rounded to dy's type, and the column sums of p before that rounding, as shares of strips of rows.
+struct SlopeArgs {
+    const void* dy;
+    const void* pre;
+    void* p;          // NULL: not wanted
+    float* partial;   // [strips][n]; NULL: not wanted
+    int64_t m, dy_stride, pre_stride, p_stride;
+    int32_t n, act;
+};
+int64_t slope_strips(int64_t m, int64_t n);
+hipError_t launch_slope(const SlopeArgs& a, int dtype, hipStream_t s);
+
+// Sums of the columns of partial [groups][width] into out[0 .. first) and more[0 .. width - first), either of which may be NULL.
+hipError_t launch_column_sums(const float* partial, int64_t groups, int64_t width, int64_t first, void* out, void* more, int dtype, int trace_kind, hipStream_t s);
+
 }  // namespace fnn

@@ -94,3 +94,58 @@ def fnn_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
                                        0 if workspace is None else workspace.numel(), _stream_ptr(stream, x.device)),
            "fnn_layer_norm_backward")
     return dx, dweight, dbias
+
+
+FNN_ACT_NONE, FNN_ACT_RELU, FNN_ACT_GELU, FNN_ACT_SILU = 0, 1, 2, 3
+_ACTS = {"none": FNN_ACT_NONE, "relu": FNN_ACT_RELU, "gelu": FNN_ACT_GELU, "silu": FNN_ACT_SILU,
+         FNN_ACT_NONE: FNN_ACT_NONE, FNN_ACT_RELU: FNN_ACT_RELU, FNN_ACT_GELU: FNN_ACT_GELU, FNN_ACT_SILU: FNN_ACT_SILU}
+
+
+def fnn_linear_workspace_bytes(rows: int, inner: int, outer: int, dtype: torch.dtype) -> int:
+    return int(load_library().fnn_linear_workspace_bytes(rows, inner, outer, _DTYPES[dtype]))
+
+
+def fnn_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+               act="none", want_pre: bool = False, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None):
+    """act(x w^T + bias) + residual for x [rows][inner], w [outer][inner]; act is "none", "relu", "gelu" or "silu".  Returns
+    (y, pre), pre = x w^T + bias for the gradient, or None without ``want_pre``.  ``out`` may be ``residual``."""
+    lib = load_library()
+    xm, wm = _matrix(x, "x"), _matrix(w, "w")
+    rows, inner = x.shape
+    outer = w.shape[0]
+    if out is None:
+        out = torch.empty((rows, outer), dtype=x.dtype, device=x.device)
+    pre = torch.empty((rows, outer), dtype=x.dtype, device=x.device) if want_pre else None
+    if workspace is None:
+        need = lib.fnn_linear_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype])
+        workspace = _workspace(need, x.device) if need else None
+    _check(lib.fnn_linear(xm, wm, _vector(bias, outer, x.dtype, "bias"), _ACTS[act], _matrix(residual, "residual"),
+                          _matrix(out, "out"), _matrix(pre, "pre"), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                          _stream_ptr(stream, x.device)), "fnn_linear")
+    return out, pre
+
+
+def fnn_linear_backward_workspace_bytes(rows: int, inner: int, outer: int, dtype: torch.dtype, act="none") -> int:
+    return int(load_library().fnn_linear_backward_workspace_bytes(rows, inner, outer, _DTYPES[dtype], _ACTS[act]))
+
+
+def fnn_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre: Optional[torch.Tensor] = None, act="none",
+                        want_x: bool = True, want_w: bool = True, want_bias: bool = True, out: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradient of fnn_linear from dy [rows][outer] and, with an activation, pre; returns (dx, dw, dbias), None where not wanted
+    (dx is written to ``out`` if given).  The residual's gradient is dy."""
+    lib = load_library()
+    rows, inner = x.shape
+    outer = w.shape[0]
+    dx = out
+    if dx is None and want_x:
+        dx = torch.empty((rows, inner), dtype=x.dtype, device=x.device)
+    dw = torch.empty((outer, inner), dtype=x.dtype, device=x.device) if want_w else None
+    dbias = torch.empty(outer, dtype=x.dtype, device=x.device) if want_bias else None
+    if workspace is None:
+        workspace = _workspace(lib.fnn_linear_backward_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype], _ACTS[act]), x.device)
+    _check(lib.fnn_linear_backward(_matrix(dy, "dy"), _matrix(x, "x"), _matrix(w, "w"), _matrix(pre, "pre"), _ACTS[act],
+                                   _matrix(dx, "dx"), _matrix(dw, "dw"), _ptr(dbias), _ptr(workspace), workspace.numel(),
+                                   _stream_ptr(stream, x.device)), "fnn_linear_backward")
+    return dx, dw, dbias

@@ -61,3 +61,52 @@ def test_layer_norm_backward_refusals(lib):  # noqa: F811
     assert call(dy=matrix(dtype=0)) == DTYPE and call(dx=matrix(dtype=2)) == DTYPE and call(weight_dtype=2) == DTYPE
     assert call(ws=None) == WORKSPACE and call(ws=0x100010) == WORKSPACE and call(ws_bytes=need - 1) == WORKSPACE
     assert call(dx=None, dweight=None) == OK     # nothing wanted
+
+
+def test_linear_refusals(lib):  # noqa: F811
+    x, w, y = matrix(n=100, d=64), matrix(n=32, d=64, data=0x20000), matrix(n=100, d=32, data=0x30000)
+    assert fnn.net._DTYPES and lib.fnn_linear_workspace_bytes(100, 64, 32, 1) == 0
+    need = lib.fnn_linear_workspace_bytes(100, 64000, 32, 1)
+    assert need > 0
+    for sizes in ((-1, 64, 32, 1), (100, -1, 32, 1), (100, 64, 2 ** 31, 1), (100, 64, 32, 5)):
+        assert lib.fnn_linear_workspace_bytes(*sizes) == 0
+
+    def call(x=x, w=w, y=y, act=0, residual=None, pre=None, ws=None, ws_bytes=0):
+        return lib.fnn_linear(x, w, None, act, residual, y, pre, ws, ws_bytes, None)
+
+    assert call(x=None) == NULL and call(w=None) == NULL and call(y=None) == NULL
+    assert call(x=matrix(n=100, d=64, data=0)) == NULL
+    for bad in (matrix(n=100, d=63), matrix(n=-1), matrix(n=100, d=64, stride=63)):
+        assert call(x=bad) == SHAPE and call(y=bad) == SHAPE and call(residual=bad) == SHAPE and call(pre=bad) == SHAPE
+    assert call(w=matrix(n=31, d=64)) == SHAPE and call(w=matrix(n=32, d=65)) == SHAPE
+    for bad in (0, 2):
+        assert call(w=matrix(n=32, d=64, dtype=bad)) == DTYPE and call(y=matrix(n=100, d=32, dtype=bad)) == DTYPE
+        assert call(residual=matrix(n=100, d=32, dtype=bad)) == DTYPE and call(pre=matrix(n=100, d=32, dtype=bad)) == DTYPE
+    assert call(x=matrix(n=100, d=64, dtype=9)) == DTYPE
+    assert call(act=-1) == RANGE and call(act=4) == RANGE
+    long = dict(x=matrix(n=100, d=64000), w=matrix(n=32, d=64000))
+    assert call(**long) == WORKSPACE and call(**long, ws=0x100001, ws_bytes=need) == WORKSPACE and call(**long, ws=0x100000, ws_bytes=need - 1) == WORKSPACE
+    nothing = dict(x=matrix(n=0, d=64, data=0), y=matrix(n=0, d=32, data=0))
+    assert call(**nothing) == OK
+
+
+def test_linear_backward_refusals(lib):  # noqa: F811
+    need = lib.fnn_linear_backward_workspace_bytes(100, 64, 32, 1, 2)
+    assert need >= 100 * 32 * 2
+    for sizes in ((-1, 64, 32, 1, 0), (100, -1, 32, 1, 0), (100, 64, 2 ** 31, 1, 0), (100, 64, 32, 5, 0), (100, 64, 32, 1, 4)):
+        assert lib.fnn_linear_backward_workspace_bytes(*sizes) == 0
+
+    def call(dy=matrix(n=100, d=32), x=matrix(n=100, d=64), w=matrix(n=32, d=64), pre=matrix(n=100, d=32), act=2, dx=matrix(n=100, d=64, data=0x20000),
+             dw=matrix(n=32, d=64, data=0x30000), dbias=None, ws=0x100000, ws_bytes=need):
+        return lib.fnn_linear_backward(dy, x, w, pre, act, dx, dw, dbias, ws, ws_bytes, None)
+
+    for name in ("dy", "x", "w", "pre"):
+        assert call(**{name: None}) == NULL
+    for name, good in (("dy", (100, 32)), ("x", (100, 64)), ("w", (32, 64)), ("pre", (100, 32)), ("dx", (100, 64)), ("dw", (32, 64))):
+        n, d = good
+        for bad in (matrix(n=n + 1, d=d), matrix(n=n, d=d - 1), matrix(n=n, d=d, stride=d - 1)):
+            assert call(**{name: bad}) == SHAPE, name
+        assert call(**{name: matrix(n=n, d=d, dtype=2)}) == DTYPE, name
+    assert call(act=4) == RANGE
+    assert call(ws=None) == WORKSPACE and call(ws=0x100008) == WORKSPACE and call(ws_bytes=need - 1) == WORKSPACE
+    assert call(dx=None, dw=None) == OK      # nothing wanted
