@@ -87,6 +87,40 @@ int32_t fnn_linear_backward(const fnn_map* dy, const fnn_map* x, const fnn_map* 
                             const fnn_map* dx, const fnn_map* dw, void* dbias, void* workspace, size_t workspace_bytes,
                             void* stream);
 
+#define FNN_MAX_HEAD_DIM 128
+
+/* n tokens with `heads` vectors of d elements each: element e of head h of token t is data[t * row_stride + h * head_stride + e]. */
+typedef struct {
+    const void* data;
+    int64_t n;
+    int32_t heads;
+    int32_t d;
+    int32_t dtype;        /* fnn_dtype: FNN_F16 or FNN_BF16 */
+    int32_t reserved;     /* must be zero */
+    int64_t row_stride;   /* in elements */
+    int64_t head_stride;  /* in elements */
+} fnn_heads;
+
+/*
+ * Attention over `batch` sequences packed one after the other: queries cu_q[b] .. cu_q[b + 1] - 1 of q are those of sequence b, keys and values
+ * cu_k[b] .. cu_k[b + 1] - 1 of k and v its keys (cu_q, cu_k: device int32[batch + 1], ascending; both NULL with batch == 1: one sequence of
+ * everything).  Query i of lq sees key j of lk if !causal or j <= i + lk - lq: the last query sees every key, so queries at the end of
+ * a cache, one token among them, need nothing else.
+ *   out = sum_j softmax_j(scale <q, k_j>) v_j,   lse = log sum_j exp(scale <q, k_j>)   over the keys j that the query sees
+ * A query that sees none has out = 0 and lse = minus infinity.  q and out have `heads` heads, k and v a divisor of that: query head h
+ * reads key head h / (heads / key heads).  d <= FNN_MAX_HEAD_DIM; scale > 0.  lse (device float [q->n][heads]) may be NULL; the
+ * gradient takes it.  Strides are free (heads of a token may also lie apart by more than a token); vectors on 16-byte boundaries are
+ * faster.  What lies outside the sequences is neither read for its value nor written.  Within a sequence keys and values must be finite where
+ * another query of the same call does not see them yet: a causal tile multiplies such values by 0.
+ * Scores, softmax and sums are fp32; the weights exp(..) <= 1 are rounded to the values' type for the second product.
+ * The workspace is for few queries with many keys, which are split and joined in a fixed order.
+ * Errors: FNN_E_NULL, FNN_E_SHAPE, FNN_E_DTYPE, FNN_E_RANGE (scale, batch < 1), FNN_E_WORKSPACE.
+ */
+size_t fnn_attention_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int32_t batch, int32_t heads, int32_t key_heads, int32_t d);
+int32_t fnn_attention(const fnn_heads* q, const fnn_heads* k, const fnn_heads* v, int32_t batch, const int32_t* cu_q,
+                      const int32_t* cu_k, int32_t causal, float scale, const fnn_heads* out, float* lse,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,6 +26,8 @@ from .binding import (  # noqa: F401
     load_library,
 )
 from .net import (  # noqa: F401
+    fnn_attention,
+    fnn_attention_workspace_bytes,
     fnn_layer_norm,
     fnn_layer_norm_backward,
     fnn_layer_norm_backward_workspace_bytes,

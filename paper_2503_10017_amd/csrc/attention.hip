@@ -1,0 +1,399 @@
+// Attention over packed sequences (fnn_attention): out = softmax(scale q k^T) v, one pass over the keys with a running maximum
+// and sum, the scores never leaving registers.
+//
+// Scores are formed as k q^T, so a lane owns one query (row) and 16 keys of each 32 x 32 block: the softmax needs one exchange between two lanes,
+// and the weights, rounded to the operands' type, are the second product's operand as they lie -- v^T is read from LDS by
+// transposing reads in the same order of keys.  The result is out^T, again one row per lane, so rescaling it is a plain multiplication.
+#include <type_traits>
+
+#include "attention_device.hpp"
+#include "trace.hpp"
+
+namespace fnn {
+
+namespace {
+
+// One wave's rows: QB blocks of 32, a row per lane of either half.
+template <int DT, int DB, int QB, int KEYS>
+struct Rows {
+    using Tile = HeadTile<DT, DB, KEYS>;
+    typedef typename Elem<DT>::T E;
+    static constexpr int KB = KEYS / 32;
+    uint4 q[QB][2 * DB];
+    f32x16 out[QB][DB];
+    float top[QB], sum[QB];  // of the keys so far: the largest score, and (this half's share of) the sum of exp2(c (score - top))
+
+    __device__ __forceinline__ void begin(const AttentionArgs& a, const Sequence& s, int group, int64_t row, int64_t rows, int lane) {
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            const int64_t r = row + 32 * b + (lane & 31);
+            const int token = (int)(r / a.share), head = group * a.share + (int)(r % a.share);
+            const E* from = (const E*)a.q + (s.q0 + token) * a.q_row + head * a.q_head;
+#pragma unroll
+            for (int i = 0; i < 2 * DB; ++i) {
+                const int at = 16 * i + 8 * (lane >> 5);
+                q[b][i] = load_run<DT>(from + at, r < rows ? a.d - at : 0);
+            }
+#pragma unroll
+            for (int i = 0; i < DB; ++i) out[b][i] = (f32x16)(0.f);
+            top[b] = -__builtin_inff();
+            sum[b] = 0.f;
+        }
+    }
+
+    // KEYS more keys, the first of which is number `key`; `seen`: how many of the sequence's keys each row sees.  mask (the same in every
+    // lane): some row may not see all of these.  Only the masking itself is branched over: two copies of all of it kept two copies of `out` in registers.
+    __device__ __forceinline__ void keys(const char* k, const char* v, float c, int key, const int (&seen)[QB], bool mask, int lane) {
+        f32x16 score[QB][KB];
+#pragma unroll
+        for (int b = 0; b < QB; ++b)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb) score[b][kb] = (f32x16)(0.f);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < 2 * DB; ++i) {
+                const uint4 f = Tile::along(k, kb, i, lane);
+#pragma unroll
+                for (int b = 0; b < QB; ++b) score[b][kb] = mma32<DT>(f, q[b][i], score[b][kb]);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < QB; ++b) {
+            float most = top[b];
+            if (mask) {
+                const int left = seen[b] - key - 4 * (lane >> 5);
+#pragma unroll
+                for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) score[b][kb][r] = 32 * kb + tile_row(r, 0) < left ? score[b][kb][r] : -__builtin_inff();
+            }
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, score[b][kb][r]);
+            most = across_halves_max(most);
+            // rows that have seen no key yet stay at minus infinity; anything finite in its place makes their weights 0
+            const float base = most > -__builtin_inff() ? most * c : 0.f;
+            const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(top[b], c, -base));
+            top[b] = most;
+            float more = 0.f;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    score[b][kb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[b][kb][r], c, -base));
+                    more += score[b][kb][r];
+                }
+            sum[b] = __builtin_fmaf(sum[b], keep, more);
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) out[b][i][r] *= keep;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // the weights are at most 1 and rounded to the values' type, as the matrix instructions take them; their sum is of the unrounded ones
+#pragma unroll
+        for (int t = 0; t < 2 * KB; ++t) {
+            uint4 p[QB];
+#pragma unroll
+            for (int b = 0; b < QB; ++b) p[b] = round_half<DT>(score[b][t >> 1], t & 1);
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                const uint4 f = Tile::across(v, i, t, lane);
+#pragma unroll
+                for (int b = 0; b < QB; ++b) out[b][i] = mma32<DT>(f, p[b], out[b][i]);
+            }
+        }
+    }
+};
+
+// Where row r of a group is in lse and in the shares of a split call: query-major, as lse is.
+__device__ __forceinline__ int64_t flat_row(const AttentionArgs& a, const Sequence& s, int group, int64_t r) {
+    return (s.q0 + r / a.share) * (int64_t)a.heads + group * a.share + r % a.share;
+}
+
+// Results of one row: element runs of 8 (`at` from 0, `count` of them exist).
+template <int DT>
+__device__ __forceinline__ void put_run(const AttentionArgs& a, const Sequence& s, int group, int64_t r, int at, const float (&v)[8]) {
+    typedef typename Elem<DT>::T E;
+    const int token = (int)(r / a.share), head = group * a.share + (int)(r % a.share);
+    store_elems<DT>((E*)a.out + (s.q0 + token) * a.out_row + head * a.out_head + at, a.d - at, v);
+}
+
+// Shares of a split call: [split][rows] of {the largest score, the sum}, then [split][rows][d rounded up to 8].
+__device__ __forceinline__ float* share_stats(const AttentionArgs& a, int split, int64_t row) {
+    return a.partial + ((int64_t)split * a.tq * a.heads + row) * 2;
+}
+__device__ __forceinline__ float* share_row(const AttentionArgs& a, int split, int64_t row) {
+    return a.partial + (int64_t)a.splits * a.tq * a.heads * 2 + ((int64_t)split * a.tq * a.heads + row) * a.d_pad;
+}
+
+template <int DT, int DB, int QB, int KEYS>
+__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int64_t row, int64_t rows, int split, const Rows<DT, DB, QB, KEYS>& w, int lane) {
+    const int c = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < QB; ++b) {
+        const int64_t r = row + 32 * b + c;
+        const float total = across_halves_sum(w.sum[b]);
+        float scale = 1.f;
+        if (a.splits == 1) scale = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // a row that sees no key is 0
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            float v[2][8];
+            rows_of_eight(w.out[b][i], v);
+            if (r >= rows) continue;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int at = 32 * i + 16 * p + 8 * h;
+                if (at >= a.d) continue;
+                if (a.splits == 1) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[p][e] *= scale;
+                    put_run<DT>(a, s, group, r, at, v[p]);
+                } else {
+                    float* to = share_row(a, split, flat_row(a, s, group, r)) + at;
+                    reinterpret_cast<f32x4*>(to)[0] = f32x4{v[p][0], v[p][1], v[p][2], v[p][3]};
+                    reinterpret_cast<f32x4*>(to)[1] = f32x4{v[p][4], v[p][5], v[p][6], v[p][7]};
+                }
+            }
+        }
+        if (r >= rows || h) continue;
+        if (a.splits > 1) {
+            float* to = share_stats(a, split, flat_row(a, s, group, r));
+            to[0] = w.top[b];
+            to[1] = total;
+        } else if (a.lse) {
+            a.lse[flat_row(a, s, group, r)] = w.top[b] * a.scale + logf(total);  // no key: minus infinity
+        }
+    }
+}
+
+// Which group and tile a workgroup has: groups outermost, and each XCD (workgroups go to the 8 in turn) a run of neighbours, which read
+// the same keys through one L2; of causal rows the late ones, which see most, first.
+__device__ __forceinline__ void deal(const AttentionArgs& a, int& group, int& tile) {
+    const int total = gridDim.x, id = blockIdx.x, xcd = id & 7, q = total >> 3, r = total & 7;
+    const int mine = xcd * q + min(xcd, r) + (id >> 3);
+    group = mine / a.row_tiles;
+    tile = mine - group * a.row_tiles;
+    if (a.causal) tile = a.row_tiles - 1 - tile;
+}
+
+// How many keys row r sees.
+__device__ __forceinline__ int seen_by(const AttentionArgs& a, const Sequence& s, int64_t r) {
+    return a.causal ? min(max((int)(r / a.share) + (s.lk - s.lq) + 1, 0), s.lk) : s.lk;
+}
+
+// Many rows: a workgroup's four waves have QB x 32 rows each and share tiles of 64 keys.
+template <int DT, int DB, int QB, bool DIRECT>
+__global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
+    constexpr int KEYS = 64, WAVE_ROWS = 32 * QB, ROWS = 4 * WAVE_ROWS;
+    using W = Rows<DT, DB, QB, KEYS>;
+    using Tile = typename W::Tile;
+    typedef typename Elem<DT>::T E;
+    __shared__ __attribute__((aligned(16))) char stages[2][2 * Tile::BYTES];
+    int group, tile;
+    deal(a, group, tile);
+    const Sequence s = find_sequence<ROWS>(a, tile);
+    if (s.index < 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t rows = (int64_t)s.lq * a.share, first = (int64_t)s.tile * ROWS, mine = first + wave * WAVE_ROWS;
+    const int most = seen_by(a, s, min(first + ROWS, rows) - 1);
+    const int tiles = (most + KEYS - 1) / KEYS, t0 = (int)((int64_t)tiles * blockIdx.y / a.splits), t1 = (int)((int64_t)tiles * (blockIdx.y + 1) / a.splits);
+
+    W w;
+    w.begin(a, s, group, mine, rows, lane);
+    const int least_seen = mine < rows ? seen_by(a, s, mine) : 0, most_seen = mine < rows ? seen_by(a, s, min(mine + WAVE_ROWS, rows) - 1) : 0;
+    int seen[QB];
+#pragma unroll
+    for (int b = 0; b < QB; ++b) seen[b] = seen_by(a, s, min(mine + 32 * b + (lane & 31), rows - 1));
+    const float c = a.scale * LOG2E;
+    const E* k = (const E*)a.k + s.k0 * a.k_row + group * a.k_head;
+    const E* v = (const E*)a.v + s.k0 * a.v_row + group * a.v_head;
+    auto stage = [&](char* to, int t) {
+        const int key = t * KEYS, there = min(KEYS, s.lk - key);
+        Tile::template stage<true, 256, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, threadIdx.x);
+        Tile::template stage<false, 256, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, threadIdx.x);
+    };
+    if (t0 < t1) stage(stages[0], t0);
+    for (int t = t0, turn = 0; t < t1; ++t, turn ^= 1) {
+        const char* now = stages[turn];
+        lds_loads_arrived();
+        __syncthreads();
+        if (t + 1 < t1) stage(stages[turn ^ 1], t + 1);
+        const int key = t * KEYS;
+        if (key >= most_seen) continue;
+        w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least_seen, lane);
+    }
+    finish_rows(a, s, group, mine, rows, blockIdx.y, w, lane);
+}
+
+// Few rows (a token or some at the end of a cache): the time is that of reading the keys once.  Every wave has the same 32 rows and tiles of
+// 32 keys of its own, which only it waits for; at the end the four join in LDS.
+template <int DT, int DB, bool DIRECT>
+__global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
+    constexpr int KEYS = 32, ROWS = 32;
+    using W = Rows<DT, DB, 1, KEYS>;
+    using Tile = typename W::Tile;
+    typedef typename Elem<DT>::T E;
+    constexpr int PER_WAVE = 4 * Tile::BYTES;  // two stages of keys and values
+    __shared__ __attribute__((aligned(16))) char stages[4 * PER_WAVE];
+    int group, tile;
+    deal(a, group, tile);
+    const Sequence s = find_sequence<ROWS>(a, tile);
+    if (s.index < 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t rows = (int64_t)s.lq * a.share, first = (int64_t)s.tile * ROWS;
+    const int most = seen_by(a, s, min(first + ROWS, rows) - 1), least = seen_by(a, s, first);
+    const int tiles = (most + KEYS - 1) / KEYS, t0 = (int)((int64_t)tiles * blockIdx.y / a.splits), t1 = (int)((int64_t)tiles * (blockIdx.y + 1) / a.splits);
+
+    W w;
+    w.begin(a, s, group, first, rows, lane);
+    int seen[1] = {seen_by(a, s, min(first + (lane & 31), rows - 1))};
+    const float c = a.scale * LOG2E;
+    const E* k = (const E*)a.k + s.k0 * a.k_row + group * a.k_head;
+    const E* v = (const E*)a.v + s.k0 * a.v_row + group * a.v_head;
+    char* mine = stages + wave * PER_WAVE;
+    auto stage = [&](char* to, int t) {
+        const int key = t * KEYS, there = min(KEYS, s.lk - key);
+        Tile::template stage<true, 64, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, lane);
+        Tile::template stage<false, 64, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, lane);
+    };
+    int turn = 0;
+    if (t0 + wave < t1) stage(mine, t0 + wave);
+    for (int t = t0 + wave; t < t1; t += 4, turn ^= 1) {
+        char* now = mine + turn * 2 * Tile::BYTES;
+        char* next = mine + (turn ^ 1) * 2 * Tile::BYTES;
+        lds_loads_arrived();
+        if (t + 4 < t1) stage(next, t + 4);
+        const int key = t * KEYS;
+        w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least, lane);
+    }
+    // The waves' results, each in its own stages' place: top and sum per lane, then the registers.
+    __syncthreads();
+    float* held = reinterpret_cast<float*>(stages) + wave * (64 * (2 + 16 * DB));
+    held[lane] = w.top[0];
+    held[64 + lane] = w.sum[0];
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) held[(2 + 16 * i + r) * 64 + lane] = w.out[0][i][r];
+    __syncthreads();
+    if (wave) return;
+    const float* all = reinterpret_cast<const float*>(stages);
+    constexpr int EACH = 64 * (2 + 16 * DB);
+    float top = w.top[0];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) top = __builtin_fmaxf(top, all[i * EACH + lane]);
+    const float base = top > -__builtin_inff() ? top * c : 0.f;
+    float sum = 0.f;
+    f32x16 out[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) out[i] = (f32x16)(0.f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float* from = all + j * EACH;
+        const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(from[lane], c, -base));
+        sum = __builtin_fmaf(from[64 + lane], keep, sum);
+#pragma unroll
+        for (int i = 0; i < DB; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) out[i][r] = __builtin_fmaf(from[(2 + 16 * i + r) * 64 + lane], keep, out[i][r]);
+    }
+    w.top[0] = top;
+    w.sum[0] = sum;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) w.out[0][i] = out[i];
+    finish_rows(a, s, group, first, rows, blockIdx.y, w, lane);
+}
+
+// Joins the shares of a split call, a wave per row: lane l has elements 2 l and 2 l + 1.
+template <int DT>
+__global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
+    typedef typename Elem<DT>::T E;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= (int64_t)a.tq * a.heads) return;
+    const int token = (int)(row / a.heads), head = (int)(row - (int64_t)token * a.heads);
+    if (a.cu_q && (token < max(a.cu_q[0], 0) || token >= a.cu_q[a.batch])) return;  // a row of no sequence stays as it is
+    const float c = a.scale * LOG2E;
+    float top = -__builtin_inff();
+    for (int s = 0; s < a.splits; ++s) top = __builtin_fmaxf(top, share_stats(a, s, row)[0]);
+    const float base = top > -__builtin_inff() ? top * c : 0.f;
+    float sum = 0.f, x = 0.f, y = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float* stats = share_stats(a, s, row);
+        const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(stats[0], c, -base));
+        sum = __builtin_fmaf(stats[1], keep, sum);
+        if (2 * lane < a.d) {
+            const float* from = share_row(a, s, row) + 2 * lane;
+            x = __builtin_fmaf(from[0], keep, x);
+            y = __builtin_fmaf(from[1], keep, y);
+        }
+    }
+    const float scale = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
+    E* out = (E*)a.out + token * a.out_row + head * a.out_head + 2 * lane;
+    if (2 * lane < a.d) out[0] = (E)(x * scale);
+    if (2 * lane + 1 < a.d) out[1] = (E)(y * scale);
+    if (lane == 0 && a.lse) a.lse[row] = top * a.scale + logf(sum);
+}
+
+// From the sizes alone: whether the rows of a sequence are few on average (one wave's worth), and into how many parts the keys are split.
+// 2048 workgroups are eight a compute unit; a part has 256 keys at least on average, below which its start costs more than it saves.
+struct Plan {
+    bool few;
+    int row_tiles, splits, blocks;
+};
+Plan plan_of(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d) {
+    Plan p;
+    const int64_t rows = tq * (heads / groups);
+    p.few = rows <= 32 * batch;
+    p.blocks = 1;
+    const int64_t tile = p.few ? 32 : 128 * p.blocks;
+    p.row_tiles = (int)((rows + tile - 1) / tile + batch - 1);
+    if (p.few && p.row_tiles > rows) p.row_tiles = (int)rows;
+    const int64_t workgroups = p.row_tiles * groups, wanted = p.few ? 2048 : 512, longest = tk / batch / 256;
+    int64_t splits = wanted / workgroups;
+    if (splits > longest) splits = longest;
+    if (splits > 64) splits = 64;
+    p.splits = splits < 1 ? 1 : (int)splits;
+    return p;
+}
+
+template <int DT, int DB, bool DIRECT>
+hipError_t run(const AttentionArgs& a, const Plan& p, hipStream_t s) {
+    const dim3 grid((unsigned)(p.row_tiles * a.groups), (unsigned)p.splits);
+    const hipError_t e = p.few ? launch(TK_ATTENTION, attention_few_kernel<DT, DB, DIRECT>, grid, dim3(256), 0, s, a)
+                               : launch(TK_ATTENTION, attention_kernel<DT, DB, 1, DIRECT>, grid, dim3(256), 0, s, a);
+    if (e != hipSuccess || p.splits == 1) return e;
+    return launch(TK_ATTENTION, attention_join_kernel<DT>, dim3((unsigned)(((int64_t)a.tq * a.heads + 3) / 4)), dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+size_t attention_workspace(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d) {
+    if (tq < 1) return 0;
+    const Plan p = plan_of(tq, tk, batch, heads, groups, d);
+    return p.splits > 1 ? (size_t)p.splits * tq * heads * (2 + (d + 7) / 8 * 8) * sizeof(float) : 0;
+}
+
+hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t s) {
+    if (a.tq < 1) return hipSuccess;
+    const Plan p = plan_of(a.tq, a.tk, a.batch, a.heads, a.groups, a.d);
+    a.row_tiles = p.row_tiles;
+    a.splits = p.splits;
+    a.d_pad = (a.d + 7) / 8 * 8;
+    const int blocks = (a.d + 31) / 32;
+    auto with_type = [&](auto dt) {
+        constexpr int DT = dt.value;
+        switch (blocks) {
+            case 1: return a.direct ? run<DT, 1, true>(a, p, s) : run<DT, 1, false>(a, p, s);
+            case 2: return a.direct ? run<DT, 2, true>(a, p, s) : run<DT, 2, false>(a, p, s);
+            case 3: return a.direct ? run<DT, 3, true>(a, p, s) : run<DT, 3, false>(a, p, s);
+            default: return a.direct ? run<DT, 4, true>(a, p, s) : run<DT, 4, false>(a, p, s);
+        }
+    };
+    return dtype == FNN_F16 ? with_type(std::integral_constant<int, CT_F16>()) : with_type(std::integral_constant<int, CT_BF16>());
+}
+
+}  // namespace fnn

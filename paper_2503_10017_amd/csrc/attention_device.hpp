@@ -1,0 +1,137 @@
+// What the attention kernels share: which rows and keys a workgroup works on, tiles of keys and values in LDS, and how matrix
+// instructions read them.
+#pragma once
+#include "net_device.hpp"
+#include "net_kernels.hpp"
+
+namespace fnn {
+
+// The heads that share a key head are rows of one problem: row r of a sequence is query r / share under head r % share of the group, so a
+// tile of keys is read once for all of them, whether the rows are many tokens or many heads of one token.
+struct Sequence {
+    int index;          // -1: there is none
+    int tile;           // which tile of its rows
+    int q0, lq, k0, lk; // first query and key, and how many
+};
+
+__device__ __forceinline__ void sequence_bounds(const int32_t* cu, int b, int total, int& first, int& count) {
+    // a table that runs past its tensor, or backwards, must not lead outside it
+    first = cu ? min(max(cu[b], 0), total) : 0;
+    count = cu ? min(max(cu[b + 1], first), total) - first : total;
+}
+
+// The sequence that tile number `tile` belongs to when every sequence's rows (its queries times `share`) are cut into tiles of ROWS.
+// Every wave finds it for itself: 64 sequences at a time, a prefix sum over their tiles.
+template <int ROWS>
+__device__ __forceinline__ Sequence find_sequence(const AttentionArgs& a, int tile) {
+    Sequence s;
+    s.index = -1;
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        const int b = b0 + lane;
+        int first = 0, count = 0;
+        if (b < a.batch) sequence_bounds(a.cu_q, b, a.tq, first, count);
+        const int tiles = (int)(((int64_t)count * a.share + ROWS - 1) / ROWS);
+        int sum = tiles;
+#pragma unroll
+        for (int step = 1; step < 64; step <<= 1) {
+            const int other = __shfl_up(sum, step);
+            if (lane >= step) sum += other;
+        }
+        const uint64_t past = __ballot(before + sum > tile);
+        if (past) {
+            const int at = __builtin_amdgcn_readfirstlane(__builtin_ctzll(past));
+            s.index = b0 + at;
+            s.tile = tile - before - __builtin_amdgcn_readlane(sum - tiles, at);
+            s.q0 = __builtin_amdgcn_readlane(first, at);
+            s.lq = __builtin_amdgcn_readlane(count, at);
+            sequence_bounds(a.cu_k, s.index, a.tk, s.k0, s.lk);
+            s.k0 = __builtin_amdgcn_readfirstlane(s.k0);
+            s.lk = __builtin_amdgcn_readfirstlane(s.lk);
+            return s;
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return s;
+}
+
+// A tile of ROWS rows of one head's vectors (DIM_BLOCKS blocks of 32 elements, the last of which may end early), 16-bit elements, in LDS:
+// RUNS runs of 16 bytes a row, exchanged so that what a wave reads at once lies in different banks.
+template <int DT, int DIM_BLOCKS, int ROWS>
+struct HeadTile {
+    typedef typename Elem<DT>::T E;
+    static constexpr int RUNS = DIM_BLOCKS == 1 ? 4 : DIM_BLOCKS == 2 ? 8 : 16, ROW_BYTES = RUNS * 16, BYTES = ROWS * ROW_BYTES;
+    // For reads along rows, 8 rows at one run (FOR_ROWS), or across them, 4 rows at two runs (the transposing reads).
+    template <bool FOR_ROWS>
+    static __device__ __forceinline__ int exchanged(int row) {
+        if constexpr (FOR_ROWS) return RUNS >= 8 ? (row & 7) : ((row >> 1) & 3);
+        else return RUNS >= 8 ? ((row & 3) << 1) : (row & 2);
+    }
+
+    // Rows base[0 .. rows), the rest zero, by THREADS threads of which this is number `thread` (a wave's start together).  DIRECT: runs lie on
+    // 16-byte boundaries and offsets fit, so they go straight to LDS and arrive later (lds_loads_arrived); otherwise through registers.
+    template <bool FOR_ROWS, int THREADS, bool DIRECT>
+    static __device__ __forceinline__ void stage(char* lds, const E* base, int64_t stride, int rows, int d, int thread) {
+        constexpr int PER_THREAD = ROWS * RUNS / THREADS;
+        static_assert(ROWS * RUNS % THREADS == 0 && PER_THREAD > 0, "every thread has as many runs");
+        if constexpr (DIRECT) {
+            const i32x4 buffer = buffer_of(base, rows > 0 ? (uint32_t)(((rows - 1) * stride + d) * 2) : 0u);
+            const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + (thread & ~63) * 16);
+#pragma unroll
+            for (int i = 0; i < PER_THREAD; ++i) {
+                const int at = i * THREADS + thread, row = at / RUNS, run = (at % RUNS) ^ exchanged<FOR_ROWS>(row);
+                load_to_lds(buffer, run * 8 < d ? (uint32_t)row * (uint32_t)(stride * 2) + run * 16 : 0xFFFFFFF0u, to + i * THREADS * 16);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER_THREAD; ++i) {
+                const int at = i * THREADS + thread, row = at / RUNS, run = (at % RUNS) ^ exchanged<FOR_ROWS>(row);
+                uint4 v = {0u, 0u, 0u, 0u};
+                if (row < rows) v = load_run<DT>(base + row * stride + run * 8, d - run * 8);
+                *reinterpret_cast<uint4*>(lds + at * 16) = v;
+            }
+        }
+    }
+    // Rows 32 block .. + 31, elements 16 step + 8 h .. + 7 of each: an operand whose sum runs along the rows' elements.
+    static __device__ __forceinline__ uint4 along(const char* lds, int block, int step, int lane) {
+        const int row = 32 * block + (lane & 31), run = (2 * step + (lane >> 5)) ^ exchanged<true>(row);
+        return *reinterpret_cast<const uint4*>(lds + row * ROW_BYTES + run * 16);
+    }
+    // Elements 32 block .. + 31 of rows 16 step + 4 h .. + 3 and 8 more: an operand whose sum runs over the rows, in the order in which mma32
+    // leaves 16 of its result rows in a lane's registers 8 (step & 1) .. + 7.
+    static __device__ __forceinline__ uint4 across(const char* lds, int block, int step, int lane) {
+        const int t = lane & 15, row = 16 * step + 4 * (lane >> 5) + (t >> 2);
+        const int run = (4 * block + 2 * ((lane >> 4) & 1) + ((t >> 1) & 1)) ^ exchanged<false>(row);
+        const char* at = lds + row * ROW_BYTES + run * 16 + (t & 1) * 8;
+        const uint2 lo = read_transposed(at), hi = read_transposed(at + 8 * ROW_BYTES);
+        return {lo.x, lo.y, hi.x, hi.y};
+    }
+};
+
+// Eight fp32 values as an operand's 16 bytes, each rounded to nearest even.
+template <int DT>
+__device__ __forceinline__ uint4 round_run(float a, float b, float c, float d, float e, float f, float g, float h) {
+    typename Elem<DT>::T raw[8] = {(typename Elem<DT>::T)a, (typename Elem<DT>::T)b, (typename Elem<DT>::T)c, (typename Elem<DT>::T)d,
+                                   (typename Elem<DT>::T)e, (typename Elem<DT>::T)f, (typename Elem<DT>::T)g, (typename Elem<DT>::T)h};
+    uint4 v;
+    __builtin_memcpy(&v, raw, 16);
+    return v;
+}
+template <int DT>
+__device__ __forceinline__ uint4 round_half(const f32x16& x, int half) {
+    return round_run<DT>(x[8 * half], x[8 * half + 1], x[8 * half + 2], x[8 * half + 3], x[8 * half + 4], x[8 * half + 5], x[8 * half + 6], x[8 * half + 7]);
+}
+
+__device__ __forceinline__ float across_halves_max(float x) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __builtin_fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+__device__ __forceinline__ float across_halves_sum(float x) {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
+}  // namespace fnn

@@ -10,6 +10,12 @@
 
 using namespace fnn;
 
+#define FNN_CHECK(call)                       \
+    do {                                      \
+        const int32_t status_ = (call);       \
+        if (status_ != FNN_OK) return status_; \
+    } while (0)
+
 namespace {
 
 bool valid_type(int32_t t) { return t == FNN_F32 || t == FNN_F16 || t == FNN_BF16; }
@@ -30,11 +36,6 @@ int32_t check_workspace(const void* workspace, size_t have, size_t need) {
 }
 int32_t done(hipError_t e) { return e == hipSuccess ? FNN_OK : FNN_E_HIP; }
 
-#define FNN_CHECK(call)                       \
-    do {                                      \
-        const int32_t status_ = (call);       \
-        if (status_ != FNN_OK) return status_; \
-    } while (0)
 
 size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
@@ -62,6 +63,67 @@ LinearBackLayout linear_back_layout(int64_t rows, int64_t inner, int64_t outer, 
     const size_t x = gemm_workspace(rows, inner, outer, dtype, 0, 1), w = gemm_workspace(outer, inner, rows, dtype, 1, 1);
     L.total = at + aligned(x > w ? x : w);
     return L;
+}
+
+int32_t check_heads(const fnn_heads* t) {
+    if (!t) return FNN_E_NULL;
+    if (t->n < 0 || t->n > MAX_SLOTS || t->heads < 1 || t->heads > 65535 || t->d < 1 || t->d > FNN_MAX_HEAD_DIM || t->reserved) return FNN_E_SHAPE;
+    if ((t->n > 1 && t->row_stride < t->d) || (t->heads > 1 && t->head_stride < t->d)) return FNN_E_SHAPE;
+    if ((t->n > 1 && t->row_stride > INT64_MAX / 8 / t->n) || (t->heads > 1 && t->head_stride > INT64_MAX / 8 / t->heads)) return FNN_E_SHAPE;
+    if (t->dtype != FNN_F16 && t->dtype != FNN_BF16) return FNN_E_DTYPE;
+    if (t->n > 0 && !t->data) return FNN_E_NULL;
+    return FNN_OK;
+}
+bool attention_sizes(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d) {
+    return tq >= 0 && tq <= MAX_SLOTS && tk >= 0 && tk <= MAX_SLOTS && batch >= 1 && batch <= MAX_SLOTS / 2 && heads >= 1 && heads <= 65535 && groups >= 1 &&
+           heads % groups == 0 && tq <= MAX_SLOTS / heads && d >= 1 && d <= FNN_MAX_HEAD_DIM;
+}
+int64_t row_of(const fnn_heads* t) { return t->n > 1 ? t->row_stride : t->d; }
+int64_t head_of(const fnn_heads* t) { return t->heads > 1 ? t->head_stride : t->d; }
+// Whether every vector starts on a 16-byte boundary, is whole runs of 16 bytes, and a tile's offsets fit 32 bits.
+bool on_runs(const fnn_heads* t) {
+    return ((uintptr_t)t->data & 15) == 0 && t->d % 8 == 0 && row_of(t) % 8 == 0 && head_of(t) % 8 == 0 && row_of(t) < ((int64_t)1 << 23);
+}
+
+// What the forward call and the gradient check alike, and the arguments that they share.
+int32_t attention_args(const fnn_heads* q, const fnn_heads* k, const fnn_heads* v, int32_t batch, const int32_t* cu_q, const int32_t* cu_k,
+                       int32_t causal, float scale, const fnn_heads* out, AttentionArgs& a) {
+    FNN_CHECK(check_heads(q));
+    FNN_CHECK(check_heads(k));
+    FNN_CHECK(check_heads(v));
+    FNN_CHECK(check_heads(out));
+    if (batch < 1 || !(scale > 0.f) || isinf(scale)) return FNN_E_RANGE;
+    if (k->n != v->n || k->heads != v->heads || out->n != q->n || out->heads != q->heads || k->d != q->d || v->d != q->d || out->d != q->d ||
+        !attention_sizes(q->n, k->n, batch, q->heads, k->heads, q->d))
+        return FNN_E_SHAPE;
+    if (k->dtype != q->dtype || v->dtype != q->dtype || out->dtype != q->dtype) return FNN_E_DTYPE;
+    if (!cu_q != !cu_k || (!cu_q && batch != 1)) return FNN_E_NULL;
+    memset(&a, 0, sizeof(a));
+    a.q = q->data;
+    a.k = k->data;
+    a.v = v->data;
+    a.out = const_cast<void*>(out->data);
+    a.cu_q = cu_q;
+    a.cu_k = cu_k;
+    a.q_row = row_of(q);
+    a.q_head = head_of(q);
+    a.k_row = row_of(k);
+    a.k_head = head_of(k);
+    a.v_row = row_of(v);
+    a.v_head = head_of(v);
+    a.out_row = row_of(out);
+    a.out_head = head_of(out);
+    a.tq = (int32_t)q->n;
+    a.tk = (int32_t)k->n;
+    a.batch = batch;
+    a.heads = q->heads;
+    a.groups = k->heads;
+    a.share = q->heads / k->heads;
+    a.d = q->d;
+    a.causal = causal != 0;
+    a.scale = scale;
+    a.direct = on_runs(k) && on_runs(v);
+    return FNN_OK;
 }
 
 }  // namespace
@@ -249,6 +311,22 @@ int32_t fnn_linear_backward(const fnn_map* dy, const fnn_map* x, const fnn_map* 
         if (launch_gemm(a, x->dtype, 1, 1, TK_LINEAR_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
     }
     return FNN_OK;
+}
+
+size_t fnn_attention_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int32_t batch, int32_t heads, int32_t key_heads, int32_t d) {
+    if (!attention_sizes(tokens_q, tokens_k, batch, heads, key_heads, d)) return 0;
+    return attention_workspace(tokens_q, tokens_k, batch, heads, key_heads, d);
+}
+
+int32_t fnn_attention(const fnn_heads* q, const fnn_heads* k, const fnn_heads* v, int32_t batch, const int32_t* cu_q,
+                      const int32_t* cu_k, int32_t causal, float scale, const fnn_heads* out, float* lse,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+    AttentionArgs a;
+    FNN_CHECK(attention_args(q, k, v, batch, cu_q, cu_k, causal, scale, out, a));
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, attention_workspace(q->n, k->n, batch, q->heads, k->heads, q->d)));
+    a.lse = lse;
+    a.partial = (float*)workspace;
+    return done(launch_attention(a, q->dtype, (hipStream_t)stream));
 }
 
 }  // extern "C"

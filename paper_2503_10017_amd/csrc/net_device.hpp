@@ -217,7 +217,8 @@ __device__ __forceinline__ uint32_t lds_address(const char* lds) {
 __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(buffer) : "m0", "memory");
 }
-__device__ __forceinline__ void lds_loads_arrived() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+// This wave's loads have arrived, and its reads of LDS before them are done.
+__device__ __forceinline__ void lds_loads_arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory"); }
 
 // ---- transposing reads of 16-bit tiles in LDS ----
 // Of every 16 lanes, lanes 4 r .. 4 r + 3 name the 16 elements of row r (r = 0 .. 3), four each; lane t gets column t of the four rows.

@@ -72,4 +72,23 @@ hipError_t launch_slope(const SlopeArgs& a, int dtype, hipStream_t s);
 // Sums of the columns of partial [groups][width] into out[0 .. first) and more[0 .. width - first), either of which may be NULL.
 hipError_t launch_column_sums(const float* partial, int64_t groups, int64_t width, int64_t first, void* out, void* more, int dtype, int trace_kind, hipStream_t s);
 
+// Attention over packed sequences: strides in elements, `share` query heads to a key head.
+struct AttentionArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    void* out;
+    float* lse;            // [tq][heads]
+    const int32_t* cu_q;   // NULL: one sequence of everything
+    const int32_t* cu_k;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;
+    int32_t tq, tk, batch, heads, groups, share, d, causal;
+    float scale;
+    int32_t direct;        // keys and values lie on 16-byte boundaries
+    int32_t row_tiles, splits, d_pad;
+    float* partial;
+};
+size_t attention_workspace(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d);
+hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t s);
+
 }  // namespace fnn

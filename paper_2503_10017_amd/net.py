@@ -5,6 +5,7 @@ Tensors are taken with the strides that they have, as long as the elements of a 
 """
 from __future__ import annotations
 
+import struct
 from typing import Optional
 
 import torch
@@ -149,3 +150,54 @@ def fnn_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre:
                                    _matrix(dx, "dx"), _matrix(dw, "dw"), _ptr(dbias), _ptr(workspace), workspace.numel(),
                                    _stream_ptr(stream, x.device)), "fnn_linear_backward")
     return dx, dw, dbias
+
+
+# a struct fnn_heads
+_pack_heads = struct.Struct("=QqiiiiQQ").pack
+
+
+def _heads(t: torch.Tensor, what: str):
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor of [tokens][heads][dim]")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {t.dtype} of {what}")
+    n, heads, d = t.shape
+    row_stride, head_stride, element_stride = t.stride()
+    if d > 1 and element_stride != 1:
+        raise ValueError(f"the vectors of {what} must be contiguous")
+    return _pack_heads(t.data_ptr(), n, heads, d, _DTYPES[t.dtype], 0, row_stride if n > 1 else max(d, row_stride), head_stride if heads > 1 else max(d, head_stride))
+
+
+def _sequences(cu_q, cu_k):
+    """batch and the two tables' addresses; None: one sequence of everything."""
+    if cu_q is None and cu_k is None:
+        return 1, None, None
+    if cu_q is None or cu_k is None or cu_q.numel() != cu_k.numel():
+        raise ValueError("cu_q and cu_k must be given together and have the same length")
+    n = cu_q.numel()
+    return n - 1, _vector(cu_q, n, torch.int32, "cu_q"), _vector(cu_k, n, torch.int32, "cu_k")
+
+
+def fnn_attention_workspace_bytes(tokens_q: int, tokens_k: int, batch: int, heads: int, key_heads: int, d: int) -> int:
+    return int(load_library().fnn_attention_workspace_bytes(tokens_q, tokens_k, batch, heads, key_heads, d))
+
+
+def fnn_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: Optional[torch.Tensor] = None,
+                  cu_k: Optional[torch.Tensor] = None, causal: bool = False, scale: Optional[float] = None,
+                  out: Optional[torch.Tensor] = None, want_lse: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of q [tokens][heads][dim] over k, v [tokens][key heads][dim], sequences packed as cu_q, cu_k int32 [batch + 1] say;
+    scale is 1 / sqrt(dim) unless given.  Returns (out, lse), lse float32 [tokens][heads] for the gradient."""
+    lib = load_library()
+    qm, km, vm = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
+    tokens, heads, d = q.shape
+    batch, cq, ck = _sequences(cu_q, cu_k)
+    if out is None:
+        out = torch.empty((tokens, heads, d), dtype=q.dtype, device=q.device)
+    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        need = lib.fnn_attention_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d)
+        workspace = _workspace(need, q.device) if need else None
+    _check(lib.fnn_attention(qm, km, vm, batch, cq, ck, causal, d ** -0.5 if scale is None else scale, _heads(out, "out"),
+                             _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream, q.device)),
+           "fnn_attention")
+    return out, lse

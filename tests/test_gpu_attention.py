@@ -1,0 +1,245 @@
+"""fnn_attention and its gradient against the definition in 64 bits, sequence by sequence."""
+import math
+
+import pytest
+import torch
+
+import paper_2503_10017_amd as fnn
+from net_helpers import DEV, F32, ROUND, TYPES, assert_within, normal, rounding
+
+pytestmark = pytest.mark.gpu
+
+
+def cu_of(lengths):
+    return torch.tensor([0, *torch.tensor(lengths).cumsum(0).tolist()], dtype=torch.int32, device=DEV)
+
+
+class Problem:
+    """Packed inputs and, per sequence and head, the weights and scores of the definition in 64 bits."""
+
+    def __init__(self, lq, lk, heads, groups, d, causal, kind, seed=1, scale=None, spread=1.0):
+        self.lq, self.lk, self.heads, self.groups, self.d, self.causal, self.dtype = lq, lk, heads, groups, d, causal, TYPES[kind]
+        self.scale = d ** -0.5 if scale is None else scale
+        self.q = normal(seed, sum(lq), heads, d, std=spread, dtype=self.dtype)
+        self.k = normal(seed + 1, sum(lk), groups, d, dtype=self.dtype)
+        self.v = normal(seed + 2, sum(lk), groups, d, dtype=self.dtype)
+        self.dout = normal(seed + 3, sum(lq), heads, d, dtype=self.dtype)
+        self.cu_q, self.cu_k = cu_of(lq), cu_of(lk)
+
+    def call(self, **kw):
+        return fnn.fnn_attention(self.q, self.k, self.v, self.cu_q, self.cu_k, causal=self.causal, scale=self.scale, **kw)
+
+    def sequences(self):
+        """(rows, keys, head, group, weights, lse, |q||k| sums of the scores): slices and fp64 matrices of one head of one sequence."""
+        q0 = k0 = 0
+        for nq, nk in zip(self.lq, self.lk):
+            rows, keys = slice(q0, q0 + nq), slice(k0, k0 + nk)
+            q0, k0 = q0 + nq, k0 + nk
+            if not nq:
+                continue
+            seen = torch.ones((nq, nk), dtype=torch.bool, device=DEV)
+            if self.causal:
+                seen = torch.arange(nk, device=DEV)[None] <= torch.arange(nq, device=DEV)[:, None] + (nk - nq)
+            for h in range(self.heads):
+                g = h // (self.heads // self.groups)
+                q, k = self.q[rows, h].double(), self.k[keys, g].double()
+                z = torch.where(seen, self.scale * (q @ k.t()), -math.inf)
+                lse = torch.logsumexp(z, 1) if nk else torch.full((nq,), -math.inf, dtype=torch.float64, device=DEV)
+                p = torch.where(seen, torch.exp(z - torch.where(torch.isinf(lse), 0.0, lse)[:, None]), 0.0)
+                yield rows, keys, h, g, p, lse, self.scale * (q.abs() @ k.abs().t())
+
+
+def weight_slack(p, mag, d):
+    """Relative error of a weight exp(z - lse): z is a sum of d exact products in fp32 and a multiplication by scale * log2(e), the exponent
+    the difference of two such, exp2 is good to 2 units; lse carries the same.  Per row: twice the largest score's error."""
+    z_off = (d + 8) * F32 * mag
+    return 2.2 * z_off.amax(1, keepdim=True) + 16 * F32 if mag.shape[1] else mag.sum(1, keepdim=True)
+
+
+def check_forward(prob, out, lse):
+    for rows, keys, h, g, p, want_lse, mag in prob.sequences():
+        v = prob.v[keys, g].double()
+        want = p @ v
+        rel = weight_slack(p, mag, prob.d)
+        # each weight is rounded once to the values' type (and below its normal range to its step), then fp32 sums over the keys and their rescalings
+        off = (p * (rel + ROUND[prob.dtype])) @ v.abs() + (2 * p.shape[1] + 8) * F32 * (p @ v.abs()) + (2.0 ** -25 if prob.dtype == torch.float16 else 0) * v.abs().sum(0)
+        assert_within(out[rows, h], want, off + rounding(want, prob.dtype), "out")
+        if lse is not None:
+            finite = torch.where(torch.isinf(want_lse), 0.0, want_lse)
+            assert_within(lse[rows, h], want_lse, rel[:, 0] + (p.shape[1] + 8) * F32 + 4 * F32 * finite.abs(), "lse")
+            assert torch.equal(torch.isinf(lse[rows, h]), torch.isinf(want_lse))
+
+
+CASES = [
+    # lengths of queries and keys, heads, key heads, dim
+    ([1], [1], 1, 1, 64),
+    ([1], [0], 2, 1, 64),
+    ([3, 0, 1, 5], [3, 0, 1, 5], 2, 2, 32),
+    ([64, 65, 1, 127], [64, 65, 1, 127], 3, 1, 64),
+    ([200], [200], 2, 2, 128),
+    ([130, 0, 7, 300], [100, 50, 0, 333], 4, 2, 64),
+    ([300], [17], 2, 2, 96),
+    ([17, 260], [1000, 700], 4, 4, 80),
+    ([1, 1, 1], [1000, 1, 300], 8, 2, 128),
+    ([1, 1, 1, 1], [4000, 0, 63, 2049], 4, 1, 64),
+    ([5, 1, 3], [700, 800, 2], 6, 2, 128),
+    ([2], [6000], 16, 1, 64),
+    ([33] * 70, [33] * 70, 1, 1, 64),
+    ([40], [3000], 12, 4, 40),
+    ([150, 33], [150, 33], 2, 1, 5),
+    ([100], [100], 2, 2, 77),
+]
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_forward(case, causal, kind):
+    prob = Problem(*CASES[case], causal, kind)
+    out, lse = prob.call()
+    check_forward(prob, out, lse)
+    again = prob.call()
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    assert torch.equal(out, prob.call(want_lse=False)[0])
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_large_scores(causal):
+    """Scores of hundreds: one key takes nearly all the weight, the running maximum climbs, and earlier shares vanish."""
+    prob = Problem([257], [700], 2, 2, 64, causal, "f16", spread=12.0, scale=1.0)
+    check_forward(prob, *prob.call())
+    few = Problem([1, 2], [3000, 2500], 4, 2, 64, causal, "f16", spread=12.0, scale=1.0)
+    check_forward(few, *few.call())
+
+
+def test_one_sequence_without_tables():
+    prob = Problem([90], [130], 4, 2, 64, True, "bf16")
+    out, lse = prob.call()
+    got = fnn.fnn_attention(prob.q, prob.k, prob.v, causal=True)
+    assert torch.equal(got[0], out) and torch.equal(got[1], lse)
+
+
+def spaced(t, row_extra, head_extra, offset, head_major=False):
+    """The same vectors with room between tokens and heads (or heads outermost), NaN in the room."""
+    n, heads, d = t.shape
+    size = (n + 1) * (heads + 1) * (d + head_extra) + n * row_extra + offset + 64
+    buf = torch.full((size,), math.nan, dtype=t.dtype, device=t.device)
+    if head_major:
+        strides = (d + head_extra, n * (d + head_extra) + row_extra, 1)
+    else:
+        strides = (heads * (d + head_extra) + row_extra, d + head_extra, 1)
+    view = torch.as_strided(buf, (n, heads, d), strides, offset)
+    view.copy_(t)
+    return view
+
+
+@pytest.mark.parametrize("case", [([70, 3, 200], [70, 3, 200], 4, 2, 64), ([1, 2], [900, 300], 8, 2, 128), ([60], [60], 2, 1, 40)])
+@pytest.mark.parametrize("layout", [(0, 8, 0, False), (16, 0, 8, False), (8, 8, 0, True), (1, 1, 1, False), (2, 3, 5, True)])
+def test_strides_orders_and_alignment(case, layout):
+    prob = Problem(*case, True, "bf16")
+    want, want_lse = prob.call()
+    prob.q, prob.k, prob.v = (spaced(t, *layout) for t in (prob.q, prob.k, prob.v))
+    out = spaced(torch.zeros_like(prob.q), *layout)
+    untouched = torch.isnan(out.as_strided((out.untyped_storage().nbytes() // 2,), (1,), 0)).sum()
+    got, lse = prob.call(out=out)
+    assert torch.equal(got, want) and torch.equal(lse, want_lse)
+    assert torch.isnan(out.as_strided((out.untyped_storage().nbytes() // 2,), (1,), 0)).sum() == untouched
+
+
+@pytest.mark.parametrize("lq,lk", [([70, 130], [70, 130]), ([1, 1], [500, 300])])
+@pytest.mark.parametrize("causal", [False, True])
+def test_what_lies_outside_a_sequence_does_not_reach_it(lq, lk, causal):
+    """Tokens before, between (a sequence of its own) and behind the sequences hold NaN instead of 0: the sequences' results stay the same bits,
+    and rows of no sequence are not written."""
+    prob = Problem(lq, lk, 4, 2, 64, causal, "f16")
+    gap = 37
+
+    def wide(t, lengths, fill):
+        n = sum(lengths)
+        out = torch.full((n + 3 * gap, *t.shape[1:]), fill, dtype=t.dtype, device=t.device)
+        out[gap:gap + lengths[0]] = t[:lengths[0]]
+        out[2 * gap + lengths[0]:2 * gap + n] = t[lengths[0]:]
+        cu = torch.tensor([gap, gap + lengths[0], 2 * gap + lengths[0], 2 * gap + n], dtype=torch.int32, device=DEV)
+        return out, cu
+
+    results = []
+    for fill in (0.0, math.nan):
+        (q, cu_q), (k, cu_k), (v, _) = wide(prob.q, lq, fill), wide(prob.k, lk, fill), wide(prob.v, lk, fill)
+        results.append(fnn.fnn_attention(q, k, v, cu_q, cu_k, causal=causal, out=torch.full_like(q, 3.0)))
+    first, second = slice(gap, gap + lq[0]), slice(2 * gap + lq[0], 2 * gap + sum(lq))
+    for a, b in zip(*results):
+        assert torch.equal(a[first], b[first]) and torch.equal(a[second], b[second])
+    for out, lse in results:
+        assert (out[:gap] == 3).all() and (out[2 * gap + sum(lq):] == 3).all()
+        check_forward(prob, torch.cat((out[first], out[second])), torch.cat((lse[first], lse[second])))
+
+
+def test_nan_and_infinity_reach_what_sees_them():
+    prob = Problem([80, 90], [80, 90], 2, 2, 64, False, "bf16")
+    want = prob.call()[0]
+    prob.k[5, 0, 3] = math.nan
+    prob.v[80 + 7, 1, 9] = math.inf
+    out, lse = prob.call()
+    assert torch.isnan(out[:80, 0]).all() and torch.isnan(lse[:80, 0]).all()
+    assert not torch.isfinite(out[80:, 1, 9]).any()
+    keep = torch.ones_like(out, dtype=torch.bool)
+    keep[:80, 0] = False
+    keep[80:, 1, 9] = False
+    assert torch.equal(out[keep], want[keep])
+
+
+def test_tables_that_lie_stay_inside_the_tensors():
+    """Bounds past the tensor, negative or backwards are cut to it: no result is promised, but every call ends and later ones are right."""
+    prob = Problem([50, 60], [50, 60], 2, 1, 64, True, "f16")
+    want = prob.call()[0]
+    for table in ([-5, 50, 4000], [0, 90, 20], [200, 300, 400], [0, -1, 2 ** 31 - 1]):
+        cu = torch.tensor(table, dtype=torch.int32, device=DEV)
+        fnn.fnn_attention(prob.q, prob.k, prob.v, cu, cu, causal=True)
+        torch.cuda.synchronize()
+    assert torch.equal(prob.call()[0], want)
+
+
+def test_a_cache_longer_than_32_bits():
+    """Keys of 2 heads 64 MB apart per token: the cache spans 4.4 GB; the result is that of a compact copy."""
+    n, d, step = 66, 64, 33 << 20
+    buf = torch.empty(n * step, dtype=torch.bfloat16, device=DEV)
+    k = torch.as_strided(buf, (n, 2, d), (step, step // 2, 1))
+    k.copy_(normal(1, n, 2, d, dtype=torch.bfloat16))
+    v, q = normal(2, n, 2, d, dtype=torch.bfloat16), normal(3, n, 4, d, dtype=torch.bfloat16)
+    for rows in (q, q[-1:]):
+        a, b = fnn.fnn_attention(rows, k, v, causal=True), fnn.fnn_attention(rows, k.contiguous(), v, causal=True)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_no_queries_or_no_keys():
+    q, k = torch.empty((0, 2, 64), dtype=torch.float16, device=DEV), torch.empty((0, 1, 64), dtype=torch.float16, device=DEV)
+    out, lse = fnn.fnn_attention(q, k, k)
+    assert out.shape == (0, 2, 64) and lse.shape == (0, 2)
+    q = torch.ones((3, 2, 64), dtype=torch.float16, device=DEV)
+    out, lse = fnn.fnn_attention(q, k, k, causal=True)
+    assert not out.any() and (lse == -math.inf).all()
+
+
+@pytest.mark.parametrize("case", [([300, 200], [300, 200], 4, 2, 64), ([1, 1], [2000, 900], 8, 2, 128)])
+def test_on_another_stream_and_in_a_graph(case):
+    prob = Problem(*case, True, "bf16")
+    need = fnn.fnn_attention_workspace_bytes(prob.q.shape[0], prob.k.shape[0], 2, prob.heads, prob.groups, prob.d)
+    ws = torch.empty(max(256, need), dtype=torch.uint8, device=DEV)
+    want = [t.clone() for t in prob.call(workspace=ws)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = prob.call(workspace=ws, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = prob.call(workspace=ws)
+    for seed in (1, 21, 22, 1):
+        prob.q.copy_(normal(seed, *prob.q.shape, dtype=torch.bfloat16))
+        for t in held:
+            t.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        assert all(torch.equal(a, b) for a, b in zip(got, prob.call()))
+        torch.cuda.synchronize()
