@@ -121,6 +121,19 @@ int32_t fnn_attention(const fnn_heads* q, const fnn_heads* k, const fnn_heads* v
                       const int32_t* cu_k, int32_t causal, float scale, const fnn_heads* out, float* lse,
                       void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Its gradient, from dout and what the forward call was given and gave.  With p = exp(scale <q, k> - lse) where the query sees the key,
+ * delta = sum_e dout out and ds = p (<dout, v> - delta):
+ *   dq = scale sum_j ds k_j,   dk = scale sum_i ds q_i,   dv = sum_i p dout_i   (over all query heads of the key head)
+ * dq, dk and dv may each be NULL: not wanted.  Keys of a sequence without queries get 0, and so do queries that see no key.
+ * p and ds are rounded to the inputs' type for the products.
+ */
+size_t fnn_attention_backward_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int32_t batch, int32_t heads, int32_t key_heads, int32_t d);
+int32_t fnn_attention_backward(const fnn_heads* dout, const fnn_heads* q, const fnn_heads* k, const fnn_heads* v, const fnn_heads* out,
+                               const float* lse, int32_t batch, const int32_t* cu_q, const int32_t* cu_k, int32_t causal, float scale,
+                               const fnn_heads* dq, const fnn_heads* dk, const fnn_heads* dv, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,8 @@ from .binding import (  # noqa: F401
 )
 from .net import (  # noqa: F401
     fnn_attention,
+    fnn_attention_backward,
+    fnn_attention_backward_workspace_bytes,
     fnn_attention_workspace_bytes,
     fnn_layer_norm,
     fnn_layer_norm_backward,

@@ -99,6 +99,10 @@ def load_library():
     lib.fnn_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
     lib.fnn_attention.restype = i32
     lib.fnn_attention.argtypes = [vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, vp, sz, vp]
+    lib.fnn_attention_backward_workspace_bytes.restype = sz
+    lib.fnn_attention_backward_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
+    lib.fnn_attention_backward.restype = i32
+    lib.fnn_attention_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 

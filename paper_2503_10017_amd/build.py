@@ -12,7 +12,7 @@ LIB_PATH = os.path.join(LIB_DIR, "libfnn.so")
 OBJ_DIR = os.path.join(_HERE, "_build")
 
 SOURCES = ["prep.hip", "search.hip", "coarse.hip", "recip.hip", "walk.hip", "tail.hip", "dense.hip", "dense_coarse.hip", "blocked.hip", "pixels.hip", "api.hip", "trace.hip", "ceiling.hip",
-           "layer_norm.hip", "linear.hip", "attention.hip", "net_api.hip"]
+           "layer_norm.hip", "linear.hip", "attention.hip", "attention_grad.hip", "net_api.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
@@ -22,7 +22,7 @@ HIPCC_FLAGS = [
 # The matching path: inputs are finite by contract; keeps max/compare chains free of NaN quieting.
 MATCHING_FLAGS = ["-fno-honor-nans"]
 # The network's operators carry infinities and NaN from the inputs to the outputs that depend on them.
-NETWORK_SOURCES = {"layer_norm.hip", "linear.hip", "attention.hip", "net_api.hip"}
+NETWORK_SOURCES = {"layer_norm.hip", "linear.hip", "attention.hip", "attention_grad.hip", "net_api.hip"}
 
 
 def _compile(src: str) -> str:

@@ -23,17 +23,10 @@ struct Rows {
     f32x16 out[QB][DB];
     float top[QB], sum[QB];  // of the keys so far: the largest score, and (this half's share of) the sum of exp2(c (score - top))
 
-    __device__ __forceinline__ void begin(const AttentionArgs& a, const Sequence& s, int group, int64_t row, int64_t rows, int lane) {
+    __device__ __forceinline__ void begin(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, int lane) {
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
-            const int64_t r = row + 32 * b + (lane & 31);
-            const int token = (int)(r / a.share), head = group * a.share + (int)(r % a.share);
-            const E* from = (const E*)a.q + (s.q0 + token) * a.q_row + head * a.q_head;
-#pragma unroll
-            for (int i = 0; i < 2 * DB; ++i) {
-                const int at = 16 * i + 8 * (lane >> 5);
-                q[b][i] = load_run<DT>(from + at, r < rows ? a.d - at : 0);
-            }
+            load_row<DT, DB>(a.q, a.q_row, a.q_head, a, s, group, row + 32 * b + (lane & 31), rows, lane, q[b]);
 #pragma unroll
             for (int i = 0; i < DB; ++i) out[b][i] = (f32x16)(0.f);
             top[b] = -__builtin_inff();
@@ -108,16 +101,11 @@ struct Rows {
     }
 };
 
-// Where row r of a group is in lse and in the shares of a split call: query-major, as lse is.
-__device__ __forceinline__ int64_t flat_row(const AttentionArgs& a, const Sequence& s, int group, int64_t r) {
-    return (s.q0 + r / a.share) * (int64_t)a.heads + group * a.share + r % a.share;
-}
-
 // Results of one row: element runs of 8 (`at` from 0, `count` of them exist).
 template <int DT>
-__device__ __forceinline__ void put_run(const AttentionArgs& a, const Sequence& s, int group, int64_t r, int at, const float (&v)[8]) {
+__device__ __forceinline__ void put_run(const AttentionArgs& a, const Sequence& s, int group, int r, int at, const float (&v)[8]) {
     typedef typename Elem<DT>::T E;
-    const int token = (int)(r / a.share), head = group * a.share + (int)(r % a.share);
+    const int token = token_of(a, r), head = group * a.share + (r - token * a.share);
     store_elems<DT>((E*)a.out + (s.q0 + token) * a.out_row + head * a.out_head + at, a.d - at, v);
 }
 
@@ -130,11 +118,11 @@ __device__ __forceinline__ float* share_row(const AttentionArgs& a, int split, i
 }
 
 template <int DT, int DB, int QB, int KEYS>
-__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int64_t row, int64_t rows, int split, const Rows<DT, DB, QB, KEYS>& w, int lane) {
+__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, int split, const Rows<DT, DB, QB, KEYS>& w, int lane) {
     const int c = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
-        const int64_t r = row + 32 * b + c;
+        const int r = row + 32 * b + c;
         const float total = across_halves_sum(w.sum[b]);
         float scale = 1.f;
         if (a.splits == 1) scale = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // a row that sees no key is 0
@@ -169,21 +157,6 @@ __device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequen
     }
 }
 
-// Which group and tile a workgroup has: groups outermost, and each XCD (workgroups go to the 8 in turn) a run of neighbours, which read
-// the same keys through one L2; of causal rows the late ones, which see most, first.
-__device__ __forceinline__ void deal(const AttentionArgs& a, int& group, int& tile) {
-    const int total = gridDim.x, id = blockIdx.x, xcd = id & 7, q = total >> 3, r = total & 7;
-    const int mine = xcd * q + min(xcd, r) + (id >> 3);
-    group = mine / a.row_tiles;
-    tile = mine - group * a.row_tiles;
-    if (a.causal) tile = a.row_tiles - 1 - tile;
-}
-
-// How many keys row r sees.
-__device__ __forceinline__ int seen_by(const AttentionArgs& a, const Sequence& s, int64_t r) {
-    return a.causal ? min(max((int)(r / a.share) + (s.lk - s.lq) + 1, 0), s.lk) : s.lk;
-}
-
 // Many rows: a workgroup's four waves have QB x 32 rows each and share tiles of 64 keys.
 template <int DT, int DB, int QB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
@@ -193,11 +166,11 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     typedef typename Elem<DT>::T E;
     __shared__ __attribute__((aligned(16))) char stages[2][2 * Tile::BYTES];
     int group, tile;
-    deal(a, group, tile);
+    deal(a.row_tiles, a.causal, group, tile);
     const Sequence s = find_sequence<ROWS>(a, tile);
     if (s.index < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t rows = (int64_t)s.lq * a.share, first = (int64_t)s.tile * ROWS, mine = first + wave * WAVE_ROWS;
+    const int rows = s.lq * a.share, first = s.tile * ROWS, mine = first + wave * WAVE_ROWS;
     const int most = seen_by(a, s, min(first + ROWS, rows) - 1);
     const int tiles = (most + KEYS - 1) / KEYS, t0 = (int)((int64_t)tiles * blockIdx.y / a.splits), t1 = (int)((int64_t)tiles * (blockIdx.y + 1) / a.splits);
 
@@ -212,8 +185,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     const E* v = (const E*)a.v + s.k0 * a.v_row + group * a.v_head;
     auto stage = [&](char* to, int t) {
         const int key = t * KEYS, there = min(KEYS, s.lk - key);
-        Tile::template stage<true, 256, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, threadIdx.x);
-        Tile::template stage<false, 256, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, threadIdx.x);
+        Tile::template stage<256, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, threadIdx.x);
+        Tile::template stage<256, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, threadIdx.x);
     };
     if (t0 < t1) stage(stages[0], t0);
     for (int t = t0, turn = 0; t < t1; ++t, turn ^= 1) {
@@ -239,11 +212,11 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     constexpr int PER_WAVE = 4 * Tile::BYTES;  // two stages of keys and values
     __shared__ __attribute__((aligned(16))) char stages[4 * PER_WAVE];
     int group, tile;
-    deal(a, group, tile);
+    deal(a.row_tiles, a.causal, group, tile);
     const Sequence s = find_sequence<ROWS>(a, tile);
     if (s.index < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t rows = (int64_t)s.lq * a.share, first = (int64_t)s.tile * ROWS;
+    const int rows = s.lq * a.share, first = s.tile * ROWS;
     const int most = seen_by(a, s, min(first + ROWS, rows) - 1), least = seen_by(a, s, first);
     const int tiles = (most + KEYS - 1) / KEYS, t0 = (int)((int64_t)tiles * blockIdx.y / a.splits), t1 = (int)((int64_t)tiles * (blockIdx.y + 1) / a.splits);
 
@@ -256,8 +229,8 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     char* mine = stages + wave * PER_WAVE;
     auto stage = [&](char* to, int t) {
         const int key = t * KEYS, there = min(KEYS, s.lk - key);
-        Tile::template stage<true, 64, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, lane);
-        Tile::template stage<false, 64, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, lane);
+        Tile::template stage<64, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, lane);
+        Tile::template stage<64, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, lane);
     };
     int turn = 0;
     if (t0 + wave < t1) stage(mine, t0 + wave);

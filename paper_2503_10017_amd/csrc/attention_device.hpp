@@ -20,9 +20,9 @@ __device__ __forceinline__ void sequence_bounds(const int32_t* cu, int b, int to
     count = cu ? min(max(cu[b + 1], first), total) - first : total;
 }
 
-// The sequence that tile number `tile` belongs to when every sequence's rows (its queries times `share`) are cut into tiles of ROWS.
-// Every wave finds it for itself: 64 sequences at a time, a prefix sum over their tiles.
-template <int ROWS>
+// The sequence that tile number `tile` belongs to when every sequence's rows (its queries times `share`; or its keys) are cut into tiles of
+// ROWS.  Every wave finds it for itself: 64 sequences at a time, a prefix sum over their tiles.
+template <int ROWS, bool BY_KEYS = false>
 __device__ __forceinline__ Sequence find_sequence(const AttentionArgs& a, int tile) {
     Sequence s;
     s.index = -1;
@@ -31,8 +31,8 @@ __device__ __forceinline__ Sequence find_sequence(const AttentionArgs& a, int ti
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
         const int b = b0 + lane;
         int first = 0, count = 0;
-        if (b < a.batch) sequence_bounds(a.cu_q, b, a.tq, first, count);
-        const int tiles = (int)(((int64_t)count * a.share + ROWS - 1) / ROWS);
+        if (b < a.batch) sequence_bounds(BY_KEYS ? a.cu_k : a.cu_q, b, BY_KEYS ? a.tk : a.tq, first, count);
+        const int tiles = (int)(((int64_t)count * (BY_KEYS ? 1 : a.share) + ROWS - 1) / ROWS);
         int sum = tiles;
 #pragma unroll
         for (int step = 1; step < 64; step <<= 1) {
@@ -44,11 +44,15 @@ __device__ __forceinline__ Sequence find_sequence(const AttentionArgs& a, int ti
             const int at = __builtin_amdgcn_readfirstlane(__builtin_ctzll(past));
             s.index = b0 + at;
             s.tile = tile - before - __builtin_amdgcn_readlane(sum - tiles, at);
-            s.q0 = __builtin_amdgcn_readlane(first, at);
-            s.lq = __builtin_amdgcn_readlane(count, at);
-            sequence_bounds(a.cu_k, s.index, a.tk, s.k0, s.lk);
-            s.k0 = __builtin_amdgcn_readfirstlane(s.k0);
-            s.lk = __builtin_amdgcn_readfirstlane(s.lk);
+            const int mine = __builtin_amdgcn_readlane(first, at), many = __builtin_amdgcn_readlane(count, at);
+            int other, others;
+            sequence_bounds(BY_KEYS ? a.cu_q : a.cu_k, s.index, BY_KEYS ? a.tq : a.tk, other, others);
+            other = __builtin_amdgcn_readfirstlane(other);
+            others = __builtin_amdgcn_readfirstlane(others);
+            s.q0 = BY_KEYS ? other : mine;
+            s.lq = BY_KEYS ? others : many;
+            s.k0 = BY_KEYS ? mine : other;
+            s.lk = BY_KEYS ? many : others;
             return s;
         }
         before += __builtin_amdgcn_readlane(sum, 63);
@@ -62,16 +66,12 @@ template <int DT, int DIM_BLOCKS, int ROWS>
 struct HeadTile {
     typedef typename Elem<DT>::T E;
     static constexpr int RUNS = DIM_BLOCKS == 1 ? 4 : DIM_BLOCKS == 2 ? 8 : 16, ROW_BYTES = RUNS * 16, BYTES = ROWS * ROW_BYTES;
-    // For reads along rows, 8 rows at one run (FOR_ROWS), or across them, 4 rows at two runs (the transposing reads).
-    template <bool FOR_ROWS>
-    static __device__ __forceinline__ int exchanged(int row) {
-        if constexpr (FOR_ROWS) return RUNS >= 8 ? (row & 7) : ((row >> 1) & 3);
-        else return RUNS >= 8 ? ((row & 3) << 1) : (row & 2);
-    }
+    // 8 rows read at one run (along) lie in 8 different sets of banks, and so do 4 rows read at a pair of runs (across).
+    static __device__ __forceinline__ int exchanged(int row) { return RUNS >= 8 ? ((row & 3) << 1 | (row >> 2 & 1)) : ((row & 2) | (row >> 2 & 1)); }
 
     // Rows base[0 .. rows), the rest zero, by THREADS threads of which this is number `thread` (a wave's start together).  DIRECT: runs lie on
     // 16-byte boundaries and offsets fit, so they go straight to LDS and arrive later (lds_loads_arrived); otherwise through registers.
-    template <bool FOR_ROWS, int THREADS, bool DIRECT>
+    template <int THREADS, bool DIRECT>
     static __device__ __forceinline__ void stage(char* lds, const E* base, int64_t stride, int rows, int d, int thread) {
         constexpr int PER_THREAD = ROWS * RUNS / THREADS;
         static_assert(ROWS * RUNS % THREADS == 0 && PER_THREAD > 0, "every thread has as many runs");
@@ -80,13 +80,13 @@ struct HeadTile {
             const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + (thread & ~63) * 16);
 #pragma unroll
             for (int i = 0; i < PER_THREAD; ++i) {
-                const int at = i * THREADS + thread, row = at / RUNS, run = (at % RUNS) ^ exchanged<FOR_ROWS>(row);
+                const int at = i * THREADS + thread, row = at / RUNS, run = (at % RUNS) ^ exchanged(row);
                 load_to_lds(buffer, run * 8 < d ? (uint32_t)row * (uint32_t)(stride * 2) + run * 16 : 0xFFFFFFF0u, to + i * THREADS * 16);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < PER_THREAD; ++i) {
-                const int at = i * THREADS + thread, row = at / RUNS, run = (at % RUNS) ^ exchanged<FOR_ROWS>(row);
+                const int at = i * THREADS + thread, row = at / RUNS, run = (at % RUNS) ^ exchanged(row);
                 uint4 v = {0u, 0u, 0u, 0u};
                 if (row < rows) v = load_run<DT>(base + row * stride + run * 8, d - run * 8);
                 *reinterpret_cast<uint4*>(lds + at * 16) = v;
@@ -95,14 +95,14 @@ struct HeadTile {
     }
     // Rows 32 block .. + 31, elements 16 step + 8 h .. + 7 of each: an operand whose sum runs along the rows' elements.
     static __device__ __forceinline__ uint4 along(const char* lds, int block, int step, int lane) {
-        const int row = 32 * block + (lane & 31), run = (2 * step + (lane >> 5)) ^ exchanged<true>(row);
+        const int row = 32 * block + (lane & 31), run = (2 * step + (lane >> 5)) ^ exchanged(row);
         return *reinterpret_cast<const uint4*>(lds + row * ROW_BYTES + run * 16);
     }
     // Elements 32 block .. + 31 of rows 16 step + 4 h .. + 3 and 8 more: an operand whose sum runs over the rows, in the order in which mma32
     // leaves 16 of its result rows in a lane's registers 8 (step & 1) .. + 7.
     static __device__ __forceinline__ uint4 across(const char* lds, int block, int step, int lane) {
         const int t = lane & 15, row = 16 * step + 4 * (lane >> 5) + (t >> 2);
-        const int run = (4 * block + 2 * ((lane >> 4) & 1) + ((t >> 1) & 1)) ^ exchanged<false>(row);
+        const int run = (4 * block + 2 * ((lane >> 4) & 1) + ((t >> 1) & 1)) ^ exchanged(row);
         const char* at = lds + row * ROW_BYTES + run * 16 + (t & 1) * 8;
         const uint2 lo = read_transposed(at), hi = read_transposed(at + 8 * ROW_BYTES);
         return {lo.x, lo.y, hi.x, hi.y};
@@ -130,6 +130,43 @@ __device__ __forceinline__ float across_halves_max(float x) {
 __device__ __forceinline__ float across_halves_sum(float x) {
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+
+// Which group and tile a workgroup has: groups outermost, and each XCD (workgroups go to the 8 in turn) a run of neighbours, which read
+// the same keys through one L2.  late_first: the last tiles first (of causal rows they are the long ones).
+__device__ __forceinline__ void deal(int tiles, bool late_first, int& group, int& tile) {
+    const int total = gridDim.x, id = blockIdx.x, xcd = id & 7, q = total >> 3, r = total & 7;
+    const int mine = xcd * q + min(xcd, r) + (id >> 3);
+    group = mine / tiles;
+    tile = mine - group * tiles;
+    if (late_first) tile = tiles - 1 - tile;
+}
+
+// Rows of a sequence are counted in 32 bits (the entry points see to it).
+__device__ __forceinline__ int token_of(const AttentionArgs& a, int r) { return a.share == 1 ? r : (int)((uint32_t)r / (uint32_t)a.share); }
+
+// How many keys row r sees.
+__device__ __forceinline__ int seen_by(const AttentionArgs& a, const Sequence& s, int r) {
+    return a.causal ? min(max(token_of(a, r) + (s.lk - s.lq) + 1, 0), s.lk) : s.lk;
+}
+
+// Where row r of a group is in lse and what else has a value per query and head.
+__device__ __forceinline__ int64_t flat_row(const AttentionArgs& a, const Sequence& s, int group, int r) {
+    const int token = token_of(a, r);
+    return (s.q0 + (int64_t)token) * a.heads + group * a.share + (r - token * a.share);
+}
+
+// One row's vector in an operand's layout: run i of lane (.., h) is elements 16 i + 8 h .. + 7; nothing of a row that there is not.
+template <int DT, int DB>
+__device__ __forceinline__ void load_row(const void* data, int64_t row_stride, int64_t head_stride, const AttentionArgs& a, const Sequence& s, int group, int r, int rows,
+                                         int lane, uint4 (&to)[2 * DB]) {
+    const int token = token_of(a, r), head = group * a.share + (r - token * a.share);
+    const typename Elem<DT>::T* from = (const typename Elem<DT>::T*)data + (s.q0 + token) * row_stride + head * head_stride;
+#pragma unroll
+    for (int i = 0; i < 2 * DB; ++i) {
+        const int at = 16 * i + 8 * (lane >> 5);
+        to[i] = load_run<DT>(from + at, r < rows ? a.d - at : 0);
+    }
 }
 
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;

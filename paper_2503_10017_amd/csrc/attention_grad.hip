@@ -1,0 +1,289 @@
+// The gradient of attention (fnn_attention_backward), without a score matrix in memory: with p = exp(scale q k^T - lse) formed again and
+// delta = sum_e dout out,  ds = p (dout v^T - delta),  dq = scale ds k,  dk = scale ds^T q,  dv = p^T dout.
+//
+// Two passes, so that every sum is one workgroup's own and its order fixed: rows by rows for dq (which also leaves delta behind), then
+// keys by keys for dk and dv.  Seven products where five would do if the first pass could add into dk and dv; atomics would, in an order of their own.
+// As in the forward pass the lane owns a row (a key) of the scores and the next product's operand is what the last one left in its registers; the
+// tiles that are read along and across their rows lie in LDS once, for both.
+#include <type_traits>
+
+#include "attention_device.hpp"
+#include "trace.hpp"
+
+namespace fnn {
+
+namespace {
+
+// fp16 weights are formed 2^14 times too large (at most 2^14): those of long rows, 1 / 16384 and less, would lose bits below the
+// type's normal range.  The factor leaves with the result.
+template <int DT>
+constexpr int WEIGHT_SHIFT = DT == CT_F16 ? 14 : 0;
+
+// dq and delta: a wave has 32 rows and runs over tiles of 64 keys, which its workgroup's four waves share.
+template <int DT, int DB, bool DIRECT>
+__global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs a) {
+    constexpr int KEYS = 64, ROWS = 128;
+    using Tile = HeadTile<DT, DB, KEYS>;
+    typedef typename Elem<DT>::T E;
+    __shared__ __attribute__((aligned(16))) char stages[2][2 * Tile::BYTES];
+    const AttentionArgs& f = a.forward;
+    int group, tile;
+    deal(f.row_tiles, f.causal, group, tile);
+    const Sequence s = find_sequence<ROWS>(f, tile);
+    if (s.index < 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = s.lq * f.share, first = s.tile * ROWS, mine = first + wave * 32, r = mine + (lane & 31);
+    const int tiles = (seen_by(f, s, min(first + ROWS, rows) - 1) + KEYS - 1) / KEYS;
+
+    uint4 q[2 * DB], dout[2 * DB];
+    float delta = 0.f, lse = -__builtin_inff();
+    {
+        uint4 out[2 * DB];
+        load_row<DT, DB>(f.q, f.q_row, f.q_head, f, s, group, r, rows, lane, q);
+        load_row<DT, DB>(a.dout, a.dout_row, a.dout_head, f, s, group, r, rows, lane, dout);
+        load_row<DT, DB>(f.out, f.out_row, f.out_head, f, s, group, r, rows, lane, out);
+#pragma unroll
+        for (int i = 0; i < 2 * DB; ++i) {
+            E x[8], y[8];
+            __builtin_memcpy(x, &dout[i], 16);
+            __builtin_memcpy(y, &out[i], 16);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)x[e], (float)y[e], delta);
+        }
+        delta = across_halves_sum(delta);
+        if (r < rows) {
+            const int64_t at = flat_row(f, s, group, r);
+            lse = f.lse[at];
+            if (lane < 32) a.delta[at] = delta;
+        }
+    }
+    // a row that sees no key has minus infinity there; plus infinity makes its weights 0
+    const float base = lse == -__builtin_inff() ? __builtin_inff() : lse * LOG2E, c = f.scale * LOG2E;
+    const int least_seen = mine < rows ? seen_by(f, s, mine) : 0, most_seen = mine < rows ? seen_by(f, s, min(mine + 32, rows) - 1) : 0;
+    const int seen = seen_by(f, s, min(r, rows - 1));
+    f32x16 dq[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) dq[i] = (f32x16)(0.f);
+
+    const E* k = (const E*)f.k + s.k0 * f.k_row + group * f.k_head;
+    const E* v = (const E*)f.v + s.k0 * f.v_row + group * f.v_head;
+    auto stage = [&](char* to, int t) {
+        const int key = t * KEYS, there = min(KEYS, s.lk - key);
+        Tile::template stage<256, DIRECT>(to, k + key * f.k_row, f.k_row, there, f.d, threadIdx.x);
+        Tile::template stage<256, DIRECT>(to + Tile::BYTES, v + key * f.v_row, f.v_row, there, f.d, threadIdx.x);
+    };
+    if (tiles) stage(stages[0], 0);
+    for (int t = 0, turn = 0; t < tiles; ++t, turn ^= 1) {
+        const char* keys = stages[turn];
+        lds_loads_arrived();
+        __syncthreads();
+        if (t + 1 < tiles) stage(stages[turn ^ 1], t + 1);
+        const int key = t * KEYS;
+        if (key >= most_seen) continue;
+#pragma unroll
+        for (int kb = 0; kb < KEYS / 32; ++kb) {
+            f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
+#pragma unroll
+            for (int i = 0; i < 2 * DB; ++i) {
+                p = mma32<DT>(Tile::along(keys, kb, i, lane), q[i], p);
+                ds = mma32<DT>(Tile::along(keys + Tile::BYTES, kb, i, lane), dout[i], ds);
+            }
+#pragma unroll
+            for (int x = 0; x < 16; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x], c, -base));
+            if (key + KEYS > least_seen) {
+                const int left = seen - key - 4 * (lane >> 5);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) p[x] = 32 * kb + tile_row(x, 0) < left ? p[x] : 0.f;
+            }
+#pragma unroll
+            for (int x = 0; x < 16; ++x) ds[x] = p[x] * (ds[x] - delta);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint4 g = round_half<DT>(ds, half);
+#pragma unroll
+                for (int i = 0; i < DB; ++i) dq[i] = mma32<DT>(Tile::across(keys, i, 2 * kb + half, lane), g, dq[i]);
+            }
+        }
+    }
+    if (!a.dq || r >= rows) return;
+    const int token = token_of(f, r), head = group * f.share + (r - token * f.share);
+    E* to = (E*)a.dq + (s.q0 + token) * a.dq_row + head * a.dq_head;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+        float x[2][8];
+        rows_of_eight(dq[i], x);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int at = 32 * i + 16 * p + 8 * (lane >> 5);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[p][e] *= f.scale;
+            if (at < f.d) store_elems<DT>(to + at, f.d - at, x[p]);
+        }
+    }
+}
+
+// dk and dv: a wave has 32 keys and runs over tiles of 32 rows (of all the heads that share the key head), which its workgroup's four waves share.
+template <int DT, int DB, bool DIRECT>
+__global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attention_dkv_kernel(AttentionBackArgs a) {
+    constexpr int KEYS = 128, ROWS = 32;
+    using Tile = HeadTile<DT, DB, ROWS>;
+    typedef typename Elem<DT>::T E;
+    // a stage: the rows' q, their dout, and lse (times log2 e, less the weights' shift) and delta (times the shift)
+    constexpr int STAGE = 2 * Tile::BYTES + 2 * ROWS * 4;
+    __shared__ __attribute__((aligned(16))) char stages[2][STAGE];
+    const AttentionArgs& f = a.forward;
+    int group, tile;
+    deal(a.key_tiles, false, group, tile);
+    const Sequence s = find_sequence<KEYS, true>(f, tile);
+    if (s.index < 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = s.lq * f.share, first = s.tile * KEYS, mine = first + wave * 32, key = mine + (lane & 31);
+    // the first row that sees key j
+    auto sees = [&](int j) { return f.causal ? (int)min((int64_t)rows, max((int64_t)0, (int64_t)f.share * ((int64_t)j - s.lk + s.lq))) : 0; };
+    const int from_row = sees(key), wave_first = sees(mine), wave_all = sees(min(mine + 32, s.lk) - 1);
+
+    uint4 k[2 * DB], v[2 * DB];
+    {
+        const E* at_k = (const E*)f.k + (s.k0 + (int64_t)key) * f.k_row + group * f.k_head;
+        const E* at_v = (const E*)f.v + (s.k0 + (int64_t)key) * f.v_row + group * f.v_head;
+#pragma unroll
+        for (int i = 0; i < 2 * DB; ++i) {
+            const int at = 16 * i + 8 * (lane >> 5), count = key < s.lk ? f.d - at : 0;
+            k[i] = load_run<DT>(at_k + at, count);
+            v[i] = load_run<DT>(at_v + at, count);
+        }
+    }
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) dk[i] = dv[i] = (f32x16)(0.f);
+    const float c = f.scale * LOG2E, unshift = 1.f / (float)(1 << WEIGHT_SHIFT<DT>);
+
+    // Rows of a group are not equally far apart in memory when heads share a key head, so a thread's rows are found one by one.
+    auto stage = [&](char* to, int row0) {
+        constexpr int PER_THREAD = ROWS * Tile::RUNS / 256 > 0 ? ROWS * Tile::RUNS / 256 : 1, THREADS = ROWS * Tile::RUNS / PER_THREAD;
+        const int thread = threadIdx.x;
+        if (THREADS == 256 || thread < THREADS) {
+            const int token0 = token_of(f, row0);
+            const E* of_q = (const E*)f.q + (s.q0 + token0) * f.q_row + group * f.share * f.q_head;
+            const E* of_dout = (const E*)a.dout + (s.q0 + token0) * a.dout_row + group * f.share * a.dout_head;
+#pragma unroll
+            for (int i = 0; i < PER_THREAD; ++i) {
+                const int at = i * THREADS + thread, row = at / Tile::RUNS, run = (at % Tile::RUNS) ^ Tile::exchanged(row), r = row0 + row;
+                const int token = token_of(f, r), head = r - token * f.share;
+                if constexpr (DIRECT) {
+                    const bool there = r < rows && run * 8 < f.d;
+                    const uint32_t chunk = (i * THREADS + (thread & ~63)) * 16;
+                    const uint32_t q_at = (uint32_t)((token - token0) * (int)f.q_row + head * (int)f.q_head + run * 8) * 2;
+                    const uint32_t dout_at = (uint32_t)((token - token0) * (int)a.dout_row + head * (int)a.dout_head + run * 8) * 2;
+                    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(to) + chunk);
+                    load_to_lds(buffer_of(of_q, 0x80000000u), there ? q_at : 0xFFFFFFF0u, lds);
+                    load_to_lds(buffer_of(of_dout, 0x80000000u), there ? dout_at : 0xFFFFFFF0u, lds + Tile::BYTES);
+                } else {
+                    const int count = r < rows ? f.d - run * 8 : 0;
+                    *reinterpret_cast<uint4*>(to + at * 16) = load_run<DT>(of_q + (token - token0) * f.q_row + head * f.q_head + run * 8, count);
+                    *reinterpret_cast<uint4*>(to + Tile::BYTES + at * 16) = load_run<DT>(of_dout + (token - token0) * a.dout_row + head * a.dout_head + run * 8, count);
+                }
+            }
+        }
+        if (thread < ROWS) {
+            const int r = row0 + thread;
+            float lse = __builtin_inff(), delta = 0.f;
+            if (r < rows) {
+                const int64_t at = flat_row(f, s, group, r);
+                lse = f.lse[at];
+                lse = lse == -__builtin_inff() ? __builtin_inff() : lse * LOG2E - (float)WEIGHT_SHIFT<DT>;
+                delta = a.delta[at] * unshift;
+            }
+            float* stats = reinterpret_cast<float*>(to + 2 * Tile::BYTES);
+            stats[thread] = lse;
+            stats[ROWS + thread] = delta;
+        }
+    };
+    const int start = sees(first) / ROWS * ROWS;
+    if (start < rows) stage(stages[0], start);
+    int turn = 0;
+    for (int row = start; row < rows; row += ROWS, turn ^= 1) {
+        const char* now = stages[turn];
+        lds_loads_arrived();
+        __syncthreads();
+        if (row + ROWS < rows) stage(stages[turn ^ 1], row + ROWS);
+        if (row + ROWS <= wave_first || mine >= s.lk) continue;
+        f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
+#pragma unroll
+        for (int i = 0; i < 2 * DB; ++i) {
+            p = mma32<DT>(Tile::along(now, 0, i, lane), k[i], p);
+            ds = mma32<DT>(Tile::along(now + Tile::BYTES, 0, i, lane), v[i], ds);
+        }
+        const float* stats = reinterpret_cast<const float*>(now + 2 * Tile::BYTES) + 4 * (lane >> 5);
+#pragma unroll
+        for (int x = 0; x < 16; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x], c, -stats[tile_row(x, 0)]));
+        if (row < wave_all) {
+            const int least = from_row - row - 4 * (lane >> 5);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) p[x] = tile_row(x, 0) >= least ? p[x] : 0.f;
+        }
+#pragma unroll
+        for (int x = 0; x < 16; ++x) ds[x] = p[x] * __builtin_fmaf(ds[x], unshift, -stats[ROWS + tile_row(x, 0)]);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const uint4 w = round_half<DT>(p, half), g = round_half<DT>(ds, half);
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+                dv[i] = mma32<DT>(Tile::across(now + Tile::BYTES, i, half, lane), w, dv[i]);
+                dk[i] = mma32<DT>(Tile::across(now, i, half, lane), g, dk[i]);
+            }
+        }
+    }
+    if (key >= s.lk) return;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if (!(which ? a.dv : a.dk)) continue;
+        E* to = which ? (E*)a.dv + (s.k0 + (int64_t)key) * a.dv_row + group * a.dv_head : (E*)a.dk + (s.k0 + (int64_t)key) * a.dk_row + group * a.dk_head;
+        const float scale = which ? unshift : f.scale;
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+            float x[2][8];
+            rows_of_eight(which ? dv[i] : dk[i], x);
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int at = 32 * i + 16 * p + 8 * (lane >> 5);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[p][e] *= scale;
+                if (at < f.d) store_elems<DT>(to + at, f.d - at, x[p]);
+            }
+        }
+    }
+}
+
+template <int DT, int DB>
+hipError_t run(const AttentionBackArgs& a, hipStream_t s) {
+    if (a.forward.tq > 0) {
+        const hipError_t e = launch(TK_ATTENTION_BACKWARD, a.forward.direct ? attention_dq_kernel<DT, DB, true> : attention_dq_kernel<DT, DB, false>,
+                                    dim3((unsigned)(a.forward.row_tiles * a.forward.groups)), dim3(256), 0, s, a);
+        if (e != hipSuccess) return e;
+    }
+    if (a.forward.tk < 1 || (!a.dk && !a.dv)) return hipSuccess;
+    return launch(TK_ATTENTION_BACKWARD, a.direct_rows ? attention_dkv_kernel<DT, DB, true> : attention_dkv_kernel<DT, DB, false>,
+                  dim3((unsigned)(a.key_tiles * a.forward.groups)), dim3(256), 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_attention_backward(AttentionBackArgs a, int dtype, hipStream_t s) {
+    const int64_t rows = (int64_t)a.forward.tq * a.forward.share;
+    a.forward.row_tiles = (int)((rows + 127) / 128 + a.forward.batch - 1);
+    a.key_tiles = (int)(((int64_t)a.forward.tk + 127) / 128 + a.forward.batch - 1);
+    const int blocks = (a.forward.d + 31) / 32;
+    auto with_type = [&](auto dt) {
+        constexpr int DT = dt.value;
+        switch (blocks) {
+            case 1: return run<DT, 1>(a, s);
+            case 2: return run<DT, 2>(a, s);
+            case 3: return run<DT, 3>(a, s);
+            default: return run<DT, 4>(a, s);
+        }
+    };
+    return dtype == FNN_F16 ? with_type(std::integral_constant<int, CT_F16>()) : with_type(std::integral_constant<int, CT_BF16>());
+}
+
+}  // namespace fnn

@@ -76,10 +76,11 @@ int32_t check_heads(const fnn_heads* t) {
 }
 bool attention_sizes(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d) {
     return tq >= 0 && tq <= MAX_SLOTS && tk >= 0 && tk <= MAX_SLOTS && batch >= 1 && batch <= MAX_SLOTS / 2 && heads >= 1 && heads <= 65535 && groups >= 1 &&
-           heads % groups == 0 && tq <= MAX_SLOTS / heads && d >= 1 && d <= FNN_MAX_HEAD_DIM;
+           heads % groups == 0 && tq <= (MAX_SLOTS - 1024) / heads && tk <= MAX_SLOTS - 1024 && d >= 1 && d <= FNN_MAX_HEAD_DIM;
 }
 int64_t row_of(const fnn_heads* t) { return t->n > 1 ? t->row_stride : t->d; }
 int64_t head_of(const fnn_heads* t) { return t->heads > 1 ? t->head_stride : t->d; }
+bool same_heads(const fnn_heads* a, const fnn_heads* b) { return a->n == b->n && a->heads == b->heads && a->d == b->d; }
 // Whether every vector starts on a 16-byte boundary, is whole runs of 16 bytes, and a tile's offsets fit 32 bits.
 bool on_runs(const fnn_heads* t) {
     return ((uintptr_t)t->data & 15) == 0 && t->d % 8 == 0 && row_of(t) % 8 == 0 && head_of(t) % 8 == 0 && row_of(t) < ((int64_t)1 << 23);
@@ -327,6 +328,51 @@ int32_t fnn_attention(const fnn_heads* q, const fnn_heads* k, const fnn_heads* v
     a.lse = lse;
     a.partial = (float*)workspace;
     return done(launch_attention(a, q->dtype, (hipStream_t)stream));
+}
+
+size_t fnn_attention_backward_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int32_t batch, int32_t heads, int32_t key_heads, int32_t d) {
+    if (!attention_sizes(tokens_q, tokens_k, batch, heads, key_heads, d)) return 0;
+    return (size_t)tokens_q * heads * sizeof(float);
+}
+
+int32_t fnn_attention_backward(const fnn_heads* dout, const fnn_heads* q, const fnn_heads* k, const fnn_heads* v, const fnn_heads* out,
+                               const float* lse, int32_t batch, const int32_t* cu_q, const int32_t* cu_k, int32_t causal, float scale,
+                               const fnn_heads* dq, const fnn_heads* dk, const fnn_heads* dv, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+    AttentionBackArgs a;
+    memset(&a, 0, sizeof(a));
+    FNN_CHECK(attention_args(q, k, v, batch, cu_q, cu_k, causal, scale, out, a.forward));
+    FNN_CHECK(check_heads(dout));
+    if (!same_heads(dout, q)) return FNN_E_SHAPE;
+    if (dout->dtype != q->dtype) return FNN_E_DTYPE;
+    const fnn_heads* grads[3] = {dq, dk, dv};
+    for (int i = 0; i < 3; ++i) {
+        if (!grads[i]) continue;
+        FNN_CHECK(check_heads(grads[i]));
+        if (!same_heads(grads[i], i ? k : q)) return FNN_E_SHAPE;
+        if (grads[i]->dtype != q->dtype) return FNN_E_DTYPE;
+    }
+    if (q->n > 0 && !lse) return FNN_E_NULL;
+    if (!dq && !dk && !dv) return FNN_OK;
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, (size_t)q->n * q->heads * sizeof(float)));
+    a.forward.lse = const_cast<float*>(lse);
+    a.dout = dout->data;
+    a.dout_row = row_of(dout);
+    a.dout_head = head_of(dout);
+    a.dq = dq ? const_cast<void*>(dq->data) : nullptr;
+    a.dk = dk ? const_cast<void*>(dk->data) : nullptr;
+    a.dv = dv ? const_cast<void*>(dv->data) : nullptr;
+    a.dq_row = dq ? row_of(dq) : 0;
+    a.dq_head = dq ? head_of(dq) : 0;
+    a.dk_row = dk ? row_of(dk) : 0;
+    a.dk_head = dk ? head_of(dk) : 0;
+    a.dv_row = dv ? row_of(dv) : 0;
+    a.dv_head = dv ? head_of(dv) : 0;
+    a.delta = (float*)workspace;
+    // the heads of a group are reached from its first by 32-bit offsets too
+    const int64_t apart = a.forward.share * (head_of(q) > head_of(dout) ? head_of(q) : head_of(dout));
+    a.direct_rows = on_runs(q) && on_runs(dout) && apart < ((int64_t)1 << 28);
+    return done(launch_attention_backward(a, q->dtype, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -91,4 +91,18 @@ struct AttentionArgs {
 size_t attention_workspace(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d);
 hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t s);
 
+// Its gradient: `forward` has q, k, v, out, lse and the tables; dq, dk, dv may be NULL.
+struct AttentionBackArgs {
+    AttentionArgs forward;
+    const void* dout;
+    void* dq;
+    void* dk;
+    void* dv;
+    float* delta;  // [tq][heads]
+    int64_t dout_row, dout_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
+    int32_t key_tiles;
+    int32_t direct_rows;   // q and dout lie on 16-byte boundaries
+};
+hipError_t launch_attention_backward(AttentionBackArgs a, int dtype, hipStream_t s);
+
 }  // namespace fnn

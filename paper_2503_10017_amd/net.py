@@ -201,3 +201,28 @@ def fnn_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: Optio
                              _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream, q.device)),
            "fnn_attention")
     return out, lse
+
+
+def fnn_attention_backward_workspace_bytes(tokens_q: int, tokens_k: int, batch: int, heads: int, key_heads: int, d: int) -> int:
+    return int(load_library().fnn_attention_backward_workspace_bytes(tokens_q, tokens_k, batch, heads, key_heads, d))
+
+
+def fnn_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                           cu_q: Optional[torch.Tensor] = None, cu_k: Optional[torch.Tensor] = None, causal: bool = False,
+                           scale: Optional[float] = None, want_q: bool = True, want_kv: bool = True,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradient of fnn_attention from dout and the forward call's inputs and outputs; returns (dq, dk, dv), None where not wanted."""
+    lib = load_library()
+    tokens, heads, d = q.shape
+    batch, cq, ck = _sequences(cu_q, cu_k)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want_q else None
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if want_kv else None
+    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if want_kv else None
+    if workspace is None:
+        workspace = _workspace(lib.fnn_attention_backward_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d), q.device)
+    grads = [None if g is None else _heads(g, "a gradient") for g in (dq, dk, dv)]
+    _check(lib.fnn_attention_backward(_heads(dout, "dout"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(out, "out"),
+                                      _vector(lse, tokens * heads, torch.float32, "lse"), batch, cq, ck, causal, d ** -0.5 if scale is None else scale,
+                                      *grads, _ptr(workspace), workspace.numel(), _stream_ptr(stream, q.device)),
+           "fnn_attention_backward")
+    return dq, dk, dv

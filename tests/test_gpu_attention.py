@@ -243,3 +243,149 @@ def test_on_another_stream_and_in_a_graph(case):
         got = [t.clone() for t in held]
         assert all(torch.equal(a, b) for a, b in zip(got, prob.call()))
         torch.cuda.synchronize()
+
+
+def check_backward(prob, out, lse, grads):
+    """Every stored product operand (p, ds) is rounded once to the type; p's relative error is weight_slack's, dout v^T and delta are fp32 sums
+    over d, delta's out is the forward call's, off by what check_forward allows."""
+    u = ROUND[prob.dtype]
+    # below the type's normal range: half a step in fp16; in bf16, whose range is fp32's, exp2 and the matrix instructions may give 0 there
+    tiny = 2.0 ** -25 if prob.dtype == torch.float16 else 2.0 ** -126
+    want = [torch.zeros(t.shape, dtype=torch.float64, device=DEV) for t in (prob.q, prob.k, prob.v)]
+    slack = [torch.zeros_like(t) for t in want]
+    for rows, keys, h, g, p, _, mag in prob.sequences():
+        q, k, v, dout, o = (t.double() for t in (prob.q[rows, h], prob.k[keys, g], prob.v[keys, g], prob.dout[rows, h], out[rows, h]))
+        rel = weight_slack(p, mag, prob.d) + 2.2 * 16 * F32
+        dp = dout @ v.t()
+        exact_out = p @ v
+        delta = (dout * exact_out).sum(1, keepdim=True)
+        delta_off = (dout.abs() * ((exact_out - o).abs() + (prob.d + 8) * F32 * o.abs())).sum(1, keepdim=True)
+        dp_off = (prob.d + 8) * F32 * (dout.abs() @ v.abs().t())
+        ds = p * (dp - delta)
+        ds_off = p * (dp_off + delta_off + 4 * F32 * (dp.abs() + delta.abs())) + (rel + u) * ds.abs() + tiny * (1 + (0 if prob.dtype == torch.float16 else dp.abs() + delta.abs()))
+        sums = (max(p.shape) + 8) * F32
+        want[0][rows, h] = prob.scale * (ds @ k)
+        slack[0][rows, h] = prob.scale * ((ds_off + sums * ds.abs()) @ k.abs())
+        want[1][keys, g] += prob.scale * (ds.t() @ q)
+        slack[1][keys, g] += prob.scale * ((ds_off + prob.heads * sums * ds.abs()).t() @ q.abs())
+        want[2][keys, g] += p.t() @ dout
+        slack[2][keys, g] += (p * (rel + u + prob.heads * sums) + tiny * (2.0 ** -14 if prob.dtype == torch.float16 else 1)).t() @ dout.abs()
+    for name, got, w, s in zip(("dq", "dk", "dv"), grads, want, slack):
+        assert_within(got, w, s + rounding(w, prob.dtype), name)
+
+
+def backward(prob, out, lse, **kw):
+    return fnn.fnn_attention_backward(prob.dout, prob.q, prob.k, prob.v, out, lse, prob.cu_q, prob.cu_k, causal=prob.causal, scale=prob.scale, **kw)
+
+
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_backward(case, causal, kind):
+    prob = Problem(*CASES[case], causal, kind)
+    out, lse = prob.call()
+    grads = backward(prob, out, lse)
+    check_backward(prob, out, lse, grads)
+    again = backward(prob, out, lse)
+    assert all(torch.equal(a, b) for a, b in zip(grads, again))
+
+
+def test_backward_large_scores():
+    prob = Problem([257], [300], 2, 2, 64, True, "bf16", spread=12.0, scale=1.0)
+    out, lse = prob.call()
+    check_backward(prob, out, lse, backward(prob, out, lse))
+
+
+def test_backward_of_long_flat_rows_in_fp16():
+    """20000 keys of nearly equal weight 5e-5, below fp16's normal range."""
+    prob = Problem([40], [20000], 1, 1, 32, False, "f16", spread=0.01)
+    out, lse = prob.call()
+    check_forward(prob, out, lse)
+    check_backward(prob, out, lse, backward(prob, out, lse))
+
+
+@pytest.mark.parametrize("case", [([70, 3, 200], [70, 3, 200], 4, 2, 64), ([60, 1], [90, 300], 8, 2, 128), ([60], [60], 2, 1, 40)])
+@pytest.mark.parametrize("layout", [(0, 8, 0, False), (8, 8, 0, True), (1, 1, 1, False)])
+def test_backward_strides_and_parts(case, layout):
+    prob = Problem(*case, True, "bf16")
+    out, lse = prob.call()
+    want = backward(prob, out, lse)
+    only_q, only_kv = backward(prob, out, lse, want_kv=False), backward(prob, out, lse, want_q=False)
+    assert torch.equal(only_q[0], want[0]) and only_q[1] is None and only_kv[0] is None
+    assert torch.equal(only_kv[1], want[1]) and torch.equal(only_kv[2], want[2])
+    prob.q, prob.k, prob.v, prob.dout = (spaced(t, *layout) for t in (prob.q, prob.k, prob.v, prob.dout))
+    got = backward(prob, spaced(out, *layout), lse)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_backward_keeps_to_its_sequences(causal):
+    prob = Problem([70, 0, 130], [70, 40, 130], 4, 2, 64, causal, "f16")
+    out, lse = prob.call()
+    want = backward(prob, out, lse)
+    assert not want[1][70:110].any() and not want[2][70:110].any()      # keys that no query has
+    for t in (prob.q, prob.dout):
+        t[:70] = math.nan                                              # the first sequence's rows: the others' gradients stay as they are
+    got = backward(prob, out, lse)
+    assert torch.equal(got[0][70:], want[0][70:]) and torch.equal(got[1][70:], want[1][70:]) and torch.equal(got[2][70:], want[2][70:])
+    assert torch.isnan(got[0][:70]).all()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_gradient_against_differences(causal):
+    """d/dt of sum(c * attention(q + t u, k + t y, v + t z)) at 0 by central differences of the definition in 64 bits.  The inputs are fp16 values; the
+    gradient's operands are rounded to 2^-11, so a part in 500 of the magnitudes' root mean square is plenty."""
+    prob = Problem([37, 20], [50, 20], 4, 2, 48, causal, "f16")
+    out, lse = prob.call()
+    grads = backward(prob, out, lse)
+    u = [normal(50 + i, *t.shape).double() for i, t in enumerate((prob.q, prob.k, prob.v))]
+    base = [t.double() for t in (prob.q, prob.k, prob.v)]
+
+    def value(t):
+        q, k, v = (b + t * x for b, x in zip(base, u))
+        total, q0, k0 = 0.0, 0, 0
+        for nq, nk in zip(prob.lq, prob.lk):
+            for h in range(prob.heads):
+                g = h // (prob.heads // prob.groups)
+                z = prob.scale * q[q0:q0 + nq, h] @ k[k0:k0 + nk, g].t()
+                if causal:
+                    z = z + torch.full_like(z, -math.inf).triu(1 + nk - nq)
+                total += (prob.dout[q0:q0 + nq, h].double() * (torch.softmax(z, 1) @ v[k0:k0 + nk, g])).sum().item()
+            q0, k0 = q0 + nq, k0 + nk
+        return total
+
+    slope = (value(1e-5) - value(-1e-5)) / 2e-5
+    parts = [(g.double() * x) for g, x in zip(grads, u)]
+    size = math.sqrt(sum((p ** 2).sum().item() for p in parts))
+    assert abs(sum(p.sum().item() for p in parts) - slope) <= size / 50
+
+
+def test_backward_in_a_graph():
+    prob = Problem([300, 200], [300, 200], 4, 2, 64, True, "bf16")
+    ws = torch.empty(fnn.fnn_attention_backward_workspace_bytes(500, 500, 2, 4, 2, 64), dtype=torch.uint8, device=DEV)
+    out, lse = prob.call()
+    backward(prob, out, lse, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = backward(prob, out, lse, workspace=ws)
+    for seed in (4, 21, 22, 4):
+        prob.dout.copy_(normal(seed, *prob.dout.shape, dtype=torch.bfloat16))
+        for t in held:
+            t.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        assert all(torch.equal(a, b) for a, b in zip(got, backward(prob, out, lse)))
+        torch.cuda.synchronize()
+
+
+def test_backward_of_no_queries_or_no_keys():
+    def empty(n, heads):
+        return torch.zeros((n, heads, 64), dtype=torch.float16, device=DEV)
+
+    for nq, nk in ((0, 5), (5, 0), (0, 0)):
+        q, k = empty(nq, 4), empty(nk, 2)
+        out, lse = fnn.fnn_attention(q, k, k)
+        dq, dk, dv = fnn.fnn_attention_backward(q, q, k, k, out, lse)
+        assert dq.shape == q.shape and dk.shape == k.shape and not dq.any() and not dk.any() and not dv.any()

@@ -110,3 +110,52 @@ def test_linear_backward_refusals(lib):  # noqa: F811
     assert call(act=4) == RANGE
     assert call(ws=None) == WORKSPACE and call(ws=0x100008) == WORKSPACE and call(ws_bytes=need - 1) == WORKSPACE
     assert call(dx=None, dw=None) == OK      # nothing wanted
+
+
+def heads(n=10, h=4, d=64, dtype=1, row=None, head=None, data=0x10000, reserved=0):
+    return fnn.net._pack_heads(data, n, h, d, dtype, reserved, h * d if row is None else row, d if head is None else head)
+
+
+def test_attention_refusals(lib):  # noqa: F811
+    assert lib.fnn_attention_workspace_bytes(1000, 1000, 4, 4, 2, 64) == 0
+    need = lib.fnn_attention_workspace_bytes(1, 100000, 1, 4, 2, 64)
+    assert need > 0
+    for sizes in ((-1, 9, 1, 4, 2, 64), (9, -1, 1, 4, 2, 64), (9, 9, 0, 4, 2, 64), (9, 9, 1, 4, 3, 64), (9, 9, 1, 0, 1, 64), (9, 9, 1, 4, 2, 129), (9, 9, 1, 4, 2, 0), (2 ** 30, 9, 1, 4, 2, 64)):
+        assert lib.fnn_attention_workspace_bytes(*sizes) == 0 and lib.fnn_attention_backward_workspace_bytes(*sizes) == 0
+
+    def call(q=heads(), k=heads(h=2), v=heads(h=2), batch=1, cu_q=0x500, cu_k=0x600, scale=0.125, out=heads(data=0x20000), ws=None, ws_bytes=0):
+        return lib.fnn_attention(q, k, v, batch, cu_q, cu_k, 0, scale, out, None, ws, ws_bytes, None)
+
+    for name, h in (("q", 4), ("k", 2), ("v", 2), ("out", 4)):
+        assert call(**{name: None}) == NULL and call(**{name: heads(h=h, data=0)}) == NULL
+        for bad in (heads(n=-1, h=h), heads(n=11, h=h), heads(h=3), heads(h=0), heads(h=h, d=63), heads(h=h, d=129), heads(h=h, d=0), heads(h=h, row=63), heads(h=h, head=63),
+                    heads(h=h, row=2 ** 62), heads(h=h, reserved=1)):
+            if name in ("k", "v") or bad != heads(n=11, h=h):
+                assert call(**{name: bad}) == SHAPE, name
+        assert call(**{name: heads(h=h, dtype=0)}) == DTYPE and call(**{name: heads(h=h, dtype=2)}) == DTYPE and call(**{name: heads(h=h, dtype=5)}) == DTYPE
+    for scale in (0.0, -1.0, math.nan, math.inf):
+        assert call(scale=scale) == RANGE
+    assert call(batch=0) == RANGE
+    assert call(cu_q=None) == NULL and call(cu_k=None) == NULL and call(cu_q=None, cu_k=None, batch=2) == NULL
+    long = dict(q=heads(n=1), out=heads(n=1), k=heads(n=100000, h=2), v=heads(n=100000, h=2))
+    assert call(**long) == WORKSPACE and call(**long, ws=0x100004, ws_bytes=need) == WORKSPACE and call(**long, ws=0x100000, ws_bytes=need - 1) == WORKSPACE
+    assert call(q=heads(n=0, data=0), out=heads(n=0, data=0)) == OK
+
+
+def test_attention_backward_refusals(lib):  # noqa: F811
+    need = lib.fnn_attention_backward_workspace_bytes(10, 10, 1, 4, 2, 64)
+    assert need == 10 * 4 * 4
+
+    def call(dout=heads(), q=heads(), k=heads(h=2), v=heads(h=2), out=heads(), lse=0x700, batch=1, scale=0.125, dq=heads(data=0x20000), dk=heads(h=2, data=0x30000),
+             dv=heads(h=2, data=0x40000), ws=0x100000, ws_bytes=need):
+        return lib.fnn_attention_backward(dout, q, k, v, out, lse, batch, 0x500, 0x600, 0, scale, dq, dk, dv, ws, ws_bytes, None)
+
+    for name in ("dout", "q", "k", "v", "out", "lse"):
+        assert call(**{name: None}) == NULL, name
+    for name, h in (("dout", 4), ("out", 4), ("dq", 4), ("dk", 2), ("dv", 2)):
+        for bad in (heads(n=11, h=h), heads(h=h + 1), heads(h=h, d=32), heads(h=h, row=1)):
+            assert call(**{name: bad}) == SHAPE, name
+        assert call(**{name: heads(h=h, dtype=2)}) == DTYPE and call(**{name: heads(h=h, dtype=0)}) == DTYPE
+    assert call(scale=0.0) == RANGE and call(batch=-1) == RANGE
+    assert call(ws=None) == WORKSPACE and call(ws=0x100080) == WORKSPACE and call(ws_bytes=need - 1) == WORKSPACE
+    assert call(dq=None, dk=None, dv=None) == OK
