@@ -112,7 +112,7 @@ typedef struct {
  * gradient takes it.  Strides are free (heads of a token may also lie apart by more than a token); vectors on 16-byte boundaries are
  * faster.  What lies outside the sequences is neither read for its value nor written.  Within a sequence keys and values must be finite where
  * another query of the same call does not see them yet: a causal tile multiplies such values by 0.
- * Scores, softmax and sums are fp32; the weights exp(..) <= 1 are rounded to the values' type for the second product.
+ * Scores, softmax and sums are fp32; the weights are rounded to the values' type for the second product.
  * The workspace is for few queries with many keys, which are split and joined in a fixed order.
  * Errors: FNN_E_NULL, FNN_E_SHAPE, FNN_E_DTYPE, FNN_E_RANGE (scale, batch < 1), FNN_E_WORKSPACE.
  */

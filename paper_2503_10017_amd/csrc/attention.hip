@@ -21,7 +21,7 @@ struct Rows {
     static constexpr int KB = KEYS / 32;
     uint4 q[QB][2 * DB];
     f32x16 out[QB][DB];
-    float top[QB], sum[QB];  // of the keys so far: the largest score, and (this half's share of) the sum of exp2(c (score - top))
+    float top[QB], sum[QB];  // of the keys so far: a score that none exceeds by 8 / c, and (this half's share of) the sum of exp2(c (score - top))
 
     __device__ __forceinline__ void begin(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, int lane) {
 #pragma unroll
@@ -53,7 +53,7 @@ struct Rows {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int b = 0; b < QB; ++b) {
-            float most = top[b];
+            float most = -__builtin_inff();
             if (mask) {
                 const int left = seen[b] - key - 4 * (lane >> 5);
 #pragma unroll
@@ -66,10 +66,20 @@ struct Rows {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, score[b][kb][r]);
             most = across_halves_max(most);
+            // What is so far is rescaled only where some row's maximum rises by a factor of 2^8 and more: weights may as well reach 256.
+            if (__ballot(!(most * c <= __builtin_fmaf(top[b], c, 8.f)))) {
+                most = __builtin_fmaxf(most, top[b]);
+                const float base = most > -__builtin_inff() ? most * c : 0.f;
+                const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(top[b], c, -base));
+                top[b] = most;
+                sum[b] *= keep;
+#pragma unroll
+                for (int i = 0; i < DB; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) out[b][i][r] *= keep;
+            }
             // rows that have seen no key yet stay at minus infinity; anything finite in its place makes their weights 0
-            const float base = most > -__builtin_inff() ? most * c : 0.f;
-            const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(top[b], c, -base));
-            top[b] = most;
+            const float base = top[b] > -__builtin_inff() ? top[b] * c : 0.f;
             float more = 0.f;
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
@@ -78,14 +88,10 @@ struct Rows {
                     score[b][kb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[b][kb][r], c, -base));
                     more += score[b][kb][r];
                 }
-            sum[b] = __builtin_fmaf(sum[b], keep, more);
-#pragma unroll
-            for (int i = 0; i < DB; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) out[b][i][r] *= keep;
+            sum[b] += more;
         }
         __builtin_amdgcn_sched_barrier(0);
-        // the weights are at most 1 and rounded to the values' type, as the matrix instructions take them; their sum is of the unrounded ones
+        // the weights are at most 256 and rounded to the values' type, as the matrix instructions take them; their sum is of the unrounded ones
 #pragma unroll
         for (int t = 0; t < 2 * KB; ++t) {
             uint4 p[QB];

@@ -66,8 +66,13 @@ template <int DT, int DIM_BLOCKS, int ROWS>
 struct HeadTile {
     typedef typename Elem<DT>::T E;
     static constexpr int RUNS = DIM_BLOCKS == 1 ? 4 : DIM_BLOCKS == 2 ? 8 : 16, ROW_BYTES = RUNS * 16, BYTES = ROWS * ROW_BYTES;
-    // 8 rows read at one run (along) lie in 8 different sets of banks, and so do 4 rows read at a pair of runs (across).
-    static __device__ __forceinline__ int exchanged(int row) { return RUNS >= 8 ? ((row & 3) << 1 | (row >> 2 & 1)) : ((row & 2) | (row >> 2 & 1)); }
+    // LDS serves 256 bytes at a time: 16 lanes of an along() read (16 rows at one run) and 32 of an across() read (4 rows at 4 runs) have to lie in
+    // different 16-byte columns of 256 bytes, which hold 4, 2 or 1 rows.
+    static __device__ __forceinline__ int exchanged(int row) {
+        if constexpr (RUNS == 4) return row >> 2 & 3;
+        else if constexpr (RUNS == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        else return (row & 3) << 2 | (row >> 2 & 3);
+    }
 
     // Rows base[0 .. rows), the rest zero, by THREADS threads of which this is number `thread` (a wave's start together).  DIRECT: runs lie on
     // 16-byte boundaries and offsets fit, so they go straight to LDS and arrive later (lds_loads_arrived); otherwise through registers.
@@ -103,24 +108,19 @@ struct HeadTile {
     static __device__ __forceinline__ uint4 across(const char* lds, int block, int step, int lane) {
         const int t = lane & 15, row = 16 * step + 4 * (lane >> 5) + (t >> 2);
         const int run = (4 * block + 2 * ((lane >> 4) & 1) + ((t >> 1) & 1)) ^ exchanged(row);
-        const char* at = lds + row * ROW_BYTES + run * 16 + (t & 1) * 8;
-        const uint2 lo = read_transposed(at), hi = read_transposed(at + 8 * ROW_BYTES);
+        const char* at = lds + row * ROW_BYTES + (t & 1) * 8;
+        const uint2 lo = read_transposed(at + run * 16), hi = read_transposed(at + 8 * ROW_BYTES + (run ^ 2) * 16);  // rows 8 apart are exchanged by 2 more
         return {lo.x, lo.y, hi.x, hi.y};
     }
 };
 
-// Eight fp32 values as an operand's 16 bytes, each rounded to nearest even.
-template <int DT>
-__device__ __forceinline__ uint4 round_run(float a, float b, float c, float d, float e, float f, float g, float h) {
-    typename Elem<DT>::T raw[8] = {(typename Elem<DT>::T)a, (typename Elem<DT>::T)b, (typename Elem<DT>::T)c, (typename Elem<DT>::T)d,
-                                   (typename Elem<DT>::T)e, (typename Elem<DT>::T)f, (typename Elem<DT>::T)g, (typename Elem<DT>::T)h};
-    uint4 v;
-    __builtin_memcpy(&v, raw, 16);
-    return v;
-}
+// Registers 8 half .. + 7 of a block of results as an operand's 16 bytes, each rounded to nearest even.
 template <int DT>
 __device__ __forceinline__ uint4 round_half(const f32x16& x, int half) {
-    return round_run<DT>(x[8 * half], x[8 * half + 1], x[8 * half + 2], x[8 * half + 3], x[8 * half + 4], x[8 * half + 5], x[8 * half + 6], x[8 * half + 7]);
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, round_two<DT>(x[8 * half + 2 * i], x[8 * half + 2 * i + 1]));
+    return {v[0], v[1], v[2], v[3]};
 }
 
 __device__ __forceinline__ float across_halves_max(float x) {

@@ -124,13 +124,16 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
 
 // dk and dv: a wave has 32 keys and runs over tiles of 32 rows (of all the heads that share the key head), which its workgroup's four waves share.
 template <int DT, int DB, bool DIRECT>
-__global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attention_dkv_kernel(AttentionBackArgs a) {
+__global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs a) {
     constexpr int KEYS = 128, ROWS = 32;
+    constexpr bool KEYS_IN_LDS = DB > 2;  // long vectors: dk, dv, k and v together are more registers than two waves a SIMD have, so k is read again and again
     using Tile = HeadTile<DT, DB, ROWS>;
+    using KeyTile = HeadTile<DT, DB, KEYS>;
     typedef typename Elem<DT>::T E;
     // a stage: the rows' q, their dout, and lse (times log2 e, less the weights' shift) and delta (times the shift)
     constexpr int STAGE = 2 * Tile::BYTES + 2 * ROWS * 4;
     __shared__ __attribute__((aligned(16))) char stages[2][STAGE];
+    __shared__ __attribute__((aligned(16))) char key_tile[KEYS_IN_LDS ? KeyTile::BYTES : 16];
     const AttentionArgs& f = a.forward;
     int group, tile;
     deal(a.key_tiles, false, group, tile);
@@ -142,14 +145,16 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attention_dkv_kernel(Att
     auto sees = [&](int j) { return f.causal ? (int)min((int64_t)rows, max((int64_t)0, (int64_t)f.share * ((int64_t)j - s.lk + s.lq))) : 0; };
     const int from_row = sees(key), wave_first = sees(mine), wave_all = sees(min(mine + 32, s.lk) - 1);
 
-    uint4 k[2 * DB], v[2 * DB];
+    uint4 k[KEYS_IN_LDS ? 1 : 2 * DB], v[2 * DB];
+    if constexpr (KEYS_IN_LDS)
+        KeyTile::template stage<256, false>(key_tile, (const E*)f.k + (s.k0 + (int64_t)first) * f.k_row + group * f.k_head, f.k_row, s.lk - first, f.d, threadIdx.x);
     {
         const E* at_k = (const E*)f.k + (s.k0 + (int64_t)key) * f.k_row + group * f.k_head;
         const E* at_v = (const E*)f.v + (s.k0 + (int64_t)key) * f.v_row + group * f.v_head;
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) {
             const int at = 16 * i + 8 * (lane >> 5), count = key < s.lk ? f.d - at : 0;
-            k[i] = load_run<DT>(at_k + at, count);
+            if constexpr (!KEYS_IN_LDS) k[i] = load_run<DT>(at_k + at, count);
             v[i] = load_run<DT>(at_v + at, count);
         }
     }
@@ -211,7 +216,7 @@ __global__ __launch_bounds__(256, DB <= 2 ? 2 : 1) void attention_dkv_kernel(Att
         f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
 #pragma unroll
         for (int i = 0; i < 2 * DB; ++i) {
-            p = mma32<DT>(Tile::along(now, 0, i, lane), k[i], p);
+            p = mma32<DT>(Tile::along(now, 0, i, lane), KEYS_IN_LDS ? KeyTile::along(key_tile, wave, i, lane) : k[KEYS_IN_LDS ? 0 : i], p);
             ds = mma32<DT>(Tile::along(now + Tile::BYTES, 0, i, lane), v[i], ds);
         }
         const float* stats = reinterpret_cast<const float*>(now + 2 * Tile::BYTES) + 4 * (lane >> 5);

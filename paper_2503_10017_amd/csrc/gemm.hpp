@@ -8,7 +8,8 @@ namespace fnn {
 // How an operand lies in memory: its rows run along k, or its rows are the k's and run along m (n).
 enum : int { ROWS = 0, COLUMNS = 1 };
 
-constexpr int STEP_BYTES = 128;  // of every row of a tile, per step: 64 elements of 16 bits, 32 of 32
+constexpr int STEP_BYTES = 64;  // of every row of a tile, per step: 32 elements of 16 bits, 16 of 32
+constexpr int STAGES = 3;
 
 // Who works on what: neighbouring workgroups are dealt to the 8 XCDs in turn, so each XCD is given a run of tiles of its own, in blocks
 // of 8 tiles of rows by as many tiles of columns as it takes, which share their operands in its L2.
@@ -29,18 +30,18 @@ __device__ __forceinline__ TileAt tile_at(const GemmArgs& a) {
     return t;
 }
 
-// One operand's tile of T rows (columns) and one step of k.  In LDS, ROWS: [T][128 bytes], the 16-byte runs of row r exchanged by
-// r & 7 so that 8 rows read at one run lie in different banks; COLUMNS: [k][T], the runs of row k exchanged by pairs by k & 3, so
-// that the four rows of a transposing read do (16-bit elements).
+// One operand's tile of T rows (columns) and one step of k, in LDS.  ROWS: [T][64 bytes]; COLUMNS: [k][T].  LDS serves 256 bytes at a time, so
+// the 16-byte runs of a row are exchanged such that what one instruction reads together lies in different columns of 256 bytes: 16 rows
+// at one run (ROWS), 4 rows at 4 runs (COLUMNS of 16 bits, transposing reads), rows k and k + 4 at 128 bytes (COLUMNS of 32 bits).
 template <int DT, int T, int THREADS, int LAYOUT>
 struct Operand {
     typedef typename Elem<DT>::T E;
     static constexpr int ES = sizeof(E), N = Elem<DT>::N, STEP = STEP_BYTES / ES;
-    static constexpr int RUNS = T * 8, PER_THREAD = RUNS / THREADS;
-    static constexpr int ROW_RUNS = LAYOUT == ROWS ? 8 : T * ES / 16;  // 16-byte runs in a row of the tile
+    static constexpr int RUNS = T * 4, PER_THREAD = RUNS / THREADS;
+    static constexpr int ROW_RUNS = LAYOUT == ROWS ? 4 : T * ES / 16;  // 16-byte runs in a row of the tile
     static_assert(RUNS % THREADS == 0 && THREADS % ROW_RUNS == 0, "every thread's runs are at one place of their rows");
     static constexpr int ROWS_APART = THREADS / ROW_RUNS;
-    static __device__ __forceinline__ int exchanged(int row) { return LAYOUT == ROWS ? (row & 7) : ES == 2 ? ((row & 3) << 1) : 0; }
+    static __device__ __forceinline__ int exchanged(int row) { return LAYOUT == ROWS ? (row >> 2 & 3) : ES == 2 ? (row & 3) << 2 : (row >> 2 & 1) << 3; }
 
     const E* base;      // ROWS: the tile's first row, at the first k of the split; COLUMNS: the first k's row, at the tile's first column
     int64_t stride;     // elements
@@ -52,7 +53,7 @@ struct Operand {
     __device__ __forceinline__ void begin(const void* data, int64_t stride_, int64_t first, int64_t total, int64_t k0) {
         stride = stride_;
         const int row = threadIdx.x / ROW_RUNS, run = (threadIdx.x % ROW_RUNS) ^ exchanged(row);
-        static_assert(LAYOUT == COLUMNS ? ROWS_APART % 4 == 0 : ROWS_APART % 8 == 0, "the exchange is the same for all of a thread's runs");
+        static_assert(ROWS_APART % (LAYOUT == ROWS ? 16 : ES == 2 ? 4 : 8) == 0, "the exchange is the same for all of a thread's runs");
         col = run * N;
         have = (int)min((int64_t)T, total - first);
         base = (const E*)data + (LAYOUT == ROWS ? first * stride + k0 : k0 * stride + first);
@@ -86,19 +87,19 @@ struct Operand {
     }
     __device__ __forceinline__ void advance() { base += LAYOUT == ROWS ? (int64_t)STEP : STEP * stride; }
 
-    // A matrix instruction's operand: rows 32 block .. + 31, the kk-th quarter of the step's k's.
+    // A matrix instruction's operand: rows 32 block .. + 31, the kk-th half of the step's k's.
     static __device__ __forceinline__ uint4 fragment(const char* lds, int block, int kk, int lane) {
         const int c = lane & 31, h = lane >> 5;
         if constexpr (LAYOUT == ROWS) {
-            return *reinterpret_cast<const uint4*>(lds + block * (32 * STEP_BYTES) + c * STEP_BYTES + (((2 * kk + h) ^ (c & 7)) << 4));
+            return *reinterpret_cast<const uint4*>(lds + block * (32 * STEP_BYTES) + c * STEP_BYTES + (((2 * kk + h) ^ (c >> 2 & 3)) << 4));
         } else if constexpr (ES == 2) {
             const int t = lane & 15, row = 16 * kk + 8 * h + (t >> 2);
-            const int run = (4 * block + 2 * ((lane >> 4) & 1) + ((t >> 1) & 1)) ^ ((t >> 2) << 1);
+            const int run = (4 * block + 2 * ((lane >> 4) & 1) + ((t >> 1) & 1)) ^ ((t >> 2) << 2);
             const char* at = lds + row * (T * ES) + run * 16 + (t & 1) * 8;
             const uint2 lo = read_transposed(at), hi = read_transposed(at + 4 * T * ES);
             return {lo.x, lo.y, hi.x, hi.y};
         } else {
-            const char* at = lds + (8 * kk + 4 * h) * (T * ES) + (32 * block + c) * ES;
+            const char* at = lds + (8 * kk + 4 * h) * (T * ES) + (((8 * block + (c >> 2)) ^ (h << 3)) << 4) + (c & 3) * 4;
             uint4 v;
             v.x = *reinterpret_cast<const uint32_t*>(at);
             v.y = *reinterpret_cast<const uint32_t*>(at + T * ES);
@@ -140,11 +141,11 @@ __device__ __forceinline__ void finish_run(const GemmArgs& a, int64_t m, int n, 
 }
 
 template <int DT, int TM, int TN, int WAVES_M, int WAVES_N, int LA, int LB, bool DIRECT>
-__global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gemm_kernel(GemmArgs a) {
+__global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 2) void gemm_kernel(GemmArgs a) {
     constexpr int THREADS = WAVES_M * WAVES_N * 64, BM = TM / WAVES_M / 32, BN = TN / WAVES_N / 32;
     using OpA = Operand<DT, TM, THREADS, LA>;
     using OpB = Operand<DT, TN, THREADS, LB>;
-    __shared__ __attribute__((aligned(16))) char stage0[(TM + TN) * STEP_BYTES], stage1[(TM + TN) * STEP_BYTES];
+    __shared__ __attribute__((aligned(16))) char stages[STAGES][(TM + TN) * STEP_BYTES];
     const TileAt tile = tile_at(a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WAVES_M, wn = wave / WAVES_M;
@@ -183,65 +184,98 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64) void gemm_kernel(GemmArgs a)
             opb.put(to + TM * STEP_BYTES, held_b);
         }
     };
+    uint4 fa[2][BM], fb[2][BN];
+    auto read = [&](const char* from, int kk) {
+#pragma unroll
+        for (int j = 0; j < BN; ++j) fb[kk][j] = OpB::fragment(from + TM * STEP_BYTES, wn * BN + j, kk, lane);
+#pragma unroll
+        for (int i = 0; i < BM; ++i) fa[kk][i] = OpA::fragment(from, wm * BM + i, kk, lane);
+    };
+    // the first half's operands have been read; the second's are while the first half is multiplied
     auto multiply = [&](const char* from) {
-        uint4 fa[2][BM], fb[2][BN];
-        auto read = [&](int kk) {
+        read(from, 1);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int j = 0; j < BN; ++j) fb[kk & 1][j] = OpB::fragment(from + TM * STEP_BYTES, wn * BN + j, kk, lane);
-#pragma unroll
-            for (int i = 0; i < BM; ++i) fa[kk & 1][i] = OpA::fragment(from, wm * BM + i, kk, lane);
-        };
-        read(0);
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-            if (kk < 3) read(kk + 1);
+        for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
             for (int i = 0; i < BM; ++i)
 #pragma unroll
-                for (int j = 0; j < BN; ++j) acc[i][j] = mma32<DT>(fb[kk & 1][j], fa[kk & 1][i], acc[i][j]);
+                for (int j = 0; j < BN; ++j) acc[i][j] = mma32<DT>(fb[kk][j], fa[kk][i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
     };
-    // A step: what was asked for has arrived, in every wave; the other stage, which everyone has left, is filled; this one is multiplied.
-    auto step = [&](char* now, char* next, bool more) {
-        if constexpr (DIRECT) lds_loads_arrived();
-        __syncthreads();
-        if (more) get(next);
+    // A step: what was asked for two steps ago has arrived, in every wave; the stage that everyone has left is filled; this one is multiplied.
+    auto step = [&](int stage, int s) {
+        char* now = stages[stage];
+        char* next = stages[(stage + 2) % STAGES];
+        if (s + 1 < s1) lds_loads_left<OpA::PER_THREAD + OpB::PER_THREAD>();
+        else lds_loads_left<0>();
+        meet();
+        read(now, 0);
+        if (s + 2 < s1) get(next);
         multiply(now);
-        if (more) put(next);
     };
-    if (s0 < s1) {
-        get(stage0);
-        put(stage0);
-    }
-    for (int s = s0; s < s1; s += 2) {
-        step(stage0, stage1, s + 1 < s1);
-        if (s + 1 < s1) step(stage1, stage0, s + 2 < s1);
+    if constexpr (DIRECT) {
+        if (s0 < s1) get(stages[0]);
+        if (s0 + 1 < s1) get(stages[1]);
+        for (int s = s0; s < s1; s += 3) {
+            step(0, s);
+            if (s + 1 < s1) step(1, s + 1);
+            if (s + 2 < s1) step(2, s + 2);
+        }
+    } else {
+        // one step ahead: stage s mod 2
+        if (s0 < s1) {
+            get(nullptr);
+            put(stages[0]);
+        }
+        for (int s = s0; s < s1; ++s) {
+            __syncthreads();
+            const bool more = s + 1 < s1;
+            read(stages[(s - s0) & 1], 0);
+            if (more) get(nullptr);
+            multiply(stages[(s - s0) & 1]);
+            if (more) put(stages[(s - s0 + 1) & 1]);
+        }
     }
 
-    const int c = lane & 31, h = lane >> 5;
+    // The results go through LDS, 32 rows of a wave at a time, so that 8 lanes have 64 consecutive columns of a row: whole lines of y, residual and
+    // pre instead of 32-byte pieces of 32 rows.  As in the tiles, the runs of a row are exchanged by its number.
+    __syncthreads();
+    static_assert(BN == 2 && 4 * 8192 <= sizeof(stages), "a wave's 32 rows have 64 columns and 8 KB");
+    char* mine = &stages[0][0] + wave * 8192;
+    const int c = lane & 31, h = lane >> 5, n = n0 + wn * 64 + 8 * (lane & 7);
 #pragma unroll
     for (int i = 0; i < BM; ++i) {
-        const int64_t m = m0 + (wm * BM + i) * 32 + c;
 #pragma unroll
-        for (int j = 0; j < BN; ++j) {
-            float v[2][8];
-            rows_of_eight(acc[i][j], v);
+        for (int j = 0; j < BN; ++j)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const int n = n0 + (wn * BN + j) * 32 + 16 * p + 8 * h;
-                if (m >= a.m || n >= a.n) continue;
-                if (a.splits > 1) {
-                    // shares lie in whole tiles, so they need no edge
-                    float* to = a.partial + (((int64_t)tile.split * a.tiles_m * TM + m) * a.tiles_n * TN + n);
-                    float lo[4] = {v[p][0], v[p][1], v[p][2], v[p][3]}, hi[4] = {v[p][4], v[p][5], v[p][6], v[p][7]};
-                    store_elems<CT_F32>(to, 4, lo);
-                    store_elems<CT_F32>(to + 4, 4, hi);
-                } else {
-                    finish_run<DT>(a, m, n, a.n - n, v[p]);
-                }
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(mine + c * 256 + (((8 * j + 2 * g + h) ^ (c & 15)) << 4)) =
+                    f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
+            const int row = 8 * part + (lane >> 3);
+            const int64_t m = m0 + (wm * BM + i) * 32 + row;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(mine + row * 256 + (((2 * (lane & 7) + e) ^ (row & 15)) << 4));
+                v[4 * e] = x[0], v[4 * e + 1] = x[1], v[4 * e + 2] = x[2], v[4 * e + 3] = x[3];
+            }
+            if (m >= a.m || n >= a.n) continue;
+            if (a.splits > 1) {
+                // shares lie in whole tiles, so they need no edge
+                float* to = a.partial + (((int64_t)tile.split * a.tiles_m * TM + m) * a.tiles_n * TN + n);
+                reinterpret_cast<f32x4*>(to)[0] = f32x4{v[0], v[1], v[2], v[3]};
+                reinterpret_cast<f32x4*>(to)[1] = f32x4{v[4], v[5], v[6], v[7]};
+            } else {
+                finish_run<DT>(a, m, n, a.n - n, v);
             }
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 

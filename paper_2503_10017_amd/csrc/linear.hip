@@ -118,26 +118,26 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float* partial,
     }
 }
 
-// The tile and the number of shares that a product is split into, from its sizes alone.
+// The tile (256 x 128 or 128 x 128) and the number of shares that a product is split into, from its sizes alone.
 struct Plan {
-    int tile, splits;
+    int tile_m, splits;
 };
+constexpr int TILE_N = 128;
 constexpr int64_t round_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 Plan plan_of(int64_t m, int64_t n, int64_t k, int dtype) {
-    const int64_t step = dtype == FNN_F32 ? 32 : 64, steps = (k + step - 1) / step;
-    const int64_t big = round_to(m, 256) / 256 * (round_to(n, 256) / 256), small = round_to(m, 128) / 128 * (round_to(n, 128) / 128);
+    const int64_t step = dtype == FNN_F32 ? 16 : 32, steps = (k + step - 1) / step;
+    const int64_t across = round_to(n, TILE_N) / TILE_N, big = round_to(m, 256) / 256 * across;
     Plan p = {128, 1};
-    int64_t tiles = small;
-    if (dtype != FNN_F32 && big * steps >= 128 * 8) p.tile = 256, tiles = big;
-    const int64_t wanted = p.tile == 256 ? 256 : 512;
-    int64_t splits = wanted / (tiles > 0 ? tiles : 1);
-    if (splits > steps / 4) splits = steps / 4;
+    int64_t tiles = round_to(m, 128) / 128 * across;
+    if (dtype != FNN_F32 && big >= 256) p.tile_m = 256, tiles = big;
+    int64_t splits = 512 / (tiles > 0 ? tiles : 1);
+    if (splits > steps / 8) splits = steps / 8;
     if (splits > 32) splits = 32;
     p.splits = splits < 1 ? 1 : (int)splits;
     return p;
 }
 size_t partial_bytes(int64_t m, int64_t n, const Plan& p) {
-    return p.splits > 1 ? (size_t)p.splits * round_to(m, p.tile) * round_to(n, p.tile) * sizeof(float) : 0;
+    return p.splits > 1 ? (size_t)p.splits * round_to(m, p.tile_m) * round_to(n, TILE_N) * sizeof(float) : 0;
 }
 
 // Whether an operand's runs of 16 bytes lie on 16-byte boundaries, a tile's offsets fit 32 bits and k ends with a run.
@@ -149,24 +149,21 @@ bool direct(const void* data, int64_t stride, int64_t rows, int64_t k, int dtype
 
 template <int DT, int LA, int LB>
 hipError_t run_gemm(GemmArgs a, bool is_direct, const Plan& p, int kind, hipStream_t s) {
-    a.tiles_m = (int)(round_to(a.m, p.tile) / p.tile);
-    a.tiles_n = (int)(round_to(a.n, p.tile) / p.tile);
+    a.tiles_m = (int)(round_to(a.m, p.tile_m) / p.tile_m);
+    a.tiles_n = (int)(round_to(a.n, TILE_N) / TILE_N);
     a.splits = p.splits;
     const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n * a.splits));
     hipError_t e;
-    if constexpr (DT == CT_F32) {
-        e = is_direct ? launch(kind, gemm_kernel<DT, 128, 128, 2, 2, LA, LB, true>, grid, dim3(256), 0, s, a)
-                      : launch(kind, gemm_kernel<DT, 128, 128, 2, 2, LA, LB, false>, grid, dim3(256), 0, s, a);
+    if (DT != CT_F32 && p.tile_m == 256) {
+        if constexpr (DT != CT_F32)
+            e = is_direct ? launch(kind, gemm_kernel<DT, 256, TILE_N, 2, 2, LA, LB, true>, grid, dim3(256), 0, s, a)
+                          : launch(kind, gemm_kernel<DT, 256, TILE_N, 2, 2, LA, LB, false>, grid, dim3(256), 0, s, a);
     } else {
-        if (p.tile == 256)
-            e = is_direct ? launch(kind, gemm_kernel<DT, 256, 256, 2, 4, LA, LB, true>, grid, dim3(512), 0, s, a)
-                          : launch(kind, gemm_kernel<DT, 256, 256, 2, 4, LA, LB, false>, grid, dim3(512), 0, s, a);
-        else
-            e = is_direct ? launch(kind, gemm_kernel<DT, 128, 128, 2, 2, LA, LB, true>, grid, dim3(256), 0, s, a)
-                          : launch(kind, gemm_kernel<DT, 128, 128, 2, 2, LA, LB, false>, grid, dim3(256), 0, s, a);
+        e = is_direct ? launch(kind, gemm_kernel<DT, 128, TILE_N, 2, 2, LA, LB, true>, grid, dim3(256), 0, s, a)
+                      : launch(kind, gemm_kernel<DT, 128, TILE_N, 2, 2, LA, LB, false>, grid, dim3(256), 0, s, a);
     }
     if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t pitch = (int64_t)a.tiles_n * p.tile, share = pitch * a.tiles_m * p.tile, runs = (int64_t)((a.n + 7) / 8) * a.m;
+    const int64_t pitch = (int64_t)a.tiles_n * TILE_N, share = pitch * a.tiles_m * p.tile_m, runs = (int64_t)((a.n + 7) / 8) * a.m;
     return launch(kind, gemm_join_kernel<DT>, dim3((unsigned)((runs + 255) / 256)), dim3(256), 0, s, a, pitch, share);
 }
 

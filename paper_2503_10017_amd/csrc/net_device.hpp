@@ -28,6 +28,14 @@ struct Elem<CT_BF16> {
     static constexpr int N = 8;
 };
 
+// Two values rounded to nearest even, as a vector: converted one by one, bf16 pairs take four instructions instead of one.
+template <int DT>
+__device__ __forceinline__ auto round_two(float a, float b) {
+    typedef float two __attribute__((ext_vector_type(2)));
+    typedef typename Elem<DT>::T pair __attribute__((ext_vector_type(2)));
+    return __builtin_convertvector((two{a, b}), pair);
+}
+
 // N elements as fp32 from p, of which the first `count` exist (the rest are 0).  p need only be aligned to an element: global
 // memory takes 16-byte accesses at any address, and rows of odd width or stride keep one load per 16 bytes that way.
 template <int DT, int N = Elem<DT>::N>
@@ -47,7 +55,11 @@ __device__ __forceinline__ void store_elems(typename Elem<DT>::T* p, int count, 
     if (count >= N) {
         typename Elem<DT>::T raw[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) raw[e] = (typename Elem<DT>::T)v[e];
+        for (int e = 0; e < N; e += 2) {
+            const auto pair = round_two<DT>(v[e], v[e + 1]);
+            raw[e] = pair[0];
+            raw[e + 1] = pair[1];
+        }
         __builtin_memcpy(p, raw, sizeof(raw));
     } else {
 #pragma unroll
@@ -216,6 +228,17 @@ __device__ __forceinline__ uint32_t lds_address(const char* lds) {
 // waits for it (vmcnt) first, and then meets the other waves at a barrier.
 __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(buffer) : "m0", "memory");
+}
+// All but this wave's last N loads have arrived (no others are under way), and its reads of LDS before them are done.
+template <int N>
+__device__ __forceinline__ void lds_loads_left() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(N) : "memory");
+}
+// A barrier alone, where the waits before it were chosen by hand; no access moves across it.
+__device__ __forceinline__ void meet() {
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
 }
 // This wave's loads have arrived, and its reads of LDS before them are done.
 __device__ __forceinline__ void lds_loads_arrived() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory"); }

@@ -10,7 +10,7 @@ from typing import Optional
 
 import torch
 
-from .binding import _DTYPES, FnnError, _pack_map, _ptr, _stream_ptr, _workspace, load_library
+from .binding import _DTYPES, FnnError, _pack_map, _ptr, _workspace, load_library
 
 
 def _matrix(t: Optional[torch.Tensor], what: str):
@@ -39,6 +39,11 @@ def _vector(t: Optional[torch.Tensor], count: int, dtype, what: str):
     return t.data_ptr()
 
 
+def _stream_ptr(stream, device):
+    # the current stream's handle as it stands: making the Stream object that names it takes 2 us, as long as these operators take on few tokens
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _check(status: int, where: str):
     if status != 0:
         raise FnnError(status, where)
@@ -58,7 +63,7 @@ def fnn_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias:
     n, d = x.shape
     wt = _weight_dtype(x, weight, bias)
     if out is None:
-        out = torch.empty((n, d), dtype=x.dtype, device=x.device)
+        out = torch.empty_like(x)
     mean = rstd = None
     if want_stats:
         mean = torch.empty(n, dtype=torch.float32, device=x.device)
@@ -82,7 +87,7 @@ def fnn_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     wt = x.dtype if weight is None else weight.dtype
     dx = out
     if dx is None and want_x:
-        dx = torch.empty((n, d), dtype=x.dtype, device=x.device)
+        dx = torch.empty_like(x)
     dweight = dbias = None
     if want_weight:
         dweight = torch.empty(d, dtype=wt, device=x.device)
