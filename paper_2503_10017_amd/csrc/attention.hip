@@ -115,6 +115,8 @@ __device__ __forceinline__ void put_run(const AttentionArgs& a, const Sequence& 
     store_elems<DT>((E*)a.out + (s.q0 + token) * a.out_row + head * a.out_head + at, a.d - at, v);
 }
 
+constexpr int MOST_SPLITS = 64, MOST_KEYS = 1 << 30;
+
 // Shares of a split call: [split][rows] of {the largest score, the sum}, then [split][rows][d rounded up to 8].
 __device__ __forceinline__ float* share_stats(const AttentionArgs& a, int split, int64_t row) {
     return a.partial + ((int64_t)split * a.tq * a.heads + row) * 2;
@@ -124,7 +126,7 @@ __device__ __forceinline__ float* share_row(const AttentionArgs& a, int split, i
 }
 
 template <int DT, int DB, int QB, int KEYS>
-__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, int split, const Rows<DT, DB, QB, KEYS>& w, int lane) {
+__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, bool any, const Rows<DT, DB, QB, KEYS>& w, int lane) {
     const int c = lane & 31, h = lane >> 5;
 #pragma unroll
     for (int b = 0; b < QB; ++b) {
@@ -145,8 +147,8 @@ __device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequen
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[p][e] *= scale;
                     put_run<DT>(a, s, group, r, at, v[p]);
-                } else {
-                    float* to = share_row(a, split, flat_row(a, s, group, r)) + at;
+                } else if (any) {  // the share of no keys is told by its statistics alone
+                    float* to = share_row(a, blockIdx.y, flat_row(a, s, group, r)) + at;
                     reinterpret_cast<f32x4*>(to)[0] = f32x4{v[p][0], v[p][1], v[p][2], v[p][3]};
                     reinterpret_cast<f32x4*>(to)[1] = f32x4{v[p][4], v[p][5], v[p][6], v[p][7]};
                 }
@@ -154,13 +156,21 @@ __device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequen
         }
         if (r >= rows || h) continue;
         if (a.splits > 1) {
-            float* to = share_stats(a, split, flat_row(a, s, group, r));
+            float* to = share_stats(a, blockIdx.y, flat_row(a, s, group, r));
             to[0] = w.top[b];
             to[1] = total;
         } else if (a.lse) {
             a.lse[flat_row(a, s, group, r)] = w.top[b] * a.scale + logf(total);  // no key: minus infinity
         }
     }
+}
+
+// The tiles of keys that this workgroup's part (blockIdx.y) of a split call has: as many parts as there are whole ones of part_tiles, so that
+// sequences of different lengths are cut into pieces of one size; the parts beyond have none.
+__device__ __forceinline__ void part_of(const AttentionArgs& a, int tiles, int& t0, int& t1) {
+    const int part = blockIdx.y, parts = min(max((tiles + a.part_tiles - 1) / a.part_tiles, 1), a.splits);
+    t0 = part < parts ? (int)((int64_t)tiles * part / parts) : 0;
+    t1 = part < parts ? (int)((int64_t)tiles * (part + 1) / parts) : 0;
 }
 
 // Many rows: a workgroup's four waves have QB x 32 rows each and share tiles of 64 keys.
@@ -178,10 +188,9 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rows = s.lq * a.share, first = s.tile * ROWS, mine = first + wave * WAVE_ROWS;
     const int most = seen_by(a, s, min(first + ROWS, rows) - 1);
-    const int tiles = (most + KEYS - 1) / KEYS, t0 = (int)((int64_t)tiles * blockIdx.y / a.splits), t1 = (int)((int64_t)tiles * (blockIdx.y + 1) / a.splits);
+    int t0, t1;
+    part_of(a, (most + KEYS - 1) / KEYS, t0, t1);
 
-    W w;
-    w.begin(a, s, group, mine, rows, lane);
     const int least_seen = mine < rows ? seen_by(a, s, mine) : 0, most_seen = mine < rows ? seen_by(a, s, min(mine + WAVE_ROWS, rows) - 1) : 0;
     int seen[QB];
 #pragma unroll
@@ -195,6 +204,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
         Tile::template stage<256, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, threadIdx.x);
     };
     if (t0 < t1) stage(stages[0], t0);
+    W w;
+    w.begin(a, s, group, mine, rows, lane);
     for (int t = t0, turn = 0; t < t1; ++t, turn ^= 1) {
         const char* now = stages[turn];
         lds_loads_arrived();
@@ -204,7 +215,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
         if (key >= most_seen) continue;
         w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least_seen, lane);
     }
-    finish_rows(a, s, group, mine, rows, blockIdx.y, w, lane);
+    finish_rows(a, s, group, mine, rows, t0 < t1, w, lane);
 }
 
 // Few rows (a token or some at the end of a cache): the time is that of reading the keys once.  Every wave has the same 32 rows and tiles of
@@ -224,10 +235,9 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rows = s.lq * a.share, first = s.tile * ROWS;
     const int most = seen_by(a, s, min(first + ROWS, rows) - 1), least = seen_by(a, s, first);
-    const int tiles = (most + KEYS - 1) / KEYS, t0 = (int)((int64_t)tiles * blockIdx.y / a.splits), t1 = (int)((int64_t)tiles * (blockIdx.y + 1) / a.splits);
+    int t0, t1;
+    part_of(a, (most + KEYS - 1) / KEYS, t0, t1);
 
-    W w;
-    w.begin(a, s, group, first, rows, lane);
     int seen[1] = {seen_by(a, s, min(first + (lane & 31), rows - 1))};
     const float c = a.scale * LOG2E;
     const E* k = (const E*)a.k + s.k0 * a.k_row + group * a.k_head;
@@ -240,6 +250,8 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     };
     int turn = 0;
     if (t0 + wave < t1) stage(mine, t0 + wave);
+    W w;
+    w.begin(a, s, group, first, rows, lane);
     for (int t = t0 + wave; t < t1; t += 4, turn ^= 1) {
         char* now = mine + turn * 2 * Tile::BYTES;
         char* next = mine + (turn ^ 1) * 2 * Tile::BYTES;
@@ -283,59 +295,70 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     w.sum[0] = sum;
 #pragma unroll
     for (int i = 0; i < DB; ++i) w.out[0][i] = out[i];
-    finish_rows(a, s, group, first, rows, blockIdx.y, w, lane);
+    finish_rows(a, s, group, first, rows, t0 < t1, w, lane);
 }
 
-// Joins the shares of a split call, a wave per row: lane l has elements 2 l and 2 l + 1.
+// Joins the shares of a split call, a workgroup per row: its eight groups of 32 lanes take shares in turn, a lane four elements of each.
 template <int DT>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
-    typedef typename Elem<DT>::T E;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (row >= (int64_t)a.tq * a.heads) return;
-    const int token = (int)(row / a.heads), head = (int)(row - (int64_t)token * a.heads);
+    __shared__ float keeps[MOST_SPLITS];
+    __shared__ f32x4 joined[8][32];
+    const int64_t row = blockIdx.x;
+    const int token = (int)(row / a.heads), head = (int)(row - (int64_t)token * a.heads), lane = threadIdx.x & 63, place = threadIdx.x & 31, group = threadIdx.x >> 5;
     if (a.cu_q && (token < max(a.cu_q[0], 0) || token >= a.cu_q[a.batch])) return;  // a row of no sequence stays as it is
     const float c = a.scale * LOG2E;
-    float top = -__builtin_inff();
-    for (int s = 0; s < a.splits; ++s) top = __builtin_fmaxf(top, share_stats(a, s, row)[0]);
-    const float base = top > -__builtin_inff() ? top * c : 0.f;
-    float sum = 0.f, x = 0.f, y = 0.f;
-    for (int s = 0; s < a.splits; ++s) {
-        const float* stats = share_stats(a, s, row);
-        const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(stats[0], c, -base));
-        sum = __builtin_fmaf(stats[1], keep, sum);
-        if (2 * lane < a.d) {
-            const float* from = share_row(a, s, row) + 2 * lane;
-            x = __builtin_fmaf(from[0], keep, x);
-            y = __builtin_fmaf(from[1], keep, y);
+    float top = -__builtin_inff(), sum = 0.f;
+    if (lane < a.splits) top = share_stats(a, lane, row)[0], sum = share_stats(a, lane, row)[1];
+    float most = top;
+#pragma unroll
+    for (int step = 1; step < 64; step <<= 1) most = __builtin_fmaxf(most, __shfl_xor(most, step));
+    const float base = most > -__builtin_inff() ? most * c : 0.f, keep = __builtin_amdgcn_exp2f(__builtin_fmaf(top, c, -base));
+    const float total = wave_sum(sum * keep);
+    if (threadIdx.x < a.splits) keeps[threadIdx.x] = keep;
+    __syncthreads();
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (4 * place < a.d) {
+#pragma unroll 4
+        for (int s = group; s < a.splits; s += 8) {
+            const float k = keeps[s];
+            if (k == 0.f) continue;  // no keys: nothing was written
+            const f32x4 y = *reinterpret_cast<const f32x4*>(share_row(a, s, row) + 4 * place);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(y[e], k, x[e]);
         }
     }
-    const float scale = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
-    E* out = (E*)a.out + token * a.out_row + head * a.out_head + 2 * lane;
-    if (2 * lane < a.d) out[0] = (E)(x * scale);
-    if (2 * lane + 1 < a.d) out[1] = (E)(y * scale);
-    if (lane == 0 && a.lse) a.lse[row] = top * a.scale + logf(sum);
+    joined[group][place] = x;
+    __syncthreads();
+    if (group) return;
+#pragma unroll
+    for (int g = 1; g < 8; ++g) x += joined[g][place];
+    const float scale = total > 0.f ? 1.f / total : total != total ? total : 0.f;
+    const float v[4] = {x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale};
+    if (4 * place < a.d) store_elems<DT, 4>((typename Elem<DT>::T*)a.out + token * a.out_row + head * a.out_head + 4 * place, a.d - 4 * place, v);
+    if (threadIdx.x == 0 && a.lse) a.lse[row] = most * a.scale + logf(total);
 }
 
-// From the sizes alone: whether the rows of a sequence are few on average (one wave's worth), and into how many parts the keys are split.
-// 2048 workgroups are eight a compute unit; a part has 256 keys at least on average, below which its start costs more than it saves.
+// From the sizes alone: whether the rows of a sequence are few on average (one wave's worth), and into how many parts the keys may be split: parts of
+// the size that makes 512 of them in all, which is what the chip holds at once, and not less than 256 keys, below which a part's start costs more than it
+// saves; twice as many as sequences of the average length would have, for the longer ones.
 struct Plan {
     bool few;
-    int row_tiles, splits, blocks;
+    int row_tiles, splits, part_keys;
 };
-Plan plan_of(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d) {
+Plan plan_of(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups) {
     Plan p;
     const int64_t rows = tq * (heads / groups);
     p.few = rows <= 32 * batch;
-    p.blocks = 1;
-    const int64_t tile = p.few ? 32 : 128 * p.blocks;
+    const int64_t tile = p.few ? 32 : 128;
     p.row_tiles = (int)((rows + tile - 1) / tile + batch - 1);
-    if (p.few && p.row_tiles > rows) p.row_tiles = (int)rows;
-    const int64_t workgroups = p.row_tiles * groups, wanted = p.few ? 2048 : 512, longest = tk / batch / 256;
-    int64_t splits = wanted / workgroups;
-    if (splits > longest) splits = longest;
-    if (splits > 64) splits = 64;
-    p.splits = splits < 1 ? 1 : (int)splits;
+    if (p.row_tiles > rows) p.row_tiles = (int)rows;
+    const int64_t average = tk / batch;
+    int64_t part = ((int64_t)p.row_tiles * groups * average / 512 + 127) / 128 * 128;
+    if (part < 256) part = 256;
+    int64_t splits = average <= part ? 1 : 2 * ((average + part - 1) / part);
+    if (splits > MOST_SPLITS) splits = MOST_SPLITS;
+    p.splits = (int)splits;
+    p.part_keys = (int)(part < MOST_KEYS ? part : MOST_KEYS);
     return p;
 }
 
@@ -345,22 +368,23 @@ hipError_t run(const AttentionArgs& a, const Plan& p, hipStream_t s) {
     const hipError_t e = p.few ? launch(TK_ATTENTION, attention_few_kernel<DT, DB, DIRECT>, grid, dim3(256), 0, s, a)
                                : launch(TK_ATTENTION, attention_kernel<DT, DB, 1, DIRECT>, grid, dim3(256), 0, s, a);
     if (e != hipSuccess || p.splits == 1) return e;
-    return launch(TK_ATTENTION, attention_join_kernel<DT>, dim3((unsigned)(((int64_t)a.tq * a.heads + 3) / 4)), dim3(256), 0, s, a);
+    return launch(TK_ATTENTION, attention_join_kernel<DT>, dim3((unsigned)((int64_t)a.tq * a.heads)), dim3(256), 0, s, a);
 }
 
 }  // namespace
 
 size_t attention_workspace(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d) {
     if (tq < 1) return 0;
-    const Plan p = plan_of(tq, tk, batch, heads, groups, d);
+    const Plan p = plan_of(tq, tk, batch, heads, groups);
     return p.splits > 1 ? (size_t)p.splits * tq * heads * (2 + (d + 7) / 8 * 8) * sizeof(float) : 0;
 }
 
 hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t s) {
     if (a.tq < 1) return hipSuccess;
-    const Plan p = plan_of(a.tq, a.tk, a.batch, a.heads, a.groups, a.d);
+    const Plan p = plan_of(a.tq, a.tk, a.batch, a.heads, a.groups);
     a.row_tiles = p.row_tiles;
     a.splits = p.splits;
+    a.part_tiles = p.part_keys / (p.few ? 32 : 64);
     a.d_pad = (a.d + 7) / 8 * 8;
     const int blocks = (a.d + 31) / 32;
     auto with_type = [&](auto dt) {

@@ -30,8 +30,11 @@ __device__ __forceinline__ Sequence find_sequence(const AttentionArgs& a, int ti
     int before = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 64) {
         const int b = b0 + lane;
-        int first = 0, count = 0;
-        if (b < a.batch) sequence_bounds(BY_KEYS ? a.cu_k : a.cu_q, b, BY_KEYS ? a.tk : a.tq, first, count);
+        int first = 0, count = 0, other = 0, others = 0;
+        if (b < a.batch) {  // both tables at once: one wait
+            sequence_bounds(BY_KEYS ? a.cu_k : a.cu_q, b, BY_KEYS ? a.tk : a.tq, first, count);
+            sequence_bounds(BY_KEYS ? a.cu_q : a.cu_k, b, BY_KEYS ? a.tq : a.tk, other, others);
+        }
         const int tiles = (int)(((int64_t)count * (BY_KEYS ? 1 : a.share) + ROWS - 1) / ROWS);
         int sum = tiles;
 #pragma unroll
@@ -45,10 +48,8 @@ __device__ __forceinline__ Sequence find_sequence(const AttentionArgs& a, int ti
             s.index = b0 + at;
             s.tile = tile - before - __builtin_amdgcn_readlane(sum - tiles, at);
             const int mine = __builtin_amdgcn_readlane(first, at), many = __builtin_amdgcn_readlane(count, at);
-            int other, others;
-            sequence_bounds(BY_KEYS ? a.cu_q : a.cu_k, s.index, BY_KEYS ? a.tq : a.tk, other, others);
-            other = __builtin_amdgcn_readfirstlane(other);
-            others = __builtin_amdgcn_readfirstlane(others);
+            other = __builtin_amdgcn_readlane(other, at);
+            others = __builtin_amdgcn_readlane(others, at);
             s.q0 = BY_KEYS ? other : mine;
             s.lq = BY_KEYS ? others : many;
             s.k0 = BY_KEYS ? mine : other;

@@ -122,10 +122,10 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
     }
 }
 
-// dk and dv: a wave has 32 keys and runs over tiles of 32 rows (of all the heads that share the key head), which its workgroup's four waves share.
+// dk and dv: a wave has 32 keys and runs over tiles of 64 rows, 32 of long vectors (of all the heads that share the key head), which its workgroup's four waves share.
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs a) {
-    constexpr int KEYS = 128, ROWS = 32;
+    constexpr int KEYS = 128, ROWS = DB <= 2 ? 64 : 32;
     constexpr bool KEYS_IN_LDS = DB > 2;  // long vectors: dk, dv, k and v together are more registers than two waves a SIMD have, so k is read again and again
     using Tile = HeadTile<DT, DB, ROWS>;
     using KeyTile = HeadTile<DT, DB, KEYS>;
@@ -163,9 +163,11 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
     for (int i = 0; i < DB; ++i) dk[i] = dv[i] = (f32x16)(0.f);
     const float c = f.scale * LOG2E, unshift = 1.f / (float)(1 << WEIGHT_SHIFT<DT>);
 
-    // Rows of a group are not equally far apart in memory when heads share a key head, so a thread's rows are found one by one.
+    // The rows of a tile are share heads of ROWS / share tokens each where share divides ROWS: then a thread's place in the tile says how far
+    // its row lies from the tile's first.  Otherwise its rows are found one by one.
+    const bool even = ROWS % f.share == 0;
     auto stage = [&](char* to, int row0) {
-        constexpr int PER_THREAD = ROWS * Tile::RUNS / 256 > 0 ? ROWS * Tile::RUNS / 256 : 1, THREADS = ROWS * Tile::RUNS / PER_THREAD;
+        constexpr int RUNS = ROWS * Tile::RUNS, PER_THREAD = RUNS / 256 > 0 ? RUNS / 256 : 1, THREADS = RUNS / PER_THREAD;
         const int thread = threadIdx.x;
         if (THREADS == 256 || thread < THREADS) {
             const int token0 = token_of(f, row0);
@@ -174,19 +176,18 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
 #pragma unroll
             for (int i = 0; i < PER_THREAD; ++i) {
                 const int at = i * THREADS + thread, row = at / Tile::RUNS, run = (at % Tile::RUNS) ^ Tile::exchanged(row), r = row0 + row;
-                const int token = token_of(f, r), head = r - token * f.share;
+                const int token = even ? token_of(f, row) : token_of(f, r) - token0, head = even ? row - token * f.share : r - (token0 + token) * f.share;
                 if constexpr (DIRECT) {
                     const bool there = r < rows && run * 8 < f.d;
-                    const uint32_t chunk = (i * THREADS + (thread & ~63)) * 16;
-                    const uint32_t q_at = (uint32_t)((token - token0) * (int)f.q_row + head * (int)f.q_head + run * 8) * 2;
-                    const uint32_t dout_at = (uint32_t)((token - token0) * (int)a.dout_row + head * (int)a.dout_head + run * 8) * 2;
-                    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(to) + chunk);
+                    const uint32_t q_at = (uint32_t)(token * (int)f.q_row + head * (int)f.q_head + run * 8) * 2;
+                    const uint32_t dout_at = (uint32_t)(token * (int)a.dout_row + head * (int)a.dout_head + run * 8) * 2;
+                    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(to) + (i * THREADS + (thread & ~63)) * 16);
                     load_to_lds(buffer_of(of_q, 0x80000000u), there ? q_at : 0xFFFFFFF0u, lds);
                     load_to_lds(buffer_of(of_dout, 0x80000000u), there ? dout_at : 0xFFFFFFF0u, lds + Tile::BYTES);
                 } else {
                     const int count = r < rows ? f.d - run * 8 : 0;
-                    *reinterpret_cast<uint4*>(to + at * 16) = load_run<DT>(of_q + (token - token0) * f.q_row + head * f.q_head + run * 8, count);
-                    *reinterpret_cast<uint4*>(to + Tile::BYTES + at * 16) = load_run<DT>(of_dout + (token - token0) * a.dout_row + head * a.dout_head + run * 8, count);
+                    *reinterpret_cast<uint4*>(to + at * 16) = load_run<DT>(of_q + token * f.q_row + head * f.q_head + run * 8, count);
+                    *reinterpret_cast<uint4*>(to + Tile::BYTES + at * 16) = load_run<DT>(of_dout + token * a.dout_row + head * a.dout_head + run * 8, count);
                 }
             }
         }
@@ -213,29 +214,32 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
         __syncthreads();
         if (row + ROWS < rows) stage(stages[turn ^ 1], row + ROWS);
         if (row + ROWS <= wave_first || mine >= s.lk) continue;
-        f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
 #pragma unroll
-        for (int i = 0; i < 2 * DB; ++i) {
-            p = mma32<DT>(Tile::along(now, 0, i, lane), KEYS_IN_LDS ? KeyTile::along(key_tile, wave, i, lane) : k[KEYS_IN_LDS ? 0 : i], p);
-            ds = mma32<DT>(Tile::along(now + Tile::BYTES, 0, i, lane), v[i], ds);
-        }
-        const float* stats = reinterpret_cast<const float*>(now + 2 * Tile::BYTES) + 4 * (lane >> 5);
+        for (int block = 0; block < ROWS / 32; ++block) {
+            f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
 #pragma unroll
-        for (int x = 0; x < 16; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x], c, -stats[tile_row(x, 0)]));
-        if (row < wave_all) {
-            const int least = from_row - row - 4 * (lane >> 5);
+            for (int i = 0; i < 2 * DB; ++i) {
+                p = mma32<DT>(Tile::along(now, block, i, lane), KEYS_IN_LDS ? KeyTile::along(key_tile, wave, i, lane) : k[KEYS_IN_LDS ? 0 : i], p);
+                ds = mma32<DT>(Tile::along(now + Tile::BYTES, block, i, lane), v[i], ds);
+            }
+            const float* stats = reinterpret_cast<const float*>(now + 2 * Tile::BYTES) + 32 * block + 4 * (lane >> 5);
 #pragma unroll
-            for (int x = 0; x < 16; ++x) p[x] = tile_row(x, 0) >= least ? p[x] : 0.f;
-        }
+            for (int x = 0; x < 16; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x], c, -stats[tile_row(x, 0)]));
+            if (row + 32 * block < wave_all) {
+                const int least = from_row - row - 32 * block - 4 * (lane >> 5);
 #pragma unroll
-        for (int x = 0; x < 16; ++x) ds[x] = p[x] * __builtin_fmaf(ds[x], unshift, -stats[ROWS + tile_row(x, 0)]);
+                for (int x = 0; x < 16; ++x) p[x] = tile_row(x, 0) >= least ? p[x] : 0.f;
+            }
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const uint4 w = round_half<DT>(p, half), g = round_half<DT>(ds, half);
+            for (int x = 0; x < 16; ++x) ds[x] = p[x] * __builtin_fmaf(ds[x], unshift, -stats[ROWS + tile_row(x, 0)]);
 #pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                dv[i] = mma32<DT>(Tile::across(now + Tile::BYTES, i, half, lane), w, dv[i]);
-                dk[i] = mma32<DT>(Tile::across(now, i, half, lane), g, dk[i]);
+            for (int half = 0; half < 2; ++half) {
+                const uint4 w = round_half<DT>(p, half), g = round_half<DT>(ds, half);
+#pragma unroll
+                for (int i = 0; i < DB; ++i) {
+                    dv[i] = mma32<DT>(Tile::across(now + Tile::BYTES, i, 2 * block + half, lane), w, dv[i]);
+                    dk[i] = mma32<DT>(Tile::across(now, i, 2 * block + half, lane), g, dk[i]);
+                }
             }
         }
     }

@@ -8,8 +8,6 @@ namespace fnn {
 // How an operand lies in memory: its rows run along k, or its rows are the k's and run along m (n).
 enum : int { ROWS = 0, COLUMNS = 1 };
 
-constexpr int STEP_BYTES = 64;  // of every row of a tile, per step: 32 elements of 16 bits, 16 of 32
-constexpr int STAGES = 3;
 
 // Who works on what: neighbouring workgroups are dealt to the 8 XCDs in turn, so each XCD is given a run of tiles of its own, in blocks
 // of 8 tiles of rows by as many tiles of columns as it takes, which share their operands in its L2.
@@ -30,18 +28,18 @@ __device__ __forceinline__ TileAt tile_at(const GemmArgs& a) {
     return t;
 }
 
-// One operand's tile of T rows (columns) and one step of k, in LDS.  ROWS: [T][64 bytes]; COLUMNS: [k][T].  LDS serves 256 bytes at a time, so
-// the 16-byte runs of a row are exchanged such that what one instruction reads together lies in different columns of 256 bytes: 16 rows
-// at one run (ROWS), 4 rows at 4 runs (COLUMNS of 16 bits, transposing reads), rows k and k + 4 at 128 bytes (COLUMNS of 32 bits).
-template <int DT, int T, int THREADS, int LAYOUT>
+// One operand's tile of T rows (columns) and one step of k (SB bytes of a row), in LDS.  ROWS: [T][SB]; COLUMNS: [k][T].  LDS serves 256 bytes at a
+// time, so the 16-byte runs of a row are exchanged such that what one instruction reads together lies in different columns of 256
+// bytes: 16 rows at one run (ROWS), 4 rows at 4 runs (COLUMNS of 16 bits, transposing reads), rows k and k + 4 at 128 bytes (COLUMNS of 32 bits).
+template <int DT, int T, int SB, int THREADS, int LAYOUT>
 struct Operand {
     typedef typename Elem<DT>::T E;
-    static constexpr int ES = sizeof(E), N = Elem<DT>::N, STEP = STEP_BYTES / ES;
-    static constexpr int RUNS = T * 4, PER_THREAD = RUNS / THREADS;
-    static constexpr int ROW_RUNS = LAYOUT == ROWS ? 4 : T * ES / 16;  // 16-byte runs in a row of the tile
+    static constexpr int ES = sizeof(E), N = Elem<DT>::N, STEP = SB / ES, BYTES = T * SB;
+    static constexpr int RUNS = BYTES / 16, PER_THREAD = RUNS / THREADS;
+    static constexpr int ROW_RUNS = LAYOUT == ROWS ? SB / 16 : T * ES / 16;  // 16-byte runs in a row of the tile
     static_assert(RUNS % THREADS == 0 && THREADS % ROW_RUNS == 0, "every thread's runs are at one place of their rows");
     static constexpr int ROWS_APART = THREADS / ROW_RUNS;
-    static __device__ __forceinline__ int exchanged(int row) { return LAYOUT == ROWS ? (row >> 2 & 3) : ES == 2 ? (row & 3) << 2 : (row >> 2 & 1) << 3; }
+    static __device__ __forceinline__ int exchanged(int row) { return LAYOUT == ROWS ? (SB == 64 ? row >> 2 & 3 : row >> 1 & 7) : ES == 2 ? (row & 3) << 2 : (row >> 2 & 1) << 3; }
 
     const E* base;      // ROWS: the tile's first row, at the first k of the split; COLUMNS: the first k's row, at the tile's first column
     int64_t stride;     // elements
@@ -87,11 +85,11 @@ struct Operand {
     }
     __device__ __forceinline__ void advance() { base += LAYOUT == ROWS ? (int64_t)STEP : STEP * stride; }
 
-    // A matrix instruction's operand: rows 32 block .. + 31, the kk-th half of the step's k's.
+    // A matrix instruction's operand: rows 32 block .. + 31, the kk-th 32 bytes of the step's k's.
     static __device__ __forceinline__ uint4 fragment(const char* lds, int block, int kk, int lane) {
         const int c = lane & 31, h = lane >> 5;
         if constexpr (LAYOUT == ROWS) {
-            return *reinterpret_cast<const uint4*>(lds + block * (32 * STEP_BYTES) + c * STEP_BYTES + (((2 * kk + h) ^ (c >> 2 & 3)) << 4));
+            return *reinterpret_cast<const uint4*>(lds + block * (32 * SB) + c * SB + (((2 * kk + h) ^ exchanged(c)) << 4));
         } else if constexpr (ES == 2) {
             const int t = lane & 15, row = 16 * kk + 8 * h + (t >> 2);
             const int run = (4 * block + 2 * ((lane >> 4) & 1) + ((t >> 1) & 1)) ^ ((t >> 2) << 2);
@@ -110,42 +108,64 @@ struct Operand {
     }
 };
 
-// Eight consecutive results of row m, from column n on (`count` of them exist): bias, activation, residual; or, of a split product, the share.
+// Eight consecutive elements, as stored: `count` of them exist.
 template <int DT>
-__device__ __forceinline__ void finish_run(const GemmArgs& a, int64_t m, int n, int count, float (&v)[8]) {
-    typedef typename Elem<DT>::T E;
+struct Eight {
+    static constexpr int N = Elem<DT>::N;
+    uint4 raw[8 / N];
+    __device__ __forceinline__ void load(const void* data, int64_t at, int count) {
+#pragma unroll
+        for (int p = 0; p < 8 / N; ++p) raw[p] = load_run<DT>((const typename Elem<DT>::T*)data + at + p * N, count - p * N);
+    }
+    __device__ __forceinline__ float operator[](int e) const {
+        typename Elem<DT>::T x[N];
+        __builtin_memcpy(x, &raw[e / N], 16);
+        return (float)x[e % N];
+    }
+};
+template <int DT>
+__device__ __forceinline__ void store_eight(void* data, int64_t at, int count, const float (&v)[8]) {
     constexpr int N = Elem<DT>::N;
 #pragma unroll
-    for (int part = 0; part < 8 / N; ++part) {
-        const int at = n + part * N, here = count - part * N;
+    for (int p = 0; p < 8 / N; ++p) {
+        if (count <= p * N) return;
         float w[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) w[e] = v[part * N + e];
-        if (here <= 0) return;
-        if (a.bias) {
-            float b[N];
-            load_elems<DT>((const E*)a.bias + at, here, b);
-#pragma unroll
-            for (int e = 0; e < N; ++e) w[e] += b[e];
-        }
-        if (a.pre) store_elems<DT>((E*)a.pre + m * a.ldp + at, here, w);
-        activate<DT != CT_F32>(w, a.act);
-        if (a.residual) {
-            float r[N];
-            load_elems<DT>((const E*)a.residual + m * a.ldr + at, here, r);
-#pragma unroll
-            for (int e = 0; e < N; ++e) w[e] += r[e];
-        }
-        store_elems<DT>((E*)a.y + m * a.ldy + at, here, w);
+        for (int e = 0; e < N; ++e) w[e] = v[p * N + e];
+        store_elems<DT>((typename Elem<DT>::T*)data + at + p * N, count - p * N, w);
     }
 }
 
-template <int DT, int TM, int TN, int WAVES_M, int WAVES_N, int LA, int LB, bool DIRECT>
-__global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 2) void gemm_kernel(GemmArgs a) {
-    constexpr int THREADS = WAVES_M * WAVES_N * 64, BM = TM / WAVES_M / 32, BN = TN / WAVES_N / 32;
-    using OpA = Operand<DT, TM, THREADS, LA>;
-    using OpB = Operand<DT, TN, THREADS, LB>;
-    __shared__ __attribute__((aligned(16))) char stages[STAGES][(TM + TN) * STEP_BYTES];
+// Eight consecutive results of row m, from column n on (`count` of them exist): bias, activation, residual.
+template <int DT>
+__device__ __forceinline__ void finish_run(const GemmArgs& a, int64_t m, int n, int count, float (&v)[8], const Eight<DT>& bias, const Eight<DT>& residual) {
+    if (a.bias) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += bias[e];
+    }
+    if (a.pre) store_eight<DT>(a.pre, m * a.ldp + n, count, v);
+    activate<DT != CT_F32>(v, a.act);
+    if (a.residual) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += residual[e];
+    }
+    store_eight<DT>(a.y, m * a.ldy + n, count, v);
+}
+// The same where what it takes is not there yet.
+template <int DT>
+__device__ __forceinline__ void finish_run(const GemmArgs& a, int64_t m, int n, int count, float (&v)[8]) {
+    Eight<DT> bias = {}, residual = {};
+    if (a.bias) bias.load(a.bias, n, count);
+    if (a.residual) residual.load(a.residual, m * a.ldr + n, count);
+    finish_run<DT>(a, m, n, count, v, bias, residual);
+}
+
+template <int DT, int TM, int TN, int WAVES_M, int WAVES_N, int SB, int STAGES, int LA, int LB, bool DIRECT>
+__global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 64)) void gemm_kernel(GemmArgs a) {
+    constexpr int THREADS = WAVES_M * WAVES_N * 64, BM = TM / WAVES_M / 32, BN = TN / WAVES_N / 32, PARTS = SB / 32;
+    using OpA = Operand<DT, TM, SB, THREADS, LA>;
+    using OpB = Operand<DT, TN, SB, THREADS, LB>;
+    __shared__ __attribute__((aligned(16))) char stages[STAGES][OpA::BYTES + OpB::BYTES];
     const TileAt tile = tile_at(a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WAVES_M, wn = wave / WAVES_M;
@@ -158,6 +178,9 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 2) void gemm_kernel(GemmArgs
     opa.begin(a.a, a.lda, m0, a.m, (int64_t)s0 * OpA::STEP);
     opb.begin(a.b, a.ldb, n0, a.n, (int64_t)s0 * OpA::STEP);
     int left = a.k - s0 * OpA::STEP;
+    const int n = n0 + wn * 64 + 8 * (lane & 7);  // the first of the eight columns that this lane finishes
+    Eight<DT> bias = {};
+    if (a.bias && a.splits == 1) bias.load(a.bias, n, a.n - n);
 
     f32x16 acc[BM][BN];
 #pragma unroll
@@ -169,7 +192,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 2) void gemm_kernel(GemmArgs
     auto get = [&](char* to) {
         if constexpr (DIRECT) {
             opa.stage(to, left);
-            opb.stage(to + TM * STEP_BYTES, left);
+            opb.stage(to + OpA::BYTES, left);
         } else {
             opa.fetch(held_a, left);
             opb.fetch(held_b, left);
@@ -181,48 +204,48 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 2) void gemm_kernel(GemmArgs
     auto put = [&](char* to) {
         if constexpr (!DIRECT) {
             opa.put(to, held_a);
-            opb.put(to + TM * STEP_BYTES, held_b);
+            opb.put(to + OpA::BYTES, held_b);
         }
     };
     uint4 fa[2][BM], fb[2][BN];
     auto read = [&](const char* from, int kk) {
 #pragma unroll
-        for (int j = 0; j < BN; ++j) fb[kk][j] = OpB::fragment(from + TM * STEP_BYTES, wn * BN + j, kk, lane);
+        for (int j = 0; j < BN; ++j) fb[kk & 1][j] = OpB::fragment(from + OpA::BYTES, wn * BN + j, kk, lane);
 #pragma unroll
-        for (int i = 0; i < BM; ++i) fa[kk][i] = OpA::fragment(from, wm * BM + i, kk, lane);
+        for (int i = 0; i < BM; ++i) fa[kk & 1][i] = OpA::fragment(from, wm * BM + i, kk, lane);
     };
-    // the first half's operands have been read; the second's are while the first half is multiplied
+    // the first part's operands have been read; each next part's are while one is multiplied
     auto multiply = [&](const char* from) {
-        read(from, 1);
-        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
+        for (int kk = 0; kk < PARTS; ++kk) {
+            if (kk + 1 < PARTS) read(from, kk + 1);
 #pragma unroll
             for (int i = 0; i < BM; ++i)
 #pragma unroll
-                for (int j = 0; j < BN; ++j) acc[i][j] = mma32<DT>(fb[kk][j], fa[kk][i], acc[i][j]);
+                for (int j = 0; j < BN; ++j) acc[i][j] = mma32<DT>(fb[kk & 1][j], fa[kk & 1][i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_s_setprio(0);
     };
-    // A step: what was asked for two steps ago has arrived, in every wave; the stage that everyone has left is filled; this one is multiplied.
+    // A step: what was asked for STAGES - 1 steps ago has arrived, in every wave; the stage that everyone has left is filled; this one is multiplied.
+    constexpr int LOADS = OpA::PER_THREAD + OpB::PER_THREAD;
     auto step = [&](int stage, int s) {
-        char* now = stages[stage];
-        char* next = stages[(stage + 2) % STAGES];
-        if (s + 1 < s1) lds_loads_left<OpA::PER_THREAD + OpB::PER_THREAD>();
+        const int later = s1 - 1 - s;  // steps whose loads may still be under way
+        if (STAGES >= 4 && later >= 2) lds_loads_left<2 * LOADS>();
+        else if (STAGES >= 3 && later >= 1) lds_loads_left<LOADS>();
         else lds_loads_left<0>();
         meet();
-        read(now, 0);
-        if (s + 2 < s1) get(next);
-        multiply(now);
+        read(stages[stage], 0);
+        if (s + STAGES - 1 < s1) get(stages[(stage + STAGES - 1) % STAGES]);
+        multiply(stages[stage]);
     };
     if constexpr (DIRECT) {
-        if (s0 < s1) get(stages[0]);
-        if (s0 + 1 < s1) get(stages[1]);
-        for (int s = s0; s < s1; s += 3) {
-            step(0, s);
-            if (s + 1 < s1) step(1, s + 1);
-            if (s + 2 < s1) step(2, s + 2);
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i)
+            if (s0 + i < s1) get(stages[i]);
+        for (int s = s0; s < s1; s += STAGES) {
+#pragma unroll
+            for (int i = 0; i < STAGES; ++i)
+                if (s + i < s1) step(i, s + i);
         }
     } else {
         // one step ahead: stage s mod 2
@@ -241,11 +264,25 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 2) void gemm_kernel(GemmArgs
     }
 
     // The results go through LDS, 32 rows of a wave at a time, so that 8 lanes have 64 consecutive columns of a row: whole lines of y, residual and
-    // pre instead of 32-byte pieces of 32 rows.  As in the tiles, the runs of a row are exchanged by its number.
+    // pre instead of 32-byte pieces of 32 rows.  As in the tiles, the runs of a row are exchanged by its number.  Loads are waited for in
+    // the order of all accesses, stores among them, so the bias is there before the first store and each 32 rows' residual before
+    // those of the rows before it (bias loaded where it is added: 12 us longer on a tile of 256 x 256).
     __syncthreads();
-    static_assert(BN == 2 && 4 * 8192 <= sizeof(stages), "a wave's 32 rows have 64 columns and 8 KB");
+    static_assert(BN == 2 && WAVES_M * WAVES_N * 8192 <= sizeof(stages), "a wave's 32 rows have 64 columns and 8 KB");
     char* mine = &stages[0][0] + wave * 8192;
-    const int c = lane & 31, h = lane >> 5, n = n0 + wn * 64 + 8 * (lane & 7);
+    const int c = lane & 31, h = lane >> 5;
+    const bool whole = a.splits == 1;
+    auto row_of = [&](int i, int part) { return m0 + (wm * BM + i) * 32 + 8 * part + (lane >> 3); };
+    Eight<DT> residual[2][4] = {};
+    auto fetch_residual = [&](int i) {
+        if (!a.residual || !whole) return;
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
+            const int64_t m = row_of(i, part);
+            if (m < a.m) residual[i & 1][part].load(a.residual, m * a.ldr + n, a.n - n);
+        }
+    };
+    fetch_residual(0);
 #pragma unroll
     for (int i = 0; i < BM; ++i) {
 #pragma unroll
@@ -255,10 +292,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 2) void gemm_kernel(GemmArgs
                 *reinterpret_cast<f32x4*>(mine + c * 256 + (((8 * j + 2 * g + h) ^ (c & 15)) << 4)) =
                     f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
         __builtin_amdgcn_wave_barrier();
+        if (i + 1 < BM) fetch_residual(i + 1);
 #pragma unroll
         for (int part = 0; part < 4; ++part) {
             const int row = 8 * part + (lane >> 3);
-            const int64_t m = m0 + (wm * BM + i) * 32 + row;
+            const int64_t m = row_of(i, part);
             float v[8];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -266,13 +304,13 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 2) void gemm_kernel(GemmArgs
                 v[4 * e] = x[0], v[4 * e + 1] = x[1], v[4 * e + 2] = x[2], v[4 * e + 3] = x[3];
             }
             if (m >= a.m || n >= a.n) continue;
-            if (a.splits > 1) {
+            if (whole) {
+                finish_run<DT>(a, m, n, a.n - n, v, bias, residual[i & 1][part]);
+            } else {
                 // shares lie in whole tiles, so they need no edge
                 float* to = a.partial + (((int64_t)tile.split * a.tiles_m * TM + m) * a.tiles_n * TN + n);
                 reinterpret_cast<f32x4*>(to)[0] = f32x4{v[0], v[1], v[2], v[3]};
                 reinterpret_cast<f32x4*>(to)[1] = f32x4{v[4], v[5], v[6], v[7]};
-            } else {
-                finish_run<DT>(a, m, n, a.n - n, v);
             }
         }
         __builtin_amdgcn_wave_barrier();

@@ -8,10 +8,12 @@ namespace fnn {
 
 namespace {
 
-constexpr int FEW_ROWS = 64;    // up to which a product is a pass over b
+// Whether a product is a pass over b with all of a in registers: up to 16 rows always; up to 64 while a, which every workgroup reads whole, is small.
+// (Microseconds, this way and in tiles: 24 x 4096 -> 1024 11.2 and 11.5, 32 x 4096 -> 1024 12.7 and 11.4, 64 x 1024 -> 4096 7.4 and 12.2.)
+bool few_rows(int64_t m, int64_t k) { return m <= 16 || (m <= 64 && m * k <= 98304); }
 constexpr int FEW_WAVES = 8;
 
-// Up to 64 rows of a: the time is that of reading b once.  A workgroup takes 16 rows of b, its waves share k between them, and every
+// Few rows of a: the time is that of reading b once.  A workgroup takes 16 rows of b, its waves share k between them, and every
 // lane asks for all of its runs of four turns before it multiplies the first; a (its rows are few) comes out of the L2.
 template <int DT, int BLOCKS>
 __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(GemmArgs a) {
@@ -118,26 +120,24 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float* partial,
     }
 }
 
-// The tile (256 x 128 or 128 x 128) and the number of shares that a product is split into, from its sizes alone.
+// The tile (256 x 256, a workgroup of eight waves a compute unit; or 128 x 128, two or three of four waves) and the number of shares that a product is
+// split into, from its sizes alone.
 struct Plan {
-    int tile_m, splits;
+    int tile, splits;
 };
-constexpr int TILE_N = 128;
 constexpr int64_t round_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 Plan plan_of(int64_t m, int64_t n, int64_t k, int dtype) {
-    const int64_t step = dtype == FNN_F32 ? 16 : 32, steps = (k + step - 1) / step;
-    const int64_t across = round_to(n, TILE_N) / TILE_N, big = round_to(m, 256) / 256 * across;
-    Plan p = {128, 1};
-    int64_t tiles = round_to(m, 128) / 128 * across;
-    if (dtype != FNN_F32 && big >= 256) p.tile_m = 256, tiles = big;
-    int64_t splits = 512 / (tiles > 0 ? tiles : 1);
+    const int64_t big = round_to(m, 256) / 256 * (round_to(n, 256) / 256), small = round_to(m, 128) / 128 * (round_to(n, 128) / 128);
+    const bool whole = dtype != FNN_F32 && big >= 160;
+    const int64_t tiles = whole ? big : small, wanted = dtype == FNN_F32 ? 512 : 256, step = dtype == FNN_F32 ? 16 : 64;
+    const int64_t steps = (k + step - 1) / step;
+    int64_t splits = wanted / (tiles > 0 ? tiles : 1);
     if (splits > steps / 8) splits = steps / 8;
     if (splits > 32) splits = 32;
-    p.splits = splits < 1 ? 1 : (int)splits;
-    return p;
+    return {whole ? 256 : 128, splits < 1 ? 1 : (int)splits};
 }
 size_t partial_bytes(int64_t m, int64_t n, const Plan& p) {
-    return p.splits > 1 ? (size_t)p.splits * round_to(m, p.tile_m) * round_to(n, TILE_N) * sizeof(float) : 0;
+    return p.splits > 1 ? (size_t)p.splits * round_to(m, p.tile) * round_to(n, p.tile) * sizeof(float) : 0;
 }
 
 // Whether an operand's runs of 16 bytes lie on 16-byte boundaries, a tile's offsets fit 32 bits and k ends with a run.
@@ -149,21 +149,22 @@ bool direct(const void* data, int64_t stride, int64_t rows, int64_t k, int dtype
 
 template <int DT, int LA, int LB>
 hipError_t run_gemm(GemmArgs a, bool is_direct, const Plan& p, int kind, hipStream_t s) {
-    a.tiles_m = (int)(round_to(a.m, p.tile_m) / p.tile_m);
-    a.tiles_n = (int)(round_to(a.n, TILE_N) / TILE_N);
+    a.tiles_m = (int)(round_to(a.m, p.tile) / p.tile);
+    a.tiles_n = (int)(round_to(a.n, p.tile) / p.tile);
     a.splits = p.splits;
     const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n * a.splits));
     hipError_t e;
-    if (DT != CT_F32 && p.tile_m == 256) {
+    if (DT != CT_F32 && p.tile == 256) {
         if constexpr (DT != CT_F32)
-            e = is_direct ? launch(kind, gemm_kernel<DT, 256, TILE_N, 2, 2, LA, LB, true>, grid, dim3(256), 0, s, a)
-                          : launch(kind, gemm_kernel<DT, 256, TILE_N, 2, 2, LA, LB, false>, grid, dim3(256), 0, s, a);
+            e = is_direct ? launch(kind, gemm_kernel<DT, 256, 256, 2, 4, 128, 2, LA, LB, true>, grid, dim3(512), 0, s, a)
+                          : launch(kind, gemm_kernel<DT, 256, 256, 2, 4, 128, 2, LA, LB, false>, grid, dim3(512), 0, s, a);
     } else {
-        e = is_direct ? launch(kind, gemm_kernel<DT, 128, TILE_N, 2, 2, LA, LB, true>, grid, dim3(256), 0, s, a)
-                      : launch(kind, gemm_kernel<DT, 128, TILE_N, 2, 2, LA, LB, false>, grid, dim3(256), 0, s, a);
+        constexpr int SB = DT == CT_F32 ? 64 : 128, STAGES = DT == CT_F32 ? 3 : 2;
+        e = is_direct ? launch(kind, gemm_kernel<DT, 128, 128, 2, 2, SB, STAGES, LA, LB, true>, grid, dim3(256), 0, s, a)
+                      : launch(kind, gemm_kernel<DT, 128, 128, 2, 2, SB, STAGES, LA, LB, false>, grid, dim3(256), 0, s, a);
     }
     if (e != hipSuccess || a.splits == 1) return e;
-    const int64_t pitch = (int64_t)a.tiles_n * TILE_N, share = pitch * a.tiles_m * p.tile_m, runs = (int64_t)((a.n + 7) / 8) * a.m;
+    const int64_t pitch = (int64_t)a.tiles_n * p.tile, share = pitch * a.tiles_m * p.tile, runs = (int64_t)((a.n + 7) / 8) * a.m;
     return launch(kind, gemm_join_kernel<DT>, dim3((unsigned)((runs + 255) / 256)), dim3(256), 0, s, a, pitch, share);
 }
 
@@ -186,7 +187,7 @@ hipError_t with_type(int dtype, F f) {
 
 size_t gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, int layout_a, int layout_b) {
     if (m < 1 || n < 1) return 0;
-    if (layout_a == ROWS && layout_b == ROWS && m <= FEW_ROWS) return 0;
+    if (layout_a == ROWS && layout_b == ROWS && few_rows(m, k)) return 0;
     return partial_bytes(m, n, plan_of(m, n, k, dtype));
 }
 
@@ -194,7 +195,7 @@ hipError_t launch_gemm(GemmArgs a, int dtype, int layout_a, int layout_b, int ki
     if (a.m < 1 || a.n < 1) return hipSuccess;
     return with_type(dtype, [&](auto dt) {
         constexpr int DT = dt.value;
-        if (layout_a == ROWS && layout_b == ROWS && a.m <= FEW_ROWS) return run_few_rows<DT>(a, kind, s);
+        if (layout_a == ROWS && layout_b == ROWS && few_rows(a.m, a.k)) return run_few_rows<DT>(a, kind, s);
         const Plan p = plan_of(a.m, a.n, a.k, dtype);
         const bool d = direct(a.a, a.lda, layout_a == ROWS ? a.m : a.k, a.k, dtype, layout_a) && direct(a.b, a.ldb, layout_b == ROWS ? a.n : a.k, a.k, dtype, layout_b);
         if (layout_a == ROWS && layout_b == ROWS) return run_gemm<DT, ROWS, ROWS>(a, d, p, kind, s);

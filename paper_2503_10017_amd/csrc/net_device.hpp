@@ -96,22 +96,23 @@ __device__ __forceinline__ float over(float a, float b) {
     if constexpr (FAST) return a * __builtin_amdgcn_rcpf(b);
     else return a / b;
 }
-// Phi(x), the integral of the normal density up to x; exp(-x^2 / 2) comes along.
+// Phi(-|x|), the integral of the normal density beyond |x|; exp(-x^2 / 2) comes along.
 template <bool FAST>
-__device__ __forceinline__ float normal_integral(float x, float& gauss) {
-    gauss = exp_of<FAST>(-0.5f * x * x);
+__device__ __forceinline__ float normal_tail(float x, float& gauss) {
     if constexpr (FAST) {
+        gauss = __builtin_amdgcn_exp2f(x * (x * -0.72134752f));
         const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(x), 0.3275911f * 0.70710678f, 1.f));
-        float p = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
-        p = __builtin_fmaf(t, p, 1.421413741f);
-        p = __builtin_fmaf(t, p, -0.284496736f);
-        p = __builtin_fmaf(t, p, 0.254829592f);
-        const float tail = 0.5f * p * t * gauss;  // Phi(-|x|)
-        return x < 0.f ? tail : 1.f - tail;
+        float p = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+        p = __builtin_fmaf(t, p, 0.5f * 1.421413741f);
+        p = __builtin_fmaf(t, p, 0.5f * -0.284496736f);
+        p = __builtin_fmaf(t, p, 0.5f * 0.254829592f);
+        return p * t * gauss;
     } else {
-        return 0.5f * erfcf(-0.70710678118654752f * x);
+        gauss = expf(-0.5f * x * x);
+        return 0.5f * erfcf(0.70710678118654752f * __builtin_fabsf(x));
     }
 }
+
 // x = act(x), for N values; the choice is the same in every lane and made once.
 template <bool FAST, int N>
 __device__ __forceinline__ void activate(float (&x)[N], int act) {
@@ -121,8 +122,10 @@ __device__ __forceinline__ void activate(float (&x)[N], int act) {
     } else if (act == ACT_GELU) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
+            // x Phi(x) = max(x, 0) - |x| Phi(-|x|), whose second term is 0 long before |x| = 64 and must stay 0 at infinity
             float gauss;
-            x[e] *= normal_integral<FAST>(x[e], gauss);
+            const float tail = normal_tail<FAST>(x[e], gauss);
+            x[e] = __builtin_fmaf(-__builtin_fminf(__builtin_fabsf(x[e]), 64.f), tail, x[e] < 0.f ? 0.f : x[e]);
         }
     } else if (act == ACT_SILU) {
 #pragma unroll
@@ -139,8 +142,8 @@ __device__ __forceinline__ void times_slope(float (&p)[N], const float (&x)[N], 
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             float gauss;
-            const float phi = normal_integral<FAST>(x[e], gauss);
-            p[e] *= __builtin_fmaf(x[e] * 0.39894228f, gauss, phi);
+            const float tail = normal_tail<FAST>(x[e], gauss);
+            p[e] *= __builtin_fmaf(x[e] * 0.39894228f, gauss, x[e] < 0.f ? tail : 1.f - tail);
         }
     } else if (act == ACT_SILU) {
 #pragma unroll

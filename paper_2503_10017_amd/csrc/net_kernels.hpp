@@ -86,6 +86,7 @@ struct AttentionArgs {
     float scale;
     int32_t direct;        // keys and values lie on 16-byte boundaries
     int32_t row_tiles, splits, d_pad;
+    int32_t part_tiles;    // tiles of keys in a part of a split call
     float* partial;
 };
 size_t attention_workspace(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d);
