@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     int t0, t1;
     part_of(a, (most + KEYS - 1) / KEYS, t0, t1);
 
-    const int least_seen = mine < rows ? seen_by(a, s, mine) : 0, most_seen = mine < rows ? seen_by(a, s, min(mine + WAVE_ROWS, rows) - 1) : 0;
+    const int least_seen = seen_by(a, s, min(mine, rows - 1));
     int seen[QB];
 #pragma unroll
     for (int b = 0; b < QB; ++b) seen[b] = seen_by(a, s, min(mine + 32 * b + (lane & 31), rows - 1));
@@ -203,16 +203,23 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
         Tile::template stage<256, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, threadIdx.x);
         Tile::template stage<256, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, threadIdx.x);
     };
-    if (t0 < t1) stage(stages[0], t0);
-    W w;
-    w.begin(a, s, group, mine, rows, lane);
-    for (int t = t0, turn = 0; t < t1; ++t, turn ^= 1) {
-        const char* now = stages[turn];
+    auto next_tile = [&](int t, int turn) {
         lds_loads_arrived();
         __syncthreads();
         if (t + 1 < t1) stage(stages[turn ^ 1], t + 1);
+    };
+    if (t0 < t1) stage(stages[0], t0);
+    if (mine >= rows) {  // a wave without rows only brings tiles
+        for (int t = t0, turn = 0; t < t1; ++t, turn ^= 1) next_tile(t, turn);
+        return;
+    }
+    W w;
+    w.begin(a, s, group, mine, rows, lane);
+    // Every wave multiplies every tile, the last causal ones too that its rows do not see: passed over, they cost a copy of `out` on every tile.
+    for (int t = t0, turn = 0; t < t1; ++t, turn ^= 1) {
+        const char* now = stages[turn];
+        next_tile(t, turn);
         const int key = t * KEYS;
-        if (key >= most_seen) continue;
         w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least_seen, lane);
     }
     finish_rows(a, s, group, mine, rows, t0 < t1, w, lane);
@@ -298,44 +305,49 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     finish_rows(a, s, group, first, rows, t0 < t1, w, lane);
 }
 
-// Joins the shares of a split call, a workgroup per row: its eight groups of 32 lanes take shares in turn, a lane four elements of each.
-template <int DT>
+// Joins the shares of a split call: groups of 32 lanes, a lane four elements of a row.  Of few rows each has a workgroup, whose eight groups take
+// shares in turn; of many (GROUPS == 1) every group has a row of its own.
+template <int DT, int GROUPS>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
-    __shared__ float keeps[MOST_SPLITS];
-    __shared__ f32x4 joined[8][32];
-    const int64_t row = blockIdx.x;
-    const int token = (int)(row / a.heads), head = (int)(row - (int64_t)token * a.heads), lane = threadIdx.x & 63, place = threadIdx.x & 31, group = threadIdx.x >> 5;
+    __shared__ f32x4 joined[GROUPS][32];
+    const int place = threadIdx.x & 31, group = threadIdx.x >> 5, mine = GROUPS == 1 ? 0 : group;
+    const int64_t row = GROUPS == 1 ? (int64_t)blockIdx.x * 8 + group : blockIdx.x;
+    if (row >= (int64_t)a.tq * a.heads) return;
+    const int token = (int)(row / a.heads), head = (int)(row - (int64_t)token * a.heads);
     if (a.cu_q && (token < max(a.cu_q[0], 0) || token >= a.cu_q[a.batch])) return;  // a row of no sequence stays as it is
     const float c = a.scale * LOG2E;
-    float top = -__builtin_inff(), sum = 0.f;
-    if (lane < a.splits) top = share_stats(a, lane, row)[0], sum = share_stats(a, lane, row)[1];
-    float most = top;
+    float top = -__builtin_inff();
+    for (int s = place; s < a.splits; s += 32) top = __builtin_fmaxf(top, share_stats(a, s, row)[0]);
 #pragma unroll
-    for (int step = 1; step < 64; step <<= 1) most = __builtin_fmaxf(most, __shfl_xor(most, step));
-    const float base = most > -__builtin_inff() ? most * c : 0.f, keep = __builtin_amdgcn_exp2f(__builtin_fmaf(top, c, -base));
-    const float total = wave_sum(sum * keep);
-    if (threadIdx.x < a.splits) keeps[threadIdx.x] = keep;
-    __syncthreads();
+    for (int step = 1; step < 32; step <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, step));
+    const float base = top > -__builtin_inff() ? top * c : 0.f;
+    float sum = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    if (4 * place < a.d) {
 #pragma unroll 4
-        for (int s = group; s < a.splits; s += 8) {
-            const float k = keeps[s];
-            if (k == 0.f) continue;  // no keys: nothing was written
+    for (int s = mine; s < a.splits; s += GROUPS) {
+        const float* stats = share_stats(a, s, row);
+        const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(stats[0], c, -base));
+        if (keep == 0.f) continue;  // no keys: nothing was written
+        sum = __builtin_fmaf(stats[1], keep, sum);
+        if (4 * place < a.d) {
             const f32x4 y = *reinterpret_cast<const f32x4*>(share_row(a, s, row) + 4 * place);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(y[e], k, x[e]);
+            for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(y[e], keep, x[e]);
         }
     }
-    joined[group][place] = x;
-    __syncthreads();
-    if (group) return;
+    if constexpr (GROUPS > 1) {
+        __shared__ float sums[GROUPS];
+        joined[group][place] = x;
+        if (place == 0) sums[group] = sum;
+        __syncthreads();
+        if (group) return;
 #pragma unroll
-    for (int g = 1; g < 8; ++g) x += joined[g][place];
-    const float scale = total > 0.f ? 1.f / total : total != total ? total : 0.f;
+        for (int g = 1; g < GROUPS; ++g) x += joined[g][place], sum += sums[g];
+    }
+    const float scale = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
     const float v[4] = {x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale};
     if (4 * place < a.d) store_elems<DT, 4>((typename Elem<DT>::T*)a.out + token * a.out_row + head * a.out_head + 4 * place, a.d - 4 * place, v);
-    if (threadIdx.x == 0 && a.lse) a.lse[row] = most * a.scale + logf(total);
+    if (place == 0 && a.lse) a.lse[row] = top * a.scale + logf(sum);
 }
 
 // From the sizes alone: whether the rows of a sequence are few on average (one wave's worth), and into how many parts the keys may be split: parts of
@@ -368,7 +380,9 @@ hipError_t run(const AttentionArgs& a, const Plan& p, hipStream_t s) {
     const hipError_t e = p.few ? launch(TK_ATTENTION, attention_few_kernel<DT, DB, DIRECT>, grid, dim3(256), 0, s, a)
                                : launch(TK_ATTENTION, attention_kernel<DT, DB, 1, DIRECT>, grid, dim3(256), 0, s, a);
     if (e != hipSuccess || p.splits == 1) return e;
-    return launch(TK_ATTENTION, attention_join_kernel<DT>, dim3((unsigned)((int64_t)a.tq * a.heads)), dim3(256), 0, s, a);
+    const int64_t rows = (int64_t)a.tq * a.heads;
+    return rows < 2048 ? launch(TK_ATTENTION, attention_join_kernel<DT, 8>, dim3((unsigned)rows), dim3(256), 0, s, a)
+                       : launch(TK_ATTENTION, attention_join_kernel<DT, 1>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, a);
 }
 
 }  // namespace

@@ -19,7 +19,7 @@ namespace {
 template <int DT>
 constexpr int WEIGHT_SHIFT = DT == CT_F16 ? 14 : 0;
 
-// dq and delta: a wave has 32 rows and runs over tiles of 64 keys, which its workgroup's four waves share.
+// dq, and what the second pass takes of each row: a wave has 32 rows and runs over tiles of 64 keys, which its workgroup's four waves share.
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs a) {
     constexpr int KEYS = 64, ROWS = 128;
@@ -51,14 +51,16 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
             for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)x[e], (float)y[e], delta);
         }
         delta = across_halves_sum(delta);
-        if (r < rows) {
-            const int64_t at = flat_row(f, s, group, r);
-            lse = f.lse[at];
-            if (lane < 32) a.delta[at] = delta;
-        }
+        if (r < rows) lse = f.lse[flat_row(f, s, group, r)];
     }
     // a row that sees no key has minus infinity there; plus infinity makes its weights 0
     const float base = lse == -__builtin_inff() ? __builtin_inff() : lse * LOG2E, c = f.scale * LOG2E;
+    if (r < rows && lane < 32) {
+        const int64_t at = flat_row(f, s, group, r);
+        a.stats[at] = base - (float)WEIGHT_SHIFT<DT>;
+        a.stats[at + (int64_t)f.tq * f.heads] = delta * (1.f / (float)(1 << WEIGHT_SHIFT<DT>));
+    }
+    if (!a.dq) return;
     const int least_seen = mine < rows ? seen_by(f, s, mine) : 0, most_seen = mine < rows ? seen_by(f, s, min(mine + 32, rows) - 1) : 0;
     const int seen = seen_by(f, s, min(r, rows - 1));
     f32x16 dq[DB];
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
             }
         }
     }
-    if (!a.dq || r >= rows) return;
+    if (r >= rows) return;
     const int token = token_of(f, r), head = group * f.share + (r - token * f.share);
     E* to = (E*)a.dq + (s.q0 + token) * a.dq_row + head * a.dq_head;
 #pragma unroll
@@ -130,9 +132,9 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
     using Tile = HeadTile<DT, DB, ROWS>;
     using KeyTile = HeadTile<DT, DB, KEYS>;
     typedef typename Elem<DT>::T E;
-    // a stage: the rows' q, their dout, and lse (times log2 e, less the weights' shift) and delta (times the shift)
-    constexpr int STAGE = 2 * Tile::BYTES + 2 * ROWS * 4;
-    __shared__ __attribute__((aligned(16))) char stages[2][STAGE];
+    // a stage: the rows' q, their dout, and two numbers for each (room for a wave's 64 lanes of both)
+    constexpr int STAGE = 2 * Tile::BYTES + 2 * 64 * 4, STAGES = DIRECT && !KEYS_IN_LDS ? 3 : 2;
+    __shared__ __attribute__((aligned(16))) char stages[STAGES][STAGE];
     __shared__ __attribute__((aligned(16))) char key_tile[KEYS_IN_LDS ? KeyTile::BYTES : 16];
     const AttentionArgs& f = a.forward;
     int group, tile;
@@ -166,53 +168,52 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
     // The rows of a tile are share heads of ROWS / share tokens each where share divides ROWS: then a thread's place in the tile says how far
     // its row lies from the tile's first.  Otherwise its rows are found one by one.
     const bool even = ROWS % f.share == 0;
+    constexpr int PER_THREAD = ROWS * Tile::RUNS / 256, LOADS = 2 * PER_THREAD + 1;  // a stage's loads of a wave
+    static_assert(PER_THREAD > 0 && ROWS * Tile::RUNS % 256 == 0, "every thread has as many runs");
+    const float* stats_of = a.stats + (wave & 1) * (int64_t)f.tq * f.heads;
     auto stage = [&](char* to, int row0) {
-        constexpr int RUNS = ROWS * Tile::RUNS, PER_THREAD = RUNS / 256 > 0 ? RUNS / 256 : 1, THREADS = RUNS / PER_THREAD;
-        const int thread = threadIdx.x;
-        if (THREADS == 256 || thread < THREADS) {
-            const int token0 = token_of(f, row0);
-            const E* of_q = (const E*)f.q + (s.q0 + token0) * f.q_row + group * f.share * f.q_head;
-            const E* of_dout = (const E*)a.dout + (s.q0 + token0) * a.dout_row + group * f.share * a.dout_head;
+        const int token0 = token_of(f, row0);
+        const E* of_q = (const E*)f.q + (s.q0 + token0) * f.q_row + group * f.share * f.q_head;
+        const E* of_dout = (const E*)a.dout + (s.q0 + token0) * a.dout_row + group * f.share * a.dout_head;
 #pragma unroll
-            for (int i = 0; i < PER_THREAD; ++i) {
-                const int at = i * THREADS + thread, row = at / Tile::RUNS, run = (at % Tile::RUNS) ^ Tile::exchanged(row), r = row0 + row;
-                const int token = even ? token_of(f, row) : token_of(f, r) - token0, head = even ? row - token * f.share : r - (token0 + token) * f.share;
-                if constexpr (DIRECT) {
-                    const bool there = r < rows && run * 8 < f.d;
-                    const uint32_t q_at = (uint32_t)(token * (int)f.q_row + head * (int)f.q_head + run * 8) * 2;
-                    const uint32_t dout_at = (uint32_t)(token * (int)a.dout_row + head * (int)a.dout_head + run * 8) * 2;
-                    const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(to) + (i * THREADS + (thread & ~63)) * 16);
-                    load_to_lds(buffer_of(of_q, 0x80000000u), there ? q_at : 0xFFFFFFF0u, lds);
-                    load_to_lds(buffer_of(of_dout, 0x80000000u), there ? dout_at : 0xFFFFFFF0u, lds + Tile::BYTES);
-                } else {
-                    const int count = r < rows ? f.d - run * 8 : 0;
-                    *reinterpret_cast<uint4*>(to + at * 16) = load_run<DT>(of_q + token * f.q_row + head * f.q_head + run * 8, count);
-                    *reinterpret_cast<uint4*>(to + Tile::BYTES + at * 16) = load_run<DT>(of_dout + token * a.dout_row + head * a.dout_head + run * 8, count);
-                }
+        for (int i = 0; i < PER_THREAD; ++i) {
+            const int at = i * 256 + threadIdx.x, row = at / Tile::RUNS, run = (at % Tile::RUNS) ^ Tile::exchanged(row), r = row0 + row;
+            const int token = even ? token_of(f, row) : token_of(f, r) - token0, head = even ? row - token * f.share : r - (token0 + token) * f.share;
+            if constexpr (DIRECT) {
+                const bool there = r < rows && run * 8 < f.d;
+                const uint32_t q_at = (uint32_t)(token * (int)f.q_row + head * (int)f.q_head + run * 8) * 2;
+                const uint32_t dout_at = (uint32_t)(token * (int)a.dout_row + head * (int)a.dout_head + run * 8) * 2;
+                const uint32_t lds = lds_address(to) + (i * 256 + wave * 64) * 16;
+                load_to_lds(buffer_of(of_q, 0x80000000u), there ? q_at : 0xFFFFFFF0u, lds);
+                load_to_lds(buffer_of(of_dout, 0x80000000u), there ? dout_at : 0xFFFFFFF0u, lds + Tile::BYTES);
+            } else {
+                const int count = r < rows ? f.d - run * 8 : 0;
+                *reinterpret_cast<uint4*>(to + at * 16) = load_run<DT>(of_q + token * f.q_row + head * f.q_head + run * 8, count);
+                *reinterpret_cast<uint4*>(to + Tile::BYTES + at * 16) = load_run<DT>(of_dout + token * a.dout_row + head * a.dout_head + run * 8, count);
             }
         }
-        if (thread < ROWS) {
-            const int r = row0 + thread;
-            float lse = __builtin_inff(), delta = 0.f;
-            if (r < rows) {
-                const int64_t at = flat_row(f, s, group, r);
-                lse = f.lse[at];
-                lse = lse == -__builtin_inff() ? __builtin_inff() : lse * LOG2E - (float)WEIGHT_SHIFT<DT>;
-                delta = a.delta[at] * unshift;
-            }
-            float* stats = reinterpret_cast<float*>(to + 2 * Tile::BYTES);
-            stats[thread] = lse;
-            stats[ROWS + thread] = delta;
+        // The two numbers of each row, the first from even waves, the second from odd ones (twice, so that all waves wait for as many loads).  Rows that
+        // there are not get 0 and so a weight of 1, and have a q and dout of 0.
+        const int r = row0 + lane, token = token_of(f, r), head = group * f.share + (r - token * f.share);
+        const bool there = lane < ROWS && r < rows;
+        if constexpr (DIRECT) {
+            const uint32_t offset = (uint32_t)((token - token0) * f.heads + head) * 4;
+            load_word_to_lds(buffer_of(stats_of + (s.q0 + (int64_t)token0) * f.heads, 0x80000000u), there ? offset : 0xFFFFFFF0u, lds_address(to) + 2 * Tile::BYTES + (wave & 1) * 256);
+        } else {
+            reinterpret_cast<float*>(to + 2 * Tile::BYTES)[(wave & 1) * 64 + lane] = there ? stats_of[(s.q0 + (int64_t)token) * f.heads + head] : 0.f;
         }
     };
     const int start = sees(first) / ROWS * ROWS;
-    if (start < rows) stage(stages[0], start);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (start + i * ROWS < rows) stage(stages[i], start + i * ROWS);
     int turn = 0;
-    for (int row = start; row < rows; row += ROWS, turn ^= 1) {
+    for (int row = start; row < rows; row += ROWS, turn = turn + 1 == STAGES ? 0 : turn + 1) {
         const char* now = stages[turn];
-        lds_loads_arrived();
+        if (STAGES == 3 && row + ROWS < rows) lds_loads_left<LOADS>();
+        else lds_loads_arrived();
         __syncthreads();
-        if (row + ROWS < rows) stage(stages[turn ^ 1], row + ROWS);
+        if (row + (STAGES - 1) * ROWS < rows) stage(stages[turn == 0 ? STAGES - 1 : turn - 1], row + (STAGES - 1) * ROWS);
         if (row + ROWS <= wave_first || mine >= s.lk) continue;
 #pragma unroll
         for (int block = 0; block < ROWS / 32; ++block) {
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
                 for (int x = 0; x < 16; ++x) p[x] = tile_row(x, 0) >= least ? p[x] : 0.f;
             }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) ds[x] = p[x] * __builtin_fmaf(ds[x], unshift, -stats[ROWS + tile_row(x, 0)]);
+            for (int x = 0; x < 16; ++x) ds[x] = p[x] * __builtin_fmaf(ds[x], unshift, -stats[64 + tile_row(x, 0)]);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint4 w = round_half<DT>(p, half), g = round_half<DT>(ds, half);

@@ -104,19 +104,44 @@ __global__ __launch_bounds__(norm_threads(LANES)) void layer_norm_backward_kerne
         for (int e = 0; e < N; ++e) w[c][e] = 1.f, dw[c][e] = 0.f, db[c][e] = 0.f;
         if (a.weight && count > 0) load_elems<WT, N>((const W*)a.weight + at, count, w[c]);
     }
-    int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < a.n; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+    // A row is asked for while the one before it is worked on: with a workgroup's few rows in flight the time is the memory's latency otherwise
+    // (24576 x 1024 bf16, cold: 49 us without, 40 with).  Where a thread has 32 elements of a row, or a workgroup 1024 threads, the registers for it are not there.
+    constexpr bool AHEAD = CHUNKS * N <= 16 && LANES < 1024;
+    uint4 next_dy[CHUNKS], next_x[CHUNKS];
+    float next_mean = 0.f, next_rstd = 0.f;
+    auto ask = [&](int64_t row) {
+        if (row >= a.n) return;
         const T* dy = (const T*)a.dy + row * a.dy_stride;
         const T* x = (const T*)a.x + row * a.x_stride;
-        const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int at = (c * LANES + lane) * N;
+            next_dy[c] = load_run<DT>(dy + at, a.d - at);
+            next_x[c] = load_run<DT>(x + at, a.d - at);
+        }
+        next_mean = a.mean[row];
+        next_rstd = a.rstd[row];
+    };
+    const int64_t rows_on = (int64_t)gridDim.x * ROWS;
+    int turn = 0;
+    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES;
+    if (AHEAD) ask(row);
+    for (; row < a.n; row += rows_on, turn ^= 1) {
+        if (!AHEAD) ask(row);
+        const float mean = next_mean, rstd = next_rstd;
         float g[CHUNKS][N], h[CHUNKS][N];
         float sum_g = 0.f, sum_gh = 0.f;
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            const int at = (c * LANES + lane) * N, count = a.d - at;
-            load_elems<DT, N>(dy + at, count, g[c]);
-            load_elems<DT, N>(x + at, count, h[c]);
+            T raw[N];
+            __builtin_memcpy(raw, &next_dy[c], 16);
+#pragma unroll
+            for (int e = 0; e < N; ++e) g[c][e] = (float)raw[e];
+            __builtin_memcpy(raw, &next_x[c], 16);
+#pragma unroll
+            for (int e = 0; e < N; ++e) h[c][e] = (float)raw[e];
         }
+        if (AHEAD) ask(row + rows_on);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             const int count = a.d - (c * LANES + lane) * N;
@@ -236,7 +261,7 @@ hipError_t launch_layer_norm(const NormArgs& a, int dtype, int weight_dtype, hip
 
 int64_t layer_norm_backward_groups(int64_t n, int32_t d) {
     const int64_t groups = (n + 3) / 4;
-    return groups < 512 ? (groups < 1 ? 1 : groups) : 512;
+    return groups < 768 ? (groups < 1 ? 1 : groups) : 768;
 }
 
 hipError_t launch_layer_norm_backward(const NormBackArgs& a, int dtype, int weight_dtype, hipStream_t s) {

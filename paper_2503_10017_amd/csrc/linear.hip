@@ -1,4 +1,5 @@
 // Linear layers with their epilogue, and what their gradients need beside matrix products (fnn_linear, fnn_linear_backward).
+#include <algorithm>
 #include <type_traits>
 
 #include "gemm.hpp"
@@ -74,17 +75,33 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, int64_t strip) 
     for (int e = 0; e < N; ++e) sum[e] = 0.f;
     if (count > 0) {
         const int64_t end = min(a.m, (blockIdx.y + 1) * strip);
-        for (int64_t m = blockIdx.y * strip + strand; m < end; m += 8) {
-            float p[N];
-            load_elems<DT>((const E*)a.dy + m * a.dy_stride + at, count, p);
-            if (a.act != ACT_NONE) {
-                float x[N];
-                load_elems<DT>((const E*)a.pre + m * a.pre_stride + at, count, x);
-                times_slope<DT != CT_F32>(p, x, a.act);
-            }
+        auto take = [&](const uint4& raw_dy, const uint4& raw_pre, int64_t m) {
+            E y[N], x[N];
+            __builtin_memcpy(y, &raw_dy, 16);
+            __builtin_memcpy(x, &raw_pre, 16);
+            float p[N], v[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) p[e] = (float)y[e], v[e] = (float)x[e];
+            times_slope<DT != CT_F32>(p, v, a.act);
 #pragma unroll
             for (int e = 0; e < N; ++e) sum[e] += p[e];
             if (a.p) store_elems<DT>((E*)a.p + m * a.p_stride + at, count, p);
+        };
+        const bool slope = a.act != ACT_NONE;
+        const E* dy = (const E*)a.dy + at;
+        const E* pre = (const E*)a.pre + at;
+        int64_t m = blockIdx.y * strip + strand;
+        for (; m + 8 < end; m += 16) {  // two rows are asked for at once
+            const uint4 y0 = load_run<DT>(dy + m * a.dy_stride, count), y1 = load_run<DT>(dy + (m + 8) * a.dy_stride, count);
+            uint4 x0 = {0u, 0u, 0u, 0u}, x1 = x0;
+            if (slope) x0 = load_run<DT>(pre + m * a.pre_stride, count), x1 = load_run<DT>(pre + (m + 8) * a.pre_stride, count);
+            take(y0, x0, m);
+            take(y1, x1, m + 8);
+        }
+        if (m < end) {
+            uint4 x0 = {0u, 0u, 0u, 0u};
+            if (slope) x0 = load_run<DT>(pre + m * a.pre_stride, count);
+            take(load_run<DT>(dy + m * a.dy_stride, count), x0, m);
         }
     }
     if (!a.partial) return;
@@ -109,8 +126,10 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float* partial,
     const int strand = threadIdx.x >> 5;
     const int64_t column = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
     float sum = 0.f;
-    if (column < width)
+    if (column < width) {
+#pragma unroll 8
         for (int64_t g = strand; g < groups; g += 32) sum += partial[g * width + column];
+    }
     part[strand][threadIdx.x & 31] = sum;
     __syncthreads();
     if (strand == 0 && column < width) {
@@ -128,13 +147,19 @@ struct Plan {
 constexpr int64_t round_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 Plan plan_of(int64_t m, int64_t n, int64_t k, int dtype) {
     const int64_t big = round_to(m, 256) / 256 * (round_to(n, 256) / 256), small = round_to(m, 128) / 128 * (round_to(n, 128) / 128);
-    const bool whole = dtype != FNN_F32 && big >= 160;
-    const int64_t tiles = whole ? big : small, wanted = dtype == FNN_F32 ? 512 : 256, step = dtype == FNN_F32 ? 16 : 64;
-    const int64_t steps = (k + step - 1) / step;
-    int64_t splits = wanted / (tiles > 0 ? tiles : 1);
-    if (splits > steps / 8) splits = steps / 8;
-    if (splits > 32) splits = 32;
-    return {whole ? 256 : 128, splits < 1 ? 1 : (int)splits};
+    const int64_t step = dtype == FNN_F32 ? 16 : 64, steps = (k + step - 1) / step;
+    auto most = [&](int64_t tiles, int64_t wanted, int64_t least_steps, int64_t limit) {
+        const int64_t splits = std::min(std::min(wanted / std::max(tiles, (int64_t)1), steps / least_steps), limit);
+        return std::max(splits, (int64_t)1);
+    };
+    // The large tiles need less of the operands' traffic per product, and win where they, or up to four long shares of each, keep 160 compute units busy
+    // (12288 x 1024 -> 1024: 34 us in 192 large tiles, 36 in 768 small ones; 4096 x 12288 -> 1024: 112 us in 64 large ones of four shares, 117 in 256 small ones of two).
+    if (dtype != FNN_F32) {
+        const int64_t shares = most(big, 256, 16, 4);
+        if (big * shares >= 160) return {256, (int)shares};
+    }
+    // fp32 products are slow enough that two workgroups a compute unit pay for their shares; 16-bit ones are not (768 x 1024 -> 4096: 15 us in 192 tiles, 25 in 384).
+    return {128, (int)most(small, dtype == FNN_F32 ? 512 : 256, 8, 32)};
 }
 size_t partial_bytes(int64_t m, int64_t n, const Plan& p) {
     return p.splits > 1 ? (size_t)p.splits * round_to(m, p.tile) * round_to(n, p.tile) * sizeof(float) : 0;
@@ -205,7 +230,7 @@ hipError_t launch_gemm(GemmArgs a, int dtype, int layout_a, int layout_b, int ki
 }
 
 int64_t slope_strips(int64_t m, int64_t n) {
-    const int64_t across = (n + 255) / 256, wanted = 1024 / (across < 1 ? 1 : across), most = (m + 31) / 32;
+    const int64_t across = (n + 255) / 256, wanted = 2048 / (across < 1 ? 1 : across), most = (m + 15) / 16;
     const int64_t strips = wanted < most ? wanted : most;
     return strips < 1 ? 1 : strips;
 }

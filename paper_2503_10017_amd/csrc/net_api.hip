@@ -332,7 +332,7 @@ int32_t fnn_attention(const fnn_heads* q, const fnn_heads* k, const fnn_heads* v
 
 size_t fnn_attention_backward_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int32_t batch, int32_t heads, int32_t key_heads, int32_t d) {
     if (!attention_sizes(tokens_q, tokens_k, batch, heads, key_heads, d)) return 0;
-    return (size_t)tokens_q * heads * sizeof(float);
+    return (size_t)tokens_q * heads * 2 * sizeof(float);
 }
 
 int32_t fnn_attention_backward(const fnn_heads* dout, const fnn_heads* q, const fnn_heads* k, const fnn_heads* v, const fnn_heads* out,
@@ -354,7 +354,7 @@ int32_t fnn_attention_backward(const fnn_heads* dout, const fnn_heads* q, const 
     }
     if (q->n > 0 && !lse) return FNN_E_NULL;
     if (!dq && !dk && !dv) return FNN_OK;
-    FNN_CHECK(check_workspace(workspace, workspace_bytes, (size_t)q->n * q->heads * sizeof(float)));
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, (size_t)q->n * q->heads * 2 * sizeof(float)));
     a.forward.lse = const_cast<float*>(lse);
     a.dout = dout->data;
     a.dout_row = row_of(dout);
@@ -368,7 +368,7 @@ int32_t fnn_attention_backward(const fnn_heads* dout, const fnn_heads* q, const 
     a.dk_head = dk ? head_of(dk) : 0;
     a.dv_row = dv ? row_of(dv) : 0;
     a.dv_head = dv ? head_of(dv) : 0;
-    a.delta = (float*)workspace;
+    a.stats = (float*)workspace;
     // the heads of a group are reached from its first by 32-bit offsets too
     const int64_t apart = a.forward.share * (head_of(q) > head_of(dout) ? head_of(q) : head_of(dout));
     a.direct_rows = on_runs(q) && on_runs(dout) && apart < ((int64_t)1 << 28);

@@ -232,6 +232,10 @@ __device__ __forceinline__ uint32_t lds_address(const char* lds) {
 __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(buffer) : "m0", "memory");
 }
+// The same with 4 bytes per lane, to `to` + 4 * lane.
+__device__ __forceinline__ void load_word_to_lds(i32x4 buffer, uint32_t offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(buffer) : "m0", "memory");
+}
 // All but this wave's last N loads have arrived (no others are under way), and its reads of LDS before them are done.
 template <int N>
 __device__ __forceinline__ void lds_loads_left() {

