@@ -80,6 +80,7 @@ struct Rows {
             }
             // rows that have seen no key yet stay at minus infinity; anything finite in its place makes their weights 0
             const float base = top[b] > -__builtin_inff() ? top[b] * c : 0.f;
+            // summed up before they are rounded: lse has fp32's precision
             float more = 0.f;
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
@@ -351,8 +352,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
 }
 
 // From the sizes alone: whether the rows of a sequence are few on average (one wave's worth), and into how many parts the keys may be split: parts of
-// the size that makes 512 of them in all, which is what the chip holds at once, and not less than 256 keys, below which a part's start costs more than it
-// saves; twice as many as sequences of the average length would have, for the longer ones.
+// the size that makes 320 of them in all, a little more than one a compute unit, and not less than 256 keys, below which a part's start costs more than it
+// saves.  Longer sequences than the average have longer parts: as many of the right size for them all would be workgroups without keys for the others, each
+// of which holds a compute unit's LDS for 2 us (32 caches of 4096 keys, 4 heads of 128: 57 us, with parts for sequences twice as long 66).
 struct Plan {
     bool few;
     int row_tiles, splits, part_keys;
@@ -365,11 +367,11 @@ Plan plan_of(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t group
     p.row_tiles = (int)((rows + tile - 1) / tile + batch - 1);
     if (p.row_tiles > rows) p.row_tiles = (int)rows;
     const int64_t average = tk / batch;
-    int64_t part = ((int64_t)p.row_tiles * groups * average / 512 + 127) / 128 * 128;
+    int64_t part = ((int64_t)p.row_tiles * groups * average / 320 + 127) / 128 * 128;
     if (part < 256) part = 256;
-    int64_t splits = average <= part ? 1 : 2 * ((average + part - 1) / part);
+    int64_t splits = (average + part - 1) / part;
     if (splits > MOST_SPLITS) splits = MOST_SPLITS;
-    p.splits = (int)splits;
+    p.splits = splits < 1 ? 1 : (int)splits;
     p.part_keys = (int)(part < MOST_KEYS ? part : MOST_KEYS);
     return p;
 }

@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
     if (r < rows && lane < 32) {
         const int64_t at = flat_row(f, s, group, r);
         a.stats[at] = base - (float)WEIGHT_SHIFT<DT>;
-        a.stats[at + (int64_t)f.tq * f.heads] = delta * (1.f / (float)(1 << WEIGHT_SHIFT<DT>));
+        a.stats[at + (int64_t)f.tq * f.heads] = -delta;
     }
     if (!a.dq) return;
     const int least_seen = mine < rows ? seen_by(f, s, mine) : 0, most_seen = mine < rows ? seen_by(f, s, min(mine + 32, rows) - 1) : 0;
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
         if (key >= most_seen) continue;
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb) {
-            f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
+            f32x16 p = (f32x16)(0.f), ds = (f32x16)(-delta);  // dout v^T - delta: the product starts there
 #pragma unroll
             for (int i = 0; i < 2 * DB; ++i) {
                 p = mma32<DT>(Tile::along(keys, kb, i, lane), q[i], p);
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
                 for (int x = 0; x < 16; ++x) p[x] = 32 * kb + tile_row(x, 0) < left ? p[x] : 0.f;
             }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) ds[x] = p[x] * (ds[x] - delta);
+            for (int x = 0; x < 16; ++x) ds[x] *= p[x];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint4 g = round_half<DT>(ds, half);
@@ -217,13 +217,15 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
         if (row + ROWS <= wave_first || mine >= s.lk) continue;
 #pragma unroll
         for (int block = 0; block < ROWS / 32; ++block) {
-            f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
+            const float* stats = reinterpret_cast<const float*>(now + 2 * Tile::BYTES) + 32 * block + 4 * (lane >> 5);
+            f32x16 p = (f32x16)(0.f), ds;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) ds[x] = stats[64 + tile_row(x, 0)];  // dout v^T - delta: the product starts there
 #pragma unroll
             for (int i = 0; i < 2 * DB; ++i) {
                 p = mma32<DT>(Tile::along(now, block, i, lane), KEYS_IN_LDS ? KeyTile::along(key_tile, wave, i, lane) : k[KEYS_IN_LDS ? 0 : i], p);
                 ds = mma32<DT>(Tile::along(now + Tile::BYTES, block, i, lane), v[i], ds);
             }
-            const float* stats = reinterpret_cast<const float*>(now + 2 * Tile::BYTES) + 32 * block + 4 * (lane >> 5);
 #pragma unroll
             for (int x = 0; x < 16; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x], c, -stats[tile_row(x, 0)]));
             if (row + 32 * block < wave_all) {
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
                 for (int x = 0; x < 16; ++x) p[x] = tile_row(x, 0) >= least ? p[x] : 0.f;
             }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) ds[x] = p[x] * __builtin_fmaf(ds[x], unshift, -stats[64 + tile_row(x, 0)]);
+            for (int x = 0; x < 16; ++x) ds[x] = WEIGHT_SHIFT<DT> ? p[x] * (ds[x] * unshift) : p[x] * ds[x];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint4 w = round_half<DT>(p, half), g = round_half<DT>(ds, half);

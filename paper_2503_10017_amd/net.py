@@ -214,15 +214,19 @@ def fnn_attention_backward_workspace_bytes(tokens_q: int, tokens_k: int, batch: 
 
 def fnn_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
                            cu_q: Optional[torch.Tensor] = None, cu_k: Optional[torch.Tensor] = None, causal: bool = False,
-                           scale: Optional[float] = None, want_q: bool = True, want_kv: bool = True,
+                           scale: Optional[float] = None, want_q: bool = True, want_kv: bool = True, out_grads=None,
                            workspace: Optional[torch.Tensor] = None, stream=None):
-    """Gradient of fnn_attention from dout and the forward call's inputs and outputs; returns (dq, dk, dv), None where not wanted."""
+    """Gradient of fnn_attention from dout and the forward call's inputs and outputs; returns (dq, dk, dv), None where not wanted.
+    ``out_grads``: three tensors to write them to (slices of one buffer, say)."""
     lib = load_library()
     tokens, heads, d = q.shape
     batch, cq, ck = _sequences(cu_q, cu_k)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want_q else None
-    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if want_kv else None
-    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if want_kv else None
+    if out_grads is not None:
+        dq, dk, dv = out_grads
+    else:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want_q else None
+        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if want_kv else None
+        dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if want_kv else None
     if workspace is None:
         workspace = _workspace(lib.fnn_attention_backward_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d), q.device)
     grads = [None if g is None else _heads(g, "a gradient") for g in (dq, dk, dv)]
