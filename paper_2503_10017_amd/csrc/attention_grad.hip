@@ -5,6 +5,7 @@
 // keys by keys for dk and dv.  Seven products where five would do if the first pass could add into dk and dv; atomics would, in an order of their own.
 // As in the forward pass the lane owns a row (a key) of the scores and the next product's operand is what the last one left in its registers; the
 // tiles that are read along and across their rows lie in LDS once, for both.
+#include <algorithm>
 #include <type_traits>
 
 #include "attention_device.hpp"
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
         if (key >= most_seen) continue;
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb) {
-            f32x16 p = (f32x16)(0.f), ds = (f32x16)(-delta);  // dout v^T - delta: the product starts there
+            f32x16 p = (f32x16)(0.f), ds = (f32x16)(0.f);
 #pragma unroll
             for (int i = 0; i < 2 * DB; ++i) {
                 p = mma32<DT>(Tile::along(keys, kb, i, lane), q[i], p);
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
                 for (int x = 0; x < 16; ++x) p[x] = 32 * kb + tile_row(x, 0) < left ? p[x] : 0.f;
             }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) ds[x] *= p[x];
+            for (int x = 0; x < 16; ++x) ds[x] = p[x] * (ds[x] - delta);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint4 g = round_half<DT>(ds, half);
@@ -282,9 +283,10 @@ hipError_t run(const AttentionBackArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_attention_backward(AttentionBackArgs a, int dtype, hipStream_t s) {
-    const int64_t rows = (int64_t)a.forward.tq * a.forward.share;
-    a.forward.row_tiles = (int)((rows + 127) / 128 + a.forward.batch - 1);
-    a.key_tiles = (int)(((int64_t)a.forward.tk + 127) / 128 + a.forward.batch - 1);
+    // at most so many tiles, whatever the sequences' lengths
+    const int64_t rows = (int64_t)a.forward.tq * a.forward.share, keys = a.forward.tk;
+    a.forward.row_tiles = (int)std::min(rows, (rows + 127) / 128 + a.forward.batch - 1);
+    a.key_tiles = (int)std::min(keys, (keys + 127) / 128 + a.forward.batch - 1);
     const int blocks = (a.forward.d + 31) / 32;
     auto with_type = [&](auto dt) {
         constexpr int DT = dt.value;

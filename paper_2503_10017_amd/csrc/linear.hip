@@ -177,6 +177,7 @@ hipError_t run_gemm(GemmArgs a, bool is_direct, const Plan& p, int kind, hipStre
     a.tiles_m = (int)(round_to(a.m, p.tile) / p.tile);
     a.tiles_n = (int)(round_to(a.n, p.tile) / p.tile);
     a.splits = p.splits;
+    if ((int64_t)a.tiles_m * a.tiles_n * a.splits > INT32_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)((int64_t)a.tiles_m * a.tiles_n * a.splits));
     hipError_t e;
     if (DT != CT_F32 && p.tile == 256) {

@@ -74,9 +74,10 @@ int32_t check_heads(const fnn_heads* t) {
     if (t->n > 0 && !t->data) return FNN_E_NULL;
     return FNN_OK;
 }
+// Rows (queries times heads) and keys times their heads are counted in 32 bits, with room for a tile beyond the last.
 bool attention_sizes(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d) {
-    return tq >= 0 && tq <= MAX_SLOTS && tk >= 0 && tk <= MAX_SLOTS && batch >= 1 && batch <= MAX_SLOTS / 2 && heads >= 1 && heads <= 65535 && groups >= 1 &&
-           heads % groups == 0 && tq <= (MAX_SLOTS - 1024) / heads && tk <= MAX_SLOTS - 1024 && d >= 1 && d <= FNN_MAX_HEAD_DIM;
+    return tq >= 0 && tk >= 0 && batch >= 1 && batch <= MAX_SLOTS / 2 && heads >= 1 && heads <= 65535 && groups >= 1 && heads % groups == 0 &&
+           tq <= (MAX_SLOTS - 1024) / heads && tk <= (MAX_SLOTS - 1024) / groups && d >= 1 && d <= FNN_MAX_HEAD_DIM;
 }
 int64_t row_of(const fnn_heads* t) { return t->n > 1 ? t->row_stride : t->d; }
 int64_t head_of(const fnn_heads* t) { return t->heads > 1 ? t->head_stride : t->d; }

@@ -44,6 +44,17 @@ def _stream_ptr(stream, device):
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _scratch(need: int, device, stream):
+    """A workspace of the call's own (None: none is needed).  One that is used on a stream other than torch's current one must not be handed
+    out again before that stream has passed the call."""
+    if not need:
+        return None
+    workspace = _workspace(need, device)
+    if stream is not None:
+        workspace.record_stream(stream)
+    return workspace
+
+
 def _check(status: int, where: str):
     if status != 0:
         raise FnnError(status, where)
@@ -93,7 +104,7 @@ def fnn_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
         dweight = torch.empty(d, dtype=wt, device=x.device)
         dbias = torch.empty(d, dtype=wt, device=x.device)
         if workspace is None:
-            workspace = _workspace(lib.fnn_layer_norm_backward_workspace_bytes(n, d), x.device)
+            workspace = _scratch(lib.fnn_layer_norm_backward_workspace_bytes(n, d), x.device, stream)
     _check(lib.fnn_layer_norm_backward(_matrix(dy, "dy"), _matrix(x, "x"), _vector(mean, n, torch.float32, "mean"),
                                        _vector(rstd, n, torch.float32, "rstd"), _vector(weight, d, wt, "weight"),
                                        _DTYPES.get(wt, -1), _matrix(dx, "dx"), _ptr(dweight), _ptr(dbias), _ptr(workspace),
@@ -124,8 +135,7 @@ def fnn_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = 
         out = torch.empty((rows, outer), dtype=x.dtype, device=x.device)
     pre = torch.empty((rows, outer), dtype=x.dtype, device=x.device) if want_pre else None
     if workspace is None:
-        need = lib.fnn_linear_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype])
-        workspace = _workspace(need, x.device) if need else None
+        workspace = _scratch(lib.fnn_linear_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype]), x.device, stream)
     _check(lib.fnn_linear(xm, wm, _vector(bias, outer, x.dtype, "bias"), _ACTS[act], _matrix(residual, "residual"),
                           _matrix(out, "out"), _matrix(pre, "pre"), _ptr(workspace), 0 if workspace is None else workspace.numel(),
                           _stream_ptr(stream, x.device)), "fnn_linear")
@@ -150,7 +160,7 @@ def fnn_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre:
     dw = torch.empty((outer, inner), dtype=x.dtype, device=x.device) if want_w else None
     dbias = torch.empty(outer, dtype=x.dtype, device=x.device) if want_bias else None
     if workspace is None:
-        workspace = _workspace(lib.fnn_linear_backward_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype], _ACTS[act]), x.device)
+        workspace = _scratch(lib.fnn_linear_backward_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype], _ACTS[act]), x.device, stream)
     _check(lib.fnn_linear_backward(_matrix(dy, "dy"), _matrix(x, "x"), _matrix(w, "w"), _matrix(pre, "pre"), _ACTS[act],
                                    _matrix(dx, "dx"), _matrix(dw, "dw"), _ptr(dbias), _ptr(workspace), workspace.numel(),
                                    _stream_ptr(stream, x.device)), "fnn_linear_backward")
@@ -200,8 +210,7 @@ def fnn_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: Optio
         out = torch.empty((tokens, heads, d), dtype=q.dtype, device=q.device)
     lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if want_lse else None
     if workspace is None:
-        need = lib.fnn_attention_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d)
-        workspace = _workspace(need, q.device) if need else None
+        workspace = _scratch(lib.fnn_attention_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d), q.device, stream)
     _check(lib.fnn_attention(qm, km, vm, batch, cq, ck, causal, d ** -0.5 if scale is None else scale, _heads(out, "out"),
                              _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream, q.device)),
            "fnn_attention")
@@ -228,10 +237,10 @@ def fnn_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
         dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if want_kv else None
         dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if want_kv else None
     if workspace is None:
-        workspace = _workspace(lib.fnn_attention_backward_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d), q.device)
+        workspace = _scratch(lib.fnn_attention_backward_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d), q.device, stream)
     grads = [None if g is None else _heads(g, "a gradient") for g in (dq, dk, dv)]
     _check(lib.fnn_attention_backward(_heads(dout, "dout"), _heads(q, "q"), _heads(k, "k"), _heads(v, "v"), _heads(out, "out"),
                                       _vector(lse, tokens * heads, torch.float32, "lse"), batch, cq, ck, causal, d ** -0.5 if scale is None else scale,
-                                      *grads, _ptr(workspace), workspace.numel(), _stream_ptr(stream, q.device)),
+                                      *grads, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream, q.device)),
            "fnn_attention_backward")
     return dq, dk, dv
