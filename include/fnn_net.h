@@ -67,8 +67,8 @@ typedef enum {
  * [rows][outer] and bias [outer], all of one dtype.  bias, residual and pre may be NULL; pre receives p, which the gradient
  * takes.  Sizes of 0 are fine (inner == 0: p = bias).  16-bit types multiply on the 16-bit matrix instructions, FNN_F32 on the
  * fp32 ones; sums are fp32.  y may be the residual itself (same rows).
- * The workspace is for few tiles with a long `inner`, whose products are split and joined in a fixed order;
- * fnn_linear_workspace_bytes may return 0, and returns 0 for invalid sizes.
+ * The workspace is for few tiles with a long `inner`, whose products are split and joined in a fixed order, and for aligned copies of
+ * the operands of large products whose `inner` is odd; fnn_linear_workspace_bytes may return 0, and returns 0 for invalid sizes.
  * Errors: FNN_E_NULL, FNN_E_SHAPE, FNN_E_DTYPE, FNN_E_RANGE (act), FNN_E_WORKSPACE.
  */
 size_t fnn_linear_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype);

@@ -177,7 +177,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     OpB opb;
     opa.begin(a.a, a.lda, m0, a.m, (int64_t)s0 * OpA::STEP);
     opb.begin(a.b, a.ldb, n0, a.n, (int64_t)s0 * OpA::STEP);
-    int left = a.k - s0 * OpA::STEP;
+    int done = s0 * OpA::STEP;
     const int n = n0 + wn * 64 + 8 * (lane & 7);  // the first of the eight columns that this lane finishes
     Eight<DT> bias = {};
     if (a.bias && a.splits == 1) bias.load(a.bias, n, a.n - n);
@@ -191,15 +191,15 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     uint4 held_a[DIRECT ? 1 : OpA::PER_THREAD], held_b[DIRECT ? 1 : OpB::PER_THREAD];
     auto get = [&](char* to) {
         if constexpr (DIRECT) {
-            opa.stage(to, left);
-            opb.stage(to + OpA::BYTES, left);
+            opa.stage(to, (LA == ROWS ? a.k_a : a.k) - done);
+            opb.stage(to + OpA::BYTES, (LB == ROWS ? a.k_b : a.k) - done);
         } else {
-            opa.fetch(held_a, left);
-            opb.fetch(held_b, left);
+            opa.fetch(held_a, a.k - done);
+            opb.fetch(held_b, a.k - done);
         }
         opa.advance();
         opb.advance();
-        left -= OpA::STEP;
+        done += OpA::STEP;
     };
     auto put = [&](char* to) {
         if constexpr (!DIRECT) {

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, int64_t strip) 
             times_slope<DT != CT_F32>(p, v, a.act);
 #pragma unroll
             for (int e = 0; e < N; ++e) sum[e] += p[e];
-            if (a.p) store_elems<DT>((E*)a.p + m * a.p_stride + at, count, p);
+            if (a.p) store_elems<DT>((E*)a.p + m * a.p_stride + at, N, p);  // what lies behind dy's last element is 0
         };
         const bool slope = a.act != ACT_NONE;
         const E* dy = (const E*)a.dy + at;
@@ -165,6 +165,17 @@ size_t partial_bytes(int64_t m, int64_t n, const Plan& p) {
     return p.splits > 1 ? (size_t)p.splits * round_to(m, p.tile) * round_to(n, p.tile) * sizeof(float) : 0;
 }
 
+// Rows on 16-byte boundaries: a thread writes 16 bytes, read from wherever they are.
+template <int DT>
+__global__ __launch_bounds__(256) void copy_rows_kernel(const void* from, int64_t from_stride, int64_t rows, int64_t width, void* to, int64_t stride) {
+    typedef typename Elem<DT>::T E;
+    constexpr int N = Elem<DT>::N;
+    const int64_t runs = stride / N, at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / runs;
+    if (row >= rows) return;
+    const int64_t e = (at - row * runs) * N;
+    reinterpret_cast<uint4*>(to)[at] = load_run<DT>((const E*)from + row * from_stride + e, (int)min(width - e, (int64_t)N));
+}
+
 // Whether an operand's runs of 16 bytes lie on 16-byte boundaries, a tile's offsets fit 32 bits and k ends with a run.
 bool direct(const void* data, int64_t stride, int64_t rows, int64_t k, int dtype, int layout) {
     const int es = dtype == FNN_F32 ? 4 : 2;
@@ -211,6 +222,20 @@ hipError_t with_type(int dtype, F f) {
 
 }  // namespace
 
+// Microseconds with operands as they are (through registers) and copied, copies included, bf16.  Forward: 12288 x 1023 -> 4095 168 and 124, 12288 x 1001 -> 1001
+// 49 and 50, 2001 x 1001 -> 2003 26 and 29.  Gradients, whose products read an operand across its rows: 733 and 345, 200 and 114, 111 and 70,
+// 600 x 1001 -> 2003 70 and 48.
+bool copies_pay(int64_t m, int64_t n, int64_t k, int64_t width, int dtype, bool backward) {
+    return width * (dtype == FNN_F32 ? 4 : 2) % 16 != 0 && (double)m * n * k >= (backward ? 5e8 : 1.2e10);
+}
+
+hipError_t launch_copy_rows(const void* from, int64_t from_stride, int64_t rows, int64_t width, void* to, int64_t stride, int dtype, int kind, hipStream_t s) {
+    return with_type(dtype, [&](auto dt) {
+        const int64_t runs = rows * (stride / Elem<dt.value>::N);
+        return launch(kind, copy_rows_kernel<dt.value>, dim3((unsigned)((runs + 255) / 256)), dim3(256), 0, s, from, from_stride, rows, width, to, stride);
+    });
+}
+
 size_t gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, int layout_a, int layout_b) {
     if (m < 1 || n < 1) return 0;
     if (layout_a == ROWS && layout_b == ROWS && few_rows(m, k)) return 0;
@@ -223,7 +248,7 @@ hipError_t launch_gemm(GemmArgs a, int dtype, int layout_a, int layout_b, int ki
         constexpr int DT = dt.value;
         if (layout_a == ROWS && layout_b == ROWS && few_rows(a.m, a.k)) return run_few_rows<DT>(a, kind, s);
         const Plan p = plan_of(a.m, a.n, a.k, dtype);
-        const bool d = direct(a.a, a.lda, layout_a == ROWS ? a.m : a.k, a.k, dtype, layout_a) && direct(a.b, a.ldb, layout_b == ROWS ? a.n : a.k, a.k, dtype, layout_b);
+        const bool d = direct(a.a, a.lda, layout_a == ROWS ? a.m : a.k, a.k_a, dtype, layout_a) && direct(a.b, a.ldb, layout_b == ROWS ? a.n : a.k, a.k_b, dtype, layout_b);
         if (layout_a == ROWS && layout_b == ROWS) return run_gemm<DT, ROWS, ROWS>(a, d, p, kind, s);
         if (layout_a == ROWS) return run_gemm<DT, ROWS, COLUMNS>(a, d, p, kind, s);
         return run_gemm<DT, COLUMNS, COLUMNS>(a, d, p, kind, s);

@@ -37,7 +37,8 @@ int32_t check_workspace(const void* workspace, size_t have, size_t need) {
 int32_t done(hipError_t e) { return e == hipSuccess ? FNN_OK : FNN_E_HIP; }
 
 
-size_t aligned(size_t bytes) { return (bytes + 255) / 256 * 256; }
+size_t aligned_to(size_t bytes, size_t to) { return (bytes + to - 1) / to * to; }
+size_t aligned(size_t bytes) { return aligned_to(bytes, 256); }
 
 // Sizes that the linear layers take: every dimension an int32, so that tiles and columns are.
 bool linear_sizes(int64_t rows, int64_t inner, int64_t outer) {
@@ -45,20 +46,52 @@ bool linear_sizes(int64_t rows, int64_t inner, int64_t outer) {
 }
 bool same_shape(const fnn_map* m, int64_t n, int64_t d) { return m->n == n && m->d == d; }
 
-// The workspace of the linear gradient: q, the shares of dbias, and one area that the two products use in turn.
+int64_t whole_runs(int64_t n, size_t es) { return (int64_t)aligned_to(n * es, 16) / (int64_t)es; }
+
+// The workspace of a linear layer: copies of its operands where their rows do not end on 16-byte boundaries, and the shares of its product.
+struct LinearLayout {
+    size_t x, w, partial, total;  // offsets
+    bool copies;
+    int64_t stride;               // of the copies
+};
+LinearLayout linear_layout(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
+    LinearLayout L;
+    const size_t es = dtype == FNN_F32 ? 4 : 2;
+    L.stride = whole_runs(inner, es);
+    L.copies = copies_pay(rows, outer, inner, inner, dtype, false);
+    size_t at = 0;
+    L.x = at;
+    if (L.copies) at += aligned((size_t)rows * L.stride * es);
+    L.w = at;
+    if (L.copies) at += aligned((size_t)outer * L.stride * es);
+    L.partial = at;
+    L.total = at + gemm_workspace(rows, outer, inner, dtype, 0, 0);
+    return L;
+}
+
+// That of its gradient: q (dy itself where it has no activation and its rows end well), the shares of dbias, copies of w and x, and one
+// area that the two products use in turn.
 struct LinearBackLayout {
-    size_t q, sums, partial, total;  // offsets
-    int64_t q_stride;
+    size_t q, sums, x, w, partial, total;  // offsets
+    bool own_q, copies;
+    int64_t q_stride, stride;
 };
 LinearBackLayout linear_back_layout(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t act) {
     LinearBackLayout L;
     const size_t es = dtype == FNN_F32 ? 4 : 2;
-    L.q_stride = (outer + 7) / 8 * 8;
+    L.own_q = act != FNN_ACT_NONE || copies_pay(rows, inner, outer, outer, dtype, true);
+    L.copies = copies_pay(rows, inner, outer, inner, dtype, true);
+    L.q_stride = whole_runs(outer, es);
+    L.stride = whole_runs(inner, es);
     size_t at = 0;
     L.q = at;
-    if (act != FNN_ACT_NONE) at += aligned((size_t)rows * L.q_stride * es);
+    if (L.own_q) at += aligned((size_t)rows * L.q_stride * es);
     L.sums = at;
     at += aligned((size_t)slope_strips(rows, outer) * outer * sizeof(float));
+    L.x = at;
+    if (L.copies) at += aligned((size_t)rows * L.stride * es);
+    L.w = at;
+    if (L.copies) at += aligned((size_t)outer * L.stride * es);
     L.partial = at;
     const size_t x = gemm_workspace(rows, inner, outer, dtype, 0, 1), w = gemm_workspace(outer, inner, rows, dtype, 1, 1);
     L.total = at + aligned(x > w ? x : w);
@@ -199,7 +232,7 @@ int32_t fnn_layer_norm_backward(const fnn_map* dy, const fnn_map* x, const float
 
 size_t fnn_linear_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
     if (!linear_sizes(rows, inner, outer) || !valid_type(dtype)) return 0;
-    return gemm_workspace(rows, outer, inner, dtype, 0, 0);
+    return linear_layout(rows, inner, outer, dtype).total;
 }
 
 int32_t fnn_linear(const fnn_map* x, const fnn_map* w, const void* bias, int32_t act, const fnn_map* residual,
@@ -215,7 +248,10 @@ int32_t fnn_linear(const fnn_map* x, const fnn_map* w, const void* bias, int32_t
     if (w->dtype != x->dtype || y->dtype != x->dtype || (residual && residual->dtype != x->dtype) || (pre && pre->dtype != x->dtype))
         return FNN_E_DTYPE;
     if (act < FNN_ACT_NONE || act > FNN_ACT_SILU) return FNN_E_RANGE;
-    FNN_CHECK(check_workspace(workspace, workspace_bytes, fnn_linear_workspace_bytes(rows, inner, outer, x->dtype)));
+    const LinearLayout L = linear_layout(rows, inner, outer, x->dtype);
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, L.total));
+    const hipStream_t s = (hipStream_t)stream;
+    char* ws = (char*)workspace;
     GemmArgs a;
     memset(&a, 0, sizeof(a));
     a.a = x->data;
@@ -224,7 +260,16 @@ int32_t fnn_linear(const fnn_map* x, const fnn_map* w, const void* bias, int32_t
     a.ldb = stride_of(w);
     a.m = rows;
     a.n = (int32_t)outer;
-    a.k = (int32_t)inner;
+    a.k = a.k_a = a.k_b = (int32_t)inner;
+    if (L.copies) {
+        if (launch_copy_rows(a.a, a.lda, rows, inner, ws + L.x, L.stride, x->dtype, TK_LINEAR, s) != hipSuccess ||
+            launch_copy_rows(a.b, a.ldb, outer, inner, ws + L.w, L.stride, x->dtype, TK_LINEAR, s) != hipSuccess)
+            return FNN_E_HIP;
+        a.a = ws + L.x;
+        a.b = ws + L.w;
+        a.lda = a.ldb = L.stride;
+        a.k_a = a.k_b = (int32_t)L.stride;
+    }
     a.y = const_cast<void*>(y->data);
     a.bias = bias;
     a.residual = residual ? residual->data : nullptr;
@@ -233,8 +278,8 @@ int32_t fnn_linear(const fnn_map* x, const fnn_map* w, const void* bias, int32_t
     a.ldr = residual ? stride_of(residual) : 0;
     a.ldp = pre ? stride_of(pre) : 0;
     a.act = act;
-    a.partial = (float*)workspace;
-    return done(launch_gemm(a, x->dtype, 0, 0, TK_LINEAR, (hipStream_t)stream));
+    a.partial = (float*)(ws + L.partial);
+    return done(launch_gemm(a, x->dtype, 0, 0, TK_LINEAR, s));
 }
 
 size_t fnn_linear_backward_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t act) {
@@ -267,12 +312,13 @@ int32_t fnn_linear_backward(const fnn_map* dy, const fnn_map* x, const fnn_map* 
 
     const void* q = dy->data;
     int64_t q_stride = stride_of(dy);
-    if (outer > 0 && ((slope && (dx || dw) && rows > 0) || dbias)) {
+    const bool own_q = L.own_q && (dx || dw);
+    if (outer > 0 && ((own_q && rows > 0) || dbias)) {
         SlopeArgs a;
         memset(&a, 0, sizeof(a));
         a.dy = dy->data;
         a.pre = slope ? pre->data : nullptr;
-        a.p = slope && (dx || dw) ? ws + L.q : nullptr;
+        a.p = own_q ? ws + L.q : nullptr;
         a.partial = dbias ? (float*)(ws + L.sums) : nullptr;
         a.m = rows;
         a.dy_stride = stride_of(dy);
@@ -283,7 +329,17 @@ int32_t fnn_linear_backward(const fnn_map* dy, const fnn_map* x, const fnn_map* 
         if (launch_slope(a, x->dtype, s) != hipSuccess) return FNN_E_HIP;
         if (dbias && launch_column_sums(a.partial, slope_strips(rows, outer), outer, outer, dbias, nullptr, x->dtype, TK_LINEAR_BACKWARD, s) != hipSuccess)
             return FNN_E_HIP;
-        if (slope) q = ws + L.q, q_stride = L.q_stride;
+    }
+    if (own_q) q = ws + L.q, q_stride = L.q_stride;
+    const void* of_x = x->data;
+    const void* of_w = w->data;
+    int64_t x_stride = stride_of(x), w_stride = stride_of(w);
+    if (L.copies) {
+        if (dw && launch_copy_rows(of_x, x_stride, rows, inner, ws + L.x, L.stride, x->dtype, TK_LINEAR_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+        if (dx && launch_copy_rows(of_w, w_stride, outer, inner, ws + L.w, L.stride, x->dtype, TK_LINEAR_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+        of_x = ws + L.x;
+        of_w = ws + L.w;
+        x_stride = w_stride = L.stride;
     }
     GemmArgs a;
     memset(&a, 0, sizeof(a));
@@ -291,11 +347,12 @@ int32_t fnn_linear_backward(const fnn_map* dy, const fnn_map* x, const fnn_map* 
     if (dx) {
         a.a = q;
         a.lda = q_stride;
-        a.b = w->data;
-        a.ldb = stride_of(w);
+        a.b = of_w;
+        a.ldb = w_stride;
         a.m = rows;
         a.n = (int32_t)inner;
-        a.k = (int32_t)outer;
+        a.k = a.k_a = a.k_b = (int32_t)outer;
+        if (own_q) a.k_a = (int32_t)L.q_stride;
         a.y = const_cast<void*>(dx->data);
         a.ldy = stride_of(dx);
         if (launch_gemm(a, x->dtype, 0, 1, TK_LINEAR_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
@@ -303,11 +360,11 @@ int32_t fnn_linear_backward(const fnn_map* dy, const fnn_map* x, const fnn_map* 
     if (dw) {
         a.a = q;
         a.lda = q_stride;
-        a.b = x->data;
-        a.ldb = stride_of(x);
+        a.b = of_x;
+        a.ldb = x_stride;
         a.m = outer;
         a.n = (int32_t)inner;
-        a.k = (int32_t)rows;
+        a.k = a.k_a = a.k_b = (int32_t)rows;
         a.y = const_cast<void*>(dw->data);
         a.ldy = stride_of(dw);
         if (launch_gemm(a, x->dtype, 1, 1, TK_LINEAR_BACKWARD, s) != hipSuccess) return FNN_E_HIP;

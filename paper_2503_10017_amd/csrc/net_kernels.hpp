@@ -44,6 +44,7 @@ struct GemmArgs {
     int64_t lda, ldb;  // elements between rows
     int64_t m;
     int32_t n, k;
+    int32_t k_a, k_b;  // what may be read of a row that runs along k, as of k elements or, where zeros follow them, more
     void* y;
     const void* bias;
     const void* residual;
@@ -57,11 +58,17 @@ struct GemmArgs {
 size_t gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, int layout_a, int layout_b);
 hipError_t launch_gemm(GemmArgs a, int dtype, int layout_a, int layout_b, int trace_kind, hipStream_t s);
 
+// Whether a product of these sizes (forward, or one of the two of a gradient) is worth copies of operands whose rows of `width` elements do not end on
+// 16-byte boundaries.
+bool copies_pay(int64_t m, int64_t n, int64_t k, int64_t width, int dtype, bool backward);
+// to[r][0 .. stride) = from[r][0 .. width), then zeros; to and its rows lie on 16-byte boundaries.
+hipError_t launch_copy_rows(const void* from, int64_t from_stride, int64_t rows, int64_t width, void* to, int64_t stride, int dtype, int trace_kind, hipStream_t s);
+
 // p = dy * act'(pre), rounded to dy's type, and the column sums of p before that rounding, as shares of strips of rows.
 struct SlopeArgs {
     const void* dy;
     const void* pre;
-    void* p;          // NULL: not wanted
+    void* p;          // rows of n elements and zeros up to a multiple of 16 bytes; NULL: not wanted
     float* partial;   // [strips][n]; NULL: not wanted
     int64_t m, dy_stride, pre_stride, p_stride;
     int32_t n, act;

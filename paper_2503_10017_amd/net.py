@@ -162,7 +162,7 @@ def fnn_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre:
     if workspace is None:
         workspace = _scratch(lib.fnn_linear_backward_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype], _ACTS[act]), x.device, stream)
     _check(lib.fnn_linear_backward(_matrix(dy, "dy"), _matrix(x, "x"), _matrix(w, "w"), _matrix(pre, "pre"), _ACTS[act],
-                                   _matrix(dx, "dx"), _matrix(dw, "dw"), _ptr(dbias), _ptr(workspace), workspace.numel(),
+                                   _matrix(dx, "dx"), _matrix(dw, "dw"), _ptr(dbias), _ptr(workspace), 0 if workspace is None else workspace.numel(),
                                    _stream_ptr(stream, x.device)), "fnn_linear_backward")
     return dx, dw, dbias
 

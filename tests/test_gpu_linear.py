@@ -182,6 +182,18 @@ def test_backward_strides_and_parts(m, k, n, act):
         assert torch.equal(part[i], whole[i]) and all(part[j] is None for j in range(3) if j != i)
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("m,k,n", [(2310, 2049, 2601), (2600, 2302, 2304), (900, 901, 903), (901, 904, 907), (800, 905, 904)])
+def test_large_products_of_odd_rows(m, k, n, kind):
+    """Operands whose rows do not end on 16-byte boundaries are copied where the product is large; zeros behind a copy's rows must not be
+    what NaN behind the caller's rows would be."""
+    dtype = TYPES[kind]
+    x, w, dy = (strided(normal(i, *s, std=t, dtype=dtype), 3, 1) for i, s, t in ((1, (m, k), 1), (2, (n, k), 1 / math.sqrt(k)), (3, (m, n), 1)))
+    check_forward(x, w, normal(4, n, dtype=dtype), None, "relu")
+    check_backward(dy, x, w, None, "none")
+    check_backward(dy, x, w, normal(5, m, n, dtype=dtype), "silu")
+
+
 def test_gradient_against_differences():
     """d/dt of sum(c * linear(x + t u, w + t v, b + t z)) at 0 by central differences of the formula in 64 bits.  pre is the exact one
     rounded to fp32."""
