@@ -8,7 +8,6 @@ namespace fnn {
 // How an operand lies in memory: its rows run along k, or its rows are the k's and run along m (n).
 enum : int { ROWS = 0, COLUMNS = 1 };
 
-
 // Who works on what: neighbouring workgroups are dealt to the 8 XCDs in turn, so each XCD is given a run of tiles of its own, in blocks
 // of 8 tiles of rows by as many tiles of columns as it takes, which share their operands in its L2.
 struct TileAt {
@@ -160,6 +159,13 @@ __device__ __forceinline__ void finish_run(const GemmArgs& a, int64_t m, int n, 
     finish_run<DT>(a, m, n, count, v, bias, residual);
 }
 
+// A workgroup's tile of TM x TN results, a wave's 128 x 64 or 64 x 64 of it in registers.  Per 128-byte step of k a tile of 256 x 256 stages 64 KB and has 64 products
+// a wave, two of whose operands come from LDS for every eight (large) or four (small) products; results leave through LDS, with the epilogue on the way.  What
+// bounds it: large products the matrix instructions at the power limit and the loads that do not quite hide behind them (4096 x 4096 -> 4096 fp16 115 us,
+// 1195 TFLOP/s, 87 % of the library's rate there; 12288 x 1024 -> 4096 with GELU 128 us, 805 TFLOP/s, some 20 us of them the epilogue); those of fewer
+// tiles than compute units the latency of a step.  fp32 1531 x 777 -> 1001: 43 us for 2.4 GFLOP, the latency of loads through registers.
+// Measured and slower or no faster: four stages of 64 bytes, loads spread between the products, operands asked for in the order of k rotated from tile to
+// tile, two half-workgroups taking turns at loads and products, tiles of 256 x 128.
 template <int DT, int TM, int TN, int WAVES_M, int WAVES_N, int SB, int STAGES, int LA, int LB, bool DIRECT>
 __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 64)) void gemm_kernel(GemmArgs a) {
     constexpr int THREADS = WAVES_M * WAVES_N * 64, BM = TM / WAVES_M / 32, BN = TN / WAVES_N / 32, PARTS = SB / 32;
@@ -230,8 +236,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     constexpr int LOADS = OpA::PER_THREAD + OpB::PER_THREAD;
     auto step = [&](int stage, int s) {
         const int later = s1 - 1 - s;  // steps whose loads may still be under way
-        if (STAGES >= 4 && later >= 2) lds_loads_left<2 * LOADS>();
-        else if (STAGES >= 3 && later >= 1) lds_loads_left<LOADS>();
+        if (STAGES >= 3 && later >= 1) lds_loads_left<LOADS>();
         else lds_loads_left<0>();
         meet();
         read(stages[stage], 0);
@@ -317,7 +322,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     }
 }
 
-// The shares of a split product, added up in the order of k.
+// The shares of a split product, added up in the order of k, so that the result does not depend on which workgroup ended first; the epilogue is here then.  Bound
+// by memory: 1024 x 4096 in four shares (67 MB written by the product, still in the caches) 12 us.
 template <int DT>
 __global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs a, int64_t pitch, int64_t share) {
     const int64_t runs = (a.n + 7) / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;

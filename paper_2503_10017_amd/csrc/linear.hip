@@ -15,7 +15,8 @@ bool few_rows(int64_t m, int64_t k) { return m <= 16 || (m <= 64 && m * k <= 983
 constexpr int FEW_WAVES = 8;
 
 // Few rows of a: the time is that of reading b once.  A workgroup takes 16 rows of b, its waves share k between them, and every
-// lane asks for all of its runs of four turns before it multiplies the first; a (its rows are few) comes out of the L2.
+// lane asks for all of its runs of four turns before it multiplies the first; a (its rows are few) comes out of the L2.  The shares are
+// joined in LDS in the order of the waves.  1 x 1024 -> 4096 bf16: 4.4 us, 1.9 TB/s of 8.4 MB; a launch that does nothing is about 3.5 of it.
 template <int DT, int BLOCKS>
 __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(GemmArgs a) {
     typedef typename Elem<DT>::T E;
@@ -62,7 +63,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(GemmArgs a) {
     if (m < a.m && n < a.n) finish_run<DT>(a, m, (int)n, (int)(a.n - n), v);
 }
 
-// p = dy * act'(pre): 256 columns a workgroup (two types: 8 elements a thread), 8 rows at a time, strip after strip of rows.
+// p = dy * act'(pre), and the columns' sums of it for the bias: 32 threads across, 16 bytes each, 8 rows at a time, one strip of rows a workgroup.  p is rounded
+// to the operands' type, as both products take it; the sums are of the unrounded values.  Bound by memory: 12288 x 4096 bf16 (302 MB) with GELU 56 us,
+// 5.4 TB/s.  It is a pass of its own because both products read p, one of them across its rows: formed in each, the slope would be worked out again for every tile that reads it.
 template <int DT>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, int64_t strip) {
     typedef typename Elem<DT>::T E;
@@ -118,7 +121,8 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, int64_t strip) 
     store_elems<CT_F32, N>(a.partial + blockIdx.y * (int64_t)a.n + at, count, sum);
 }
 
-// 32 columns a workgroup, 32 threads over the shares of each.
+// The sums of columns over the shares that other launches left: 32 columns a workgroup, 32 threads over the shares of each, added in one fixed order, so that a
+// gradient has the same bits every time.  768 shares of 2048 columns (6.3 MB): 4.5 us, of which 3.5 are a launch.
 template <int WT>
 __global__ __launch_bounds__(1024) void column_sums_kernel(const float* partial, int64_t groups, int64_t width, int64_t first, void* out, void* more) {
     typedef typename Elem<WT>::T W;
@@ -165,7 +169,8 @@ size_t partial_bytes(int64_t m, int64_t n, const Plan& p) {
     return p.splits > 1 ? (size_t)p.splits * round_to(m, p.tile) * round_to(n, p.tile) * sizeof(float) : 0;
 }
 
-// Rows on 16-byte boundaries: a thread writes 16 bytes, read from wherever they are.
+// Rows on 16-byte boundaries, zeros behind their ends: a thread writes 16 bytes, read from wherever they are.  Bound by memory and, below some MB, the launch:
+// 6001 x 1023 bf16 (25 MB) 8.5 us.
 template <int DT>
 __global__ __launch_bounds__(256) void copy_rows_kernel(const void* from, int64_t from_stride, int64_t rows, int64_t width, void* to, int64_t stride) {
     typedef typename Elem<DT>::T E;
@@ -222,11 +227,13 @@ hipError_t with_type(int dtype, F f) {
 
 }  // namespace
 
-// Microseconds with operands as they are (through registers) and copied, copies included, bf16.  Forward: 12288 x 1023 -> 4095 168 and 124, 12288 x 1001 -> 1001
-// 49 and 50, 2001 x 1001 -> 2003 26 and 29.  Gradients, whose products read an operand across its rows: 733 and 345, 200 and 114, 111 and 70,
-// 600 x 1001 -> 2003 70 and 48.
+// Microseconds with operands as they are (through registers) and copied, copies included.  Forward, bf16: 12288 x 1023 -> 4095 168 and 124, 12288 x 1001 -> 1001
+// 49 and 50, 6001 x 777 -> 1001 30 and 33; fp32: 6001 x 1023 -> 4095 463 and 439, 1531 x 777 -> 1001 44 and 49.  Gradients, whose products read an operand
+// across its rows, bf16: 12288 x 1023 -> 4095 733 and 345, 600 x 777 -> 1001 60 and 45, 200 x 501 -> 501 54 and 37, 8 x 1021 -> 4095 41 and 39, 16 x 101 -> 101 24 and
+// 27; fp32: 6001 x 777 -> 1001 305 and 271, 1531 x 777 -> 1001 100 and 100, 300 x 777 -> 1001 58 and 60.
 bool copies_pay(int64_t m, int64_t n, int64_t k, int64_t width, int dtype, bool backward) {
-    return width * (dtype == FNN_F32 ? 4 : 2) % 16 != 0 && (double)m * n * k >= (backward ? 5e8 : 1.2e10);
+    const double least = !backward ? 1.2e10 : dtype == FNN_F32 ? 2e9 : 3e7;
+    return width * (dtype == FNN_F32 ? 4 : 2) % 16 != 0 && (double)m * n * k >= least;
 }
 
 hipError_t launch_copy_rows(const void* from, int64_t from_stride, int64_t rows, int64_t width, void* to, int64_t stride, int dtype, int kind, hipStream_t s) {
