@@ -106,6 +106,28 @@ struct Rows {
             }
         }
     }
+
+    // A causal tile that some rows see only a part of is multiplied with its values' infinities and NaN cleared, since a weight of 0 would not keep them
+    // out; here the rows that see them get them.  No call without such values comes here.
+    __device__ __forceinline__ void add_not_finite(const E* v, int64_t stride, int d, int key, int end, const int (&seen)[QB], int lane) {
+#pragma unroll 1
+        for (int j = key; j < end; ++j) {
+            const E* of_key = v + j * stride;
+            if (!not_finite(of_key, d, lane)) continue;
+#pragma unroll
+            for (int i = 0; i < DB; ++i) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int e = 32 * i + tile_row(r, lane >> 5);
+                    const float x = e < d ? (float)of_key[e] : 0.f;
+                    const bool bad = !(__builtin_fabsf(x) < __builtin_inff());
+#pragma unroll
+                    for (int b = 0; b < QB; ++b) out[b][i][r] += bad && j < seen[b] ? x : 0.f;
+                    if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+    }
 };
 
 // Results of one row: element runs of 8 (`at` from 0, `count` of them exist).
@@ -174,7 +196,9 @@ __device__ __forceinline__ void part_of(const AttentionArgs& a, int tiles, int& 
     t1 = part < parts ? (int)((int64_t)tiles * (part + 1) / parts) : 0;
 }
 
-// Many rows: a workgroup's four waves have QB x 32 rows each and share tiles of 64 keys.
+// Many rows: a workgroup's four waves have QB x 32 rows each and share tiles of 64 keys.  Bound by the vector operations between the two products (per
+// score a multiply-add, a maximum, an exponential, an addition and half a rounding), which take longer than the products do: 32 sequences of 768 rows and keys, 16
+// heads of 64, bf16: 127 us, 610 TFLOP/s; packed causal rows up to 4001, 16 heads on 8, 128 elements, fp16: 568 us, 722 TFLOP/s.
 template <int DT, int DB, int QB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     constexpr int KEYS = 64, WAVE_ROWS = 32 * QB, ROWS = 4 * WAVE_ROWS;
@@ -182,10 +206,12 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     using Tile = typename W::Tile;
     typedef typename Elem<DT>::T E;
     __shared__ __attribute__((aligned(16))) char stages[2][2 * Tile::BYTES];
+    __shared__ int any_not_finite;
     int group, tile;
     deal(a.row_tiles, a.causal, group, tile);
     const Sequence s = find_sequence<ROWS>(a, tile);
     if (s.index < 0) return;
+    if (threadIdx.x == 0) any_not_finite = 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rows = s.lq * a.share, first = s.tile * ROWS, mine = first + wave * WAVE_ROWS;
     const int most = seen_by(a, s, min(first + ROWS, rows) - 1);
@@ -204,10 +230,14 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
         Tile::template stage<256, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, threadIdx.x);
         Tile::template stage<256, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, threadIdx.x);
     };
+    const int least_of_all = seen_by(a, s, first);  // of the workgroup's rows: the same for all its waves
     auto next_tile = [&](int t, int turn) {
         lds_loads_arrived();
         __syncthreads();
         if (t + 1 < t1) stage(stages[turn ^ 1], t + 1);
+        if (min((t + 1) * KEYS, s.lk) <= least_of_all) return;
+        if (Tile::template clear_not_finite<256>(stages[turn] + Tile::BYTES, threadIdx.x)) any_not_finite = 1;
+        __syncthreads();
     };
     if (t0 < t1) stage(stages[0], t0);
     if (mine >= rows) {  // a wave without rows only brings tiles
@@ -223,11 +253,14 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
         const int key = t * KEYS;
         w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least_seen, lane);
     }
+    if (t0 < t1 && any_not_finite) w.add_not_finite(v, a.v_row, a.d, max(t0, least_of_all / KEYS) * KEYS, min(t1 * KEYS, s.lk), seen, lane);
     finish_rows(a, s, group, mine, rows, t0 < t1, w, lane);
 }
 
 // Few rows (a token or some at the end of a cache): the time is that of reading the keys once.  Every wave has the same 32 rows and tiles of
-// 32 keys of its own, which only it waits for; at the end the four join in LDS.
+// 32 keys of its own, which only it waits for; at the end the four join in LDS.  32 caches of up to 4096 keys, one row for each of 16 heads on 4 of 128, bf16:
+// 51 us for 119 MB, 2.3 TB/s (one workgroup a compute unit at 128 KB of stages, and caches whose lengths differ); 32 equal caches of 4096 keys 57 us for
+// 268 MB, 4.7 TB/s.
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     constexpr int KEYS = 32, ROWS = 32;
@@ -257,6 +290,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
         Tile::template stage<64, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, lane);
     };
     int turn = 0;
+    bool cleared = false;
     if (t0 + wave < t1) stage(mine, t0 + wave);
     W w;
     w.begin(a, s, group, first, rows, lane);
@@ -266,8 +300,16 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
         lds_loads_arrived();
         if (t + 4 < t1) stage(next, t + 4);
         const int key = t * KEYS;
+        if (min(key + KEYS, s.lk) > least) {
+            cleared |= __ballot(Tile::template clear_not_finite<64>(now + Tile::BYTES, lane)) != 0;
+            __builtin_amdgcn_wave_barrier();
+        }
         w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least, lane);
     }
+    if (cleared)
+#pragma unroll 1
+        for (int t = t0 + wave; t < t1; t += 4)
+            if (min((t + 1) * KEYS, s.lk) > least) w.add_not_finite(v, a.v_row, a.d, t * KEYS, min((t + 1) * KEYS, s.lk), seen, lane);
     // The waves' results, each in its own stages' place: top and sum per lane, then the registers.
     __syncthreads();
     float* held = reinterpret_cast<float*>(stages) + wave * (64 * (2 + 16 * DB));
@@ -306,7 +348,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     finish_rows(a, s, group, first, rows, t0 < t1, w, lane);
 }
 
-// Joins the shares of a split call: groups of 32 lanes, a lane four elements of a row.  Of few rows each has a workgroup, whose eight groups take
+// Joins the shares of a split call, each share scaled by exp of its maximum less the largest, in the order of the shares (32 x 16 rows: 4.2 us, a launch): groups of 32 lanes, a lane four elements of a row.  Of few rows each has a workgroup, whose eight groups take
 // shares in turn; of many (GROUPS == 1) every group has a row of its own.
 template <int DT, int GROUPS>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {

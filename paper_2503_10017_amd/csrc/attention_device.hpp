@@ -99,6 +99,27 @@ struct HeadTile {
             }
         }
     }
+    // Infinities and NaN of a tile that has arrived become 0, by THREADS threads of which this is number `thread`; whether it had any.
+    template <int THREADS>
+    static __device__ __forceinline__ bool clear_not_finite(char* lds, int thread) {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < BYTES / 16 / THREADS; ++i) {
+            uint4* at = reinterpret_cast<uint4*>(lds + (i * THREADS + thread) * 16);
+            E v[8];
+            __builtin_memcpy(v, at, 16);
+            bool found = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const bool bad = !(__builtin_fabsf((float)v[e]) < __builtin_inff());
+                v[e] = bad ? (E)0.f : v[e];
+                found |= bad;
+            }
+            if (found) __builtin_memcpy(at, v, 16);
+            any |= found;
+        }
+        return any;
+    }
     // Rows 32 block .. + 31, elements 16 step + 8 h .. + 7 of each: an operand whose sum runs along the rows' elements.
     static __device__ __forceinline__ uint4 along(const char* lds, int block, int step, int lane) {
         const int row = 32 * block + (lane & 31), run = (2 * step + (lane >> 5)) ^ exchanged(row);
@@ -149,6 +170,14 @@ __device__ __forceinline__ int token_of(const AttentionArgs& a, int r) { return 
 // How many keys row r sees.
 __device__ __forceinline__ int seen_by(const AttentionArgs& a, const Sequence& s, int r) {
     return a.causal ? min(max(token_of(a, r) + (s.lk - s.lq) + 1, 0), s.lk) : s.lk;
+}
+
+// Whether one of a vector's d elements is an infinity or NaN; the same in all of a wave's lanes.
+template <typename E>
+__device__ __forceinline__ bool not_finite(const E* x, int d, int lane) {
+    bool bad = false;
+    for (int e = lane; e < d; e += 64) bad |= !(__builtin_fabsf((float)x[e]) < __builtin_inff());
+    return __ballot(bad) != 0;
 }
 
 // Where row r of a group is in lse and what else has a value per query and head.

@@ -20,13 +20,16 @@ namespace {
 template <int DT>
 constexpr int WEIGHT_SHIFT = DT == CT_F16 ? 14 : 0;
 
-// dq, and what the second pass takes of each row: a wave has 32 rows and runs over tiles of 64 keys, which its workgroup's four waves share.
+// dq, and what the second pass takes of each row: a wave has 32 rows and runs over tiles of 64 keys, which its workgroup's four waves share.  Three products a tile.
+// 12 sequences of up to 2048 rows, 12 heads of 64, bf16: 117 us, bound by the latency from product to exponential to product, of which a SIMD's two
+// waves hide part, and by the vector operations between them.
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs a) {
     constexpr int KEYS = 64, ROWS = 128;
     using Tile = HeadTile<DT, DB, KEYS>;
     typedef typename Elem<DT>::T E;
     __shared__ __attribute__((aligned(16))) char stages[2][2 * Tile::BYTES];
+    __shared__ int any_not_finite;
     const AttentionArgs& f = a.forward;
     int group, tile;
     deal(f.row_tiles, f.causal, group, tile);
@@ -75,13 +78,21 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
         Tile::template stage<256, DIRECT>(to, k + key * f.k_row, f.k_row, there, f.d, threadIdx.x);
         Tile::template stage<256, DIRECT>(to + Tile::BYTES, v + key * f.v_row, f.v_row, there, f.d, threadIdx.x);
     };
+    if (threadIdx.x == 0) any_not_finite = 0;
     if (tiles) stage(stages[0], 0);
+    const int least_of_all = seen_by(f, s, first);  // of the workgroup's rows: the same for all its waves
     for (int t = 0, turn = 0; t < tiles; ++t, turn ^= 1) {
-        const char* keys = stages[turn];
+        char* keys = stages[turn];
         lds_loads_arrived();
         __syncthreads();
         if (t + 1 < tiles) stage(stages[turn ^ 1], t + 1);
         const int key = t * KEYS;
+        // Keys that only some rows see: a weight of 0 would not keep an infinity or NaN out, so they are cleared, and rows that see them are spoiled at the end.
+        if (min(key + KEYS, s.lk) > least_of_all) {
+            const bool of_keys = Tile::template clear_not_finite<256>(keys, threadIdx.x), of_values = Tile::template clear_not_finite<256>(keys + Tile::BYTES, threadIdx.x);
+            if (of_keys || of_values) any_not_finite = 1;
+            __syncthreads();
+        }
         if (key >= most_seen) continue;
 #pragma unroll
         for (int kb = 0; kb < KEYS / 32; ++kb) {
@@ -108,6 +119,13 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
             }
         }
     }
+    float scale = f.scale;
+    if (tiles && any_not_finite) {
+        for (int j = least_of_all / KEYS * KEYS; j < min(tiles * KEYS, s.lk); ++j) {
+            const bool bad = not_finite(k + j * f.k_row, f.d, lane) || not_finite(v + j * f.v_row, f.d, lane);
+            if (bad && j < seen) scale = __builtin_nanf("");
+        }
+    }
     if (r >= rows) return;
     const int token = token_of(f, r), head = group * f.share + (r - token * f.share);
     E* to = (E*)a.dq + (s.q0 + token) * a.dq_row + head * a.dq_head;
@@ -119,13 +137,14 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
         for (int p = 0; p < 2; ++p) {
             const int at = 32 * i + 16 * p + 8 * (lane >> 5);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[p][e] *= f.scale;
+            for (int e = 0; e < 8; ++e) x[p][e] *= scale;
             if (at < f.d) store_elems<DT>(to + at, f.d - at, x[p]);
         }
     }
 }
 
 // dk and dv: a wave has 32 keys and runs over tiles of 64 rows, 32 of long vectors (of all the heads that share the key head), which its workgroup's four waves share.
+// Four products a tile: 166 us on the sequences above, bound as the first pass is.
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs a) {
     constexpr int KEYS = 128, ROWS = DB <= 2 ? 64 : 32;
@@ -137,6 +156,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
     constexpr int STAGE = 2 * Tile::BYTES + 2 * 64 * 4, STAGES = DIRECT && !KEYS_IN_LDS ? 3 : 2;
     __shared__ __attribute__((aligned(16))) char stages[STAGES][STAGE];
     __shared__ __attribute__((aligned(16))) char key_tile[KEYS_IN_LDS ? KeyTile::BYTES : 16];
+    __shared__ int any_not_finite;
     const AttentionArgs& f = a.forward;
     int group, tile;
     deal(a.key_tiles, false, group, tile);
@@ -204,17 +224,29 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
             reinterpret_cast<float*>(to + 2 * Tile::BYTES)[(wave & 1) * 64 + lane] = there ? stats_of[(s.q0 + (int64_t)token) * f.heads + head] : 0.f;
         }
     };
-    const int start = sees(first) / ROWS * ROWS;
+    const int start = sees(first) / ROWS * ROWS, all_see = sees(min(first + KEYS, s.lk) - 1);  // rows from all_see on see all of the workgroup's keys
+    if (threadIdx.x == 0) any_not_finite = 0;
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
         if (start + i * ROWS < rows) stage(stages[i], start + i * ROWS);
     int turn = 0;
     for (int row = start; row < rows; row += ROWS, turn = turn + 1 == STAGES ? 0 : turn + 1) {
-        const char* now = stages[turn];
+        char* now = stages[turn];
         if (STAGES == 3 && row + ROWS < rows) lds_loads_left<LOADS>();
         else lds_loads_arrived();
         __syncthreads();
         if (row + (STAGES - 1) * ROWS < rows) stage(stages[turn == 0 ? STAGES - 1 : turn - 1], row + (STAGES - 1) * ROWS);
+        // Rows that do not see all keys: as in the first pass, what is no number in them is cleared, and spoils the keys that they see at the end.
+        if (row < all_see) {
+            const bool of_q = Tile::template clear_not_finite<256>(now, threadIdx.x), of_dout = Tile::template clear_not_finite<256>(now + Tile::BYTES, threadIdx.x);
+            bool bad = of_q || of_dout;
+            if (threadIdx.x < ROWS) {
+                float& delta = reinterpret_cast<float*>(now + 2 * Tile::BYTES)[64 + threadIdx.x];
+                if (!(__builtin_fabsf(delta) < __builtin_inff())) delta = 0.f, bad = true;
+            }
+            if (bad) any_not_finite = 1;
+            __syncthreads();
+        }
         if (row + ROWS <= wave_first || mine >= s.lk) continue;
 #pragma unroll
         for (int block = 0; block < ROWS / 32; ++block) {
@@ -247,12 +279,24 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
             }
         }
     }
+    float spoiled[2] = {1.f, 1.f};  // dk, dv
+    if (start < rows && any_not_finite) {
+        for (int r = start; r < min((all_see + ROWS - 1) / ROWS * ROWS, rows); ++r) {
+            const int token = token_of(f, r), head = group * f.share + (r - token * f.share);
+            const bool bad = not_finite((const E*)f.q + (s.q0 + token) * f.q_row + head * f.q_head, f.d, lane) ||
+                             not_finite((const E*)a.dout + (s.q0 + token) * a.dout_row + head * a.dout_head, f.d, lane);
+            const float delta = a.stats[flat_row(f, s, group, r) + (int64_t)f.tq * f.heads];
+            if (r < from_row) continue;
+            if (bad) spoiled[1] = __builtin_nanf("");
+            if (bad || !(__builtin_fabsf(delta) < __builtin_inff())) spoiled[0] = __builtin_nanf("");
+        }
+    }
     if (key >= s.lk) return;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         if (!(which ? a.dv : a.dk)) continue;
         E* to = which ? (E*)a.dv + (s.k0 + (int64_t)key) * a.dv_row + group * a.dv_head : (E*)a.dk + (s.k0 + (int64_t)key) * a.dk_row + group * a.dk_head;
-        const float scale = which ? unshift : f.scale;
+        const float scale = (which ? unshift : f.scale) * spoiled[which];
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
             float x[2][8];

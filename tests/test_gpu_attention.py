@@ -188,6 +188,67 @@ def test_nan_and_infinity_reach_what_sees_them():
     assert torch.equal(out[keep], want[keep])
 
 
+NOT_YET_SEEN = [
+    # queries, keys, heads, key heads, dim, and a key that some queries see and some do not
+    (200, 200, 4, 2, 64, 1),
+    (200, 200, 2, 2, 128, 197),
+    (130, 300, 2, 1, 77, 200),
+    (90, 90, 3, 3, 32, 64),
+    (5, 700, 8, 2, 128, 697),
+    (9, 3000, 2, 2, 40, 2995),
+]
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("nq,nk,heads,groups,d,j", NOT_YET_SEEN)
+def test_causal_queries_know_nothing_of_later_keys(nq, nk, heads, groups, d, j, bad):
+    prob = Problem([nq], [nk], heads, groups, d, True, "bf16")
+    want, want_lse = prob.call()
+    first = j - (nk - nq)                                   # the first query that sees it
+    assert 0 < first < nq
+    share = heads // groups
+    kept = prob.v[j, 0, 3].clone()
+    prob.v[j, 0, 3] = bad
+    out, lse = prob.call()
+    assert not torch.isfinite(out[first:, :share, 3]).any()
+    out[first:, :share, 3] = want[first:, :share, 3]
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    prob.v[j, 0, 3] = kept
+    kept = prob.k[j, 0, 3].clone()
+    prob.k[j, 0, 3] = bad
+    out, lse = prob.call()
+    prob.k[j, 0, 3] = kept
+    if math.isnan(bad):
+        assert torch.isnan(out[first:, :share]).all() and torch.isnan(lse[first:, :share]).all()
+    out[first:, :share], lse[first:, :share] = want[first:, :share], want_lse[first:, :share]
+    check_forward(prob, out, lse)
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("which", ["q", "k", "v", "dout"])
+@pytest.mark.parametrize("nq,nk,heads,groups,d,j", NOT_YET_SEEN)
+def test_causal_gradients_know_nothing_of_what_is_not_seen(nq, nk, heads, groups, d, j, which, bad):
+    """out and lse are those of finite inputs, so only what sees the value itself can be reached by it."""
+    prob = Problem([nq], [nk], heads, groups, d, True, "bf16")
+    out, lse = prob.call()
+    want = backward(prob, out, lse)
+    i, share = j - (nk - nq), heads // groups               # query i sees keys up to j
+    if which in "kv":
+        getattr(prob, which)[j, 0, 3] = bad
+        dq, dk, dv = backward(prob, out, lse)
+        assert not torch.isfinite(dq[i:, :share]).all(-1).any() and not torch.isfinite(dk[j, 0]).all()
+        for got, w in ((dq[:i], want[0][:i]), (dq[:, share:], want[0][:, share:]), (dk[:j], want[1][:j]), (dk[j + 1:], want[1][j + 1:]), (dv[:j], want[2][:j]),
+                       (dv[j + 1:], want[2][j + 1:])):
+            assert torch.equal(got, w)
+    else:
+        getattr(prob, which)[i, 0, 3] = bad
+        dq, dk, dv = backward(prob, out, lse)
+        if math.isnan(bad):  # a query with an infinity may have scores of minus infinity alone, weights of 0 and gradients of 0
+            assert torch.isnan(dq[i, 0]).all() and not torch.isfinite(dk[:j + 1, 0]).all(-1).any()
+        for got, w in ((dq[:i], want[0][:i]), (dq[i + 1:], want[0][i + 1:]), (dk[j + 1:], want[1][j + 1:]), (dv[j + 1:], want[2][j + 1:]), (dk[:, 1:], want[1][:, 1:])):
+            assert torch.equal(got, w)
+
+
 def test_tables_that_lie_stay_inside_the_tensors():
     """Bounds past the tensor, negative or backwards are cut to it: no result is promised, but every call ends and later ones are right."""
     prob = Problem([50, 60], [50, 60], 2, 1, 64, True, "f16")
