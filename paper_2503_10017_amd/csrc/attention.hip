@@ -230,12 +230,12 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
         Tile::template stage<256, DIRECT>(to, k + key * a.k_row, a.k_row, there, a.d, threadIdx.x);
         Tile::template stage<256, DIRECT>(to + Tile::BYTES, v + key * a.v_row, a.v_row, there, a.d, threadIdx.x);
     };
-    const int least_of_all = seen_by(a, s, first);  // of the workgroup's rows: the same for all its waves
+    const int unseen = first_unseen<KEYS>(s, seen_by(a, s, first));  // by one of the workgroup's rows: the same for all its waves
     auto next_tile = [&](int t, int turn) {
         lds_loads_arrived();
         __syncthreads();
         if (t + 1 < t1) stage(stages[turn ^ 1], t + 1);
-        if (min((t + 1) * KEYS, s.lk) <= least_of_all) return;
+        if (t < unseen) return;
         if (Tile::template clear_not_finite<256>(stages[turn] + Tile::BYTES, threadIdx.x)) any_not_finite = 1;
         __syncthreads();
     };
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
         const int key = t * KEYS;
         w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least_seen, lane);
     }
-    if (t0 < t1 && any_not_finite) w.add_not_finite(v, a.v_row, a.d, max(t0, least_of_all / KEYS) * KEYS, min(t1 * KEYS, s.lk), seen, lane);
+    if (__builtin_expect(t0 < t1 && any_not_finite, 0)) w.add_not_finite(v, a.v_row, a.d, max(t0, unseen) * KEYS, min(t1 * KEYS, s.lk), seen, lane);
     finish_rows(a, s, group, mine, rows, t0 < t1, w, lane);
 }
 
@@ -291,6 +291,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     };
     int turn = 0;
     bool cleared = false;
+    const int unseen = first_unseen<KEYS>(s, least);
     if (t0 + wave < t1) stage(mine, t0 + wave);
     W w;
     w.begin(a, s, group, first, rows, lane);
@@ -300,16 +301,16 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
         lds_loads_arrived();
         if (t + 4 < t1) stage(next, t + 4);
         const int key = t * KEYS;
-        if (min(key + KEYS, s.lk) > least) {
+        if (__builtin_expect(t >= unseen, 0)) {  // (51 us for one token's caches; laid out as if it were usual, 53)
             cleared |= __ballot(Tile::template clear_not_finite<64>(now + Tile::BYTES, lane)) != 0;
             __builtin_amdgcn_wave_barrier();
         }
         w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least, lane);
     }
-    if (cleared)
+    if (__builtin_expect(cleared, 0))
 #pragma unroll 1
         for (int t = t0 + wave; t < t1; t += 4)
-            if (min((t + 1) * KEYS, s.lk) > least) w.add_not_finite(v, a.v_row, a.d, t * KEYS, min((t + 1) * KEYS, s.lk), seen, lane);
+            if (t >= unseen) w.add_not_finite(v, a.v_row, a.d, t * KEYS, min((t + 1) * KEYS, s.lk), seen, lane);
     // The waves' results, each in its own stages' place: top and sum per lane, then the registers.
     __syncthreads();
     float* held = reinterpret_cast<float*>(stages) + wave * (64 * (2 + 16 * DB));

@@ -106,17 +106,21 @@ struct HeadTile {
 #pragma unroll
         for (int i = 0; i < BYTES / 16 / THREADS; ++i) {
             uint4* at = reinterpret_cast<uint4*>(lds + (i * THREADS + thread) * 16);
-            E v[8];
-            __builtin_memcpy(v, at, 16);
-            bool found = false;
+            // an exponent of ones only: what is missing of it is 0, and 0x8000 less that has its top bit set
+            constexpr uint32_t EXPONENTS = DT == CT_F16 ? 0x7C007C00u : 0x7F807F80u;
+            uint32_t w[4], found = 0u;
+            __builtin_memcpy(w, at, 16);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool bad = !(__builtin_fabsf((float)v[e]) < __builtin_inff());
-                v[e] = bad ? (E)0.f : v[e];
-                found |= bad;
+            for (int e = 0; e < 4; ++e) found |= 0x80008000u - (~w[e] & EXPONENTS);
+            if (found & 0x80008000u) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t bad = (0x80008000u - (~w[e] & EXPONENTS)) & 0x80008000u;
+                    w[e] &= ~(bad | (bad - (bad >> 15)));
+                }
+                __builtin_memcpy(at, w, 16);
+                any = true;
             }
-            if (found) __builtin_memcpy(at, v, 16);
-            any |= found;
         }
         return any;
     }
@@ -198,6 +202,10 @@ __device__ __forceinline__ void load_row(const void* data, int64_t row_stride, i
         to[i] = load_run<DT>(from + at, r < rows ? a.d - at : 0);
     }
 }
+
+// The first tile of KEYS keys that holds one which a row that sees only `least` keys does not see.
+template <int KEYS>
+__device__ __forceinline__ int first_unseen(const Sequence& s, int least) { return least < s.lk ? least / KEYS : 0x7FFFFFFF; }
 
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
