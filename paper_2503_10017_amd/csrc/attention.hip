@@ -198,7 +198,7 @@ __device__ __forceinline__ void part_of(const AttentionArgs& a, int tiles, int& 
 
 // Many rows: a workgroup's four waves have QB x 32 rows each and share tiles of 64 keys.  Bound by the vector operations between the two products (per
 // score a multiply-add, a maximum, an exponential, an addition and half a rounding), which take longer than the products do: 32 sequences of 768 rows and keys, 16
-// heads of 64, bf16: 127 us, 610 TFLOP/s; packed causal rows up to 4001, 16 heads on 8, 128 elements, fp16: 568 us, 722 TFLOP/s.
+// heads of 64, bf16: 127 us, 610 TFLOP/s; packed causal rows up to 4001, 16 heads on 8, 128 elements, fp16: 578 us, 710 TFLOP/s (567 before tiles were cleared).
 template <int DT, int DB, int QB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     constexpr int KEYS = 64, WAVE_ROWS = 32 * QB, ROWS = 4 * WAVE_ROWS;
