@@ -13,103 +13,91 @@ namespace fnn {
 
 namespace {
 
-// One wave's rows: QB blocks of 32, a row per lane of either half.
-template <int DT, int DB, int QB, int KEYS>
+// One wave's 32 rows, a row per lane of either half.
+template <int DT, int DB, int KEYS>
 struct Rows {
     using Tile = HeadTile<DT, DB, KEYS>;
     typedef typename Elem<DT>::T E;
     static constexpr int KB = KEYS / 32;
-    uint4 q[QB][2 * DB];
-    f32x16 out[QB][DB];
-    float top[QB], sum[QB];  // of the keys so far: a score that none exceeds by 8 / c, and (this half's share of) the sum of exp2(c (score - top))
+    uint4 q[2 * DB];
+    f32x16 out[DB];
+    float top, sum;  // of the keys so far: a score that none exceeds by 8 / c, and (this half's share of) the sum of exp2(c (score - top))
 
     __device__ __forceinline__ void begin(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, int lane) {
+        load_row<DT, DB>(a.q, a.q_row, a.q_head, a, s, group, row + (lane & 31), rows, lane, q);
 #pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            load_row<DT, DB>(a.q, a.q_row, a.q_head, a, s, group, row + 32 * b + (lane & 31), rows, lane, q[b]);
-#pragma unroll
-            for (int i = 0; i < DB; ++i) out[b][i] = (f32x16)(0.f);
-            top[b] = -__builtin_inff();
-            sum[b] = 0.f;
-        }
+        for (int i = 0; i < DB; ++i) out[i] = (f32x16)(0.f);
+        top = -__builtin_inff();
+        sum = 0.f;
     }
 
     // KEYS more keys, the first of which is number `key`; `seen`: how many of the sequence's keys each row sees.  mask (the same in every
     // lane): some row may not see all of these.  Only the masking itself is branched over: two copies of all of it kept two copies of `out` in registers.
-    __device__ __forceinline__ void keys(const char* k, const char* v, float c, int key, const int (&seen)[QB], bool mask, int lane) {
-        f32x16 score[QB][KB];
+    __device__ __forceinline__ void keys(const char* k, const char* v, float c, int key, int seen, bool mask, int lane) {
+        f32x16 score[KB];
 #pragma unroll
-        for (int b = 0; b < QB; ++b)
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) score[b][kb] = (f32x16)(0.f);
+        for (int kb = 0; kb < KB; ++kb) score[kb] = (f32x16)(0.f);
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int i = 0; i < 2 * DB; ++i) {
                 const uint4 f = Tile::along(k, kb, i, lane);
-#pragma unroll
-                for (int b = 0; b < QB; ++b) score[b][kb] = mma32<DT>(f, q[b][i], score[b][kb]);
+                score[kb] = mma32<DT>(f, q[i], score[kb]);
             }
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int b = 0; b < QB; ++b) {
-            float most = -__builtin_inff();
-            if (mask) {
-                const int left = seen[b] - key - 4 * (lane >> 5);
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) score[b][kb][r] = 32 * kb + tile_row(r, 0) < left ? score[b][kb][r] : -__builtin_inff();
-            }
+        float most = -__builtin_inff();
+        if (mask) {
+            const int left = seen - key - 4 * (lane >> 5);
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, score[b][kb][r]);
-            most = across_halves_max(most);
-            // What is so far is rescaled only where some row's maximum rises by a factor of 2^8 and more: weights may as well reach 256.
-            if (__ballot(!(most * c <= __builtin_fmaf(top[b], c, 8.f)))) {
-                most = __builtin_fmaxf(most, top[b]);
-                const float base = most > -__builtin_inff() ? most * c : 0.f;
-                const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(top[b], c, -base));
-                top[b] = most;
-                sum[b] *= keep;
-#pragma unroll
-                for (int i = 0; i < DB; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) out[b][i][r] *= keep;
-            }
-            // rows that have seen no key yet stay at minus infinity; anything finite in its place makes their weights 0
-            const float base = top[b] > -__builtin_inff() ? top[b] * c : 0.f;
-            // summed up before they are rounded: lse has fp32's precision
-            float more = 0.f;
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    score[b][kb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[b][kb][r], c, -base));
-                    more += score[b][kb][r];
-                }
-            sum[b] += more;
+                for (int r = 0; r < 16; ++r) score[kb][r] = 32 * kb + tile_row(r, 0) < left ? score[kb][r] : -__builtin_inff();
         }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, score[kb][r]);
+        most = across_halves_max(most);
+        // What is so far is rescaled only where some row's maximum rises by a factor of 2^8 and more: weights may as well reach 256.
+        if (__ballot(!(most * c <= __builtin_fmaf(top, c, 8.f)))) {
+            most = __builtin_fmaxf(most, top);
+            const float base = most > -__builtin_inff() ? most * c : 0.f;
+            const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(top, c, -base));
+            top = most;
+            sum *= keep;
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) out[i][r] *= keep;
+        }
+        // rows that have seen no key yet stay at minus infinity; anything finite in its place makes their weights 0
+        const float base = top > -__builtin_inff() ? top * c : 0.f;
+        // summed up before they are rounded: lse has fp32's precision
+        float more = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                score[kb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[kb][r], c, -base));
+                more += score[kb][r];
+            }
+        sum += more;
         __builtin_amdgcn_sched_barrier(0);
         // the weights are at most 256 and rounded to the values' type, as the matrix instructions take them; their sum is of the unrounded ones
 #pragma unroll
         for (int t = 0; t < 2 * KB; ++t) {
-            uint4 p[QB];
-#pragma unroll
-            for (int b = 0; b < QB; ++b) p[b] = round_half<DT>(score[b][t >> 1], t & 1);
+            const uint4 p = round_half<DT>(score[t >> 1], t & 1);
 #pragma unroll
             for (int i = 0; i < DB; ++i) {
                 const uint4 f = Tile::across(v, i, t, lane);
-#pragma unroll
-                for (int b = 0; b < QB; ++b) out[b][i] = mma32<DT>(f, p[b], out[b][i]);
+                out[i] = mma32<DT>(f, p, out[i]);
             }
         }
     }
 
     // A causal tile that some rows see only a part of is multiplied with its values' infinities and NaN cleared, since a weight of 0 would not keep them
     // out; here the rows that see them get them.  No call without such values comes here.
-    __device__ __forceinline__ void add_not_finite(const E* v, int64_t stride, int d, int key, int end, const int (&seen)[QB], int lane) {
+    __device__ __forceinline__ void add_not_finite(const E* v, int64_t stride, int d, int key, int end, int seen, int lane) {
 #pragma unroll 1
         for (int j = key; j < end; ++j) {
             const E* of_key = v + j * stride;
@@ -121,8 +109,7 @@ struct Rows {
                     const int e = 32 * i + tile_row(r, lane >> 5);
                     const float x = e < d ? (float)of_key[e] : 0.f;
                     const bool bad = !(__builtin_fabsf(x) < __builtin_inff());
-#pragma unroll
-                    for (int b = 0; b < QB; ++b) out[b][i][r] += bad && j < seen[b] ? x : 0.f;
+                    out[i][r] += bad && j < seen ? x : 0.f;
                     if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -148,43 +135,40 @@ __device__ __forceinline__ float* share_row(const AttentionArgs& a, int split, i
     return a.partial + (int64_t)a.splits * a.tq * a.heads * 2 + ((int64_t)split * a.tq * a.heads + row) * a.d_pad;
 }
 
-template <int DT, int DB, int QB, int KEYS>
-__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, bool any, const Rows<DT, DB, QB, KEYS>& w, int lane) {
+template <int DT, int DB, int KEYS>
+__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, bool any, const Rows<DT, DB, KEYS>& w, int lane) {
     const int c = lane & 31, h = lane >> 5;
+    const int r = row + c;
+    const float total = across_halves_sum(w.sum);
+    float scale = 1.f;
+    if (a.splits == 1) scale = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // a row that sees no key is 0
 #pragma unroll
-    for (int b = 0; b < QB; ++b) {
-        const int r = row + 32 * b + c;
-        const float total = across_halves_sum(w.sum[b]);
-        float scale = 1.f;
-        if (a.splits == 1) scale = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // a row that sees no key is 0
+    for (int i = 0; i < DB; ++i) {
+        float v[2][8];
+        rows_of_eight(w.out[i], v);
+        if (r >= rows) continue;
 #pragma unroll
-        for (int i = 0; i < DB; ++i) {
-            float v[2][8];
-            rows_of_eight(w.out[b][i], v);
-            if (r >= rows) continue;
+        for (int p = 0; p < 2; ++p) {
+            const int at = 32 * i + 16 * p + 8 * h;
+            if (at >= a.d) continue;
+            if (a.splits == 1) {
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const int at = 32 * i + 16 * p + 8 * h;
-                if (at >= a.d) continue;
-                if (a.splits == 1) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[p][e] *= scale;
-                    put_run<DT>(a, s, group, r, at, v[p]);
-                } else if (any) {  // the share of no keys is told by its statistics alone
-                    float* to = share_row(a, blockIdx.y, flat_row(a, s, group, r)) + at;
-                    reinterpret_cast<f32x4*>(to)[0] = f32x4{v[p][0], v[p][1], v[p][2], v[p][3]};
-                    reinterpret_cast<f32x4*>(to)[1] = f32x4{v[p][4], v[p][5], v[p][6], v[p][7]};
-                }
+                for (int e = 0; e < 8; ++e) v[p][e] *= scale;
+                put_run<DT>(a, s, group, r, at, v[p]);
+            } else if (any) {  // the share of no keys is told by its statistics alone
+                float* to = share_row(a, blockIdx.y, flat_row(a, s, group, r)) + at;
+                reinterpret_cast<f32x4*>(to)[0] = f32x4{v[p][0], v[p][1], v[p][2], v[p][3]};
+                reinterpret_cast<f32x4*>(to)[1] = f32x4{v[p][4], v[p][5], v[p][6], v[p][7]};
             }
         }
-        if (r >= rows || h) continue;
-        if (a.splits > 1) {
-            float* to = share_stats(a, blockIdx.y, flat_row(a, s, group, r));
-            to[0] = w.top[b];
-            to[1] = total;
-        } else if (a.lse) {
-            a.lse[flat_row(a, s, group, r)] = w.top[b] * a.scale + logf(total);  // no key: minus infinity
-        }
+    }
+    if (r >= rows || h) return;
+    if (a.splits > 1) {
+        float* to = share_stats(a, blockIdx.y, flat_row(a, s, group, r));
+        to[0] = w.top;
+        to[1] = total;
+    } else if (a.lse) {
+        a.lse[flat_row(a, s, group, r)] = w.top * a.scale + logf(total);  // no key: minus infinity
     }
 }
 
@@ -196,13 +180,13 @@ __device__ __forceinline__ void part_of(const AttentionArgs& a, int tiles, int& 
     t1 = part < parts ? (int)((int64_t)tiles * (part + 1) / parts) : 0;
 }
 
-// Many rows: a workgroup's four waves have QB x 32 rows each and share tiles of 64 keys.  Bound by the vector operations between the two products (per
+// Many rows: a workgroup's four waves have 32 rows each and share tiles of 64 keys.  Bound by the vector operations between the two products (per
 // score a multiply-add, a maximum, an exponential, an addition and half a rounding), which take longer than the products do: 32 sequences of 768 rows and keys, 16
 // heads of 64, bf16: 127 us, 610 TFLOP/s; packed causal rows up to 4001, 16 heads on 8, 128 elements, fp16: 578 us, 710 TFLOP/s (567 before tiles were cleared).
-template <int DT, int DB, int QB, bool DIRECT>
+template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
-    constexpr int KEYS = 64, WAVE_ROWS = 32 * QB, ROWS = 4 * WAVE_ROWS;
-    using W = Rows<DT, DB, QB, KEYS>;
+    constexpr int KEYS = 64, ROWS = 128;
+    using W = Rows<DT, DB, KEYS>;
     using Tile = typename W::Tile;
     typedef typename Elem<DT>::T E;
     __shared__ __attribute__((aligned(16))) char stages[2][2 * Tile::BYTES];
@@ -213,15 +197,13 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     if (s.index < 0) return;
     if (threadIdx.x == 0) any_not_finite = 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rows = s.lq * a.share, first = s.tile * ROWS, mine = first + wave * WAVE_ROWS;
+    const int rows = s.lq * a.share, first = s.tile * ROWS, mine = first + wave * 32;
     const int most = seen_by(a, s, min(first + ROWS, rows) - 1);
     int t0, t1;
     part_of(a, (most + KEYS - 1) / KEYS, t0, t1);
 
     const int least_seen = seen_by(a, s, min(mine, rows - 1));
-    int seen[QB];
-#pragma unroll
-    for (int b = 0; b < QB; ++b) seen[b] = seen_by(a, s, min(mine + 32 * b + (lane & 31), rows - 1));
+    const int seen = seen_by(a, s, min(mine + (lane & 31), rows - 1));
     const float c = a.scale * LOG2E;
     const E* k = (const E*)a.k + s.k0 * a.k_row + group * a.k_head;
     const E* v = (const E*)a.v + s.k0 * a.v_row + group * a.v_head;
@@ -264,7 +246,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     constexpr int KEYS = 32, ROWS = 32;
-    using W = Rows<DT, DB, 1, KEYS>;
+    using W = Rows<DT, DB, KEYS>;
     using Tile = typename W::Tile;
     typedef typename Elem<DT>::T E;
     constexpr int PER_WAVE = 4 * Tile::BYTES;  // two stages of keys and values
@@ -279,7 +261,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     int t0, t1;
     part_of(a, (most + KEYS - 1) / KEYS, t0, t1);
 
-    int seen[1] = {seen_by(a, s, min(first + (lane & 31), rows - 1))};
+    const int seen = seen_by(a, s, min(first + (lane & 31), rows - 1));
     const float c = a.scale * LOG2E;
     const E* k = (const E*)a.k + s.k0 * a.k_row + group * a.k_head;
     const E* v = (const E*)a.v + s.k0 * a.v_row + group * a.v_head;
@@ -314,17 +296,17 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     // The waves' results, each in its own stages' place: top and sum per lane, then the registers.
     __syncthreads();
     float* held = reinterpret_cast<float*>(stages) + wave * (64 * (2 + 16 * DB));
-    held[lane] = w.top[0];
-    held[64 + lane] = w.sum[0];
+    held[lane] = w.top;
+    held[64 + lane] = w.sum;
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) held[(2 + 16 * i + r) * 64 + lane] = w.out[0][i][r];
+        for (int r = 0; r < 16; ++r) held[(2 + 16 * i + r) * 64 + lane] = w.out[i][r];
     __syncthreads();
     if (wave) return;
     const float* all = reinterpret_cast<const float*>(stages);
     constexpr int EACH = 64 * (2 + 16 * DB);
-    float top = w.top[0];
+    float top = w.top;
 #pragma unroll
     for (int i = 1; i < 4; ++i) top = __builtin_fmaxf(top, all[i * EACH + lane]);
     const float base = top > -__builtin_inff() ? top * c : 0.f;
@@ -342,10 +324,10 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) out[i][r] = __builtin_fmaf(from[(2 + 16 * i + r) * 64 + lane], keep, out[i][r]);
     }
-    w.top[0] = top;
-    w.sum[0] = sum;
+    w.top = top;
+    w.sum = sum;
 #pragma unroll
-    for (int i = 0; i < DB; ++i) w.out[0][i] = out[i];
+    for (int i = 0; i < DB; ++i) w.out[i] = out[i];
     finish_rows(a, s, group, first, rows, t0 < t1, w, lane);
 }
 
@@ -423,7 +405,7 @@ template <int DT, int DB, bool DIRECT>
 hipError_t run(const AttentionArgs& a, const Plan& p, hipStream_t s) {
     const dim3 grid((unsigned)(p.row_tiles * a.groups), (unsigned)p.splits);
     const hipError_t e = p.few ? launch(TK_ATTENTION, attention_few_kernel<DT, DB, DIRECT>, grid, dim3(256), 0, s, a)
-                               : launch(TK_ATTENTION, attention_kernel<DT, DB, 1, DIRECT>, grid, dim3(256), 0, s, a);
+                               : launch(TK_ATTENTION, attention_kernel<DT, DB, DIRECT>, grid, dim3(256), 0, s, a);
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t rows = (int64_t)a.tq * a.heads;
     return rows < 2048 ? launch(TK_ATTENTION, attention_join_kernel<DT, 8>, dim3((unsigned)rows), dim3(256), 0, s, a)
