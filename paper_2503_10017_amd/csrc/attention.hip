@@ -352,8 +352,9 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
 #pragma unroll 4
     for (int s = mine; s < a.splits; s += GROUPS) {
         const float* stats = share_stats(a, s, row);
+        if (stats[1] == 0.f) continue;  // no keys: nothing was written
+        // a factor of 0 is no reason to pass a share over: it may hold NaN alone, which no maximum tells of, or infinite values
         const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(stats[0], c, -base));
-        if (keep == 0.f) continue;  // no keys: nothing was written
         sum = __builtin_fmaf(stats[1], keep, sum);
         if (4 * place < a.d) {
             const f32x4 y = *reinterpret_cast<const f32x4*>(share_row(a, s, row) + 4 * place);
