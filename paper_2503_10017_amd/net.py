@@ -1,7 +1,8 @@
 """ctypes binding of the network's operators in libfnn.so (include/fnn_net.h): argument marshalling only.
 
 Every function has the name and meaning of the C entry point it wraps; torch supplies device memory and the current stream.
-Tensors are taken with the strides that they have, as long as the elements of a row are contiguous.
+Tensors are taken with the strides that they have, as long as the elements of a row are contiguous.  With ``stream`` a call runs on that stream: outputs and
+workspaces that it is not given are of that stream's memory, and the inputs have to be ready there.
 """
 from __future__ import annotations
 
@@ -44,15 +45,26 @@ def _stream_ptr(stream, device):
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory for an output.  The caching allocator hands a block out again in the order of the stream that it was asked for on: what a call on `stream` writes has to
+    be asked for there, since the current stream may still work in a block that it has given up.  The caller reads the output on the current stream, which
+    the allocator is told of."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _scratch(need: int, device, stream):
-    """A workspace of the call's own (None: none is needed).  One that is used on a stream other than torch's current one must not be handed
-    out again before that stream has passed the call."""
+    """A workspace of the call's own (None: none is needed), of `stream`'s memory as in _empty."""
     if not need:
         return None
-    workspace = _workspace(need, device)
-    if stream is not None:
-        workspace.record_stream(stream)
-    return workspace
+    if stream is None:
+        return _workspace(need, device)
+    with torch.cuda.stream(stream):
+        return _workspace(need, device)
 
 
 def _check(status: int, where: str):
@@ -74,11 +86,11 @@ def fnn_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias:
     n, d = x.shape
     wt = _weight_dtype(x, weight, bias)
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(x.shape, x.dtype, x.device, stream)
     mean = rstd = None
     if want_stats:
-        mean = torch.empty(n, dtype=torch.float32, device=x.device)
-        rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+        mean = _empty(n, torch.float32, x.device, stream)
+        rstd = _empty(n, torch.float32, x.device, stream)
     _check(lib.fnn_layer_norm(xm, _vector(weight, d, wt, "weight"), _vector(bias, d, wt, "bias"), _DTYPES.get(wt, -1), eps,
                               _matrix(out, "out"), _ptr(mean), _ptr(rstd), _stream_ptr(stream, x.device)), "fnn_layer_norm")
     return out, mean, rstd
@@ -98,11 +110,11 @@ def fnn_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     wt = x.dtype if weight is None else weight.dtype
     dx = out
     if dx is None and want_x:
-        dx = torch.empty_like(x)
+        dx = _empty(x.shape, x.dtype, x.device, stream)
     dweight = dbias = None
     if want_weight:
-        dweight = torch.empty(d, dtype=wt, device=x.device)
-        dbias = torch.empty(d, dtype=wt, device=x.device)
+        dweight = _empty(d, wt, x.device, stream)
+        dbias = _empty(d, wt, x.device, stream)
         if workspace is None:
             workspace = _scratch(lib.fnn_layer_norm_backward_workspace_bytes(n, d), x.device, stream)
     _check(lib.fnn_layer_norm_backward(_matrix(dy, "dy"), _matrix(x, "x"), _vector(mean, n, torch.float32, "mean"),
@@ -132,8 +144,8 @@ def fnn_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = 
     rows, inner = x.shape
     outer = w.shape[0]
     if out is None:
-        out = torch.empty((rows, outer), dtype=x.dtype, device=x.device)
-    pre = torch.empty((rows, outer), dtype=x.dtype, device=x.device) if want_pre else None
+        out = _empty((rows, outer), x.dtype, x.device, stream)
+    pre = _empty((rows, outer), x.dtype, x.device, stream) if want_pre else None
     if workspace is None:
         workspace = _scratch(lib.fnn_linear_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype]), x.device, stream)
     _check(lib.fnn_linear(xm, wm, _vector(bias, outer, x.dtype, "bias"), _ACTS[act], _matrix(residual, "residual"),
@@ -156,9 +168,9 @@ def fnn_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, pre:
     outer = w.shape[0]
     dx = out
     if dx is None and want_x:
-        dx = torch.empty((rows, inner), dtype=x.dtype, device=x.device)
-    dw = torch.empty((outer, inner), dtype=x.dtype, device=x.device) if want_w else None
-    dbias = torch.empty(outer, dtype=x.dtype, device=x.device) if want_bias else None
+        dx = _empty((rows, inner), x.dtype, x.device, stream)
+    dw = _empty((outer, inner), x.dtype, x.device, stream) if want_w else None
+    dbias = _empty(outer, x.dtype, x.device, stream) if want_bias else None
     if workspace is None:
         workspace = _scratch(lib.fnn_linear_backward_workspace_bytes(rows, inner, outer, _DTYPES[x.dtype], _ACTS[act]), x.device, stream)
     _check(lib.fnn_linear_backward(_matrix(dy, "dy"), _matrix(x, "x"), _matrix(w, "w"), _matrix(pre, "pre"), _ACTS[act],
@@ -207,8 +219,8 @@ def fnn_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: Optio
     tokens, heads, d = q.shape
     batch, cq, ck = _sequences(cu_q, cu_k)
     if out is None:
-        out = torch.empty((tokens, heads, d), dtype=q.dtype, device=q.device)
-    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if want_lse else None
+        out = _empty((tokens, heads, d), q.dtype, q.device, stream)
+    lse = _empty((tokens, heads), torch.float32, q.device, stream) if want_lse else None
     if workspace is None:
         workspace = _scratch(lib.fnn_attention_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d), q.device, stream)
     _check(lib.fnn_attention(qm, km, vm, batch, cq, ck, causal, d ** -0.5 if scale is None else scale, _heads(out, "out"),
@@ -233,9 +245,9 @@ def fnn_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
     if out_grads is not None:
         dq, dk, dv = out_grads
     else:
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if want_q else None
-        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if want_kv else None
-        dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if want_kv else None
+        dq = _empty(q.shape, q.dtype, q.device, stream) if want_q else None
+        dk = _empty(k.shape, k.dtype, k.device, stream) if want_kv else None
+        dv = _empty(v.shape, v.dtype, v.device, stream) if want_kv else None
     if workspace is None:
         workspace = _scratch(lib.fnn_attention_backward_workspace_bytes(tokens, k.shape[0], batch, heads, k.shape[1], d), q.device, stream)
     grads = [None if g is None else _heads(g, "a gradient") for g in (dq, dk, dv)]
