@@ -2,7 +2,8 @@
 
 Every function here has the name and meaning of the C entry point it wraps (see
 include/fnn.h, include/fnn_measure.h).  torch supplies device memory and the current stream; all arithmetic of
-the matching path runs inside the library's kernels.
+the matching path runs inside the library's kernels.  With ``stream`` a call runs on that stream: outputs and workspaces that it
+is not given are of that stream's memory, and the inputs have to be ready there.
 """
 from __future__ import annotations
 
@@ -207,8 +208,24 @@ def fnn_workspace_bytes_opts(batch: int, n: int, m: int, d: int, n_queries: int,
     return int(load_library().fnn_workspace_bytes_opts(batch, n, m, d, n_queries, ctypes.byref(o)))
 
 
-def _workspace(need, device):
-    return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+def _empty(shape, dtype, device, stream):
+    """Memory for an output.  The caching allocator hands a block out again in the order of the stream that it was asked for on: what a call on `stream` writes has to
+    be asked for there, since the current stream may still work in a block that it has given up.  The caller reads the output on the current stream, which
+    the allocator is told of."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _workspace(need, device, stream):
+    """A workspace of the call's own, of `stream`'s memory as in _empty."""
+    if stream is None:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
 
 
 def fnn_nearest(src: MapsLike, tgt: MapsLike, q_idx: Optional[torch.Tensor] = None,
@@ -226,12 +243,12 @@ def fnn_nearest(src: MapsLike, tgt: MapsLike, q_idx: Optional[torch.Tensor] = No
     if nq is None:
         nq = q_idx.shape[-1] if q_idx is not None else n
     if out_idx is None:
-        out_idx = torch.empty((batch, nq), dtype=torch.int32, device=device)
+        out_idx = _empty((batch, nq), torch.int32, device, stream)
     if out_score is None and want_score:
-        out_score = torch.empty((batch, nq), dtype=torch.float32, device=device)
+        out_score = _empty((batch, nq), torch.float32, device, stream)
     o = _opts(compute, normalize=normalize, l2=l2, split=split)
     if workspace is None:
-        workspace = _workspace(fnn_workspace_bytes_opts(batch, n, m, d, nq, compute, l2=l2, split=split), device)
+        workspace = _workspace(fnn_workspace_bytes_opts(batch, n, m, d, nq, compute, l2=l2, split=split), device, stream)
     sa, ta = _map_array(sv), _map_array(tv)
     st = lib.fnn_nearest(batch, sa, _ptr(q_idx), nq, _ptr(nq_active),
                          ta, ctypes.byref(o), _ptr(out_idx), _ptr(out_score),
@@ -253,15 +270,15 @@ def fnn_reciprocal(d1: MapsLike, d2: MapsLike, seeds: torch.Tensor, max_iter: in
     n_seeds = seeds.shape[-1]
     if out is None:
         out = {
-            "seed_i": torch.empty((batch, n_seeds), dtype=torch.int32, device=device),
-            "seed_j": torch.empty((batch, n_seeds), dtype=torch.int32, device=device),
-            "seed_iter": torch.empty((batch, n_seeds), dtype=torch.int32, device=device),
-            "pairs": torch.empty((batch, n_seeds, 2), dtype=torch.int32, device=device),
-            "n_pairs": torch.empty((batch,), dtype=torch.int32, device=device),
+            "seed_i": _empty((batch, n_seeds), torch.int32, device, stream),
+            "seed_j": _empty((batch, n_seeds), torch.int32, device, stream),
+            "seed_iter": _empty((batch, n_seeds), torch.int32, device, stream),
+            "pairs": _empty((batch, n_seeds, 2), torch.int32, device, stream),
+            "n_pairs": _empty((batch,), torch.int32, device, stream),
         }
     o = _opts(compute, max_iter, normalize, l2=l2, split=split)
     if workspace is None:
-        workspace = _workspace(fnn_workspace_bytes_opts(batch, n, m, d, n_seeds, compute, l2=l2, split=split), device)
+        workspace = _workspace(fnn_workspace_bytes_opts(batch, n, m, d, n_seeds, compute, l2=l2, split=split), device, stream)
     a1, a2 = _map_array(v1), _map_array(v2)
     st = lib.fnn_reciprocal(batch, a1, a2, _ptr(seeds), n_seeds, ctypes.byref(o),
                             _ptr(out["seed_i"]), _ptr(out["seed_j"]), _ptr(out["seed_iter"]),
@@ -303,16 +320,16 @@ def fnn_mutual_dense(d1: MapsLike, d2: MapsLike, compute="f16", out: Optional[di
     m = _dims(v2)[1]
     if out is None:
         out = {
-            "nn12": torch.empty((batch, n), dtype=torch.int32, device=device),
-            "s12": torch.empty((batch, n), dtype=torch.float32, device=device),
-            "nn21": torch.empty((batch, m), dtype=torch.int32, device=device),
-            "s21": torch.empty((batch, m), dtype=torch.float32, device=device),
-            "pairs": torch.empty((batch, min(n, m), 2), dtype=torch.int32, device=device),
-            "n_pairs": torch.empty((batch,), dtype=torch.int32, device=device),
+            "nn12": _empty((batch, n), torch.int32, device, stream),
+            "s12": _empty((batch, n), torch.float32, device, stream),
+            "nn21": _empty((batch, m), torch.int32, device, stream),
+            "s21": _empty((batch, m), torch.float32, device, stream),
+            "pairs": _empty((batch, min(n, m), 2), torch.int32, device, stream),
+            "n_pairs": _empty((batch,), torch.int32, device, stream),
         }
     o = _opts(compute, normalize=normalize, l2=l2, split=split)
     if workspace is None:
-        workspace = _workspace(fnn_workspace_bytes_opts(batch, n, m, d, 0, compute, l2=l2, split=split), device)
+        workspace = _workspace(fnn_workspace_bytes_opts(batch, n, m, d, 0, compute, l2=l2, split=split), device, stream)
     a1, a2 = _map_array(v1), _map_array(v2)
     st = lib.fnn_mutual_dense(batch, a1, a2, ctypes.byref(o), _ptr(out["nn12"]), _ptr(out.get("s12")), _ptr(out["nn21"]),
                               _ptr(out.get("s21")), _ptr(out["pairs"]), _ptr(out["n_pairs"]),
@@ -330,12 +347,12 @@ def fnn_nearest_blocked(src: torch.Tensor, tgt: torch.Tensor, block_rows: int, b
     lib = load_library()
     device = src.device
     nq = q_idx.shape[-1] if q_idx is not None else src.shape[0]
-    out_idx = torch.empty((nq,), dtype=torch.int32, device=device)
-    out_score = torch.empty((nq,), dtype=torch.float32, device=device)
+    out_idx = _empty((nq,), torch.int32, device, stream)
+    out_score = _empty((nq,), torch.float32, device, stream)
     need = int(lib.fnn_blocked_workspace_bytes(src.shape[0], tgt.shape[0], src.shape[1], block_rows, block_cols,
                                                _COMPUTE[compute]))
     if workspace is None:
-        workspace = _workspace(need, device)
+        workspace = _workspace(need, device, stream)
     o = _opts(compute, normalize=normalize, half_accumulate=half_accumulate)
     sa, ta = _map_array([src]), _map_array([tgt])
     st = lib.fnn_nearest_blocked(sa, _ptr(q_idx), nq, ta, ctypes.byref(o), block_rows, block_cols, _ptr(out_idx), _ptr(out_score),
@@ -353,8 +370,8 @@ def fnn_pairs_to_pixels(pairs: torch.Tensor, n_pairs: torch.Tensor, n: int, widt
     lib = load_library()
     batch, max_pairs = pairs.shape[0], pairs.shape[1]
     device = pairs.device
-    out_xy = torch.empty((batch, max_pairs, 4), dtype=torch.int32, device=device)
-    out_count = torch.empty((batch,), dtype=torch.int32, device=device)
+    out_xy = _empty((batch, max_pairs, 4), torch.int32, device, stream)
+    out_count = _empty((batch,), torch.int32, device, stream)
     st = lib.fnn_pairs_to_pixels(batch, _ptr(pairs), _ptr(n_pairs), max_pairs, n, width1, m, width2, _ptr(conf1),
                                  _ptr(conf2), float(min_conf1), float(min_conf2), _ptr(out_xy), _ptr(out_count),
                                  _stream_ptr(stream, device))
@@ -390,7 +407,7 @@ def fnn_measure_ceiling(mix: int, blocks_per_wave: int = 65536, scratch: Optiona
     """Nanoseconds per 32x32 score block and SIMD for the bare instruction mix ``mix`` (see fnn_measure.h); waits for the result."""
     lib = load_library()
     if scratch is None:
-        scratch = torch.empty(4 << 20, dtype=torch.uint8, device="cuda")
+        scratch = _workspace(4 << 20, "cuda", stream)
     ns = ctypes.c_float(0.0)
     st = lib.fnn_measure_ceiling(mix, blocks_per_wave, _ptr(scratch), scratch.numel() * scratch.element_size(),
                                  ctypes.byref(ns), _stream_ptr(stream, scratch.device))

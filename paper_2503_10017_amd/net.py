@@ -11,7 +11,7 @@ from typing import Optional
 
 import torch
 
-from .binding import _DTYPES, FnnError, _pack_map, _ptr, _workspace, load_library
+from .binding import _DTYPES, FnnError, _empty, _pack_map, _ptr, _workspace, load_library
 
 
 def _matrix(t: Optional[torch.Tensor], what: str):
@@ -45,26 +45,9 @@ def _stream_ptr(stream, device):
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
 
 
-def _empty(shape, dtype, device, stream):
-    """Memory for an output.  The caching allocator hands a block out again in the order of the stream that it was asked for on: what a call on `stream` writes has to
-    be asked for there, since the current stream may still work in a block that it has given up.  The caller reads the output on the current stream, which
-    the allocator is told of."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        t = torch.empty(shape, dtype=dtype, device=device)
-    t.record_stream(torch.cuda.current_stream(device))
-    return t
-
-
 def _scratch(need: int, device, stream):
-    """A workspace of the call's own (None: none is needed), of `stream`'s memory as in _empty."""
-    if not need:
-        return None
-    if stream is None:
-        return _workspace(need, device)
-    with torch.cuda.stream(stream):
-        return _workspace(need, device)
+    """A workspace of the call's own (None: none is needed)."""
+    return _workspace(need, device, stream) if need else None
 
 
 def _check(status: int, where: str):
