@@ -127,12 +127,13 @@ __device__ __forceinline__ void put_run(const AttentionArgs& a, const Sequence& 
 
 constexpr int MOST_SPLITS = 64, MOST_KEYS = 1 << 30;
 
-// Shares of a split call: [split][rows] of {the largest score, the sum}, then [split][rows][d rounded up to 8].
+// Shares of a split call: [split][rows] of {the largest score, the sum}, then, from the next 16 bytes on, [split][rows][d rounded up to 8].
+__host__ __device__ __forceinline__ int64_t stats_floats(int64_t shares) { return (shares * 2 + 3) & ~(int64_t)3; }
 __device__ __forceinline__ float* share_stats(const AttentionArgs& a, int split, int64_t row) {
     return a.partial + ((int64_t)split * a.tq * a.heads + row) * 2;
 }
 __device__ __forceinline__ float* share_row(const AttentionArgs& a, int split, int64_t row) {
-    return a.partial + (int64_t)a.splits * a.tq * a.heads * 2 + ((int64_t)split * a.tq * a.heads + row) * a.d_pad;
+    return a.partial + stats_floats((int64_t)a.splits * a.tq * a.heads) + ((int64_t)split * a.tq * a.heads + row) * a.d_pad;
 }
 
 template <int DT, int DB, int KEYS>
@@ -418,7 +419,8 @@ hipError_t run(const AttentionArgs& a, const Plan& p, hipStream_t s) {
 size_t attention_workspace(int64_t tq, int64_t tk, int64_t batch, int64_t heads, int64_t groups, int64_t d) {
     if (tq < 1) return 0;
     const Plan p = plan_of(tq, tk, batch, heads, groups);
-    return p.splits > 1 ? (size_t)p.splits * tq * heads * (2 + (d + 7) / 8 * 8) * sizeof(float) : 0;
+    const int64_t shares = p.splits * tq * heads;
+    return p.splits > 1 ? (size_t)(stats_floats(shares) + shares * ((d + 7) / 8 * 8)) * sizeof(float) : 0;
 }
 
 hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t s) {
