@@ -81,8 +81,8 @@ __device__ __forceinline__ float wave_sum(float x) {
 }
 
 // ---- activations and their slopes ----
-// 16-bit outputs take exp and the reciprocal from the hardware (2 units in the last place of fp32) and erfc from Abramowitz and Stegun, formula
-// 7.1.26 (its error, 1.5e-7, is far below half a step of the output); fp32 outputs take the library's functions.
+// 16-bit outputs take exp and the reciprocal from the hardware (2 units in the last place of fp32) and the normal tail from a fit of its own whose relative
+// error is 1e-6 everywhere, since far to the left the tail is what GELU consists of; fp32 outputs take the library's functions.
 
 enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
@@ -96,16 +96,20 @@ __device__ __forceinline__ float over(float a, float b) {
     if constexpr (FAST) return a * __builtin_amdgcn_rcpf(b);
     else return a / b;
 }
-// Phi(-|x|), the integral of the normal density beyond |x|; exp(-x^2 / 2) comes along.
+// Phi(-|x|), the integral of the normal density beyond |x|; exp(-x^2 / 2) comes along.  FAST: Phi(-x) exp(x^2 / 2) falls like 1 / x, and is a polynomial of
+// t = 1 / (1 + 0.265 x) without a constant term.  Degree 7, its coefficients and the 0.265 are the least relative error over 0 <= x <= 14.4, where the
+// exponential ends (linear programming over 1200 points): 6e-7, 9.6e-7 as computed; a step of fp16 is 1000 times that.
 template <bool FAST>
 __device__ __forceinline__ float normal_tail(float x, float& gauss) {
     if constexpr (FAST) {
         gauss = __builtin_amdgcn_exp2f(x * (x * -0.72134752f));
-        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(x), 0.3275911f * 0.70710678f, 1.f));
-        float p = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-        p = __builtin_fmaf(t, p, 0.5f * 1.421413741f);
-        p = __builtin_fmaf(t, p, 0.5f * -0.284496736f);
-        p = __builtin_fmaf(t, p, 0.5f * 0.254829592f);
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(x), 0.265f, 1.f));
+        float p = __builtin_fmaf(t, -0.06778702f, 0.19527303f);
+        p = __builtin_fmaf(t, p, -0.06636281f);
+        p = __builtin_fmaf(t, p, 0.14249325f);
+        p = __builtin_fmaf(t, p, 0.08294662f);
+        p = __builtin_fmaf(t, p, 0.10783678f);
+        p = __builtin_fmaf(t, p, 0.10559984f);
         return p * t * gauss;
     } else {
         gauss = expf(-0.5f * x * x);
