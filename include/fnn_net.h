@@ -107,11 +107,12 @@ typedef struct {
  * everything).  Query i of lq sees key j of lk if !causal or j <= i + lk - lq: the last query sees every key, so queries at the end of
  * a cache, one token among them, need nothing else.
  *   out = sum_j softmax_j(scale <q, k_j>) v_j,   lse = log sum_j exp(scale <q, k_j>)   over the keys j that the query sees
- * A query that sees none has out = 0 and lse = minus infinity.  q and out have `heads` heads, k and v a divisor of that: query head h
- * reads key head h / (heads / key heads).  d <= FNN_MAX_HEAD_DIM; scale > 0.  lse (device float [q->n][heads]) may be NULL; the
- * gradient takes it.  Strides are free (heads of a token may also lie apart by more than a token); vectors on 16-byte boundaries are
- * faster.  What lies outside the sequences is neither read for its value nor written.  Neither do infinities and NaN of keys
- * and values reach a query of a causal call that does not see them; in the gradient they spoil what sees them.
+ * A query that sees none has out = 0 and lse = minus infinity; one that sees some, each with a score of minus infinity, has no softmax: its out
+ * is NaN.  q and out have `heads` heads, k and v a divisor of that: query head h reads key head h / (heads / key heads).
+ * d <= FNN_MAX_HEAD_DIM; scale > 0.  lse (device float [q->n][heads]) may be NULL; the gradient takes it.  Strides are free (heads of
+ * a token may also lie apart by more than a token); vectors on 16-byte boundaries are faster.  What lies outside the sequences is neither
+ * read for its value nor written.  Neither do infinities and NaN of keys and values reach a query of a causal call that does not see them;
+ * in the gradient they spoil what sees them.
  * Scores, softmax and sums are fp32; the weights are rounded to the values' type for the second product.
  * The workspace is for few queries with many keys, which are split and joined in a fixed order.
  * Errors: FNN_E_NULL, FNN_E_SHAPE, FNN_E_DTYPE, FNN_E_RANGE (scale, batch < 1), FNN_E_WORKSPACE.

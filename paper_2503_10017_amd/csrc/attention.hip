@@ -136,13 +136,19 @@ __device__ __forceinline__ float* share_row(const AttentionArgs& a, int split, i
     return a.partial + stats_floats((int64_t)a.splits * a.tq * a.heads) + ((int64_t)split * a.tq * a.heads + row) * a.d_pad;
 }
 
+// The sum of a share whose row sees keys, each with a score of minus infinity: they weigh nothing beside others, but are no softmax by themselves.  The share of
+// no keys has a sum of 0.
+constexpr float NO_WEIGHT = -1.f;
+
+// `part`: the first of the keys that `w` is of; `any`: whether there are some.
 template <int DT, int DB, int KEYS>
-__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, bool any, const Rows<DT, DB, KEYS>& w, int lane) {
+__device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, int part, bool any, const Rows<DT, DB, KEYS>& w, int lane) {
     const int c = lane & 31, h = lane >> 5;
     const int r = row + c;
     const float total = across_halves_sum(w.sum);
+    const bool sees = any && seen_by(a, s, min(r, rows - 1)) > part;
     float scale = 1.f;
-    if (a.splits == 1) scale = total > 0.f ? 1.f / total : total != total ? total : 0.f;  // a row that sees no key is 0
+    if (a.splits == 1) scale = total > 0.f ? 1.f / total : sees ? __builtin_nanf("") : 0.f;  // a row that sees no key is 0
 #pragma unroll
     for (int i = 0; i < DB; ++i) {
         float v[2][8];
@@ -167,7 +173,7 @@ __device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequen
     if (a.splits > 1) {
         float* to = share_stats(a, blockIdx.y, flat_row(a, s, group, r));
         to[0] = w.top;
-        to[1] = total;
+        to[1] = sees && total == 0.f ? NO_WEIGHT : total;
     } else if (a.lse) {
         a.lse[flat_row(a, s, group, r)] = w.top * a.scale + logf(total);  // no key: minus infinity
     }
@@ -237,7 +243,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
         w.keys(now, now + Tile::BYTES, c, key, seen, key + KEYS > least_seen, lane);
     }
     if (__builtin_expect(t0 < t1 && any_not_finite, 0)) w.add_not_finite(v, a.v_row, a.d, max(t0, unseen) * KEYS, min(t1 * KEYS, s.lk), seen, lane);
-    finish_rows(a, s, group, mine, rows, t0 < t1, w, lane);
+    finish_rows(a, s, group, mine, rows, t0 * KEYS, t0 < t1, w, lane);
 }
 
 // Few rows (a token or some at the end of a cache): the time is that of reading the keys once.  Every wave has the same 32 rows and tiles of
@@ -329,7 +335,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     w.sum = sum;
 #pragma unroll
     for (int i = 0; i < DB; ++i) w.out[i] = out[i];
-    finish_rows(a, s, group, first, rows, t0 < t1, w, lane);
+    finish_rows(a, s, group, first, rows, t0 * KEYS, t0 < t1, w, lane);
 }
 
 // Joins the shares of a split call, each share scaled by exp of its maximum less the largest, in the order of the shares (32 x 16 rows: 4.2 us, a launch): groups of 32 lanes, a lane four elements of a row.  Of few rows each has a workgroup, whose eight groups take
@@ -344,9 +350,15 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     if (a.cu_q && (token < max(a.cu_q[0], 0) || token >= a.cu_q[a.batch])) return;  // a row of no sequence stays as it is
     const float c = a.scale * LOG2E;
     float top = -__builtin_inff();
-    for (int s = place; s < a.splits; s += 32) top = __builtin_fmaxf(top, share_stats(a, s, row)[0]);
+    bool sees = false;
+    for (int s = place; s < a.splits; s += 32) {
+        const float* stats = share_stats(a, s, row);
+        top = __builtin_fmaxf(top, stats[0]);
+        sees |= stats[1] != 0.f;
+    }
 #pragma unroll
     for (int step = 1; step < 32; step <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, step));
+    sees = (uint32_t)(__ballot(sees) >> (threadIdx.x & 32)) != 0u;
     const float base = top > -__builtin_inff() ? top * c : 0.f;
     float sum = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
@@ -356,7 +368,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
         if (stats[1] == 0.f) continue;  // no keys: nothing was written
         // a factor of 0 is no reason to pass a share over: it may hold NaN alone, which no maximum tells of, or infinite values
         const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(stats[0], c, -base));
-        sum = __builtin_fmaf(stats[1], keep, sum);
+        sum = __builtin_fmaf(stats[1] == NO_WEIGHT ? 0.f : stats[1], keep, sum);
         if (4 * place < a.d) {
             const f32x4 y = *reinterpret_cast<const f32x4*>(share_row(a, s, row) + 4 * place);
 #pragma unroll
@@ -372,7 +384,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
 #pragma unroll
         for (int g = 1; g < GROUPS; ++g) x += joined[g][place], sum += sums[g];
     }
-    const float scale = sum > 0.f ? 1.f / sum : sum != sum ? sum : 0.f;
+    const float scale = sum > 0.f ? 1.f / sum : sees ? __builtin_nanf("") : 0.f;
     const float v[4] = {x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale};
     if (4 * place < a.d) store_elems<DT, 4>((typename Elem<DT>::T*)a.out + token * a.out_row + head * a.out_head + 4 * place, a.d - 4 * place, v);
     if (place == 0 && a.lse) a.lse[row] = top * a.scale + logf(sum);

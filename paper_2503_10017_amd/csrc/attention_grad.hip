@@ -57,8 +57,9 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
         delta = across_halves_sum(delta);
         if (r < rows) lse = f.lse[flat_row(f, s, group, r)];
     }
-    // a row that sees no key has minus infinity there; plus infinity makes its weights 0
-    const float base = lse == -__builtin_inff() ? __builtin_inff() : lse * LOG2E, c = f.scale * LOG2E;
+    // a row that sees no key: plus infinity makes its weights 0; one that sees keys of no weight alone has minus infinity there, and no weights
+    const int seen = seen_by(f, s, min(r, rows - 1));
+    const float base = r < rows && seen > 0 ? lse * LOG2E : __builtin_inff(), c = f.scale * LOG2E;
     if (r < rows && lane < 32) {
         const int64_t at = flat_row(f, s, group, r);
         a.stats[at] = base - (float)WEIGHT_SHIFT<DT>;
@@ -66,7 +67,6 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
     }
     if (!a.dq) return;
     const int least_seen = mine < rows ? seen_by(f, s, mine) : 0, most_seen = mine < rows ? seen_by(f, s, min(mine + 32, rows) - 1) : 0;
-    const int seen = seen_by(f, s, min(r, rows - 1));
     f32x16 dq[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) dq[i] = (f32x16)(0.f);
