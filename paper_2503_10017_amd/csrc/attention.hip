@@ -13,6 +13,11 @@ namespace fnn {
 
 namespace {
 
+// What the weights of keys whose largest score is `top` are multiplied by beside others whose largest is `most`: 0 for no keys.
+__device__ __forceinline__ float weight_beside(float top, float most, float c) {
+    return top > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - most) * c) : 0.f;
+}
+
 // One wave's 32 rows, a row per lane of either half.
 template <int DT, int DB, int KEYS>
 struct Rows {
@@ -59,10 +64,9 @@ struct Rows {
             for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, score[kb][r]);
         most = across_halves_max(most);
         // What is so far is rescaled only where some row's maximum rises by a factor of 2^8 and more: weights may as well reach 256.
-        if (__ballot(!(most * c <= __builtin_fmaf(top, c, 8.f)))) {
+        if (__ballot((most - top) * c > 8.f)) {
             most = __builtin_fmaxf(most, top);
-            const float base = most > -__builtin_inff() ? most * c : 0.f;
-            const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(top, c, -base));
+            const float keep = weight_beside(top, most, c);
             top = most;
             sum *= keep;
 #pragma unroll
@@ -70,8 +74,17 @@ struct Rows {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) out[i][r] *= keep;
         }
-        // rows that have seen no key yet stay at minus infinity; anything finite in its place makes their weights 0
-        const float base = top > -__builtin_inff() ? top * c : 0.f;
+        // exp2(c score - c top), for rows that have seen no key yet of anything finite in top's place: their weights are 0.  c top is rounded, which all weights of a row
+        // have in common; where it is so large that this is a factor to notice (2^31: one that overflows), the difference comes first.
+        const float shown = top > -__builtin_inff() ? top : 0.f;
+        float base = shown * c;
+        if (__ballot(__builtin_fabsf(base) > 1024.f)) {
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) score[kb][r] -= shown;
+            base = 0.f;
+        }
         // summed up before they are rounded: lse has fp32's precision
         float more = 0.f;
 #pragma unroll
@@ -316,7 +329,6 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     float top = w.top;
 #pragma unroll
     for (int i = 1; i < 4; ++i) top = __builtin_fmaxf(top, all[i * EACH + lane]);
-    const float base = top > -__builtin_inff() ? top * c : 0.f;
     float sum = 0.f;
     f32x16 out[DB];
 #pragma unroll
@@ -324,7 +336,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const float* from = all + j * EACH;
-        const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(from[lane], c, -base));
+        const float keep = weight_beside(from[lane], top, c);
         sum = __builtin_fmaf(from[64 + lane], keep, sum);
 #pragma unroll
         for (int i = 0; i < DB; ++i)
@@ -359,7 +371,6 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
 #pragma unroll
     for (int step = 1; step < 32; step <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, step));
     sees = (uint32_t)(__ballot(sees) >> (threadIdx.x & 32)) != 0u;
-    const float base = top > -__builtin_inff() ? top * c : 0.f;
     float sum = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -367,7 +378,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
         const float* stats = share_stats(a, s, row);
         if (stats[1] == 0.f) continue;  // no keys: nothing was written
         // a factor of 0 is no reason to pass a share over: it may hold NaN alone, which no maximum tells of, or infinite values
-        const float keep = __builtin_amdgcn_exp2f(__builtin_fmaf(stats[0], c, -base));
+        const float keep = weight_beside(stats[0], top, c);
         sum = __builtin_fmaf(stats[1] == NO_WEIGHT ? 0.f : stats[1], keep, sum);
         if (4 * place < a.d) {
             const f32x4 y = *reinterpret_cast<const f32x4*>(share_row(a, s, row) + 4 * place);

@@ -59,7 +59,11 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
     }
     // a row that sees no key: plus infinity makes its weights 0; one that sees keys of no weight alone has minus infinity there, and no weights
     const int seen = seen_by(f, s, min(r, rows - 1));
-    const float base = r < rows && seen > 0 ? lse * LOG2E : __builtin_inff(), c = f.scale * LOG2E;
+    float base = r < rows && seen > 0 ? lse * LOG2E : __builtin_inff();
+    const float c = f.scale * LOG2E;
+    // lse and what it is compared with are off by up to five roundings: where those are whole units of the exponent, too much is taken off rather than too
+    // little, so that no weight passes 1 by far, let alone overflows (below, by 2^1.25 at most)
+    if (__builtin_fabsf(base) > 4194304.f && __builtin_fabsf(base) < __builtin_inff()) base += __builtin_fabsf(base) * 0x1p-21f;
     if (r < rows && lane < 32) {
         const int64_t at = flat_row(f, s, group, r);
         a.stats[at] = base - (float)WEIGHT_SHIFT<DT>;
