@@ -375,15 +375,16 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int s = mine; s < a.splits; s += GROUPS) {
+        // What the share of no keys has for a row was not written, and is read all the same (its memory is there) so that no load waits for another.  A factor of
+        // 0 is no reason to pass a share over: it may hold NaN alone, which no maximum tells of, or infinite values.
         const float* stats = share_stats(a, s, row);
-        if (stats[1] == 0.f) continue;  // no keys: nothing was written
-        // a factor of 0 is no reason to pass a share over: it may hold NaN alone, which no maximum tells of, or infinite values
+        const bool empty = stats[1] == 0.f;
         const float keep = weight_beside(stats[0], top, c);
-        sum = __builtin_fmaf(stats[1] == NO_WEIGHT ? 0.f : stats[1], keep, sum);
+        sum = empty ? sum : __builtin_fmaf(stats[1] == NO_WEIGHT ? 0.f : stats[1], keep, sum);
         if (4 * place < a.d) {
             const f32x4 y = *reinterpret_cast<const f32x4*>(share_row(a, s, row) + 4 * place);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(y[e], keep, x[e]);
+            for (int e = 0; e < 4; ++e) x[e] = empty ? x[e] : __builtin_fmaf(y[e], keep, x[e]);
         }
     }
     if constexpr (GROUPS > 1) {
