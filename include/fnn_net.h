@@ -127,7 +127,7 @@ int32_t fnn_attention(const fnn_heads* q, const fnn_heads* k, const fnn_heads* v
  * delta = sum_e dout out and ds = p (<dout, v> - delta):
  *   dq = scale sum_j ds k_j,   dk = scale sum_i ds q_i,   dv = sum_i p dout_i   (over all query heads of the key head)
  * dq, dk and dv may each be NULL: not wanted.  Keys of a sequence without queries get 0, and so do queries that see no key.
- * p and ds are rounded to the inputs' type for the products.  lse has 24 bits, so where it passes 2^12 in size p is less exact than the
+ * p and ds are rounded to the inputs' type for the products (in FNN_F16 times powers of two, so that neither dout's size nor long rows cost digits).  lse has 24 bits, so where it passes 2^12 in size p is less exact than the
  * inputs' type, and where it passes 2^22 p tells no more than that the gradient is finite.
  */
 size_t fnn_attention_backward_workspace_bytes(int64_t tokens_q, int64_t tokens_k, int32_t batch, int32_t heads, int32_t key_heads, int32_t d);

@@ -15,10 +15,47 @@ namespace fnn {
 
 namespace {
 
-// fp16 weights are formed 2^14 times too large (at most 2^14): those of long rows, 1 / 16384 and less, would lose bits below the
+// fp16 weights are formed 2^14 times too large (at most 2^14) for dv: those of long rows, 1 / 16384 and less, would lose bits below the
 // type's normal range.  The factor leaves with the result.
 template <int DT>
 constexpr int WEIGHT_SHIFT = DT == CT_F16 ? 14 : 0;
+
+// ds is of any size: p, down to 0, times what dout and v are.  In fp16 it is rounded as ds times a power of two (`by`) of its row (dq) or key (dk), chosen such that the largest so
+// far is between 1 and 2^15: nothing overflows, and half of the type's last step is 2^-25 of that largest or less.  As with the maximum of a softmax, what
+// has been summed is rescaled in the rare case that the largest leaves that range; it starts again at 2^8.  bf16 has fp32's range and needs none of it.
+// The largest costs 5 % of the two passes and the branch, which the products wait for, 6 % (6 x 2048 causal rows, 12 heads of 64: 242 and 268 us without and with it; 4 x 2048,
+// 16 heads on 8 of 128: 532 and 587).  Looked at once for 64 keys with both blocks' ds held back, it is slower: the registers are not there.
+template <int DT>
+struct Digits {
+    static constexpr bool USED = DT == CT_F16;
+    static constexpr int LEAST = -40, MOST = 64;  // of by's exponent: |ds| <= 2^40 in fp16; smaller ones than 2^-64 are far below what a result shows
+    float by = 1.f, largest = 0.f;
+
+    // `ds`: 16 of the lane's row (key), the other half's lane has 16 more.  DB blocks of results so far.
+    template <int DB>
+    __device__ __forceinline__ void fit(f32x16& ds, f32x16 (&sums)[DB]) {
+        if constexpr (!USED) return;
+        float most = 0.f;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) most = __builtin_fmaxf(most, __builtin_fabsf(ds[x]));
+        largest = __builtin_fmaxf(largest, across_halves_max(most));
+        const bool out = largest > 32768.f || (largest < 1.f && largest > 0.f);
+        if (__builtin_expect(__ballot(out) != 0, 0)) {
+            const int now = exponent(by), wanted = now + 8 - exponent(largest);
+            const int step = out ? min(max(wanted, LEAST), MOST) - now : 0;
+            const float factor = __uint_as_float((uint32_t)(127 + step) << 23);
+            by *= factor;
+            largest *= factor;
+#pragma unroll
+            for (int x = 0; x < 16; ++x) ds[x] *= factor;
+#pragma unroll
+            for (int i = 0; i < DB; ++i)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) sums[i][x] *= factor;
+        }
+    }
+    static __device__ __forceinline__ int exponent(float x) { return (int)(__float_as_uint(x) >> 23 & 255u) - 127; }
+};
 
 // dq, and what the second pass takes of each row: a wave has 32 rows and runs over tiles of 64 keys, which its workgroup's four waves share.  Three products a tile.
 // 12 sequences of up to 2048 rows, 12 heads of 64, bf16: 117 us, bound by the latency from product to exponential to product, of which a SIMD's two
@@ -74,6 +111,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
     f32x16 dq[DB];
 #pragma unroll
     for (int i = 0; i < DB; ++i) dq[i] = (f32x16)(0.f);
+    Digits<DT> digits;
 
     const E* k = (const E*)f.k + s.k0 * f.k_row + group * f.k_head;
     const E* v = (const E*)f.v + s.k0 * f.v_row + group * f.v_head;
@@ -113,8 +151,10 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
 #pragma unroll
                 for (int x = 0; x < 16; ++x) p[x] = 32 * kb + tile_row(x, 0) < left ? p[x] : 0.f;
             }
+            const float less = delta * digits.by;
 #pragma unroll
-            for (int x = 0; x < 16; ++x) ds[x] = p[x] * (ds[x] - delta);
+            for (int x = 0; x < 16; ++x) ds[x] = p[x] * (digits.USED ? __builtin_fmaf(ds[x], digits.by, -less) : ds[x] - delta);
+            digits.fit(ds, dq);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint4 g = round_half<DT>(ds, half);
@@ -123,7 +163,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
             }
         }
     }
-    float scale = f.scale;
+    float scale = f.scale / digits.by;
     if (__builtin_expect(tiles && any_not_finite, 0)) {
         for (int j = unseen * KEYS; j < min(tiles * KEYS, s.lk); ++j) {
             const bool bad = not_finite(k + j * f.k_row, f.d, lane) || not_finite(v + j * f.v_row, f.d, lane);
@@ -189,6 +229,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
 #pragma unroll
     for (int i = 0; i < DB; ++i) dk[i] = dv[i] = (f32x16)(0.f);
     const float c = f.scale * LOG2E, unshift = 1.f / (float)(1 << WEIGHT_SHIFT<DT>);
+    Digits<DT> digits;
 
     // The rows of a tile are share heads of ROWS / share tokens each where share divides ROWS: then a thread's place in the tile says how far
     // its row lies from the tile's first.  Otherwise its rows are found one by one.
@@ -266,13 +307,15 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
             }
 #pragma unroll
             for (int x = 0; x < 16; ++x) p[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x], c, -stats[tile_row(x, 0)]));
+            const float by = unshift * digits.by;
             if (row + 32 * block < wave_all) {
                 const int least = from_row - row - 32 * block - 4 * (lane >> 5);
 #pragma unroll
                 for (int x = 0; x < 16; ++x) p[x] = tile_row(x, 0) >= least ? p[x] : 0.f;
             }
 #pragma unroll
-            for (int x = 0; x < 16; ++x) ds[x] = WEIGHT_SHIFT<DT> ? p[x] * (ds[x] * unshift) : p[x] * ds[x];
+            for (int x = 0; x < 16; ++x) ds[x] = digits.USED ? p[x] * (ds[x] * by) : p[x] * ds[x];
+            digits.fit(ds, dk);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const uint4 w = round_half<DT>(p, half), g = round_half<DT>(ds, half);
@@ -301,7 +344,7 @@ __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs
     for (int which = 0; which < 2; ++which) {
         if (!(which ? a.dv : a.dk)) continue;
         E* to = which ? (E*)a.dv + (s.k0 + (int64_t)key) * a.dv_row + group * a.dv_head : (E*)a.dk + (s.k0 + (int64_t)key) * a.dk_row + group * a.dk_head;
-        const float scale = (which ? unshift : f.scale) * spoiled[which];
+        const float scale = (which ? unshift : f.scale / digits.by) * spoiled[which];
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
             float x[2][8];
