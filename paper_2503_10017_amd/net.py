@@ -45,6 +45,11 @@ def _stream_ptr(stream, device):
     return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _like(t: torch.Tensor, stream):
+    """_empty of t's shape and type; empty_like takes 2 us less on the host, a fifth of a call on one token."""
+    return torch.empty_like(t) if stream is None else _empty(t.shape, t.dtype, t.device, stream)
+
+
 def _scratch(need: int, device, stream):
     """A workspace of the call's own (None: none is needed)."""
     return _workspace(need, device, stream) if need else None
@@ -69,7 +74,7 @@ def fnn_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias:
     n, d = x.shape
     wt = _weight_dtype(x, weight, bias)
     if out is None:
-        out = _empty(x.shape, x.dtype, x.device, stream)
+        out = _like(x, stream)
     mean = rstd = None
     if want_stats:
         mean = _empty(n, torch.float32, x.device, stream)
@@ -93,7 +98,7 @@ def fnn_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tenso
     wt = x.dtype if weight is None else weight.dtype
     dx = out
     if dx is None and want_x:
-        dx = _empty(x.shape, x.dtype, x.device, stream)
+        dx = _like(x, stream)
     dweight = dbias = None
     if want_weight:
         dweight = _empty(d, wt, x.device, stream)
