@@ -200,9 +200,10 @@ __device__ __forceinline__ void part_of(const AttentionArgs& a, int tiles, int& 
     t1 = part < parts ? (int)((int64_t)tiles * (part + 1) / parts) : 0;
 }
 
-// Many rows: a workgroup's four waves have 32 rows each and share tiles of 64 keys.  Bound by the vector operations between the two products (per
-// score a multiply-add, a maximum, an exponential, an addition and half a rounding), which take longer than the products do: 32 sequences of 768 rows and keys, 16
-// heads of 64, bf16: 127 us, 610 TFLOP/s; packed causal rows up to 4001, 16 heads on 8, 128 elements, fp16: 578 us, 710 TFLOP/s (567 before tiles were cleared).
+// Many rows: a workgroup's four waves have 32 rows each and share tiles of 64 keys.  32 sequences of 768 rows and keys, 16 heads of 64, bf16: 121 us, 640 TFLOP/s; packed
+// causal rows up to 4001, 16 heads on 8, 128 elements, fp16: 545 us, 750 TFLOP/s.  Neither the matrix cores (busy 26 and 34 % of the cycles) nor the vector units (51 and 38 %) bound
+// it: a wave's chain of product, softmax (per score a multiply-add, a maximum, an exponential, an addition and half a rounding) and product is serial, and the
+// two waves or so of a SIMD do not fill its waits (waves wait 48 and 40 % of their cycles).
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
     constexpr int KEYS = 64, ROWS = 128;
@@ -261,8 +262,8 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttentionArgs a) {
 
 // Few rows (a token or some at the end of a cache): the time is that of reading the keys once.  Every wave has the same 32 rows and tiles of
 // 32 keys of its own, which only it waits for; at the end the four join in LDS.  32 caches of up to 4096 keys, one row for each of 16 heads on 4 of 128, bf16:
-// 51 us for 119 MB, 2.3 TB/s (one workgroup a compute unit at 128 KB of stages, and caches whose lengths differ); 32 equal caches of 4096 keys 57 us for
-// 268 MB, 4.7 TB/s.
+// 49 us for 119 MB, 2.4 TB/s (one workgroup a compute unit at 128 KB of stages, and caches whose lengths differ); 32 equal caches of 4096 keys 55 us for
+// 268 MB, 4.9 TB/s.
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
     constexpr int KEYS = 32, ROWS = 32;
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttentionArgs a) {
         lds_loads_arrived();
         if (t + 4 < t1) stage(next, t + 4);
         const int key = t * KEYS;
-        if (__builtin_expect(t >= unseen, 0)) {  // (51 us for one token's caches; laid out as if it were usual, 53)
+        if (__builtin_expect(t >= unseen, 0)) {  // (laid out as if it were usual, 2 us more for one token's caches)
             cleared |= __ballot(Tile::template clear_not_finite<64>(now + Tile::BYTES, lane)) != 0;
             __builtin_amdgcn_wave_barrier();
         }
@@ -405,7 +406,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
 // From the sizes alone: whether the rows of a sequence are few on average (one wave's worth), and into how many parts the keys may be split: parts of
 // the size that makes 320 of them in all, a little more than one a compute unit, and not less than 256 keys, below which a part's start costs more than it
 // saves.  Longer sequences than the average have longer parts: as many of the right size for them all would be workgroups without keys for the others, each
-// of which holds a compute unit's LDS for 2 us (32 caches of 4096 keys, 4 heads of 128: 57 us, with parts for sequences twice as long 66).
+// of which holds a compute unit's LDS for 2 us (32 caches of 4096 keys, 4 heads of 128: 57 us when it was measured, with parts for sequences twice as long 66).
 struct Plan {
     bool few;
     int row_tiles, splits, part_keys;

@@ -58,8 +58,8 @@ struct Digits {
 };
 
 // dq, and what the second pass takes of each row: a wave has 32 rows and runs over tiles of 64 keys, which its workgroup's four waves share.  Three products a tile.
-// 12 sequences of up to 2048 rows, 12 heads of 64, bf16: 117 us, bound by the latency from product to exponential to product, of which a SIMD's two
-// waves hide part, and by the vector operations between them.
+// 12 sequences of up to 2048 rows, 12 heads of 64, bf16: 116 us, bound by the latency from product to exponential to product, of which a SIMD's two
+// waves hide part: the matrix cores are busy 34 % of the cycles, the vector units 42 %.
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs a) {
     constexpr int KEYS = 64, ROWS = 128;
@@ -188,7 +188,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(AttentionBackArgs 
 }
 
 // dk and dv: a wave has 32 keys and runs over tiles of 64 rows, 32 of long vectors (of all the heads that share the key head), which its workgroup's four waves share.
-// Four products a tile: 166 us on the sequences above, bound as the first pass is.
+// Four products a tile: 168 us on the sequences above, bound as the first pass is (matrix cores 30 %, vector units 33 %).  At more than 96 elements 48 bytes a lane (fp16: 92) are
+// in scratch memory.
 template <int DT, int DB, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attention_dkv_kernel(AttentionBackArgs a) {
     constexpr int KEYS = 128, ROWS = DB <= 2 ? 64 : 32;

@@ -3,6 +3,8 @@
 Every function has the name and meaning of the C entry point it wraps; torch supplies device memory and the current stream.
 Tensors are taken with the strides that they have, as long as the elements of a row are contiguous.  With ``stream`` a call runs on that stream: outputs and
 workspaces that it is not given are of that stream's memory, and the inputs have to be ready there.
+
+Nothing here enters torch's autograd graph, whether or not a tensor requires a gradient: gradients are calls of their own (fnn_..._backward).
 """
 from __future__ import annotations
 
