@@ -13,6 +13,15 @@ namespace fnn {
 
 namespace {
 
+// Weights are formed 2^7 times too large in fp16, at most 2^15: those of many keys far below the largest, which may weigh as much together, would lose bits below
+// the type's normal range.  The factor leaves with the sum.
+template <int DT>
+constexpr float WEIGHT_LIFT = DT == CT_F16 ? 7.f : 0.f;
+// lse from the largest score and the sum of lifted weights; no key: minus infinity
+template <int DT>
+__device__ __forceinline__ float lse_of(float top, float sum, float scale) {
+    return top * scale + logf(DT == CT_F16 ? sum * 0x1p-7f : sum);
+}
 // What the weights of keys whose largest score is `top` are multiplied by beside others whose largest is `most`: 0 for no keys.
 __device__ __forceinline__ float weight_beside(float top, float most, float c) {
     return top > -__builtin_inff() ? __builtin_amdgcn_exp2f((top - most) * c) : 0.f;
@@ -26,7 +35,7 @@ struct Rows {
     static constexpr int KB = KEYS / 32;
     uint4 q[2 * DB];
     f32x16 out[DB];
-    float top, sum;  // of the keys so far: a score that none exceeds by 8 / c, and (this half's share of) the sum of exp2(c (score - top))
+    float top, sum;  // of the keys so far: a score that none exceeds by 8 / c, and (this half's share of) the sum of exp2(c (score - top) + WEIGHT_LIFT)
 
     __device__ __forceinline__ void begin(const AttentionArgs& a, const Sequence& s, int group, int row, int rows, int lane) {
         load_row<DT, DB>(a.q, a.q_row, a.q_head, a, s, group, row + (lane & 31), rows, lane, q);
@@ -77,13 +86,13 @@ struct Rows {
         // exp2(c score - c top), for rows that have seen no key yet of anything finite in top's place: their weights are 0.  c top is rounded, which all weights of a row
         // have in common; where it is so large that this is a factor to notice (2^31: one that overflows), the difference comes first.
         const float shown = top > -__builtin_inff() ? top : 0.f;
-        float base = shown * c;
+        float base = shown * c - WEIGHT_LIFT<DT>;
         if (__ballot(__builtin_fabsf(base) > 1024.f)) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) score[kb][r] -= shown;
-            base = 0.f;
+            base = -WEIGHT_LIFT<DT>;
         }
         // summed up before they are rounded: lse has fp32's precision
         float more = 0.f;
@@ -96,7 +105,7 @@ struct Rows {
             }
         sum += more;
         __builtin_amdgcn_sched_barrier(0);
-        // the weights are at most 256 and rounded to the values' type, as the matrix instructions take them; their sum is of the unrounded ones
+        // the weights are at most 2^8, lifted, and rounded to the values' type, as the matrix instructions take them; their sum is of the unrounded ones
 #pragma unroll
         for (int t = 0; t < 2 * KB; ++t) {
             const uint4 p = round_half<DT>(score[t >> 1], t & 1);
@@ -188,7 +197,7 @@ __device__ __forceinline__ void finish_rows(const AttentionArgs& a, const Sequen
         to[0] = w.top;
         to[1] = sees && total == 0.f ? NO_WEIGHT : total;
     } else if (a.lse) {
-        a.lse[flat_row(a, s, group, r)] = w.top * a.scale + logf(total);  // no key: minus infinity
+        a.lse[flat_row(a, s, group, r)] = lse_of<DT>(w.top, total, a.scale);
     }
 }
 
@@ -400,7 +409,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     const float scale = sum > 0.f ? 1.f / sum : sees ? __builtin_nanf("") : 0.f;
     const float v[4] = {x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale};
     if (4 * place < a.d) store_elems<DT, 4>((typename Elem<DT>::T*)a.out + token * a.out_row + head * a.out_head + 4 * place, a.d - 4 * place, v);
-    if (place == 0 && a.lse) a.lse[row] = top * a.scale + logf(sum);
+    if (place == 0 && a.lse) a.lse[row] = lse_of<DT>(top, sum, a.scale);
 }
 
 // From the sizes alone: whether the rows of a sequence are few on average (one wave's worth), and into how many parts the keys may be split: parts of
