@@ -232,6 +232,7 @@ hipError_t with_type(int dtype, F f) {
 // across its rows, bf16: 12288 x 1023 -> 4095 733 and 345, 600 x 777 -> 1001 60 and 45, 200 x 501 -> 501 54 and 37, 8 x 1021 -> 4095 41 and 39, 16 x 101 -> 101 24 and
 // 27; fp32: 6001 x 777 -> 1001 305 and 271, 1531 x 777 -> 1001 100 and 100, 300 x 777 -> 1001 58 and 60.
 bool copies_pay(int64_t m, int64_t n, int64_t k, int64_t width, int dtype, bool backward) {
+    if (!backward && few_rows(m, k)) return false;  // that pass takes rows at any address (16 x 20001 -> 40003 fp16: 960 us, 1080 with copies, and no 1.6 GB for them)
     const double least = !backward ? 1.2e10 : dtype == FNN_F32 ? 2e9 : 3e7;
     return width * (dtype == FNN_F32 ? 4 : 2) % 16 != 0 && (double)m * n * k >= least;
 }

@@ -28,3 +28,13 @@ def test_odd_numbers_of_shares(case):
 
     prob = Problem(*case, True, "bf16")
     check_forward(prob, *prob.call())
+
+
+def test_few_rows_need_no_copies(lib):  # noqa: F811
+    """Up to 16 rows the product is one pass over the weights at any alignment: there is nothing to copy, however large and odd they are."""
+    import torch
+
+    for rows in (1, 16):
+        for dtype in (torch.float16, torch.float32):
+            assert fnn.fnn_linear_workspace_bytes(rows, 50001, 250001, dtype) == 0
+    assert fnn.fnn_linear_workspace_bytes(17, 50001, 250001, torch.float16) > 2 * 50001 * 250001
