@@ -209,8 +209,8 @@ __device__ __forceinline__ void part_of(const AttentionArgs& a, int tiles, int& 
     t1 = part < parts ? (int)((int64_t)tiles * (part + 1) / parts) : 0;
 }
 
-// Many rows: a workgroup's four waves have 32 rows each and share tiles of 64 keys.  32 sequences of 768 rows and keys, 16 heads of 64, bf16: 121 us, 640 TFLOP/s; packed
-// causal rows up to 4001, 16 heads on 8, 128 elements, fp16: 545 us, 750 TFLOP/s.  Neither the matrix cores (busy 26 and 34 % of the cycles) nor the vector units (51 and 38 %) bound
+// Many rows: a workgroup's four waves have 32 rows each and share tiles of 64 keys.  32 sequences of 768 rows and keys, 16 heads of 64, bf16: 123 us, 630 TFLOP/s; packed
+// causal rows up to 4001, 16 heads on 8, 128 elements, fp16: 555 us, 740 TFLOP/s.  Neither the matrix cores (busy 26 and 34 % of the cycles) nor the vector units (51 and 38 %) bound
 // it: a wave's chain of product, softmax (per score a multiply-add, a maximum, an exponential, an addition and half a rounding) and product is serial, and the
 // two waves or so of a SIMD do not fill its waits (waves wait 48 and 40 % of their cycles).
 template <int DT, int DB, bool DIRECT>

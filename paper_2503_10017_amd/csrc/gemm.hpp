@@ -162,7 +162,7 @@ __device__ __forceinline__ void finish_run(const GemmArgs& a, int64_t m, int n, 
 // A workgroup's tile of TM x TN results, a wave's 128 x 64 or 64 x 64 of it in registers.  Per 128-byte step of k a tile of 256 x 256 stages 64 KB and has 64 products
 // a wave, two of whose operands come from LDS for every eight (large) or four (small) products; results leave through LDS, with the epilogue on the way.  What
 // bounds it: large products the matrix instructions at the power limit and the loads that do not quite hide behind them (4096 x 4096 -> 4096 fp16 115 us,
-// 1195 TFLOP/s, 87 % of the library's rate there; 12288 x 1024 -> 4096 with GELU 134 us, 770 TFLOP/s, some 25 us of them GELU); those of fewer
+// 1195 TFLOP/s, 87 % of the library's rate there; 12288 x 1024 -> 4096 with GELU 127 us, 810 TFLOP/s, some 20 us of them GELU); those of fewer
 // tiles than compute units the latency of a step.  fp32 1531 x 777 -> 1001: 43 us for 2.4 GFLOP, the latency of loads through registers.
 // Measured and slower or no faster: four stages of 64 bytes, loads spread between the products, operands asked for in the order of k rotated from tile to
 // tile, two half-workgroups taking turns at loads and products, tiles of 256 x 128.
