@@ -275,7 +275,7 @@ def run(state):
 def _nearest_e4m3(v):
     """The nearest e4m3 value of numbers up to 448 in 64 bits, halves to the even one: steps of an eighth of the power of two below, of 2^-9 under 2^-6."""
     _, exponent = torch.frexp(v)
-    step = torch.ldexp(torch.ones_like(v), (exponent - 1).clamp(min=-6) - 3)
+    step = (((exponent - 1).clamp(min=-6).long() + (1023 - 3)) << 52).view(torch.float64)  # ldexp and pow are a little off on a GPU
     return torch.round(v / step) * step
 
 
