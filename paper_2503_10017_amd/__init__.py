@@ -38,3 +38,14 @@ from .net import (  # noqa: F401
     fnn_linear_backward_workspace_bytes,
     fnn_linear_workspace_bytes,
 )
+from .net8 import (  # noqa: F401
+    FnnScaled,
+    fnn_linear_e4m3,
+    fnn_linear_e4m3_backward,
+    fnn_linear_e4m3_backward_workspace_bytes,
+    fnn_linear_e4m3_workspace_bytes,
+    fnn_quantize,
+    fnn_rms_norm,
+    fnn_rms_norm_backward,
+    fnn_rms_norm_backward_workspace_bytes,
+)

@@ -104,6 +104,22 @@ def load_library():
     lib.fnn_attention_backward_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
     lib.fnn_attention_backward.restype = i32
     lib.fnn_attention_backward.argtypes = [vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, ctypes.c_float, vp, vp, vp, vp, sz, vp]
+    lib.fnn_quantize.restype = i32
+    lib.fnn_quantize.argtypes = [vp, i32, vp, vp]
+    lib.fnn_rms_norm.restype = i32
+    lib.fnn_rms_norm.argtypes = [vp, vp, vp, i32, ctypes.c_float, vp, vp, vp, vp, vp]
+    lib.fnn_rms_norm_backward_workspace_bytes.restype = sz
+    lib.fnn_rms_norm_backward_workspace_bytes.argtypes = [i64, i32]
+    lib.fnn_rms_norm_backward.restype = i32
+    lib.fnn_rms_norm_backward.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.fnn_linear_e4m3_workspace_bytes.restype = sz
+    lib.fnn_linear_e4m3_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.fnn_linear_e4m3.restype = i32
+    lib.fnn_linear_e4m3.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    lib.fnn_linear_e4m3_backward_workspace_bytes.restype = sz
+    lib.fnn_linear_e4m3_backward_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    lib.fnn_linear_e4m3_backward.restype = i32
+    lib.fnn_linear_e4m3_backward.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 

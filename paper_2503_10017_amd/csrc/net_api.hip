@@ -161,6 +161,53 @@ int32_t attention_args(const fnn_heads* q, const fnn_heads* k, const fnn_heads* 
     return FNN_OK;
 }
 
+// Shape, then pointers, of a matrix in 8 bits; the strides of what there is one of are not looked at.
+int32_t check_scaled(const fnn_scaled* m) {
+    if (!m) return FNN_E_NULL;
+    if (m->n < 0 || m->n > MAX_SLOTS || m->d < 0 || (m->block_rows != 1 && m->block_rows != SCALED_BLOCK)) return FNN_E_SHAPE;
+    const int64_t high = m->block_rows == 1 ? m->n : scaled_blocks(m->n), blocks = scaled_blocks(m->d);
+    if (m->n > 1 && (m->row_stride < m->d || m->row_stride > INT64_MAX / 8 / m->n)) return FNN_E_SHAPE;
+    if (high > 1 && (m->scale_row < 1 || m->scale_row > INT64_MAX / 16 / high)) return FNN_E_SHAPE;
+    if (blocks > 1 && (m->scale_block < 1 || m->scale_block > INT64_MAX / 16 / blocks)) return FNN_E_SHAPE;
+    if (m->n > 0 && m->d > 0 && (!m->data || !m->scale)) return FNN_E_NULL;
+    return FNN_OK;
+}
+int64_t stride_of(const fnn_scaled* m) { return m->n > 1 ? m->row_stride : m->d; }
+// A stride that is not looked at is 0: a product reads the scale of the first row, or block, in place of those behind the last.
+int64_t scale_row_of(const fnn_scaled* m) { return (m->block_rows == 1 ? m->n : scaled_blocks(m->n)) > 1 ? m->scale_row : 0; }
+int64_t scale_block_of(const fnn_scaled* m) { return m->d > SCALED_BLOCK ? m->scale_block : 0; }
+CodesOut codes_of(const fnn_scaled* m) {
+    return {(uint8_t*)const_cast<void*>(m->data), const_cast<float*>(m->scale), stride_of(m), scale_row_of(m), scale_block_of(m)};
+}
+
+// The workspace of the gradient of a layer in 8 bits: q by rows with w's transpose, or q and x across, in turn; the shares of dbias; and one area that the two products use in turn.
+struct E4m3BackLayout {
+    size_t q, q_scale, w, q_across, q_across_scale, x, x_scale, sums, partial, total;  // offsets
+    int64_t outer_stride, rows_stride;  // of codes along outer and along the rows
+};
+E4m3BackLayout e4m3_back_layout(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
+    E4m3BackLayout L;
+    L.outer_stride = whole_runs(outer, 1);
+    L.rows_stride = whole_runs(rows, 1);
+    size_t at = 0;
+    auto area = [&](size_t& place, int64_t bytes) {
+        place = at;
+        at += aligned((size_t)bytes);
+    };
+    area(L.q, rows * L.outer_stride);
+    area(L.q_scale, rows * scaled_blocks(outer) * 4);
+    area(L.w, inner * L.outer_stride);
+    area(L.q_across, outer * L.rows_stride);
+    area(L.q_across_scale, outer * scaled_blocks(rows) * 4);
+    area(L.x, inner * L.rows_stride);
+    area(L.x_scale, inner * scaled_blocks(rows) * 4);
+    area(L.sums, scaled_blocks(rows) * outer * 4);
+    L.partial = at;
+    const size_t x = scaled_gemm_workspace(rows, inner, outer, dtype), w = scaled_gemm_workspace(outer, inner, rows, dtype);
+    L.total = at + aligned(x > w ? x : w);
+    return L;
+}
+
 }  // namespace
 
 #pragma GCC visibility push(default)
@@ -431,6 +478,246 @@ int32_t fnn_attention_backward(const fnn_heads* dout, const fnn_heads* q, const 
     const int64_t apart = a.forward.share * (head_of(q) > head_of(dout) ? head_of(q) : head_of(dout));
     a.direct_rows = on_runs(q) && on_runs(dout) && apart < ((int64_t)1 << 28);
     return done(launch_attention_backward(a, q->dtype, (hipStream_t)stream));
+}
+
+int32_t fnn_quantize(const fnn_map* x, int32_t transposed, const fnn_scaled* q, void* stream) {
+    FNN_CHECK(check_matrix(x));
+    FNN_CHECK(check_scaled(q));
+    if (transposed ? q->n != x->d || q->d != x->n : q->n != x->n || q->d != x->d) return FNN_E_SHAPE;
+    if (x->n == 0 || x->d == 0) return FNN_OK;
+    const hipStream_t s = (hipStream_t)stream;
+    if (!transposed && q->block_rows == 1)
+        return done(launch_quantize_rows(x->data, stride_of(x), x->n, x->d, codes_of(q), x->dtype, TK_QUANTIZE, s));
+    QuantizeArgs a;
+    memset(&a, 0, sizeof(a));
+    a.x = x->data;
+    (transposed ? a.across : a.rows) = codes_of(q);
+    a.n = x->n;
+    a.x_stride = stride_of(x);
+    a.d = x->d;
+    return done(launch_quantize_tiles(a, q->block_rows != 1, false, x->dtype, TK_QUANTIZE, s));
+}
+
+int32_t fnn_rms_norm(const fnn_map* x, const fnn_map* residual, const void* weight, int32_t weight_dtype, float eps,
+                     const fnn_map* sum, const fnn_map* y, const fnn_scaled* codes, float* rstd, void* stream) {
+    FNN_CHECK(check_matrix(x));
+    if (x->d < 1 || x->d > FNN_MAX_NORM_WIDTH) return FNN_E_SHAPE;
+    const fnn_map* others[3] = {residual, sum, y};
+    for (const fnn_map* m : others) {
+        if (!m) continue;
+        FNN_CHECK(check_matrix(m));
+        if (m->n != x->n || m->d != x->d) return FNN_E_SHAPE;
+        if (m->dtype != x->dtype) return FNN_E_DTYPE;
+    }
+    if (codes) {
+        FNN_CHECK(check_scaled(codes));
+        // of one row the two are the same
+        if (codes->n != x->n || codes->d != x->d || (codes->block_rows != 1 && x->n > 1)) return FNN_E_SHAPE;
+    }
+    if (weight_dtype != x->dtype && weight_dtype != FNN_F32) return FNN_E_DTYPE;
+    if (!(eps >= 0.f) || isinf(eps)) return FNN_E_RANGE;
+    if (x->n == 0 || (!sum && !y && !codes && !rstd)) return FNN_OK;
+    RmsArgs a;
+    memset(&a, 0, sizeof(a));
+    a.x = x->data;
+    a.residual = residual ? residual->data : nullptr;
+    a.weight = weight;
+    a.sum = sum ? const_cast<void*>(sum->data) : nullptr;
+    a.y = y ? const_cast<void*>(y->data) : nullptr;
+    if (codes) a.codes = codes_of(codes);
+    a.rstd = rstd;
+    a.n = x->n;
+    a.x_stride = stride_of(x);
+    a.residual_stride = residual ? stride_of(residual) : 0;
+    a.sum_stride = sum ? stride_of(sum) : 0;
+    a.y_stride = y ? stride_of(y) : 0;
+    a.d = x->d;
+    a.eps = eps;
+    return done(launch_rms_norm(a, x->dtype, weight_dtype, (hipStream_t)stream));
+}
+
+size_t fnn_rms_norm_backward_workspace_bytes(int64_t n, int32_t d) {
+    if (n < 0 || n > MAX_SLOTS || d < 1 || d > FNN_MAX_NORM_WIDTH) return 0;
+    return (size_t)rms_norm_backward_groups(n, d) * d * sizeof(float);
+}
+
+int32_t fnn_rms_norm_backward(const fnn_map* dy, const fnn_map* sum, const float* rstd, const void* weight, int32_t weight_dtype, const fnn_map* dsum,
+                              const fnn_map* dx, void* dweight, void* workspace, size_t workspace_bytes, void* stream) {
+    FNN_CHECK(check_matrix(dy));
+    FNN_CHECK(check_matrix(sum));
+    if (sum->d < 1 || sum->d > FNN_MAX_NORM_WIDTH) return FNN_E_SHAPE;
+    const fnn_map* others[3] = {dy, dsum, dx};
+    for (const fnn_map* m : others) {
+        if (!m) continue;
+        FNN_CHECK(check_matrix(m));
+        if (m->n != sum->n || m->d != sum->d) return FNN_E_SHAPE;
+        if (m->dtype != sum->dtype) return FNN_E_DTYPE;
+    }
+    if (weight_dtype != sum->dtype && weight_dtype != FNN_F32) return FNN_E_DTYPE;
+    if (sum->n > 0 && !rstd) return FNN_E_NULL;
+    if (dweight) FNN_CHECK(check_workspace(workspace, workspace_bytes, fnn_rms_norm_backward_workspace_bytes(sum->n, sum->d)));
+    if (!dweight && (!dx || sum->n == 0)) return FNN_OK;
+    RmsBackArgs a;
+    memset(&a, 0, sizeof(a));
+    a.dy = dy->data;
+    a.x = sum->data;
+    a.dsum = dsum ? dsum->data : nullptr;
+    a.rstd = rstd;
+    a.weight = weight;
+    a.dx = dx ? const_cast<void*>(dx->data) : nullptr;
+    a.dweight = dweight;
+    a.partial = dweight ? (float*)workspace : nullptr;
+    a.n = sum->n;
+    a.dy_stride = stride_of(dy);
+    a.x_stride = stride_of(sum);
+    a.dsum_stride = dsum ? stride_of(dsum) : 0;
+    a.dx_stride = dx ? stride_of(dx) : 0;
+    a.d = sum->d;
+    return done(launch_rms_norm_backward(a, sum->dtype, weight_dtype, (hipStream_t)stream));
+}
+
+size_t fnn_linear_e4m3_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
+    if (!linear_sizes(rows, inner, outer) || !valid_type(dtype)) return 0;
+    return scaled_gemm_workspace(rows, outer, inner, dtype);
+}
+
+int32_t fnn_linear_e4m3(const fnn_scaled* x, const fnn_scaled* w, const void* bias, int32_t act, const fnn_map* residual,
+                        const fnn_map* y, const fnn_map* pre, void* workspace, size_t workspace_bytes, void* stream) {
+    FNN_CHECK(check_scaled(x));
+    FNN_CHECK(check_scaled(w));
+    FNN_CHECK(check_matrix(y));
+    const int64_t rows = x->n, inner = x->d, outer = w->n;
+    if (w->d != inner || !same_shape(y, rows, outer)) return FNN_E_SHAPE;
+    const fnn_map* others[2] = {residual, pre};
+    for (const fnn_map* m : others) {
+        if (!m) continue;
+        FNN_CHECK(check_matrix(m));
+        if (!same_shape(m, rows, outer)) return FNN_E_SHAPE;
+        if (m->dtype != y->dtype) return FNN_E_DTYPE;
+    }
+    if (act < FNN_ACT_NONE || act > FNN_ACT_SILU) return FNN_E_RANGE;
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, scaled_gemm_workspace(rows, outer, inner, y->dtype)));
+    ScaledGemmArgs a;
+    memset(&a, 0, sizeof(a));
+    a.g.a = x->data;
+    a.g.b = w->data;
+    a.g.lda = stride_of(x);
+    a.g.ldb = stride_of(w);
+    a.g.m = rows;
+    a.g.n = (int32_t)outer;
+    a.g.k = (int32_t)inner;
+    a.g.y = const_cast<void*>(y->data);
+    a.g.bias = bias;
+    a.g.residual = residual ? residual->data : nullptr;
+    a.g.pre = pre ? const_cast<void*>(pre->data) : nullptr;
+    a.g.ldy = stride_of(y);
+    a.g.ldr = residual ? stride_of(residual) : 0;
+    a.g.ldp = pre ? stride_of(pre) : 0;
+    a.g.act = act;
+    a.g.partial = (float*)workspace;
+    a.scale_a = x->scale;
+    a.scale_b = w->scale;
+    a.sa_row = scale_row_of(x);
+    a.sa_block = scale_block_of(x);
+    a.sb_row = scale_row_of(w);
+    a.sb_block = scale_block_of(w);
+    a.shift_a = x->block_rows == 1 ? 0 : 7;
+    a.shift_b = w->block_rows == 1 ? 0 : 7;
+    return done(launch_scaled_gemm(a, y->dtype, TK_LINEAR_E4M3, (hipStream_t)stream));
+}
+
+size_t fnn_linear_e4m3_backward_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
+    if (!linear_sizes(rows, inner, outer) || !valid_type(dtype)) return 0;
+    return e4m3_back_layout(rows, inner, outer, dtype).total;
+}
+
+int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_scaled* w, const fnn_map* pre, int32_t act,
+                                 const fnn_map* dx, const fnn_map* dw, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+    FNN_CHECK(check_matrix(dy));
+    FNN_CHECK(check_matrix(x));
+    FNN_CHECK(check_scaled(w));
+    if (act < FNN_ACT_NONE || act > FNN_ACT_SILU) return FNN_E_RANGE;
+    const bool slope = act != FNN_ACT_NONE;
+    if (slope) FNN_CHECK(check_matrix(pre));
+    if (dx) FNN_CHECK(check_matrix(dx));
+    if (dw) FNN_CHECK(check_matrix(dw));
+    const int64_t rows = x->n, inner = x->d, outer = w->n;
+    if (w->d != inner || (w->block_rows != SCALED_BLOCK && outer > 1) || !same_shape(dy, rows, outer) || (slope && !same_shape(pre, rows, outer)) ||
+        (dx && !same_shape(dx, rows, inner)) || (dw && !same_shape(dw, outer, inner)))
+        return FNN_E_SHAPE;
+    if (dy->dtype != x->dtype || (slope && pre->dtype != x->dtype) || (dx && dx->dtype != x->dtype) || (dw && dw->dtype != x->dtype)) return FNN_E_DTYPE;
+    if (!dx && !dw && !dbias) return FNN_OK;
+    const E4m3BackLayout L = e4m3_back_layout(rows, inner, outer, x->dtype);
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, L.total));
+    const hipStream_t s = (hipStream_t)stream;
+    char* ws = (char*)workspace;
+
+    // q in one pass: by rows for dx, across for dw, the columns' sums for dbias
+    QuantizeArgs q;
+    memset(&q, 0, sizeof(q));
+    q.x = dy->data;
+    q.pre = slope ? pre->data : nullptr;
+    if (dx) q.rows = {(uint8_t*)ws + L.q, (float*)(ws + L.q_scale), L.outer_stride, 1, rows};
+    if (dw) q.across = {(uint8_t*)ws + L.q_across, (float*)(ws + L.q_across_scale), L.rows_stride, 1, outer};
+    q.partial = dbias ? (float*)(ws + L.sums) : nullptr;
+    q.n = rows;
+    q.x_stride = stride_of(dy);
+    q.pre_stride = slope ? stride_of(pre) : 0;
+    q.d = (int32_t)outer;
+    q.act = act;
+    if (launch_quantize_tiles(q, false, true, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+    if (dbias && outer > 0 &&
+        launch_column_sums(q.partial, scaled_blocks(rows), outer, outer, dbias, nullptr, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess)
+        return FNN_E_HIP;
+    ScaledGemmArgs a;
+    memset(&a, 0, sizeof(a));
+    a.g.partial = (float*)(ws + L.partial);
+    if (dx) {
+        if (launch_transpose_codes(w->data, stride_of(w), outer, (int32_t)inner, ws + L.w, L.outer_stride, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+        a.g.a = ws + L.q;
+        a.g.b = ws + L.w;
+        a.g.lda = a.g.ldb = L.outer_stride;
+        a.g.m = rows;
+        a.g.n = (int32_t)inner;
+        a.g.k = (int32_t)outer;
+        a.g.y = const_cast<void*>(dx->data);
+        a.g.ldy = stride_of(dx);
+        a.scale_a = (float*)(ws + L.q_scale);
+        a.sa_row = 1;
+        a.sa_block = rows;
+        a.scale_b = w->scale;          // of the transpose: rows and blocks change places
+        a.sb_row = scale_block_of(w);
+        a.sb_block = scale_row_of(w);
+        a.shift_b = 7;
+        if (launch_scaled_gemm(a, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+    }
+    if (dw) {
+        QuantizeArgs of_x;
+        memset(&of_x, 0, sizeof(of_x));
+        of_x.x = x->data;
+        of_x.across = {(uint8_t*)ws + L.x, (float*)(ws + L.x_scale), L.rows_stride, 1, inner};
+        of_x.n = rows;
+        of_x.x_stride = stride_of(x);
+        of_x.d = (int32_t)inner;
+        if (launch_quantize_tiles(of_x, false, false, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+        a.g.a = ws + L.q_across;
+        a.g.b = ws + L.x;
+        a.g.lda = a.g.ldb = L.rows_stride;
+        a.g.m = outer;
+        a.g.n = (int32_t)inner;
+        a.g.k = (int32_t)rows;
+        a.g.y = const_cast<void*>(dw->data);
+        a.g.ldy = stride_of(dw);
+        a.scale_a = (float*)(ws + L.q_across_scale);
+        a.sa_row = 1;
+        a.sa_block = outer;
+        a.scale_b = (float*)(ws + L.x_scale);
+        a.sb_row = 1;
+        a.sb_block = inner;
+        a.shift_b = 0;
+        if (launch_scaled_gemm(a, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+    }
+    return FNN_OK;
 }
 
 }  // extern "C"

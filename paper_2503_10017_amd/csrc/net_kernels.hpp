@@ -113,4 +113,68 @@ struct AttentionBackArgs {
 };
 hipError_t launch_attention_backward(AttentionBackArgs a, int dtype, hipStream_t s);
 
+// ---- matrices in 8 bits with a scale for each block ----
+constexpr int SCALED_BLOCK = 128;
+__host__ __device__ constexpr int64_t scaled_blocks(int64_t n) { return (n + SCALED_BLOCK - 1) / SCALED_BLOCK; }
+
+// One that a kernel writes: the places of its codes and scales, and their strides.  Without data it is not wanted.
+struct CodesOut {
+    uint8_t* data;
+    float* scale;
+    int64_t row, scale_row, scale_block;
+};
+hipError_t launch_quantize_rows(const void* x, int64_t x_stride, int64_t n, int32_t d, const CodesOut& out, int dtype, int trace_kind, hipStream_t s);
+
+// Tiles of 128 x 128 of x, or with `slope` of x * act'(pre): by rows, across (transposed), one scale per block of a row or per tile.
+struct QuantizeArgs {
+    const void* x;
+    const void* pre;
+    CodesOut rows, across;
+    float* partial;   // [tiles of rows][d]: the columns' sums with `slope`; NULL: not wanted
+    int64_t n, x_stride, pre_stride;
+    int32_t d, act;
+};
+hipError_t launch_quantize_tiles(const QuantizeArgs& a, bool tiles, bool slope, int dtype, int trace_kind, hipStream_t s);
+hipError_t launch_transpose_codes(const void* from, int64_t from_stride, int64_t n, int32_t d, void* to, int64_t to_stride, int trace_kind, hipStream_t s);
+
+// Root-mean-square norm of x + residual, and its gradient.
+struct RmsArgs {
+    const void* x;
+    const void* residual;  // NULL: 0
+    const void* weight;    // NULL: 1
+    void* sum;             // outputs, each of which may be NULL
+    void* y;
+    CodesOut codes;
+    float* rstd;
+    int64_t n, x_stride, residual_stride, sum_stride, y_stride;
+    int32_t d;
+    float eps;
+};
+hipError_t launch_rms_norm(const RmsArgs& a, int dtype, int weight_dtype, hipStream_t s);
+struct RmsBackArgs {
+    const void* dy;
+    const void* x;
+    const void* dsum;      // NULL: 0
+    const float* rstd;
+    const void* weight;
+    void* dx;
+    void* dweight;
+    float* partial;        // [workgroups][d]: a workgroup's share of dweight
+    int64_t n, dy_stride, x_stride, dsum_stride, dx_stride;
+    int32_t d;
+};
+int64_t rms_norm_backward_groups(int64_t n, int32_t d);
+hipError_t launch_rms_norm_backward(const RmsBackArgs& a, int dtype, int weight_dtype, hipStream_t s);
+
+// The product behind the layers in 8 bits: C[m][n] = sum over blocks of k of scale_a(m, block) scale_b(n, block) sum over the block of A(m, k) B(n, k).
+struct ScaledGemmArgs {
+    GemmArgs g;                                     // codes, sizes and epilogue
+    const float* scale_a;
+    const float* scale_b;
+    int64_t sa_row, sa_block, sb_row, sb_block;     // strides of the scales
+    int32_t shift_a, shift_b;                       // log2 of the rows that share a scale: 0 or 7
+};
+size_t scaled_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype);
+hipError_t launch_scaled_gemm(ScaledGemmArgs a, int dtype, int trace_kind, hipStream_t s);
+
 }  // namespace fnn

@@ -110,6 +110,11 @@ const char* fnn_trace_kind_name(int32_t kind) {
         case TK_LINEAR_BACKWARD: return "linear_backward_kernels";
         case TK_ATTENTION: return "attention_kernels";
         case TK_ATTENTION_BACKWARD: return "attention_backward_kernels";
+        case TK_RMS_NORM: return "rms_norm_kernel";
+        case TK_RMS_NORM_BACKWARD: return "rms_norm_backward_kernels";
+        case TK_QUANTIZE: return "quantize_kernels";
+        case TK_LINEAR_E4M3: return "linear_e4m3_kernels";
+        case TK_LINEAR_E4M3_BACKWARD: return "linear_e4m3_backward_kernels";
         default: return "unknown";
     }
 }

@@ -36,7 +36,12 @@ enum TraceKind : int {
     TK_LINEAR_BACKWARD = 25,
     TK_ATTENTION = 26,
     TK_ATTENTION_BACKWARD = 27,
-    TK_COUNT = 28
+    TK_RMS_NORM = 28,
+    TK_RMS_NORM_BACKWARD = 29,
+    TK_QUANTIZE = 30,
+    TK_LINEAR_E4M3 = 31,
+    TK_LINEAR_E4M3_BACKWARD = 32,
+    TK_COUNT = 33
 };
 
 // Returns false when no trace is open or it is full; otherwise hands out the next event pair.

@@ -1,0 +1,107 @@
+"""fnn_quantize against its definition: codes and scales to the bit."""
+import math
+
+import pytest
+import torch
+
+import paper_2503_10017_amd as fnn
+from e4m3_helpers import blocks, quantized, same
+from net_helpers import DEV, TYPES, normal, strided
+
+pytestmark = pytest.mark.gpu
+
+MODES = [(tiles, transposed) for tiles in (False, True) for transposed in (False, True)]
+
+
+def check(x, tiles, transposed, **kw):
+    got = fnn.fnn_quantize(x, tiles=tiles, transposed=transposed, **kw)
+    want, scale = quantized(x.t() if transposed else x, tiles)
+    assert got.data.shape == want.shape and got.scale.shape == scale.shape
+    assert torch.equal(got.scale, scale)
+    assert same(got.data.double(), want), (got.data.double() - want).abs().max()
+    return got
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,d", [(1, 1), (1, 1024), (3, 130), (127, 64), (128, 128), (129, 127), (16, 777), (300, 1001), (1000, 24), (17, 4096), (515, 2048)])
+@pytest.mark.parametrize("tiles,transposed", MODES)
+def test_codes_and_scales(n, d, kind, tiles, transposed):
+    dtype = TYPES[kind]
+    spread = torch.exp(normal(2, d, std=1.5))                   # columns of different size
+    check((normal(1, n, d) * spread).to(dtype), tiles, transposed)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+def test_every_value_of_few_digits(kind):
+    """Whole numbers and halves beside a largest of every size from 1 to 256: many quotients lie on the border of two codes or next to it."""
+    x = torch.arange(-256, 256, dtype=torch.float64, device=DEV).view(4, 128).repeat(64, 1) / 2
+    for i in range(256):
+        x[i, 0] = 129 + i / 2
+    for tiles, transposed in MODES:
+        check(x.to(TYPES[kind]), tiles, transposed)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("tiles,transposed", MODES)
+def test_large_small_and_missing(kind, tiles, transposed):
+    dtype = TYPES[kind]
+    x = normal(1, 300, 400, dtype=dtype)
+    x[0] = 0
+    x[1] *= 1e-38
+    x[2] *= 1e-44
+    x[3] = torch.finfo(dtype).max
+    x[4, 7], x[5, 130], x[6, 399] = math.inf, -math.inf, math.nan
+    x[7] = math.nan
+    x[8, ::2] = math.inf
+    x[9, 128:256] = -0.0
+    x[:, 300] = 0
+    got = check(x, tiles, transposed)
+    assert torch.isfinite(got.scale).all() and (got.scale >= 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+@pytest.mark.parametrize("n,d", [(5, 130), (130, 260), (200, 77)])
+@pytest.mark.parametrize("tiles,transposed", MODES)
+def test_strides_and_what_lies_between(n, d, kind, tiles, transposed):
+    x = normal(1, n, d, dtype=TYPES[kind])
+    want = fnn.fnn_quantize(x, tiles=tiles, transposed=transposed)
+    rows, columns = want.data.shape
+    for extra, offset, gap in ((16, 0, 0), (1, 1, 3), (5, 3, 1)):
+        room = torch.full((offset + rows * (columns + extra) + 16,), 0x55, dtype=torch.uint8, device=DEV)
+        data = room.view(torch.float8_e4m3fn)[offset:offset + rows * (columns + extra)].view(rows, columns + extra)[:, :columns]
+        scales = torch.full((want.scale.shape[0], want.scale.shape[1] + gap), -1.0, device=DEV)
+        out = fnn.FnnScaled(data, scales[:, :want.scale.shape[1]])
+        fnn.fnn_quantize(strided(x, extra, offset), tiles=tiles, transposed=transposed, out=out)
+        assert torch.equal(out.data.float(), want.data.float()) and torch.equal(out.scale, want.scale)
+        kept = torch.ones_like(room, dtype=torch.bool)
+        kept[offset:offset + rows * (columns + extra)].view(rows, columns + extra)[:, :columns] = False
+        assert (room[kept] == 0x55).all() and (scales[:, want.scale.shape[1]:] == -1).all()
+
+
+def test_empty_and_refused():
+    for shape in ((0, 5), (5, 0), (0, 0)):
+        got = fnn.fnn_quantize(torch.zeros(shape, device=DEV))
+        assert got.data.shape == shape and got.scale.shape == (shape[0], blocks(shape[1]))
+        got = fnn.fnn_quantize(torch.zeros(shape, device=DEV), tiles=True, transposed=True)
+        assert got.data.shape == shape[::-1]
+    x = normal(1, 10, 300)
+    good = fnn.fnn_quantize(x)
+    for bad in (fnn.FnnScaled(good.data, good.scale[:9]), fnn.FnnScaled(good.data, good.scale[:, :2]), fnn.FnnScaled(good.data.view(torch.uint8), good.scale),
+                fnn.FnnScaled(good.data, good.scale.double()), fnn.FnnScaled(good.data.t(), good.scale), fnn.FnnScaled(good.data, good.scale.cpu())):
+        with pytest.raises(ValueError):
+            fnn.fnn_quantize(x, out=bad)
+    with pytest.raises(fnn.FnnError):
+        fnn.fnn_quantize(x, transposed=True, out=good)
+    with pytest.raises(ValueError):
+        fnn.fnn_quantize(x.to(torch.float64))
+
+
+def test_offsets_past_32_bits():
+    """A view whose rows lie 2^31 bytes and more apart from the first."""
+    rows, d, stride = 70, 130, 33 << 20
+    buf = torch.empty(rows * stride, dtype=torch.bfloat16, device=DEV)
+    x = buf.view(rows, stride)[:, :d]
+    x.copy_(normal(1, rows, d, dtype=torch.bfloat16))
+    for tiles, transposed in MODES:
+        got, want = (fnn.fnn_quantize(t, tiles=tiles, transposed=transposed) for t in (x, x.contiguous()))
+        assert torch.equal(got.data.float(), want.data.float()) and torch.equal(got.scale, want.scale)
