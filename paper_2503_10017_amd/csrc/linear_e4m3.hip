@@ -131,6 +131,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_e4m3_kernel(ScaledGem
 
 // ---- tiles ----
 
+// A mask of the first `count` bytes of a word.
+__device__ __forceinline__ uint32_t first_bytes(int count) { return count >= 4 ? 0xFFFFFFFFu : count <= 0 ? 0u : (1u << (8 * count)) - 1u; }
 
 // A workgroup's tile of TM x TN results, a wave's (TM / WAVES_M) x (TN / WAVES_N) of it in registers.  As in gemm_kernel the step's codes are staged by direct loads to LDS
 // through a buffer that ends with the operand, two stages in turn, and so are its scales.  SHARED: a wave's columns have one scale a step (weights in tiles).
@@ -162,18 +164,23 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     Eight<DT> bias = {};
     if (a.bias && a.splits == 1) bias.load(a.bias, n, a.n - n);
 
-    // this thread's scales of a step
+    // This wave's scales of a step: 64 rows of one operand, or several times as many, one a lane.
     const float* scale[SCALES];
-    int64_t scale_on[SCALES];
+    uint32_t scale_offset[SCALES];
+    int64_t scale_on[SCALES], scale_rows[SCALES];
+    float held_scale[SCALES];
 #pragma unroll
     for (int i = 0; i < SCALES; ++i) {
-        const int at = i * THREADS + threadIdx.x;
+        const int at = i * THREADS + wave * 64;  // the first of the stage's scales that this wave brings
         const bool of_a = at < TM;
-        const int64_t row = of_a ? min(m0 + at, a.m - 1) : min((int64_t)n0 + at - TM, (int64_t)a.n - 1);
+        const int shift = of_a ? s.shift_a : s.shift_b;
+        const int64_t first = of_a ? m0 + at : n0 + at - TM, last = (of_a ? a.m : (int64_t)a.n) - 1, row = min(first + lane, last);
+        const int64_t base = min(first, last) >> shift, stride = of_a ? s.sa_row : s.sb_row;
         scale_on[i] = of_a ? s.sa_block : s.sb_block;
-        scale[i] = (of_a ? s.scale_a + (row >> s.shift_a) * s.sa_row : s.scale_b + (row >> s.shift_b) * s.sb_row) + s0 * scale_on[i];
+        scale[i] = (of_a ? s.scale_a : s.scale_b) + base * stride + s0 * scale_on[i];
+        scale_offset[i] = (uint32_t)(((row >> shift) - base) * stride * 4);
+        scale_rows[i] = (((min(first + 63, last) >> shift) - base) * stride + 1) * 4;
     }
-    float held_scale[SCALES];
 
     f32x4 acc[BM][BN];
 #pragma unroll
@@ -186,15 +193,17 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
         if constexpr (DIRECT) {
             opa.stage(to.a, a.k - done);
             opb.stage(to.b, a.k - done);
+#pragma unroll
+            for (int i = 0; i < SCALES; ++i)
+                load_word_to_lds(buffer_of(scale[i], (uint32_t)scale_rows[i]), scale_offset[i], lds_address((const char*)&to.scale[i * THREADS]) + wave * 256);
         } else {
             opa.fetch(held_a, a.k - done);
             opb.fetch(held_b, a.k - done);
+#pragma unroll
+            for (int i = 0; i < SCALES; ++i) held_scale[i] = *reinterpret_cast<const float*>((const char*)scale[i] + scale_offset[i]);
         }
 #pragma unroll
-        for (int i = 0; i < SCALES; ++i) {
-            held_scale[i] = *scale[i];
-            scale[i] += scale_on[i];
-        }
+        for (int i = 0; i < SCALES; ++i) scale[i] += scale_on[i];
         opa.advance();
         opb.advance();
         done += SCALED_BLOCK;
@@ -203,41 +212,53 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
         if constexpr (!DIRECT) {
             opa.put(to.a, held_a);
             opb.put(to.b, held_b);
-        }
 #pragma unroll
-        for (int i = 0; i < SCALES; ++i) to.scale[i * THREADS + threadIdx.x] = held_scale[i];
+            for (int i = 0; i < SCALES; ++i) to.scale[i * THREADS + threadIdx.x] = held_scale[i];
+        }
     };
+    const int a0 = wm * (TM / WAVES_M), b0 = wn * (TN / WAVES_N);
     auto read = [&](const char* from, int row) {
         Codes c;
 #pragma unroll
         for (int h = 0; h < 2; ++h) c.run[h] = *reinterpret_cast<const uint4*>(from + (row + r) * SCALED_BLOCK + (((4 * h + q) ^ Op::exchanged(r)) << 4));
         return c;
     };
+    // 16 rows of a after the other against all of the wave's columns.  The products of 16 rows are scaled and added while the next ones are formed.
     auto multiply = [&](const Stage& from) {
-        Codes fb[BN];
-        float sb[SHARED ? 1 : BN][4];
-        const int a0 = wm * (TM / WAVES_M), b0 = wn * (TN / WAVES_N);
+        Codes fb[BN], fa[2];
+        f32x4 t[2][BN];
+        float sa[BM], sb[SHARED ? 1 : BN][4];
 #pragma unroll
         for (int j = 0; j < BN; ++j) fb[j] = read(from.b, b0 + 16 * j);
+        fa[0] = read(from.a, a0);
         if constexpr (SHARED) {
             sb[0][0] = from.scale[TM + b0];
         } else {
 #pragma unroll
-            for (int j = 0; j < BN; ++j)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) sb[j][v] = from.scale[TM + b0 + 16 * j + 4 * q + v];
-        }
-#pragma unroll
-        for (int i = 0; i < BM; ++i) {
-            const Codes fa = read(from.a, a0 + 16 * i);
-            const float sa = from.scale[a0 + 16 * i + r];
-#pragma unroll
             for (int j = 0; j < BN; ++j) {
-                const f32x4 t = block_product<WIDE>(fb[j], fa);
+                const f32x4 four = *reinterpret_cast<const f32x4*>(&from.scale[TM + b0 + 16 * j + 4 * q]);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(t[v], sa * (SHARED ? sb[0][0] : sb[j][v]), acc[i][j][v]);
+                for (int v = 0; v < 4; ++v) sb[j][v] = four[v];
             }
         }
+#pragma unroll
+        for (int i = 0; i < BM; ++i) sa[i] = from.scale[a0 + 16 * i + r];
+        auto add = [&](int i) {
+            const float both = SHARED ? sa[i] * sb[0][0] : 0.f;
+#pragma unroll
+            for (int j = 0; j < BN; ++j)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(t[i & 1][j][v], SHARED ? both : sa[i] * sb[j][v], acc[i][j][v]);
+        };
+#pragma unroll
+        for (int i = 0; i < BM; ++i) {
+            if (i + 1 < BM) fa[(i + 1) & 1] = read(from.a, a0 + 16 * (i + 1));
+#pragma unroll
+            for (int j = 0; j < BN; ++j) t[i & 1][j] = block_product<WIDE>(fb[j], fa[i & 1]);
+            if (i > 0) add(i - 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        add(BM - 1);
     };
     // What lies behind k in the last run of a row is not zero: it is cleared before anything is read.
     const int tail = a.k % 16;
@@ -246,12 +267,13 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
 #pragma unroll
         for (int i = 0; i < SCALES; ++i) {
             const int row = i * THREADS + threadIdx.x;
-            char* place = (row < TM ? of.a + row * SCALED_BLOCK : of.b + (row - TM) * SCALED_BLOCK) + ((at ^ Op::exchanged(row & 15)) << 4);
-            uint8_t raw[16];
-            __builtin_memcpy(raw, place, 16);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) raw[e] = e < tail ? raw[e] : 0;
-            __builtin_memcpy(place, raw, 16);
+            uint4* place = reinterpret_cast<uint4*>((row < TM ? of.a + row * SCALED_BLOCK : of.b + (row - TM) * SCALED_BLOCK) + ((at ^ Op::exchanged(row & 15)) << 4));
+            uint4 codes = *place;
+            codes.x &= first_bytes(tail);
+            codes.y &= first_bytes(tail - 4);
+            codes.z &= first_bytes(tail - 8);
+            codes.w &= first_bytes(tail - 12);
+            *place = codes;
         }
     };
     // One step ahead: stage s mod 2.
@@ -262,10 +284,14 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     for (int step = s0; step < s1; ++step) {
         Stage& here = stages[(step - s0) & 1];
         Stage& next = stages[(step - s0 + 1) & 1];
-        lds_loads_arrived();
-        __syncthreads();
-        if (DIRECT && tail && step == steps - 1) {
-            clear_tail(here);
+        if constexpr (DIRECT) {
+            lds_loads_arrived();
+            meet();
+            if (tail && step == steps - 1) {
+                clear_tail(here);
+                __syncthreads();
+            }
+        } else {
             __syncthreads();
         }
         const bool more = step + 1 < s1;
@@ -340,13 +366,15 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int dtype) {
     return {128, (int)most(small, 256, 4, 32)};
 }
 
-bool direct(const void* data, int64_t stride, int64_t rows) {
-    return ((uintptr_t)data & 15) == 0 && (rows < 2 || stride % 16 == 0) && stride < ((int64_t)1 << 31) / 256;
+// Whether an operand's rows start on 16-byte boundaries, and the offsets of a tile's codes and of 64 rows' scales fit 32 bits.
+bool direct(const void* data, int64_t stride, int64_t rows, int64_t scale_row) {
+    return ((uintptr_t)data & 15) == 0 && (rows < 2 || stride % 16 == 0) && stride < ((int64_t)1 << 31) / 256 && scale_row < ((int64_t)1 << 31) / 256;
 }
 
 template <int DT, bool SHARED>
-hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, const Plan& p, int kind, hipStream_t s) {
+hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStream_t s) {
     GemmArgs& g = a.g;
+    if (!is_direct) p.tile = 128;  // a large tile has no registers for what it fetches; the shares need no more room
     g.tiles_m = (int)(round_to(g.m, p.tile) / p.tile);
     g.tiles_n = (int)(round_to(g.n, p.tile) / p.tile);
     g.splits = p.splits;
@@ -355,8 +383,7 @@ hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, const Plan& p, int kind, 
     hipError_t e;
     if (DT != CT_F32 && p.tile == 256) {
         if constexpr (DT != CT_F32)
-            e = is_direct ? launch(kind, gemm_e4m3_kernel<DT, 256, 256, 2, 4, SHARED, true>, grid, dim3(512), 0, s, a)
-                          : launch(kind, gemm_e4m3_kernel<DT, 256, 256, 2, 4, SHARED, false>, grid, dim3(512), 0, s, a);
+            e = launch(kind, gemm_e4m3_kernel<DT, 256, 256, 2, 4, SHARED, true>, grid, dim3(512), 0, s, a);
     } else {
         e = is_direct ? launch(kind, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, true>, grid, dim3(256), 0, s, a)
                       : launch(kind, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, false>, grid, dim3(256), 0, s, a);
@@ -396,7 +423,7 @@ hipError_t launch_scaled_gemm(ScaledGemmArgs a, int dtype, int kind, hipStream_t
         constexpr int DT = dt.value;
         if (few_rows(g.m, g.k)) return run_few_rows<DT>(a, kind, s);
         const Plan p = plan_of(g.m, g.n, g.k, dtype);
-        const bool d = direct(g.a, g.lda, g.m) && direct(g.b, g.ldb, g.n);
+        const bool d = direct(g.a, g.lda, g.m, a.sa_row) && direct(g.b, g.ldb, g.n, a.sb_row);
         return a.shift_b ? run_tiles<DT, true>(a, d, p, kind, s) : run_tiles<DT, false>(a, d, p, kind, s);
     });
 }
