@@ -13,8 +13,8 @@ enum : int { ROWS = 0, COLUMNS = 1 };
 struct TileAt {
     int m, n, split;
 };
-__device__ __forceinline__ TileAt tile_at(const GemmArgs& a) {
-    const int per = a.tiles_m * a.tiles_n, total = per * a.splits, id = blockIdx.x;
+__device__ __forceinline__ TileAt tile_at(const GemmArgs& a, int id) {
+    const int per = a.tiles_m * a.tiles_n, total = per * a.splits;
     const int xcd = id & 7, q = total >> 3, r = total & 7;
     const int mine = xcd * q + min(xcd, r) + (id >> 3);
     TileAt t;
@@ -52,10 +52,14 @@ struct Operand {
         const int row = threadIdx.x / ROW_RUNS, run = (threadIdx.x % ROW_RUNS) ^ exchanged(row);
         static_assert(ROWS_APART % (LAYOUT == ROWS ? 16 : ES == 2 ? 4 : 8) == 0, "the exchange is the same for all of a thread's runs");
         col = run * N;
-        have = (int)min((int64_t)T, total - first);
-        base = (const E*)data + (LAYOUT == ROWS ? first * stride + k0 : k0 * stride + first);
         offset = (uint32_t)((row * stride + col) * ES);
         apart = (uint32_t)(ROWS_APART * stride * ES);
+        move(data, first, total, k0);
+    }
+    // To another tile of the same operand: what a thread holds stays.
+    __device__ __forceinline__ void move(const void* data, int64_t first, int64_t total, int64_t k0) {
+        have = (int)min((int64_t)T, total - first);
+        base = (const E*)data + (LAYOUT == ROWS ? first * stride + k0 : k0 * stride + first);
     }
 
     // Direct loads to LDS through a buffer that ends with the operand, so that what lies behind it arrives as zero: rows past the last, and
@@ -172,7 +176,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     using OpA = Operand<DT, TM, SB, THREADS, LA>;
     using OpB = Operand<DT, TN, SB, THREADS, LB>;
     __shared__ __attribute__((aligned(16))) char stages[STAGES][OpA::BYTES + OpB::BYTES];
-    const TileAt tile = tile_at(a);
+    const TileAt tile = tile_at(a, blockIdx.x);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WAVES_M, wn = wave / WAVES_M;
     const int steps = (a.k + OpA::STEP - 1) / OpA::STEP;

@@ -131,220 +131,334 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_e4m3_kernel(ScaledGem
 
 // ---- tiles ----
 
+// finish_run of fewer than eight results, one after the other: there is one such place in a row at most, and in line they would be most of the kernel's code.
+template <int DT>
+__device__ __forceinline__ void finish_few(const GemmArgs& a, int64_t m, int n, int count, float (&v)[8]) {
+    typedef typename Elem<DT>::T E;
+#pragma unroll 1
+    for (int e = 0; e < count; ++e) {
+        float x[1] = {v[0]};
+#pragma unroll
+        for (int i = 0; i < 7; ++i) v[i] = v[i + 1];
+        if (a.bias) x[0] += (float)((const E*)a.bias)[n + e];
+        if (a.pre) ((E*)a.pre)[m * a.ldp + n + e] = (E)x[0];
+        activate<DT != CT_F32>(x, a.act);
+        if (a.residual) x[0] += (float)((const E*)a.residual)[m * a.ldr + n + e];
+        ((E*)a.y)[m * a.ldy + n + e] = (E)x[0];
+    }
+}
+
 // A mask of the first `count` bytes of a word.
 __device__ __forceinline__ uint32_t first_bytes(int count) { return count >= 4 ? 0xFFFFFFFFu : count <= 0 ? 0u : (1u << (8 * count)) - 1u; }
 
-// A workgroup's tile of TM x TN results, a wave's (TM / WAVES_M) x (TN / WAVES_N) of it in registers.  As in gemm_kernel the step's codes are staged by direct loads to LDS
-// through a buffer that ends with the operand, two stages in turn, and so are its scales.  SHARED: a wave's columns have one scale a step (weights in tiles).
+// f(0), f(1), .. f(N - 1), the numbers as types.
+template <int N, typename F>
+__device__ __forceinline__ void ask_pieces(F f) {
+    if constexpr (N > 0) {
+        ask_pieces<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
+
+// A workgroup has one tile of TM x TN results after the other, a wave (TM / WAVES_M) x (TN / WAVES_N) of it in registers.  A step's codes and scales are staged by direct loads to LDS
+// through buffers that end with the operand, two stages in turn.  The steps of all its tiles are one sequence: before a wave's last products of a step the next step has arrived and the
+// waves meet, then it reads that step's first operands beside these products and asks for the step after, of the next tile where this one ends; so neither the meeting nor a tile's end stops
+// the products for long.  SHARED: a wave's columns have one scale a step (weights in tiles).
 template <int DT, int TM, int TN, int WAVES_M, int WAVES_N, bool SHARED, bool DIRECT>
 __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 64)) void gemm_e4m3_kernel(ScaledGemmArgs s) {
     constexpr int THREADS = WAVES_M * WAVES_N * 64, BM = TM / WAVES_M / 16, BN = TN / WAVES_N / 16, SCALES = (TM + TN) / THREADS;
     constexpr bool WIDE = DT == CT_F32;
-    static_assert((TM + TN) % THREADS == 0 && TM % THREADS % 64 == 0, "a wave's scales are of one operand");
     using Op = Operand<CT_E4M3, TM, SCALED_BLOCK, THREADS, ROWS>;
-    static_assert(TM == TN, "both operands' tiles are alike");
+    static_assert(TM == TN && (TM + TN) % THREADS == 0 && TM % 128 == 0, "both operands' tiles are alike, and 64 scales are of one of them");
+    static_assert(BM % 2 == 0 && 2 * Op::PER_THREAD <= BN * (BM - 1), "everything is asked for before the last rows' products");
     struct Stage {
         char a[Op::BYTES], b[Op::BYTES];
         float scale[TM + TN];
     };
-    __shared__ __attribute__((aligned(16))) Stage stages[2];
+    __shared__ __attribute__((aligned(128))) Stage stages[2];
     const GemmArgs& a = s.g;
-    const TileAt tile = tile_at(a);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WAVES_M, wn = wave / WAVES_M, r = lane & 15, q = lane >> 4;
-    const int steps = (int)scaled_blocks(a.k);
-    const int s0 = (int)((int64_t)steps * tile.split / a.splits), s1 = (int)((int64_t)steps * (tile.split + 1) / a.splits);
-    const int64_t m0 = (int64_t)tile.m * TM;
-    const int n0 = tile.n * TN;
-    Op opa, opb;
-    opa.begin(a.a, a.lda, m0, a.m, (int64_t)s0 * SCALED_BLOCK);
-    opb.begin(a.b, a.ldb, n0, a.n, (int64_t)s0 * SCALED_BLOCK);
-    int done = s0 * SCALED_BLOCK;
-    const int n = n0 + wn * (TN / WAVES_N) + 8 * (lane & 7);  // the first of the eight columns that this lane finishes
-    Eight<DT> bias = {};
-    if (a.bias && a.splits == 1) bias.load(a.bias, n, a.n - n);
+    const uint32_t lds = lds_address((const char*)&stages[0]);
+    const int a0 = wm * (TM / WAVES_M), b0 = wn * (TN / WAVES_N);  // the wave's first row and column
+    const int steps = max((int)scaled_blocks(a.k), 1), total = a.tiles_m * a.tiles_n * a.splits;  // without k one step of zeros
+    auto first_step = [&](int split) { return (int)((uint32_t)(steps * split) / (uint32_t)a.splits); };  // at most 2^24 steps and 32 shares
 
-    // This wave's scales of a step: 64 rows of one operand, or several times as many, one a lane.
-    const float* scale[SCALES];
+    // What is asked for next: a step's codes and scales, through buffers that move along k and end with the operand.  (Every instruction of the loop counts: a wave has one in four
+    // cycles, and 32 products a step.)  A wave brings 64 scales of one operand, or several times as many, one a lane; of a tile of rows they are one.
+    Op opa, opb;  // where a thread's runs are; with their bases, what goes through registers
+    i32x4 buffer_a = buffer_of(a.a, 0), buffer_b = buffer_of(a.b, 0), buffer_scale[SCALES];
     uint32_t scale_offset[SCALES];
-    int64_t scale_on[SCALES], scale_rows[SCALES];
-    float held_scale[SCALES];
+    int ask_id = blockIdx.x, ask_steps = 0, left = 0;  // the tile, how many of its steps, and of k (0: nothing is left)
+    opa.begin(a.a, a.lda, 0, a.m, 0);
+    opb.begin(a.b, a.ldb, 0, a.n, 0);
 #pragma unroll
     for (int i = 0; i < SCALES; ++i) {
-        const int at = i * THREADS + wave * 64;  // the first of the stage's scales that this wave brings
-        const bool of_a = at < TM;
-        const int shift = of_a ? s.shift_a : s.shift_b;
-        const int64_t first = of_a ? m0 + at : n0 + at - TM, last = (of_a ? a.m : (int64_t)a.n) - 1, row = min(first + lane, last);
-        const int64_t base = min(first, last) >> shift, stride = of_a ? s.sa_row : s.sb_row;
-        scale_on[i] = of_a ? s.sa_block : s.sb_block;
-        scale[i] = (of_a ? s.scale_a : s.scale_b) + base * stride + s0 * scale_on[i];
-        scale_offset[i] = (uint32_t)(((row >> shift) - base) * stride * 4);
-        scale_rows[i] = (((min(first + 63, last) >> shift) - base) * stride + 1) * 4;
+        const bool of_a = i * THREADS + wave * 64 < TM;
+        scale_offset[i] = (of_a ? s.shift_a : s.shift_b) ? 0u : (uint32_t)(lane * (of_a ? s.sa_row : s.sb_row) * 4);
+        buffer_scale[i] = buffer_of(s.scale_a, 0);
     }
-
-    f32x4 acc[BM][BN];
+    uint32_t offset_a[Op::PER_THREAD], offset_b[Op::PER_THREAD];
 #pragma unroll
-    for (int i = 0; i < BM; ++i)
+    for (int i = 0; i < Op::PER_THREAD; ++i) {
+        offset_a[i] = opa.offset + i * opa.apart;
+        offset_b[i] = opb.offset + i * opb.apart;
+    }
+    auto begin = [&] {
+        const TileAt t = tile_at(a, ask_id);
+        const int s0 = first_step(t.split);
+        const int64_t k0 = (int64_t)s0 * SCALED_BLOCK;
+        ask_steps = first_step(t.split + 1) - s0;
+        left = (int)(a.k - k0);
+        opa.move(a.a, (int64_t)t.m * TM, a.m, k0);
+        opb.move(a.b, (int64_t)t.n * TN, a.n, k0);
+        const bool some = left > 0;  // without k nothing is
+        buffer_a = buffer_of(opa.base, some ? (uint32_t)((opa.have - 1) * (int)a.lda + left + 3) & ~3u : 0u);
+        buffer_b = buffer_of(opb.base, some ? (uint32_t)((opb.have - 1) * (int)a.ldb + left + 3) & ~3u : 0u);
 #pragma unroll
-        for (int j = 0; j < BN; ++j) acc[i][j] = (f32x4)(0.f);
-
-    uint4 held_a[DIRECT ? 1 : Op::PER_THREAD], held_b[DIRECT ? 1 : Op::PER_THREAD];
-    auto get = [&](Stage& to) {
-        if constexpr (DIRECT) {
-            opa.stage(to.a, a.k - done);
-            opb.stage(to.b, a.k - done);
-#pragma unroll
-            for (int i = 0; i < SCALES; ++i)
-                load_word_to_lds(buffer_of(scale[i], (uint32_t)scale_rows[i]), scale_offset[i], lds_address((const char*)&to.scale[i * THREADS]) + wave * 256);
-        } else {
-            opa.fetch(held_a, a.k - done);
-            opb.fetch(held_b, a.k - done);
-#pragma unroll
-            for (int i = 0; i < SCALES; ++i) held_scale[i] = *reinterpret_cast<const float*>((const char*)scale[i] + scale_offset[i]);
+        for (int i = 0; i < SCALES; ++i) {
+            const int at = i * THREADS + wave * 64;  // the first of the stage's scales that this wave brings
+            const bool of_a = at < TM;
+            const int shift = of_a ? s.shift_a : s.shift_b;
+            const int64_t first = of_a ? (int64_t)t.m * TM + at : (int64_t)t.n * TN + at - TM, have = (of_a ? a.m : (int64_t)a.n) - first;
+            const int64_t row = of_a ? s.sa_row : s.sb_row, block = of_a ? s.sa_block : s.sb_block;
+            buffer_scale[i] = buffer_of((of_a ? s.scale_a : s.scale_b) + (have > 0 ? (first >> shift) * row : 0) + s0 * block,
+                                        some && have > 0 ? (uint32_t)(shift ? 4 : (min(have, (int64_t)64) - 1) * row * 4 + 4) : 0u);
         }
-#pragma unroll
-        for (int i = 0; i < SCALES; ++i) scale[i] += scale_on[i];
-        opa.advance();
-        opb.advance();
-        done += SCALED_BLOCK;
     };
-    auto put = [&](Stage& to) {
+    auto moved = [](i32x4& buffer, int64_t by) {
+        const uint64_t at = (((uint64_t)(uint32_t)buffer[1] << 32) | (uint32_t)buffer[0]) + by;
+        buffer[0] = (int)(uint32_t)at;
+        buffer[1] = (int)(uint32_t)(at >> 32);
+    };
+    auto ask_on = [&] {
+        if (--ask_steps > 0) {
+            moved(buffer_a, SCALED_BLOCK);
+            moved(buffer_b, SCALED_BLOCK);
+            buffer_a[2] -= SCALED_BLOCK;
+            buffer_b[2] -= SCALED_BLOCK;
+            left -= SCALED_BLOCK;
+            if constexpr (!DIRECT) {
+                opa.advance();
+                opb.advance();
+            }
+#pragma unroll
+            for (int i = 0; i < SCALES; ++i) moved(buffer_scale[i], (i * THREADS + wave * 64 < TM ? s.sa_block : s.sb_block) * 4);
+        } else if (ask_id + (int)gridDim.x < total) {
+            ask_id += gridDim.x;
+            begin();
+        } else {
+            left = buffer_a[2] = buffer_b[2] = 0;
+#pragma unroll
+            for (int i = 0; i < SCALES; ++i) buffer_scale[i][2] = 0;
+        }
+    };
+    // It is asked for in pieces between the products.
+    constexpr int PIECES = 2 * Op::PER_THREAD;
+    uint4 held_a[DIRECT ? 1 : Op::PER_THREAD], held_b[DIRECT ? 1 : Op::PER_THREAD];
+    float held_scale[SCALES];
+    uint32_t place = lds + wave * 1024;  // of this wave's first piece in the stage that is asked for
+    auto ask_scales = [&] {
+#pragma unroll
+        for (int i = 0; i < SCALES; ++i) {
+            if constexpr (DIRECT) {
+                const uint32_t to = place - wave * 768;
+                if (i == 0) load_word_to_lds<2 * Op::BYTES>(buffer_scale[i], scale_offset[i], to);
+                else load_word_to_lds<2 * Op::BYTES + THREADS * 4>(buffer_scale[i], scale_offset[i], to);
+            } else {
+                const uint64_t at = ((uint64_t)(uint32_t)buffer_scale[i][1] << 32) | (uint32_t)buffer_scale[i][0];
+                held_scale[i] = scale_offset[i] < (uint32_t)buffer_scale[i][2] ? *reinterpret_cast<const float*>(at + scale_offset[i]) : 0.f;
+            }
+        }
+    };
+    auto ask_piece = [&](auto piece) {
+        constexpr int i = decltype(piece)::value;
+        if constexpr (DIRECT) {
+            if constexpr (i < Op::PER_THREAD) load_to_lds<Op::BYTES + i * THREADS * 16>(buffer_b, offset_b[i], place);
+            else load_to_lds<(i - Op::PER_THREAD) * THREADS * 16>(buffer_a, offset_a[i - Op::PER_THREAD], place);
+        } else if constexpr (i == 0) {
+            opa.fetch(held_a, left);
+            opb.fetch(held_b, left);
+        }
+    };
+    // What was asked for is in its stage, and everyone has left the other one, which is asked for next.  What lies behind k in a row is not zero: it is cleared before anything is read.
+    auto arrive = [&](int into) {
+        Stage& to = stages[into];
         if constexpr (!DIRECT) {
             opa.put(to.a, held_a);
             opb.put(to.b, held_b);
 #pragma unroll
             for (int i = 0; i < SCALES; ++i) to.scale[i * THREADS + threadIdx.x] = held_scale[i];
         }
-    };
-    const int a0 = wm * (TM / WAVES_M), b0 = wn * (TN / WAVES_N);
-    auto read = [&](const char* from, int row) {
-        Codes c;
+        lds_loads_arrived();
+        meet();
+        if (DIRECT && left > 0 && left < SCALED_BLOCK) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) c.run[h] = *reinterpret_cast<const uint4*>(from + (row + r) * SCALED_BLOCK + (((4 * h + q) ^ Op::exchanged(r)) << 4));
+            for (int i = 0; i < SCALES; ++i) {
+                const int row = i * THREADS + threadIdx.x;
+                char* of = row < TM ? to.a + row * SCALED_BLOCK : to.b + (row - TM) * SCALED_BLOCK;
+#pragma unroll 1
+                for (int run = left / 16; run < 8; ++run) {
+                    uint4* at = reinterpret_cast<uint4*>(of + ((run ^ Op::exchanged(row & 15)) << 4));
+                    const int count = left - run * 16;
+                    uint4 codes = *at;
+                    codes.x &= first_bytes(count);
+                    codes.y &= first_bytes(count - 4);
+                    codes.z &= first_bytes(count - 8);
+                    codes.w &= first_bytes(count - 12);
+                    *at = codes;
+                }
+            }
+            __syncthreads();
+        }
+        place = lds + wave * 1024 + (into ? 0 : (uint32_t)sizeof(Stage));
+    };
+
+    // A step's operands in registers: all columns of the wave, 16 rows and the next 16.  A lane's places in the stage that is read.
+    Codes fb[BN], fa[2];
+    float sa[2], sb[SHARED ? 1 : BN][4];
+    const char* at_a = stages[0].a + (a0 + r) * SCALED_BLOCK + ((q ^ Op::exchanged(r)) << 4);
+    const char* at_b = stages[0].b + (b0 + r) * SCALED_BLOCK + ((q ^ Op::exchanged(r)) << 4);
+    const char* at_scale_a = (const char*)&stages[0].scale[a0 + r];
+    const char* at_scale_b = (const char*)&stages[0].scale[TM + b0 + (SHARED ? 0 : 4 * q)];
+    int other = (int)((4 ^ Op::exchanged(r) ^ q) - (q ^ Op::exchanged(r))) * 16;  // from a lane's first run of a row to its second, four on before the exchange
+    auto read = [&](const char* at) {
+        Codes c;
+        c.run[0] = *reinterpret_cast<const uint4*>(at);
+        c.run[1] = *reinterpret_cast<const uint4*>(at + other);
         return c;
     };
-    // 16 rows of a after the other against all of the wave's columns.  The products of 16 rows are scaled and added while the next ones are formed.
-    auto multiply = [&](const Stage& from) {
-        Codes fb[BN], fa[2];
-        f32x4 t[2][BN];
-        float sa[BM], sb[SHARED ? 1 : BN][4];
-#pragma unroll
-        for (int j = 0; j < BN; ++j) fb[j] = read(from.b, b0 + 16 * j);
-        fa[0] = read(from.a, a0);
+    auto read_rows = [&](int i) {
+        fa[i & 1] = read(at_a + 16 * SCALED_BLOCK * i);
+        sa[i & 1] = *reinterpret_cast<const float*>(at_scale_a + 64 * i);
+    };
+    auto read_columns = [&](int j) { fb[j] = read(at_b + 16 * SCALED_BLOCK * j); };
+    auto read_scales = [&] {
         if constexpr (SHARED) {
-            sb[0][0] = from.scale[TM + b0];
+            sb[0][0] = *reinterpret_cast<const float*>(at_scale_b);
         } else {
 #pragma unroll
             for (int j = 0; j < BN; ++j) {
-                const f32x4 four = *reinterpret_cast<const f32x4*>(&from.scale[TM + b0 + 16 * j + 4 * q]);
+                const f32x4 four = *reinterpret_cast<const f32x4*>(at_scale_b + 64 * j);
 #pragma unroll
                 for (int v = 0; v < 4; ++v) sb[j][v] = four[v];
             }
         }
+    };
+    auto turn = [&](int stage) {
+        const int by = stage ? (int)sizeof(Stage) : -(int)sizeof(Stage);
+        at_a += by;
+        at_b += by;
+        at_scale_a += by;
+        at_scale_b += by;
+    };
+
+    int stage = 0;
+    begin();
+    ask_scales();
+    ask_pieces<PIECES>(ask_piece);
+    arrive(0);
+    ask_on();
+    ask_scales();
+    if constexpr (!DIRECT) ask_piece(std::integral_constant<int, 0>());
+
+    for (int id = blockIdx.x; id < total; id += gridDim.x) {
+        const TileAt tile = tile_at(a, id);
+        f32x4 acc[BM][BN];
 #pragma unroll
-        for (int i = 0; i < BM; ++i) sa[i] = from.scale[a0 + 16 * i + r];
-        auto add = [&](int i) {
-            const float both = SHARED ? sa[i] * sb[0][0] : 0.f;
+        for (int i = 0; i < BM; ++i)
 #pragma unroll
-            for (int j = 0; j < BN; ++j)
+            for (int j = 0; j < BN; ++j) acc[i][j] = (f32x4)(0.f);
+        read_rows(0);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(t[i & 1][j][v], SHARED ? both : sa[i] * sb[j][v], acc[i][j][v]);
+        for (int j = 0; j < BN; ++j) read_columns(j);
+        read_scales();
+        // 16 rows of a after the other against all of the wave's columns.  A product is scaled and added while the third after it is formed.
+        constexpr int LAG = 3;
+        for (int step = first_step(tile.split + 1) - first_step(tile.split);;) {
+            f32x4 t[LAG + 1];
+            float factor[2];
+            auto add = [&](int p) {
+                const int i = p / BN, j = p % BN;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(t[p % (LAG + 1)][v], SHARED ? factor[i & 1] : factor[i & 1] * sb[j][v], acc[i][j][v]);
+                asm volatile("" : "+v"(acc[i][j]));  // here, and not where the sums are next used, which is behind a branch
+            };
+            ask_pieces<BM * BN>([&](auto product) {
+                constexpr int at = decltype(product)::value, i = at / BN, j = at % BN;
+                if constexpr (i == BM - 1 && j == 0) {
+                    arrive(stage ^ 1);
+                    ask_on();
+                    ask_scales();
+                    if constexpr (!DIRECT) ask_piece(std::integral_constant<int, 0>());
+                    turn(stage ^ 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                t[at % (LAG + 1)] = block_product<WIDE>(fb[j], fa[i & 1]);
+                if constexpr (j == 0) read_rows(i + 1 < BM ? i + 1 : 0);
+                if constexpr (i == BM - 1) read_columns(j);
+                if constexpr (DIRECT && at < PIECES) ask_piece(product);
+                if constexpr (at >= LAG) add(at - LAG);
+                if constexpr (j == LAG - 1) factor[i & 1] = SHARED ? sa[i & 1] * sb[0][0] : sa[i & 1];
+                if constexpr (!WIDE) __builtin_amdgcn_sched_barrier(0);
+            });
+#pragma unroll
+            for (int p = BM * BN - LAG; p < BM * BN; ++p) add(p);
+            read_scales();
+            stage ^= 1;
+            if (--step == 0) break;
+        }
+
+        // Of 16 rows and 64 columns a lane has four columns each in four places of one row; exchanged with the lane 16 away they are eight each in two places, and the
+        // four lanes of a row have 32 columns next to each other.
+        static_assert(BN == 4, "64 columns a wave");
+        const bool whole = a.splits == 1;
+        int of = lane;
+        asm volatile("" : "+v"(of));  // what follows from it is formed here, not before the loop and kept
+        const int64_t m0 = (int64_t)tile.m * TM + a0 + (of & 15);
+        const int n = tile.n * TN + b0 + 16 * ((of >> 4) & 1) + 8 * (of >> 5);  // the first of the eight columns, and 32 on
+        Eight<DT> bias[2] = {}, residual[2][2] = {};
+        auto fetch_residual = [&](int i) {
+            const int64_t m = m0 + 16 * i;
+            if (!a.residual || !whole || m >= a.m) return;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (n + 32 * h + 8 <= a.n) residual[i & 1][h].load(a.residual, m * a.ldr + n + 32 * h, 8);
         };
+        if (a.bias && whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (n + 32 * h + 8 <= a.n) bias[h].load(a.bias, n + 32 * h, 8);
+        }
+        fetch_residual(0);
 #pragma unroll
         for (int i = 0; i < BM; ++i) {
-            if (i + 1 < BM) fa[(i + 1) & 1] = read(from.a, a0 + 16 * (i + 1));
+            if (i + 1 < BM) fetch_residual(i + 1);
+            const int64_t m = m0 + 16 * i;
 #pragma unroll
-            for (int j = 0; j < BN; ++j) t[i & 1][j] = block_product<WIDE>(fb[j], fa[i & 1]);
-            if (i > 0) add(i - 1);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        add(BM - 1);
-    };
-    // What lies behind k in the last run of a row is not zero: it is cleared before anything is read.
-    const int tail = a.k % 16;
-    auto clear_tail = [&](Stage& of) {
-        const int at = (a.k % SCALED_BLOCK) / 16;
+            for (int h = 0; h < 2; ++h) {
+                float v[8];
 #pragma unroll
-        for (int i = 0; i < SCALES; ++i) {
-            const int row = i * THREADS + threadIdx.x;
-            uint4* place = reinterpret_cast<uint4*>((row < TM ? of.a + row * SCALED_BLOCK : of.b + (row - TM) * SCALED_BLOCK) + ((at ^ Op::exchanged(row & 15)) << 4));
-            uint4 codes = *place;
-            codes.x &= first_bytes(tail);
-            codes.y &= first_bytes(tail - 4);
-            codes.z &= first_bytes(tail - 8);
-            codes.w &= first_bytes(tail - 12);
-            *place = codes;
-        }
-    };
-    // One step ahead: stage s mod 2.
-    if (s0 < s1) {
-        get(stages[0]);
-        put(stages[0]);
-    }
-    for (int step = s0; step < s1; ++step) {
-        Stage& here = stages[(step - s0) & 1];
-        Stage& next = stages[(step - s0 + 1) & 1];
-        if constexpr (DIRECT) {
-            lds_loads_arrived();
-            meet();
-            if (tail && step == steps - 1) {
-                clear_tail(here);
-                __syncthreads();
-            }
-        } else {
-            __syncthreads();
-        }
-        const bool more = step + 1 < s1;
-        if (more) get(next);
-        multiply(here);
-        if (more) put(next);
-    }
-
-    // The results go through LDS, 32 rows of a wave at a time, so that 8 lanes have 64 consecutive columns of a row (as in gemm_kernel).
-    __syncthreads();
-    static_assert(BN == 4 && BM % 2 == 0 && WAVES_M * WAVES_N * 8192 <= sizeof(stages), "a wave's 32 rows have 64 columns and 8 KB");
-    char* mine = (char*)&stages[0] + wave * 8192;
-    const bool whole = a.splits == 1;
-    auto row_of = [&](int i, int part) { return m0 + wm * (TM / WAVES_M) + i * 32 + 8 * part + (lane >> 3); };
-    Eight<DT> residual[2][4] = {};
-    auto fetch_residual = [&](int i) {
-        if (!a.residual || !whole) return;
-#pragma unroll
-        for (int part = 0; part < 4; ++part) {
-            const int64_t m = row_of(i, part);
-            if (m < a.m) residual[i & 1][part].load(a.residual, m * a.ldr + n, a.n - n);
-        }
-    };
-    fetch_residual(0);
-#pragma unroll
-    for (int i = 0; i < BM / 2; ++i) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int j = 0; j < BN; ++j) *reinterpret_cast<f32x4*>(mine + (16 * half + r) * 256 + (((4 * j + q) ^ r) << 4)) = acc[2 * i + half][j];
-        __builtin_amdgcn_wave_barrier();
-        if (i + 1 < BM / 2) fetch_residual(i + 1);
-#pragma unroll
-        for (int part = 0; part < 4; ++part) {
-            const int row = 8 * part + (lane >> 3);
-            const int64_t m = row_of(i, part);
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const f32x4 x = *reinterpret_cast<const f32x4*>(mine + row * 256 + (((2 * (lane & 7) + e) ^ (row & 15)) << 4));
-                v[4 * e] = x[0], v[4 * e + 1] = x[1], v[4 * e + 2] = x[2], v[4 * e + 3] = x[3];
-            }
-            if (m >= a.m || n >= a.n) continue;
-            if (whole) {
-                finish_run<DT>(a, m, n, a.n - n, v, bias, residual[i & 1][part]);
-            } else {
-                float* to = a.partial + (((int64_t)tile.split * a.tiles_m * TM + m) * a.tiles_n * TN + n);
-                reinterpret_cast<f32x4*>(to)[0] = f32x4{v[0], v[1], v[2], v[3]};
-                reinterpret_cast<f32x4*>(to)[1] = f32x4{v[4], v[5], v[6], v[7]};
+                for (int e = 0; e < 4; ++e) {
+                    const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][2 * h][e]), __float_as_uint(acc[i][2 * h + 1][e]), false, false);
+                    v[e] = __uint_as_float(both[0]);
+                    v[4 + e] = __uint_as_float(both[1]);
+                }
+                const int at = n + 32 * h;
+                if (m >= a.m || at >= a.n) continue;
+                if (whole) {
+                    if (at + 8 <= a.n) finish_run<DT>(a, m, at, 8, v, bias[h], residual[i & 1][h]);
+                    else finish_few<DT>(a, m, at, a.n - at, v);
+                } else {
+                    // shares lie in whole tiles, so they need no edge
+                    float* to = a.partial + (((int64_t)tile.split * a.tiles_m * TM + m) * a.tiles_n * TN + at);
+                    reinterpret_cast<f32x4*>(to)[0] = f32x4{v[0], v[1], v[2], v[3]};
+                    reinterpret_cast<f32x4*>(to)[1] = f32x4{v[4], v[5], v[6], v[7]};
+                }
             }
         }
-        __builtin_amdgcn_wave_barrier();
     }
+    lds_loads_arrived();  // what was asked for last ends before its place is given away
 }
 
 struct Plan {
@@ -379,7 +493,8 @@ hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStre
     g.tiles_n = (int)(round_to(g.n, p.tile) / p.tile);
     g.splits = p.splits;
     if ((int64_t)g.tiles_m * g.tiles_n * g.splits > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((int64_t)g.tiles_m * g.tiles_n * g.splits));
+    // as many workgroups as the card's 256 compute units hold
+    const dim3 grid((unsigned)std::min((int64_t)g.tiles_m * g.tiles_n * g.splits, (int64_t)(p.tile == 256 ? 256 : 512)));
     hipError_t e;
     if (DT != CT_F32 && p.tile == 256) {
         if constexpr (DT != CT_F32)

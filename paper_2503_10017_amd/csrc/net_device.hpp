@@ -240,6 +240,15 @@ __device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, uint3
 __device__ __forceinline__ void load_word_to_lds(i32x4 buffer, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(buffer) : "m0", "memory");
 }
+// Both with a constant further on in LDS, to be had for an instruction less where several follow one another.
+template <int ON>
+__device__ __forceinline__ void load_to_lds(i32x4 buffer, uint32_t offset, uint32_t to) {
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(buffer), "n"(ON) : "m0", "scc", "memory");
+}
+template <int ON>
+__device__ __forceinline__ void load_word_to_lds(i32x4 buffer, uint32_t offset, uint32_t to) {
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(offset), "s"(buffer), "n"(ON) : "m0", "scc", "memory");
+}
 // All but this wave's last N loads have arrived (no others are under way), and its reads of LDS before them are done.
 template <int N>
 __device__ __forceinline__ void lds_loads_left() {
