@@ -189,6 +189,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     Op opa, opb;  // where a thread's runs are; with their bases, what goes through registers
     i32x4 buffer_a = buffer_of(a.a, 0), buffer_b = buffer_of(a.b, 0), buffer_scale[SCALES];
     uint32_t scale_offset[SCALES];
+    int64_t scale_by[SCALES];  // bytes from a step's scales to the next one's
     int ask_id = blockIdx.x, ask_steps = 0, left = 0;  // the tile, how many of its steps, and of k (0: nothing is left)
     opa.begin(a.a, a.lda, 0, a.m, 0);
     opb.begin(a.b, a.ldb, 0, a.n, 0);
@@ -196,6 +197,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     for (int i = 0; i < SCALES; ++i) {
         const bool of_a = i * THREADS + wave * 64 < TM;
         scale_offset[i] = (of_a ? s.shift_a : s.shift_b) ? 0u : (uint32_t)(lane * (of_a ? s.sa_row : s.sb_row) * 4);
+        scale_by[i] = (of_a ? s.sa_block : s.sb_block) * 4;
         buffer_scale[i] = buffer_of(s.scale_a, 0);
     }
     uint32_t offset_a[Op::PER_THREAD], offset_b[Op::PER_THREAD];
@@ -243,7 +245,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
                 opb.advance();
             }
 #pragma unroll
-            for (int i = 0; i < SCALES; ++i) moved(buffer_scale[i], (i * THREADS + wave * 64 < TM ? s.sa_block : s.sb_block) * 4);
+            for (int i = 0; i < SCALES; ++i) moved(buffer_scale[i], scale_by[i]);
         } else if (ask_id + (int)gridDim.x < total) {
             ask_id += gridDim.x;
             begin();
@@ -409,51 +411,55 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
             if (--step == 0) break;
         }
 
-        // Of 16 rows and 64 columns a lane has four columns each in four places of one row; exchanged with the lane 16 away they are eight each in two places, and the
-        // four lanes of a row have 32 columns next to each other.
+        // Of 16 rows and 64 columns a lane has four columns each in four places of one row.  Exchanged with the lane 16 away they are eight each in two places, 32 columns apart, and with the lane
+        // 8 away eight columns each of two rows, 8 apart: eight lanes have a row's 64 columns, whole lines of 16-bit results.
         static_assert(BN == 4, "64 columns a wave");
         const bool whole = a.splits == 1;
         int of = lane;
         asm volatile("" : "+v"(of));  // what follows from it is formed here, not before the loop and kept
-        const int64_t m0 = (int64_t)tile.m * TM + a0 + (of & 15);
-        const int n = tile.n * TN + b0 + 16 * ((of >> 4) & 1) + 8 * (of >> 5);  // the first of the eight columns, and 32 on
-        Eight<DT> bias[2] = {}, residual[2][2] = {};
+        const int64_t m0 = (int64_t)tile.m * TM + a0 + (of & 7);
+        const int n = tile.n * TN + b0 + 32 * ((of >> 3) & 1) + 16 * ((of >> 4) & 1) + 8 * (of >> 5);  // the first of the eight columns
+        Eight<DT> bias = {}, residual[2][2] = {};
         auto fetch_residual = [&](int i) {
-            const int64_t m = m0 + 16 * i;
-            if (!a.residual || !whole || m >= a.m) return;
+            if (!a.residual || !whole || n + 8 > a.n) return;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (n + 32 * h + 8 <= a.n) residual[i & 1][h].load(a.residual, m * a.ldr + n + 32 * h, 8);
+            for (int h = 0; h < 2; ++h) {
+                const int64_t m = m0 + 16 * i + 8 * h;
+                if (m < a.m) residual[i & 1][h].load(a.residual, m * a.ldr + n, 8);
+            }
         };
-        if (a.bias && whole) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (n + 32 * h + 8 <= a.n) bias[h].load(a.bias, n + 32 * h, 8);
-        }
+        if (a.bias && whole && n + 8 <= a.n) bias.load(a.bias, n, 8);
         fetch_residual(0);
 #pragma unroll
         for (int i = 0; i < BM; ++i) {
             if (i + 1 < BM) fetch_residual(i + 1);
-            const int64_t m = m0 + 16 * i;
+            float v[2][8];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float v[8];
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][2 * h][e]), __float_as_uint(acc[i][2 * h + 1][e]), false, false);
-                    v[e] = __uint_as_float(both[0]);
-                    v[4 + e] = __uint_as_float(both[1]);
+                    v[h][e] = __uint_as_float(both[0]);
+                    v[h][4 + e] = __uint_as_float(both[1]);
                 }
-                const int at = n + 32 * h;
-                if (m >= a.m || at >= a.n) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {  // lanes 8 to 15 of 16 give the first rows' half for the last rows' of lanes 0 to 7
+                const uint32_t x = __float_as_uint(v[0][e]), y = __float_as_uint(v[1][e]);
+                v[0][e] = __uint_as_float(__builtin_amdgcn_update_dpp(x, y, 0x128, 0xF, 0xC, false));  // row_ror:8
+                v[1][e] = __uint_as_float(__builtin_amdgcn_update_dpp(y, x, 0x128, 0xF, 0x3, false));
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t m = m0 + 16 * i + 8 * h;
+                if (m >= a.m || n >= a.n) continue;
                 if (whole) {
-                    if (at + 8 <= a.n) finish_run<DT>(a, m, at, 8, v, bias[h], residual[i & 1][h]);
-                    else finish_few<DT>(a, m, at, a.n - at, v);
+                    if (n + 8 <= a.n) finish_run<DT>(a, m, n, 8, v[h], bias, residual[i & 1][h]);
+                    else finish_few<DT>(a, m, n, a.n - n, v[h]);
                 } else {
                     // shares lie in whole tiles, so they need no edge
-                    float* to = a.partial + (((int64_t)tile.split * a.tiles_m * TM + m) * a.tiles_n * TN + at);
-                    reinterpret_cast<f32x4*>(to)[0] = f32x4{v[0], v[1], v[2], v[3]};
-                    reinterpret_cast<f32x4*>(to)[1] = f32x4{v[4], v[5], v[6], v[7]};
+                    float* to = a.partial + (((int64_t)tile.split * a.tiles_m * TM + m) * a.tiles_n * TN + n);
+                    reinterpret_cast<f32x4*>(to)[0] = f32x4{v[h][0], v[h][1], v[h][2], v[h][3]};
+                    reinterpret_cast<f32x4*>(to)[1] = f32x4{v[h][4], v[h][5], v[h][6], v[h][7]};
                 }
             }
         }
