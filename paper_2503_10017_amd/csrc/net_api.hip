@@ -180,7 +180,7 @@ CodesOut codes_of(const fnn_scaled* m) {
     return {(uint8_t*)const_cast<void*>(m->data), const_cast<float*>(m->scale), stride_of(m), scale_row_of(m), scale_block_of(m)};
 }
 
-// The workspace of the gradient of a layer in 8 bits: q by rows with w's transpose, or q and x across, in turn; the shares of dbias; and one area that the two products use in turn.
+// The workspace of the gradient of a layer in 8 bits: q by rows, w's transpose, q and x across, the shares of dbias, and one area that the two products use in turn.
 struct E4m3BackLayout {
     size_t q, q_scale, w, q_across, q_across_scale, x, x_scale, sums, partial, total;  // offsets
     int64_t outer_stride, rows_stride;  // of codes along outer and along the rows
@@ -495,7 +495,7 @@ int32_t fnn_quantize(const fnn_map* x, int32_t transposed, const fnn_scaled* q, 
     a.n = x->n;
     a.x_stride = stride_of(x);
     a.d = x->d;
-    return done(launch_quantize_tiles(a, q->block_rows != 1, false, x->dtype, TK_QUANTIZE, s));
+    return done(launch_quantize_tiles(a, q->block_rows != 1, x->dtype, TK_QUANTIZE, s));
 }
 
 int32_t fnn_rms_norm(const fnn_map* x, const fnn_map* residual, const void* weight, int32_t weight_dtype, float eps,
@@ -653,27 +653,36 @@ int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_
     char* ws = (char*)workspace;
 
     // q in one pass: by rows for dx, across for dw, the columns' sums for dbias
-    QuantizeArgs q;
-    memset(&q, 0, sizeof(q));
-    q.x = dy->data;
-    q.pre = slope ? pre->data : nullptr;
-    if (dx) q.rows = {(uint8_t*)ws + L.q, (float*)(ws + L.q_scale), L.outer_stride, 1, rows};
-    if (dw) q.across = {(uint8_t*)ws + L.q_across, (float*)(ws + L.q_across_scale), L.rows_stride, 1, outer};
-    q.partial = dbias ? (float*)(ws + L.sums) : nullptr;
-    q.n = rows;
-    q.x_stride = stride_of(dy);
-    q.pre_stride = slope ? stride_of(pre) : 0;
-    q.d = (int32_t)outer;
-    q.act = act;
-    if (launch_quantize_tiles(q, false, true, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+    GradientOperands o;
+    memset(&o, 0, sizeof(o));
+    if (rows > 0 && outer > 0) {
+        o.q.x = dy->data;
+        o.q.pre = slope ? pre->data : nullptr;
+        if (dx) o.q.rows = {(uint8_t*)ws + L.q, (float*)(ws + L.q_scale), L.outer_stride, 1, rows};
+        if (dw) o.q.across = {(uint8_t*)ws + L.q_across, (float*)(ws + L.q_across_scale), L.rows_stride, 1, outer};
+        o.q.partial = dbias ? (float*)(ws + L.sums) : nullptr;
+        o.q.n = rows;
+        o.q.x_stride = stride_of(dy);
+        o.q.pre_stride = slope ? stride_of(pre) : 0;
+        o.q.d = (int32_t)outer;
+        o.q.act = act;
+    }
+    if (dw && rows > 0 && inner > 0) {
+        o.x.x = x->data;
+        o.x.across = {(uint8_t*)ws + L.x, (float*)(ws + L.x_scale), L.rows_stride, 1, inner};
+        o.x.n = rows;
+        o.x.x_stride = stride_of(x);
+        o.x.d = (int32_t)inner;
+    }
+    if (dx && inner > 0 && outer > 0) o.w = {(const uint8_t*)w->data, (uint8_t*)ws + L.w, stride_of(w), L.outer_stride, outer, (int32_t)inner};
+    if (launch_gradient_operands(o, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
     if (dbias && outer > 0 &&
-        launch_column_sums(q.partial, scaled_blocks(rows), outer, outer, dbias, nullptr, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess)
+        launch_column_sums(o.q.partial, scaled_blocks(rows), outer, outer, dbias, nullptr, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess)
         return FNN_E_HIP;
     ScaledGemmArgs a;
     memset(&a, 0, sizeof(a));
     a.g.partial = (float*)(ws + L.partial);
     if (dx) {
-        if (launch_transpose_codes(w->data, stride_of(w), outer, (int32_t)inner, ws + L.w, L.outer_stride, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
         a.g.a = ws + L.q;
         a.g.b = ws + L.w;
         a.g.lda = a.g.ldb = L.outer_stride;
@@ -692,14 +701,6 @@ int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_
         if (launch_scaled_gemm(a, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
     }
     if (dw) {
-        QuantizeArgs of_x;
-        memset(&of_x, 0, sizeof(of_x));
-        of_x.x = x->data;
-        of_x.across = {(uint8_t*)ws + L.x, (float*)(ws + L.x_scale), L.rows_stride, 1, inner};
-        of_x.n = rows;
-        of_x.x_stride = stride_of(x);
-        of_x.d = (int32_t)inner;
-        if (launch_quantize_tiles(of_x, false, false, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
         a.g.a = ws + L.q_across;
         a.g.b = ws + L.x;
         a.g.lda = a.g.ldb = L.rows_stride;

@@ -125,17 +125,30 @@ struct CodesOut {
 };
 hipError_t launch_quantize_rows(const void* x, int64_t x_stride, int64_t n, int32_t d, const CodesOut& out, int dtype, int trace_kind, hipStream_t s);
 
-// Tiles of 128 x 128 of x, or with `slope` of x * act'(pre): by rows, across (transposed), one scale per block of a row or per tile.
+// Tiles of 128 x 128 of x: by rows, across (transposed), one scale per block of a row or per tile.  What is of x * act'(pre), and the sums, launch_gradient_operands takes.
 struct QuantizeArgs {
     const void* x;
     const void* pre;
     CodesOut rows, across;
-    float* partial;   // [tiles of rows][d]: the columns' sums with `slope`; NULL: not wanted
+    float* partial;   // [tiles of rows][d]: the columns' sums; NULL: not wanted
     int64_t n, x_stride, pre_stride;
     int32_t d, act;
 };
-hipError_t launch_quantize_tiles(const QuantizeArgs& a, bool tiles, bool slope, int dtype, int trace_kind, hipStream_t s);
-hipError_t launch_transpose_codes(const void* from, int64_t from_stride, int64_t n, int32_t d, void* to, int64_t to_stride, int trace_kind, hipStream_t s);
+hipError_t launch_quantize_tiles(const QuantizeArgs& a, bool tiles, int dtype, int trace_kind, hipStream_t s);
+
+// What the products of the gradient of a layer in 8 bits take: q = x * act'(pre) of `q` by rows, across and summed, `x` across, `w`'s codes transposed.  Without x (from) one is not wanted.
+struct TransposeArgs {
+    const uint8_t* from;
+    uint8_t* to;
+    int64_t from_stride, to_stride, n;
+    int32_t d;
+};
+struct GradientOperands {
+    QuantizeArgs q, x;
+    TransposeArgs w;
+    uint32_t tiles_q, tiles_x;
+};
+hipError_t launch_gradient_operands(GradientOperands a, int dtype, int trace_kind, hipStream_t s);
 
 // Root-mean-square norm of x + residual, and its gradient.
 struct RmsArgs {

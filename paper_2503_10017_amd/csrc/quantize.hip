@@ -28,17 +28,48 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const void* x, int64
     if (lane == 0) out.scale[row * out.scale_row + block * out.scale_block] = s.scale;
 }
 
-// A tile of 128 x 128 a workgroup of 256 threads, 64 values a thread: N neighbouring columns of R rows.  From it come, as wanted, codes by rows, codes
-// across (the matrix transposed, its codes gathered in LDS so that 16 of a row leave together), with TILES one scale for the whole of it, and the columns' sums.  With
-// SLOPE the values are dy * act'(pre).
+constexpr int TILE_THREADS = 512;
+
+// Of a value in each of 128 columns of every strand of rows (a thread has N columns of one strand): join(x, y) over all strands, for the thread's columns.  First over the wave's
+// strands, then over the waves.  `parts` and `whole`: LDS; the caller has met the others since their last use.
+template <int N, typename Join>
+__device__ __forceinline__ void over_strands(float (&x)[N], float (*parts)[SCALED_BLOCK], float* whole, Join join) {
+    constexpr int LANES = SCALED_BLOCK / N, WAVES = TILE_THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        if constexpr (LANES == 16) {
+            const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(x[e]), false, false);
+            x[e] = join(__uint_as_float(a[0]), __uint_as_float(a[1]));
+        }
+        const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[e]), __float_as_uint(x[e]), false, false);
+        x[e] = join(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    }
+    if (lane < LANES) store_elems<CT_F32, N>(&parts[wave][lane * N], N, x);
+    __syncthreads();
+    if (threadIdx.x < SCALED_BLOCK) {
+        float total = parts[0][threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) total = join(total, parts[w][threadIdx.x]);
+        whole[threadIdx.x] = total;
+    }
+    __syncthreads();
+    load_elems<CT_F32, N>(&whole[lane % LANES * N], N, x);
+}
+
+struct TileRoom {
+    __attribute__((aligned(16))) char codes[SCALED_BLOCK * SCALED_BLOCK];
+    float parts[2][TILE_THREADS / 64][SCALED_BLOCK], whole[2][SCALED_BLOCK];
+};
+
+// A tile of 128 x 128 a workgroup, 32 values a thread: N neighbouring columns of R rows.  From it come, as wanted, codes by rows, codes across (the matrix transposed, its codes gathered in
+// LDS so that 16 of a row leave together), with TILES one scale for the whole of it, and the columns' sums.  With SLOPE the values are dy * act'(pre).
 template <int DT, bool TILES, bool SLOPE>
-__global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
+__device__ __forceinline__ void quantize_tile(const QuantizeArgs& a, uint32_t tile, TileRoom& room) {
     typedef typename Elem<DT>::T T;
-    constexpr int N = Elem<DT>::N, LANES = SCALED_BLOCK / N, STRANDS = 256 / LANES, R = SCALED_BLOCK / STRANDS;
-    __shared__ __attribute__((aligned(16))) char codes[SCALED_BLOCK * SCALED_BLOCK];
-    __shared__ float joined[STRANDS][SCALED_BLOCK];
+    constexpr int N = Elem<DT>::N, LANES = SCALED_BLOCK / N, R = SCALED_BLOCK * SCALED_BLOCK / TILE_THREADS / N;
     const int run = threadIdx.x % LANES, strand = threadIdx.x / LANES;
-    const uint32_t tiles_c = (uint32_t)scaled_blocks(a.d), tile_r = blockIdx.x / tiles_c, tile_c = blockIdx.x % tiles_c;
+    const uint32_t tiles_c = (uint32_t)scaled_blocks(a.d), tile_r = tile / tiles_c, tile_c = tile % tiles_c;
     const int64_t r0 = (int64_t)tile_r * SCALED_BLOCK + strand * R;
     const int c0 = (int)tile_c * SCALED_BLOCK, at = c0 + run * N, count = a.d - at;
     float v[R][N];
@@ -49,12 +80,20 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
     }
     if constexpr (SLOPE) {
         if (a.act != ACT_NONE) {
+            uint4 pre[R];
 #pragma unroll
             for (int i = 0; i < R; ++i) {
                 const bool there = r0 + i < a.n && count > 0;
-                float pre[N];
-                load_elems<DT, N>((const T*)a.pre + (there ? (r0 + i) * a.pre_stride + at : 0), there ? count : 0, pre);
-                times_slope<DT != CT_F32>(v[i], pre, a.act);
+                pre[i] = load_run<DT>((const T*)a.pre + (there ? (r0 + i) * a.pre_stride + at : 0), there ? count : 0);
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                T raw[N];
+                float p[N];
+                __builtin_memcpy(raw, &pre[i], 16);
+#pragma unroll
+                for (int e = 0; e < N; ++e) p[e] = (float)raw[e];
+                times_slope<DT != CT_F32>(v[i], p, a.act);
             }
         }
         if (a.partial) {
@@ -64,17 +103,9 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
                 sum[e] = 0.f;
 #pragma unroll
                 for (int i = 0; i < R; ++i) sum[e] += v[i][e];
-                joined[strand][e * LANES + run] = sum[e];
             }
-            __syncthreads();
-            if (threadIdx.x < SCALED_BLOCK) {
-                const int column = c0 + (int)(threadIdx.x % LANES) * N + threadIdx.x / LANES;
-                float total = 0.f;
-#pragma unroll
-                for (int s = 0; s < STRANDS; ++s) total += joined[s][threadIdx.x];
-                if (column < a.d) a.partial[tile_r * (int64_t)a.d + column] = total;
-            }
-            __syncthreads();
+            over_strands<N>(sum, room.parts[0], room.whole[0], [](float x, float y) { return x + y; });
+            if (strand == 0 && count > 0) store_elems<CT_F32, N>(a.partial + tile_r * (int64_t)a.d + at, count, sum);
         }
     }
     float whole = 0.f;
@@ -83,9 +114,10 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
 #pragma unroll
         for (int i = 0; i < R; ++i) top = __builtin_fmaxf(top, top_of<true>(v[i]));
         top = lanes_max<64>(top);
-        if ((threadIdx.x & 63) == 0) joined[0][threadIdx.x >> 6] = top;
+        if ((threadIdx.x & 63) == 0) room.whole[0][threadIdx.x >> 6] = top;
         __syncthreads();
-        whole = __builtin_fmaxf(__builtin_fmaxf(joined[0][0], joined[0][1]), __builtin_fmaxf(joined[0][2], joined[0][3]));
+#pragma unroll
+        for (int w = 0; w < TILE_THREADS / 64; ++w) whole = __builtin_fmaxf(whole, room.whole[0][w]);
         const Scale s(whole);
         if (threadIdx.x == 0) {
             if (a.rows.data) a.rows.scale[tile_r * a.rows.scale_row + tile_c * a.rows.scale_block] = s.scale;
@@ -102,27 +134,15 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
         }
     }
     if (!a.across.data) return;
-    // a column's largest magnitude, over the strands
     float top[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-        top[e] = whole;
-        if constexpr (!TILES) {
-            float column[R];
+        float column[R];
 #pragma unroll
-            for (int i = 0; i < R; ++i) column[i] = v[i][e];
-            joined[strand][e * LANES + run] = top_of<true>(column);
-        }
+        for (int i = 0; i < R; ++i) column[i] = v[i][e];
+        top[e] = TILES ? whole : top_of<true>(column);
     }
-    if constexpr (!TILES) {
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            top[e] = joined[0][e * LANES + run];
-#pragma unroll
-            for (int s = 1; s < STRANDS; ++s) top[e] = __builtin_fmaxf(top[e], joined[s][e * LANES + run]);
-        }
-    }
+    if constexpr (!TILES) over_strands<N>(top, room.parts[1], room.whole[1], [](float x, float y) { return __builtin_fmaxf(x, y); });
     // Column c lies at 128 c, the 16-byte runs of its codes exchanged by the thread that had it, so that the writes of one instruction spread over LDS.
 #pragma unroll
     for (int e = 0; e < N; ++e) {
@@ -131,16 +151,16 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
 #pragma unroll
         for (int i = 0; i < R; i += 4) raw[i / 4] = four_codes(v[i][e], v[i + 1][e], v[i + 2][e], v[i + 3][e], s);
         const int first = strand * R, slot = ((first >> 4) ^ (run & 7)) * 16 + (first & 15);
-        __builtin_memcpy(codes + (run * N + e) * SCALED_BLOCK + slot, raw, R);
+        __builtin_memcpy(room.codes + (run * N + e) * SCALED_BLOCK + slot, raw, R);
         if (!TILES && strand == 0 && e < count) a.across.scale[(at + e) * a.across.scale_row + tile_r * a.across.scale_block] = s.scale;
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int column = i * 32 + threadIdx.x / 8, piece = threadIdx.x % 8;
+    for (int i = 0; i < 1024 / TILE_THREADS; ++i) {
+        const int column = i * (TILE_THREADS / 8) + threadIdx.x / 8, piece = threadIdx.x % 8;
         const int64_t row = (int64_t)tile_r * SCALED_BLOCK + piece * 16;
         if (c0 + column >= a.d || row >= a.n) continue;
-        const uint4 got = *reinterpret_cast<const uint4*>(codes + column * SCALED_BLOCK + ((piece ^ ((column / N) & 7)) << 4));
+        const uint4 got = *reinterpret_cast<const uint4*>(room.codes + column * SCALED_BLOCK + ((piece ^ ((column / N) & 7)) << 4));
         uint8_t* to = a.across.data + (c0 + column) * a.across.row + row;
         if (row + 16 <= a.n) {
             __builtin_memcpy(to, &got, 16);
@@ -154,41 +174,48 @@ __global__ __launch_bounds__(256) void quantize_tile_kernel(QuantizeArgs a) {
     }
 }
 
-// Codes transposed as they are: a tile of 128 x 128 bytes a workgroup, through LDS.
-__global__ __launch_bounds__(256) void transpose_codes_kernel(const uint8_t* from, int64_t from_stride, int64_t n, int32_t d, uint8_t* to, int64_t to_stride) {
-    __shared__ __attribute__((aligned(16))) uint8_t tile[SCALED_BLOCK][SCALED_BLOCK + 4];
-    const uint32_t tiles_c = (uint32_t)scaled_blocks(d);
-    const int64_t r0 = (int64_t)(blockIdx.x / tiles_c) * SCALED_BLOCK;
-    const int c0 = (int)(blockIdx.x % tiles_c) * SCALED_BLOCK;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = i * 32 + threadIdx.x / 8, column = threadIdx.x % 8 * 16;
-        const uint4 got = r0 + row < n ? load_run<CT_E4M3>(from + (r0 + row) * from_stride + c0 + column, d - c0 - column) : uint4{0u, 0u, 0u, 0u};
+template <int DT, bool TILES>
+__global__ __launch_bounds__(TILE_THREADS) void quantize_tile_kernel(QuantizeArgs a) {
+    __shared__ TileRoom room;
+    quantize_tile<DT, TILES, false>(a, blockIdx.x, room);
+}
+
+// Codes transposed as they are: a tile of 128 x 64 bytes a workgroup, through LDS.
+__device__ __forceinline__ void transpose_tile(const TransposeArgs& a, uint32_t tile, char* room) {
+    constexpr int PITCH = 64 + 4;
+    const uint32_t tiles_c = (uint32_t)((a.d + 63) / 64);
+    const int64_t r0 = (int64_t)(tile / tiles_c) * 128;
+    const int c0 = (int)(tile % tiles_c) * 64;
+    {
+        const int row = threadIdx.x / 4, column = threadIdx.x % 4 * 16;
+        const uint4 got = r0 + row < a.n ? load_run<CT_E4M3>(a.from + (r0 + row) * a.from_stride + c0 + column, a.d - c0 - column) : uint4{0u, 0u, 0u, 0u};
         const uint32_t words[4] = {got.x, got.y, got.z, got.w};
 #pragma unroll
-        for (int w = 0; w < 4; ++w) *reinterpret_cast<uint32_t*>(&tile[row][column + 4 * w]) = words[w];
+        for (int w = 0; w < 4; ++w) *reinterpret_cast<uint32_t*>(room + row * PITCH + column + 4 * w) = words[w];
     }
     __syncthreads();
-    // a thread: 16 rows of four columns, read as words and turned
-    const int column = threadIdx.x % 32 * 4, row = threadIdx.x / 32 * 16;
-    uint32_t word[16];
+    const int column = threadIdx.x / 8, row = threadIdx.x % 8 * 16;
+    if (c0 + column >= a.d) return;
+    uint8_t out[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) word[i] = *reinterpret_cast<const uint32_t*>(&tile[row + i][column]);
+    for (int i = 0; i < 16; ++i) out[i] = room[(row + i) * PITCH + column];
+    uint8_t* at = a.to + (int64_t)(c0 + column) * a.to_stride + r0 + row;
+    if (r0 + row + 16 <= a.n) {
+        __builtin_memcpy(at, out, 16);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (c0 + column + e >= d) break;
-        uint8_t out[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) out[i] = (uint8_t)(word[i] >> (8 * e));
-        uint8_t* at = to + (int64_t)(c0 + column + e) * to_stride + r0 + row;
-        if (r0 + row + 16 <= n) {
-            __builtin_memcpy(at, out, 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 15; ++i)
-                if (r0 + row + i < n) at[i] = out[i];
-        }
+        for (int i = 0; i < 15; ++i)
+            if (r0 + row + i < a.n) at[i] = out[i];
     }
+}
+
+// What the products of a gradient take, in one launch: q by rows and across with its columns' sums, x across, w transposed; as many of these as are wanted.
+template <int DT>
+__global__ __launch_bounds__(TILE_THREADS) void gradient_operands_kernel(GradientOperands a) {
+    __shared__ TileRoom room;
+    if (blockIdx.x < a.tiles_q) quantize_tile<DT, false, true>(a.q, blockIdx.x, room);
+    else if (blockIdx.x < a.tiles_q + a.tiles_x) quantize_tile<DT, false, false>(a.x, blockIdx.x - a.tiles_q, room);
+    else transpose_tile(a.w, blockIdx.x - a.tiles_q - a.tiles_x, room.codes);
 }
 
 template <typename F>
@@ -210,24 +237,24 @@ hipError_t launch_quantize_rows(const void* x, int64_t x_stride, int64_t n, int3
     });
 }
 
-hipError_t launch_quantize_tiles(const QuantizeArgs& a, bool tiles, bool slope, int dtype, int kind, hipStream_t s) {
+hipError_t launch_quantize_tiles(const QuantizeArgs& a, bool tiles, int dtype, int kind, hipStream_t s) {
     if (a.n < 1 || a.d < 1) return hipSuccess;
     const int64_t count = scaled_blocks(a.n) * scaled_blocks(a.d);
     if (count > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)count);
+    const dim3 grid((unsigned)count), block(TILE_THREADS);
     return with_type(dtype, [&](auto dt) {
-        constexpr int DT = dt.value;
-        if (slope) return launch(kind, quantize_tile_kernel<DT, false, true>, grid, dim3(256), 0, s, a);
-        if (tiles) return launch(kind, quantize_tile_kernel<DT, true, false>, grid, dim3(256), 0, s, a);
-        return launch(kind, quantize_tile_kernel<DT, false, false>, grid, dim3(256), 0, s, a);
+        return tiles ? launch(kind, quantize_tile_kernel<dt.value, true>, grid, block, 0, s, a) : launch(kind, quantize_tile_kernel<dt.value, false>, grid, block, 0, s, a);
     });
 }
 
-hipError_t launch_transpose_codes(const void* from, int64_t from_stride, int64_t n, int32_t d, void* to, int64_t to_stride, int kind, hipStream_t s) {
-    if (n < 1 || d < 1) return hipSuccess;
-    const int64_t count = scaled_blocks(n) * scaled_blocks(d);
+hipError_t launch_gradient_operands(GradientOperands a, int dtype, int kind, hipStream_t s) {
+    const int64_t q = a.q.x ? scaled_blocks(a.q.n) * scaled_blocks(a.q.d) : 0, x = a.x.x ? scaled_blocks(a.x.n) * scaled_blocks(a.x.d) : 0;
+    const int64_t w = a.w.from ? (a.w.n + 127) / 128 * ((a.w.d + 63) / 64) : 0, count = q + x + w;
     if (count > INT32_MAX) return hipErrorInvalidValue;
-    return launch(kind, transpose_codes_kernel, dim3((unsigned)count), dim3(256), 0, s, (const uint8_t*)from, from_stride, n, d, (uint8_t*)to, to_stride);
+    if (count == 0) return hipSuccess;
+    a.tiles_q = (uint32_t)q;
+    a.tiles_x = (uint32_t)x;
+    return with_type(dtype, [&](auto dt) { return launch(kind, gradient_operands_kernel<dt.value>, dim3((unsigned)count), dim3(TILE_THREADS), 0, s, a); });
 }
 
 }  // namespace fnn
