@@ -2,6 +2,8 @@
 //
 // C[m][n] = sum over the blocks b of k of scale_a(m, b) scale_b(n, b) sum over b of A(m, k) B(n, k): a step of the loop is one block, whose products are summed
 // by the matrix instructions from zero and then added, times the two scales, to the fp32 sums in registers.
+#include <math.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -55,8 +57,9 @@ __device__ __forceinline__ f32x4 block_product(const Codes& a, const Codes& b) {
 
 // ---- few rows ----
 
-// Whether a product is a pass over b with all of a in registers.
-bool few_rows(int64_t m, int64_t k) { return m <= 16 || (m <= 64 && m * k <= 98304); }
+// Whether a product is a pass over b with all of a in registers: up to 16 rows always, up to 32 while a, which every workgroup reads whole, is small.  (Microseconds, this way and in
+// tiles: 32 x 1024 -> 4096 4.2 and 6.0, 48 x 1024 -> 4096 5.5 and 6.0, 48 x 512 -> 8192 7.0 and 4.7, 24 x 4096 -> 1024 7.5 and 8.6.)
+bool few_rows(int64_t m, int64_t k) { return m <= 16 || (m <= 32 && m * k <= 98304); }
 constexpr int FEW_WAVES = 8;
 
 // Few rows of a: the time is that of reading b once.  A workgroup takes 16 rows of b, its waves share the blocks of k between them, and a lane asks for all of
@@ -150,6 +153,21 @@ __device__ __forceinline__ void finish_few(const GemmArgs& a, int64_t m, int n, 
 
 // A mask of the first `count` bytes of a word.
 __device__ __forceinline__ uint32_t first_bytes(int count) { return count >= 4 ? 0xFFFFFFFFu : count <= 0 ? 0u : (1u << (8 * count)) - 1u; }
+
+// Clears a row of a step in LDS from its `left`-th code on.
+__device__ __forceinline__ void clear_behind(char* row, int exchanged, int left) {
+#pragma unroll 1
+    for (int run = left / 16; run < SCALED_BLOCK / 16; ++run) {
+        uint4* at = reinterpret_cast<uint4*>(row + ((run ^ exchanged) << 4));
+        const int count = left - run * 16;
+        uint4 codes = *at;
+        codes.x &= first_bytes(count);
+        codes.y &= first_bytes(count - 4);
+        codes.z &= first_bytes(count - 8);
+        codes.w &= first_bytes(count - 12);
+        *at = codes;
+    }
+}
 
 // f(0), f(1), .. f(N - 1), the numbers as types.
 template <int N, typename F>
@@ -298,18 +316,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
 #pragma unroll
             for (int i = 0; i < SCALES; ++i) {
                 const int row = i * THREADS + threadIdx.x;
-                char* of = row < TM ? to.a + row * SCALED_BLOCK : to.b + (row - TM) * SCALED_BLOCK;
-#pragma unroll 1
-                for (int run = left / 16; run < 8; ++run) {
-                    uint4* at = reinterpret_cast<uint4*>(of + ((run ^ Op::exchanged(row & 15)) << 4));
-                    const int count = left - run * 16;
-                    uint4 codes = *at;
-                    codes.x &= first_bytes(count);
-                    codes.y &= first_bytes(count - 4);
-                    codes.z &= first_bytes(count - 8);
-                    codes.w &= first_bytes(count - 12);
-                    *at = codes;
-                }
+                clear_behind(row < TM ? to.a + row * SCALED_BLOCK : to.b + (row - TM) * SCALED_BLOCK, Op::exchanged(row & 15), left);
             }
             __syncthreads();
         }
@@ -467,23 +474,165 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     lds_loads_arrived();  // what was asked for last ends before its place is given away
 }
 
+// Small products: tiles of 64 x 64, a wave 32 x 32 of one, and a ring of stages, since the time is the latency of the loads and not what they bring: STAGES - 1 steps are under way while one is
+// multiplied.  Every wave has five loads a step (waves 2 and 3 bring the scales that 0 and 1 do), behind the last step of zeros, so that it can wait by their number.
+constexpr int SMALL = 64;
+template <int DT, bool SHARED, int STAGES>
+__global__ __launch_bounds__(256) void gemm_small_e4m3_kernel(ScaledGemmArgs s) {
+    constexpr bool WIDE = DT == CT_F32;
+    constexpr int BM = 2, BN = 2;
+    using Op = Operand<CT_E4M3, SMALL, SCALED_BLOCK, 256, ROWS>;
+    static_assert(Op::PER_THREAD == 2, "five loads a step");
+    struct Stage {
+        char a[Op::BYTES], b[Op::BYTES];
+        float scale[2 * SMALL];
+    };
+    __shared__ __attribute__((aligned(128))) Stage stages[STAGES];
+    const GemmArgs& a = s.g;
+    const TileAt tile = tile_at(a, blockIdx.x);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, q = lane >> 4, a0 = (wave & 1) * 32, b0 = (wave >> 1) * 32;
+    const int steps = (int)scaled_blocks(a.k);
+    const int s0 = (int)((uint32_t)(steps * tile.split) / (uint32_t)a.splits), s1 = (int)((uint32_t)(steps * (tile.split + 1)) / (uint32_t)a.splits);
+    const int64_t m0 = (int64_t)tile.m * SMALL, k0 = (int64_t)s0 * SCALED_BLOCK;
+    const int n0 = tile.n * SMALL;
+    Op opa, opb;
+    opa.begin(a.a, a.lda, m0, a.m, k0);
+    opb.begin(a.b, a.ldb, n0, a.n, k0);
+    const bool of_a = (wave & 1) == 0;
+    const int shift = of_a ? s.shift_a : s.shift_b;
+    const int64_t first = of_a ? m0 : n0, last = (of_a ? a.m : (int64_t)a.n) - 1, row = of_a ? s.sa_row : s.sb_row, block = of_a ? s.sa_block : s.sb_block;
+    const float* scale = (of_a ? s.scale_a : s.scale_b) + (first >> shift) * row + s0 * block;
+    const uint32_t scale_offset = shift ? 0u : (uint32_t)(lane * row * 4), scale_bytes = (uint32_t)(shift ? 4 : (min(last - first, (int64_t)63) * row + 1) * 4);
+    int left = (int)(a.k - k0), asked = s0;
+    const uint32_t lds = lds_address((const char*)&stages[0]);
+    auto ask = [&](int stage) {
+        const bool some = asked < s1;
+        const uint32_t place = lds + stage * (uint32_t)sizeof(Stage);
+        const i32x4 from_a = buffer_of(opa.base, some ? (uint32_t)((opa.have - 1) * (int)a.lda + left + 3) & ~3u : 0u);
+        const i32x4 from_b = buffer_of(opb.base, some ? (uint32_t)((opb.have - 1) * (int)a.ldb + left + 3) & ~3u : 0u);
+        load_to_lds<0>(from_a, opa.offset, place + wave * 1024);
+        load_to_lds<4096>(from_a, opa.offset + opa.apart, place + wave * 1024);
+        load_to_lds<Op::BYTES>(from_b, opb.offset, place + wave * 1024);
+        load_to_lds<Op::BYTES + 4096>(from_b, opb.offset + opb.apart, place + wave * 1024);
+        load_word_to_lds<2 * Op::BYTES>(buffer_of(scale, some ? scale_bytes : 0u), scale_offset, place + (wave & 1) * 256);
+        opa.advance();
+        opb.advance();
+        scale += block;
+        left -= SCALED_BLOCK;
+        ++asked;
+    };
+    f32x4 acc[BM][BN];
+#pragma unroll
+    for (int i = 0; i < BM; ++i)
+#pragma unroll
+        for (int j = 0; j < BN; ++j) acc[i][j] = (f32x4)(0.f);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) ask(i);
+    const bool whole = a.splits == 1;
+    const int n = n0 + b0 + 16 * (q & 1) + 8 * (q >> 1);  // the first of the eight columns that this lane finishes
+    int stage = 0;
+    for (int step = s0; step < s1; ++step, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+        lds_loads_left<5 * (STAGES - 2)>();
+        meet();
+        Stage& here = stages[stage];
+        const int k_left = a.k - step * SCALED_BLOCK;
+        if (k_left < SCALED_BLOCK) {  // what lies behind k in a row is not zero
+            if (threadIdx.x < 2 * SMALL) clear_behind(here.a + threadIdx.x * SCALED_BLOCK, Op::exchanged(threadIdx.x & 15), k_left);
+            __syncthreads();
+        }
+        ask(stage == 0 ? STAGES - 1 : stage - 1);
+        Codes fa[BM], fb[BN];
+        float sa[BM], sb[BN][4];
+        auto read = [&](const char* from) {
+            Codes c;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) c.run[h] = *reinterpret_cast<const uint4*>(from + r * SCALED_BLOCK + (((4 * h + q) ^ Op::exchanged(r)) << 4));
+            return c;
+        };
+#pragma unroll
+        for (int i = 0; i < BM; ++i) fa[i] = read(here.a + (a0 + 16 * i) * SCALED_BLOCK), sa[i] = here.scale[a0 + 16 * i + r];
+#pragma unroll
+        for (int j = 0; j < BN; ++j) {
+            fb[j] = read(here.b + (b0 + 16 * j) * SCALED_BLOCK);
+            const f32x4 four = *reinterpret_cast<const f32x4*>(&here.scale[SMALL + b0 + 16 * j + 4 * q]);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sb[j][v] = SHARED ? four[0] : four[v];
+        }
+        f32x4 t[BM][BN];
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) t[i][j] = block_product<WIDE>(fb[j], fa[i]);
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(t[i][j][v], sa[i] * sb[j][v], acc[i][j][v]);
+    }
+    lds_loads_arrived();  // what was asked for last ends before its place is given away
+#pragma unroll
+    for (int i = 0; i < BM; ++i) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const auto both = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][0][e]), __float_as_uint(acc[i][1][e]), false, false);
+            v[e] = __uint_as_float(both[0]);
+            v[4 + e] = __uint_as_float(both[1]);
+        }
+        const int64_t m = m0 + a0 + 16 * i + r;
+        if (m >= a.m || n >= a.n) continue;
+        if (!whole) {
+            float* to = a.partial + (((int64_t)tile.split * a.tiles_m * SMALL + m) * a.tiles_n * SMALL + n);
+            reinterpret_cast<f32x4*>(to)[0] = f32x4{v[0], v[1], v[2], v[3]};
+            reinterpret_cast<f32x4*>(to)[1] = f32x4{v[4], v[5], v[6], v[7]};
+        } else if (n + 8 <= a.n) {
+            finish_run<DT>(a, m, n, 8, v);
+        } else {
+            finish_few<DT>(a, m, n, a.n - n, v);
+        }
+    }
+}
+
+// The tile and the shares of k of a product, from its sizes alone: those that take the least time by a count of what they do.  A card holds 256 workgroups with a tile of 256 x 256, 512 with
+// smaller ones, and a step takes less where there are 256 of them at most.  Microseconds, fitted to 14000 timings of 1500 products of 17 to 24576 rows: what is chosen takes 1.4 % longer than the
+// best of all tiles and shares on average, 45 % at most.  (By numbers of tiles alone, as for gemm_kernel: 36 % on average.)
 struct Plan {
     int tile, splits;
 };
 constexpr int64_t round_to(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
-// The tile (256 x 256, a workgroup of eight waves a compute unit; or 128 x 128, two of four waves) and the shares of k, from the sizes alone.
+struct TileCosts {
+    int tile;
+    double each, step_alone, step;  // a tile, a step with at most 256 workgroups and with more
+};
 Plan plan_of(int64_t m, int64_t n, int64_t k, int dtype) {
-    const int64_t big = round_to(m, 256) / 256 * (round_to(n, 256) / 256), small = round_to(m, 128) / 128 * (round_to(n, 128) / 128);
-    const int64_t steps = scaled_blocks(k);
-    auto most = [&](int64_t tiles, int64_t wanted, int64_t least_steps, int64_t limit) {
-        const int64_t splits = std::min(std::min(wanted / std::max(tiles, (int64_t)1), steps / least_steps), limit);
-        return std::max(splits, (int64_t)1);
-    };
-    if (dtype != FNN_F32) {
-        const int64_t shares = most(big, 256, 8, 4);
-        if (big * shares >= 160) return {256, (int)shares};
+#ifdef FORCE_TILE
+    if (getenv("FT")) return {atoi(getenv("FT")), atoi(getenv("FS"))};
+#endif
+    constexpr TileCosts halves[3] = {{SMALL, 2.0, 0.35, 0.66}, {128, 2.9, 0.94, 1.1}, {256, 5.8, 1.66, 1.66}}, floats[2] = {{SMALL, 2.1, 0.45, 0.74}, {128, 2.7, 1.3, 1.4}};
+    constexpr int shares_of[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+    const int64_t steps = std::max(scaled_blocks(k), (int64_t)1);
+    Plan best = {SMALL, 1};
+    double least = HUGE_VAL;
+    for (int t = 0; t < (dtype == FNN_F32 ? 2 : 3); ++t) {
+        const TileCosts& c = dtype == FNN_F32 ? floats[t] : halves[t];
+        const int64_t tiles = round_to(m, c.tile) / c.tile * (round_to(n, c.tile) / c.tile), slots = c.tile == 256 ? 256 : 512;
+        for (const int splits : shares_of) {
+            if (splits > 1 && (steps / splits < 2 || tiles * splits > 1100)) break;
+            const int64_t shares = tiles * splits, rest = shares % slots;
+            const double per = (double)steps / splits, few = c.each + per * c.step_alone, many = c.each + per * c.step;
+            double time;
+            if (c.tile == SMALL) time = std::max(1.0, shares / 512.0) * (shares <= 256 ? few : many);  // not one after the other in a workgroup
+            else time = (double)(shares / slots) * many + (rest == 0 ? 0.0 : rest <= 256 ? few : many);
+            if (splits > 1) time += 2.5 + 0.26 * splits + (double)splits * m * n * 4 / 3.9e6;
+            if (time < least) {
+                least = time;
+                best = {c.tile, splits};
+            }
+        }
     }
-    return {128, (int)most(small, 256, 4, 32)};
+    return best;
 }
 
 // Whether an operand's rows start on 16-byte boundaries, and the offsets of a tile's codes and of 64 rows' scales fit 32 bits.
@@ -494,20 +643,22 @@ bool direct(const void* data, int64_t stride, int64_t rows, int64_t scale_row) {
 template <int DT, bool SHARED>
 hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStream_t s) {
     GemmArgs& g = a.g;
-    if (!is_direct) p.tile = 128;  // a large tile has no registers for what it fetches; the shares need no more room
+    if (!is_direct) p.tile = 128;  // what goes through registers; the workspace has room for its shares, too
     g.tiles_m = (int)(round_to(g.m, p.tile) / p.tile);
     g.tiles_n = (int)(round_to(g.n, p.tile) / p.tile);
     g.splits = p.splits;
-    if ((int64_t)g.tiles_m * g.tiles_n * g.splits > INT32_MAX) return hipErrorInvalidValue;
-    // as many workgroups as the card's 256 compute units hold
-    const dim3 grid((unsigned)std::min((int64_t)g.tiles_m * g.tiles_n * g.splits, (int64_t)(p.tile == 256 ? 256 : 512)));
+    const int64_t count = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+    if (count > INT32_MAX) return hipErrorInvalidValue;
     hipError_t e;
-    if (DT != CT_F32 && p.tile == 256) {
-        if constexpr (DT != CT_F32)
-            e = launch(kind, gemm_e4m3_kernel<DT, 256, 256, 2, 4, SHARED, true>, grid, dim3(512), 0, s, a);
+    // of the larger tiles as many workgroups as the card's 256 compute units hold
+    const dim3 few((unsigned)std::min(count, (int64_t)256)), more((unsigned)std::min(count, (int64_t)512));
+    if (p.tile == SMALL) {
+        e = launch(kind, gemm_small_e4m3_kernel<DT, SHARED, 4>, dim3((unsigned)count), dim3(256), 0, s, a);
+    } else if (DT != CT_F32 && p.tile == 256) {
+        if constexpr (DT != CT_F32) e = launch(kind, gemm_e4m3_kernel<DT, 256, 256, 2, 4, SHARED, true>, few, dim3(512), 0, s, a);
     } else {
-        e = is_direct ? launch(kind, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, true>, grid, dim3(256), 0, s, a)
-                      : launch(kind, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, false>, grid, dim3(256), 0, s, a);
+        e = is_direct ? launch(kind, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, true>, more, dim3(256), 0, s, a)
+                      : launch(kind, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, false>, more, dim3(256), 0, s, a);
     }
     if (e != hipSuccess || g.splits == 1) return e;
     const int64_t pitch = (int64_t)g.tiles_n * p.tile, share = pitch * g.tiles_m * p.tile, runs = (int64_t)((g.n + 7) / 8) * g.m;
@@ -517,9 +668,7 @@ hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStre
 template <int DT>
 hipError_t run_few_rows(const ScaledGemmArgs& a, int kind, hipStream_t s) {
     const dim3 grid((unsigned)((a.g.n + 15) / 16)), block(FEW_WAVES * 64);
-    if (a.g.m <= 16) return launch(kind, few_rows_e4m3_kernel<DT, 1>, grid, block, 0, s, a);
-    if (a.g.m <= 32) return launch(kind, few_rows_e4m3_kernel<DT, 2>, grid, block, 0, s, a);
-    return launch(kind, few_rows_e4m3_kernel<DT, 4>, grid, block, 0, s, a);
+    return a.g.m <= 16 ? launch(kind, few_rows_e4m3_kernel<DT, 1>, grid, block, 0, s, a) : launch(kind, few_rows_e4m3_kernel<DT, 2>, grid, block, 0, s, a);
 }
 
 template <typename F>
@@ -534,7 +683,8 @@ hipError_t with_type(int dtype, F f) {
 size_t scaled_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype) {
     if (m < 1 || n < 1 || few_rows(m, k)) return 0;
     const Plan p = plan_of(m, n, k, dtype);
-    return p.splits > 1 ? (size_t)p.splits * round_to(m, p.tile) * round_to(n, p.tile) * sizeof(float) : 0;
+    const int64_t tile = std::max(p.tile, 128);
+    return p.splits > 1 ? (size_t)p.splits * round_to(m, tile) * round_to(n, tile) * sizeof(float) : 0;
 }
 
 hipError_t launch_scaled_gemm(ScaledGemmArgs a, int dtype, int kind, hipStream_t s) {
