@@ -59,17 +59,19 @@ __device__ __forceinline__ float over_scale(float v, const Scale& s) {
     const float q = v * s.over;
     return __builtin_fmaf(__builtin_fmaf(-q, s.scale, v), s.over, q);
 }
-// Four values as codes, to nearest even; infinities and NaN as NaN.
+// Four values as codes, to nearest even; infinities and NaN as NaN.  Values that are themselves computed, and so off by some units in the last place, may do without the correction.
+template <bool DIVIDED = true>
 __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d, const Scale& s) {
-    const int low = __builtin_amdgcn_cvt_pk_fp8_f32(over_scale(a, s), over_scale(b, s), 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(over_scale(c, s), over_scale(d, s), low, true);
+    auto quotient = [&](float v) { return DIVIDED ? over_scale(v, s) : v * s.over; };
+    const int low = __builtin_amdgcn_cvt_pk_fp8_f32(quotient(a), quotient(b), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(quotient(c), quotient(d), low, true);
 }
 // N codes (4 or 8) to p, of which the first `count` exist.
-template <int N>
+template <int N, bool DIVIDED = true>
 __device__ __forceinline__ void store_codes(uint8_t* p, int count, const float (&v)[N], const Scale& s) {
     uint32_t raw[N / 4];
 #pragma unroll
-    for (int e = 0; e < N; e += 4) raw[e / 4] = four_codes(v[e], v[e + 1], v[e + 2], v[e + 3], s);
+    for (int e = 0; e < N; e += 4) raw[e / 4] = four_codes<DIVIDED>(v[e], v[e + 1], v[e + 2], v[e + 3], s);
     if (count >= N) {
         __builtin_memcpy(p, raw, N);
     } else {

@@ -607,9 +607,6 @@ struct TileCosts {
     double each, step_alone, step;  // a tile, a step with at most 256 workgroups and with more
 };
 Plan plan_of(int64_t m, int64_t n, int64_t k, int dtype) {
-#ifdef FORCE_TILE
-    if (getenv("FT")) return {atoi(getenv("FT")), atoi(getenv("FS"))};
-#endif
     constexpr TileCosts halves[3] = {{SMALL, 2.0, 0.35, 0.66}, {128, 2.9, 0.94, 1.1}, {256, 5.8, 1.66, 1.66}}, floats[2] = {{SMALL, 2.1, 0.45, 0.74}, {128, 2.7, 1.3, 1.4}};
     constexpr int shares_of[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
     const int64_t steps = std::max(scaled_blocks(k), (int64_t)1);
@@ -640,6 +637,7 @@ bool direct(const void* data, int64_t stride, int64_t rows, int64_t scale_row) {
     return ((uintptr_t)data & 15) == 0 && (rows < 2 || stride % 16 == 0) && stride < ((int64_t)1 << 31) / 256 && scale_row < ((int64_t)1 << 31) / 256;
 }
 
+// (The numbers that go with the launches name what ran to a trace: a tile's side, 129 for what goes through registers, 16 or 32 for few rows.)
 template <int DT, bool SHARED>
 hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStream_t s) {
     GemmArgs& g = a.g;
@@ -653,12 +651,12 @@ hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStre
     // of the larger tiles as many workgroups as the card's 256 compute units hold
     const dim3 few((unsigned)std::min(count, (int64_t)256)), more((unsigned)std::min(count, (int64_t)512));
     if (p.tile == SMALL) {
-        e = launch(kind, gemm_small_e4m3_kernel<DT, SHARED, 4>, dim3((unsigned)count), dim3(256), 0, s, a);
+        e = launch_detail(kind, SMALL, gemm_small_e4m3_kernel<DT, SHARED, 4>, dim3((unsigned)count), dim3(256), 0, s, a);
     } else if (DT != CT_F32 && p.tile == 256) {
-        if constexpr (DT != CT_F32) e = launch(kind, gemm_e4m3_kernel<DT, 256, 256, 2, 4, SHARED, true>, few, dim3(512), 0, s, a);
+        if constexpr (DT != CT_F32) e = launch_detail(kind, 256, gemm_e4m3_kernel<DT, 256, 256, 2, 4, SHARED, true>, few, dim3(512), 0, s, a);
     } else {
-        e = is_direct ? launch(kind, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, true>, more, dim3(256), 0, s, a)
-                      : launch(kind, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, false>, more, dim3(256), 0, s, a);
+        e = is_direct ? launch_detail(kind, 128, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, true>, more, dim3(256), 0, s, a)
+                      : launch_detail(kind, 129, gemm_e4m3_kernel<DT, 128, 128, 2, 2, SHARED, false>, more, dim3(256), 0, s, a);
     }
     if (e != hipSuccess || g.splits == 1) return e;
     const int64_t pitch = (int64_t)g.tiles_n * p.tile, share = pitch * g.tiles_m * p.tile, runs = (int64_t)((g.n + 7) / 8) * g.m;
@@ -668,7 +666,7 @@ hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStre
 template <int DT>
 hipError_t run_few_rows(const ScaledGemmArgs& a, int kind, hipStream_t s) {
     const dim3 grid((unsigned)((a.g.n + 15) / 16)), block(FEW_WAVES * 64);
-    return a.g.m <= 16 ? launch(kind, few_rows_e4m3_kernel<DT, 1>, grid, block, 0, s, a) : launch(kind, few_rows_e4m3_kernel<DT, 2>, grid, block, 0, s, a);
+    return a.g.m <= 16 ? launch_detail(kind, 16, few_rows_e4m3_kernel<DT, 1>, grid, block, 0, s, a) : launch_detail(kind, 32, few_rows_e4m3_kernel<DT, 2>, grid, block, 0, s, a);
 }
 
 template <typename F>

@@ -124,36 +124,57 @@ __device__ __forceinline__ void quantize_tile(const QuantizeArgs& a, uint32_t ti
             if (a.across.data) a.across.scale[tile_c * a.across.scale_row + tile_r * a.across.scale_block] = s.scale;
         }
     }
-    if (a.rows.data) {
+    // DIVIDED: see four_codes
+    auto by_rows = [&](auto divided) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const Scale s(TILES ? whole : block_top<LANES>(v[i]));
             if (r0 + i >= a.n) continue;
-            if (count > 0) store_codes<N>(a.rows.data + (r0 + i) * a.rows.row + at, count, v[i], s);
+            if (count > 0) store_codes<N, decltype(divided)::value>(a.rows.data + (r0 + i) * a.rows.row + at, count, v[i], s);
             if (!TILES && run == 0) a.rows.scale[(r0 + i) * a.rows.scale_row + tile_c * a.rows.scale_block] = s.scale;
         }
+    };
+    // Column c lies at 128 c, the 16-byte runs of its codes exchanged by the thread that had it, so that the writes of one instruction spread over LDS.
+    auto across = [&](auto divided) {
+        float top[N];
+        bool rare = false;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            float column[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) column[i] = v[i][e];
+            top[e] = TILES ? whole : top_of<false>(column);
+            rare |= top[e] == __builtin_inff();
+        }
+        if (!TILES && rare) {  // infinities do not enter the scale
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                float column[R];
+#pragma unroll
+                for (int i = 0; i < R; ++i) column[i] = v[i][e];
+                top[e] = top_of<true>(column);
+            }
+        }
+        if constexpr (!TILES) over_strands<N>(top, room.parts[1], room.whole[1], [](float x, float y) { return __builtin_fmaxf(x, y); });
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const Scale s(top[e]);
+            uint32_t raw[R / 4];
+#pragma unroll
+            for (int i = 0; i < R; i += 4) raw[i / 4] = four_codes<decltype(divided)::value>(v[i][e], v[i + 1][e], v[i + 2][e], v[i + 3][e], s);
+            const int first = strand * R, slot = ((first >> 4) ^ (run & 7)) * 16 + (first & 15);
+            __builtin_memcpy(room.codes + (run * N + e) * SCALED_BLOCK + slot, raw, R);
+            if (!TILES && strand == 0 && e < count) a.across.scale[(at + e) * a.across.scale_row + tile_r * a.across.scale_block] = s.scale;
+        }
+    };
+    if (SLOPE && DT != CT_F32 && a.act >= ACT_GELU) {
+        if (a.rows.data) by_rows(std::false_type());
+        if (a.across.data) across(std::false_type());
+    } else {
+        if (a.rows.data) by_rows(std::true_type());
+        if (a.across.data) across(std::true_type());
     }
     if (!a.across.data) return;
-    float top[N];
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        float column[R];
-#pragma unroll
-        for (int i = 0; i < R; ++i) column[i] = v[i][e];
-        top[e] = TILES ? whole : top_of<true>(column);
-    }
-    if constexpr (!TILES) over_strands<N>(top, room.parts[1], room.whole[1], [](float x, float y) { return __builtin_fmaxf(x, y); });
-    // Column c lies at 128 c, the 16-byte runs of its codes exchanged by the thread that had it, so that the writes of one instruction spread over LDS.
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const Scale s(top[e]);
-        uint32_t raw[R / 4];
-#pragma unroll
-        for (int i = 0; i < R; i += 4) raw[i / 4] = four_codes(v[i][e], v[i + 1][e], v[i + 2][e], v[i + 3][e], s);
-        const int first = strand * R, slot = ((first >> 4) ^ (run & 7)) * 16 + (first & 15);
-        __builtin_memcpy(room.codes + (run * N + e) * SCALED_BLOCK + slot, raw, R);
-        if (!TILES && strand == 0 && e < count) a.across.scale[(at + e) * a.across.scale_row + tile_r * a.across.scale_block] = s.scale;
-    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 1024 / TILE_THREADS; ++i) {

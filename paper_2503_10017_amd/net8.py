@@ -55,17 +55,21 @@ def _scaled(s: Optional[FnnScaled], what: str):
 def _empty_scaled(n: int, d: int, tiles: bool, device, stream) -> FnnScaled:
     """Rows of codes on 16-byte boundaries; the scales of a column of blocks next to each other."""
     high, blocks = _blocks(n) if tiles else n, _blocks(d)
-    data = _empty((n, d) if d % 16 == 0 else (n, (d + 15) // 16 * 16), torch.float8_e4m3fn, device, stream)
-    scale = _empty((1, blocks), torch.float32, device, stream) if high == 1 else _empty((blocks, high), torch.float32, device, stream).t()
-    return FnnScaled(data if d % 16 == 0 else data[:, :d], scale)
+    data = _empty((n, d if d % 16 == 0 else (d + 15) // 16 * 16), torch.float8_e4m3fn, device, stream)
+    if d % 16:
+        data = data[:, :d]
+    if high == 1:
+        return FnnScaled(data, _empty((1, blocks), torch.float32, device, stream))
+    return FnnScaled(data, _empty((blocks, high), torch.float32, device, stream).t())
 
 
 def _call(where: str, function, device, others, *args):
     """The call, on `device`; the tensors of `others` have to be there too."""
+    index = -1 if device.index is None else device.index
     for t in others:
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != index:
             raise ValueError(f"{where}: tensors on {device} and {t.device}")
-    if device.index is None or device.index == torch._C._cuda_getDevice():
+    if index < 0 or index == torch._C._cuda_getDevice():
         _check(function(*args), where)
     else:
         with torch.cuda.device(device):

@@ -123,6 +123,9 @@ class Placed(OnDevice):
     """On a device that the test names."""
     device = property(lambda self: self.place)
 
+    def get_device(self):
+        return self.place.index
+
 
 def codes(n, d, tiles=False):
     return fnn.FnnScaled(given(n, d, dtype=torch.float8_e4m3fn), given(net8._blocks(n) if tiles else n, net8._blocks(d), dtype=torch.float32))
