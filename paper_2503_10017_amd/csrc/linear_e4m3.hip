@@ -207,7 +207,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     Op opa, opb;  // where a thread's runs are; with their bases, what goes through registers
     i32x4 buffer_a = buffer_of(a.a, 0), buffer_b = buffer_of(a.b, 0), buffer_scale[SCALES];
     uint32_t scale_offset[SCALES];
-    int64_t scale_by[SCALES];  // bytes from a step's scales to the next one's
+    int64_t scale_by[SCALES];         // bytes from a step's scales to the next one's
+    const float* lane_scale[SCALES];  // through registers a lane's scale; NULL for a row that is not there
     int ask_id = blockIdx.x, ask_steps = 0, left = 0;  // the tile, how many of its steps, and of k (0: nothing is left)
     opa.begin(a.a, a.lda, 0, a.m, 0);
     opb.begin(a.b, a.ldb, 0, a.n, 0);
@@ -242,8 +243,9 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
             const int shift = of_a ? s.shift_a : s.shift_b;
             const int64_t first = of_a ? (int64_t)t.m * TM + at : (int64_t)t.n * TN + at - TM, have = (of_a ? a.m : (int64_t)a.n) - first;
             const int64_t row = of_a ? s.sa_row : s.sb_row, block = of_a ? s.sa_block : s.sb_block;
-            buffer_scale[i] = buffer_of((of_a ? s.scale_a : s.scale_b) + (have > 0 ? (first >> shift) * row : 0) + s0 * block,
-                                        some && have > 0 ? (uint32_t)(shift ? 4 : (min(have, (int64_t)64) - 1) * row * 4 + 4) : 0u);
+            const float* from = (of_a ? s.scale_a : s.scale_b) + (have > 0 ? (first >> shift) * row : 0) + s0 * block;
+            if constexpr (DIRECT) buffer_scale[i] = buffer_of(from, some && have > 0 ? (uint32_t)(shift ? 4 : (min(have, (int64_t)64) - 1) * row * 4 + 4) : 0u);
+            else lane_scale[i] = lane < have ? from + (shift ? 0 : lane * row) : nullptr;
         }
     };
     auto moved = [](i32x4& buffer, int64_t by) {
@@ -263,7 +265,10 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
                 opb.advance();
             }
 #pragma unroll
-            for (int i = 0; i < SCALES; ++i) moved(buffer_scale[i], scale_by[i]);
+            for (int i = 0; i < SCALES; ++i) {
+                if constexpr (DIRECT) moved(buffer_scale[i], scale_by[i]);
+                else if (lane_scale[i]) lane_scale[i] += scale_by[i] / 4;
+            }
         } else if (ask_id + (int)gridDim.x < total) {
             ask_id += gridDim.x;
             begin();
@@ -286,8 +291,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
                 if (i == 0) load_word_to_lds<2 * Op::BYTES>(buffer_scale[i], scale_offset[i], to);
                 else load_word_to_lds<2 * Op::BYTES + THREADS * 4>(buffer_scale[i], scale_offset[i], to);
             } else {
-                const uint64_t at = ((uint64_t)(uint32_t)buffer_scale[i][1] << 32) | (uint32_t)buffer_scale[i][0];
-                held_scale[i] = scale_offset[i] < (uint32_t)buffer_scale[i][2] ? *reinterpret_cast<const float*>(at + scale_offset[i]) : 0.f;
+                held_scale[i] = left > 0 && lane_scale[i] ? *lane_scale[i] : 0.f;
             }
         }
     };

@@ -164,7 +164,8 @@ int32_t attention_args(const fnn_heads* q, const fnn_heads* k, const fnn_heads* 
 // Shape, then pointers, of a matrix in 8 bits; the strides of what there is one of are not looked at.
 int32_t check_scaled(const fnn_scaled* m) {
     if (!m) return FNN_E_NULL;
-    if (m->n < 0 || m->n > MAX_SLOTS || m->d < 0 || (m->block_rows != 1 && m->block_rows != SCALED_BLOCK)) return FNN_E_SHAPE;
+    // columns are counted in 32 bits, up to the end of a block
+    if (m->n < 0 || m->n > MAX_SLOTS || m->d < 0 || m->d > MAX_SLOTS || (m->block_rows != 1 && m->block_rows != SCALED_BLOCK)) return FNN_E_SHAPE;
     const int64_t high = m->block_rows == 1 ? m->n : scaled_blocks(m->n), blocks = scaled_blocks(m->d);
     if (m->n > 1 && (m->row_stride < m->d || m->row_stride > INT64_MAX / 8 / m->n)) return FNN_E_SHAPE;
     if (high > 1 && (m->scale_row < 1 || m->scale_row > INT64_MAX / 16 / high)) return FNN_E_SHAPE;

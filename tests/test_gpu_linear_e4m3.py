@@ -204,6 +204,26 @@ def test_offsets_past_32_bits():
     assert torch.equal(fnn.fnn_linear_e4m3(w, fnn.FnnScaled(codes, plain.scale))[0], fnn.fnn_linear_e4m3(w, plain)[0])
 
 
+@pytest.mark.parametrize("m", [9, 100, 140])
+def test_scales_far_apart(m):
+    """Scales that lie 2^31 bytes and more apart: their offsets do not fit 32 bits."""
+    k, n, apart = 300, 130, 9 << 20
+    x, w = fnn.fnn_quantize(normal(1, m, k)), fnn.fnn_quantize(normal(2, n, k))
+    want = fnn.fnn_linear_e4m3(x, w)[0]
+    buf = torch.zeros(max(m, n) * apart, device=DEV)             # 5 GB
+
+    def far(s):
+        scale = buf.view(-1, apart)[:s.scale.shape[0], :s.scale.shape[1]]
+        scale.copy_(s.scale)
+        return fnn.FnnScaled(s.data, scale)
+
+    assert torch.equal(fnn.fnn_linear_e4m3(far(x), w)[0], want)
+    assert torch.equal(fnn.fnn_linear_e4m3(x, far(w))[0], want)
+    by_blocks = torch.zeros(3 * (200 << 20), device=DEV).view(3, -1)[:, :m].t()     # or the blocks' do
+    by_blocks.copy_(x.scale)
+    assert torch.equal(fnn.fnn_linear_e4m3(fnn.FnnScaled(x.data, by_blocks), w)[0], want)
+
+
 @pytest.mark.parametrize("m,k,n", [(8, 512, 768), (300, 2048, 200), (2304, 256, 2304)])
 def test_on_another_stream_and_in_a_graph(m, k, n):
     """The norm, the layer on its codes and both gradients, as a training step takes them, captured and replayed."""

@@ -16,7 +16,7 @@ def scaled(n=4, d=300, high=1, stride=None, scale_row=1, scale_block=None, data=
     return net8._pack_scaled(data, scale, n, d, high, d if stride is None else stride, scale_row, n if scale_block is None else scale_block)
 
 
-BAD = [dict(n=-1), dict(n=2 ** 31), dict(d=-1, stride=300), dict(high=0), dict(high=2), dict(high=64), dict(stride=299), dict(stride=2 ** 62), dict(scale_row=0), dict(scale_row=-5),
+BAD = [dict(n=-1), dict(n=2 ** 31), dict(d=-1, stride=300), dict(d=2 ** 31 - 63, stride=2 ** 31), dict(high=0), dict(high=2), dict(high=64), dict(stride=299), dict(stride=2 ** 62), dict(scale_row=0), dict(scale_row=-5),
        dict(scale_row=2 ** 61), dict(scale_block=0), dict(scale_block=-1), dict(scale_block=2 ** 61)]
 
 
