@@ -196,7 +196,8 @@ int32_t fnn_rms_norm_backward(const fnn_map* dy, const fnn_map* sum, const float
  * [outer], the latter four of one dtype, which may be any.  The products of a block of 128 are summed first, then multiplied by the product of the two scales (fp32, so this has to be a number that
  * fp32 has), and added to the fp32 sum over the blocks.  16-bit results take the matrix instructions for 8 bits, which cut each of eight products at 2^-13 of the largest of the eight before they
  * add them: an error of some 10^-5 of the sum's size, below what the result is rounded by.  FNN_F32 results take exact products and fp32 sums, at half the rate or less.
- * The workspace is for few tiles with a long `inner`.  y may be the residual itself (same rows).  dtype: that of y.
+ * The workspace is for few tiles with a long `inner`, whose products are split and joined in a fixed order, and for aligned copies of operands with an `inner` that is no multiple of 16;
+ * fnn_linear_e4m3_workspace_bytes may return 0, and returns 0 for invalid sizes.  dtype: that of y.  y may be the residual itself (same rows).
  * Errors: FNN_E_NULL, FNN_E_SHAPE, FNN_E_DTYPE, FNN_E_RANGE (act), FNN_E_WORKSPACE.
  */
 size_t fnn_linear_e4m3_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype);

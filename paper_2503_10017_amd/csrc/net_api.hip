@@ -204,7 +204,7 @@ E4m3BackLayout e4m3_back_layout(int64_t rows, int64_t inner, int64_t outer, int3
     area(L.x_scale, inner * scaled_blocks(rows) * 4);
     area(L.sums, scaled_blocks(rows) * outer * 4);
     L.partial = at;
-    const size_t x = scaled_gemm_workspace(rows, inner, outer, dtype), w = scaled_gemm_workspace(outer, inner, rows, dtype);
+    const size_t x = scaled_gemm_workspace(rows, inner, outer, dtype, false), w = scaled_gemm_workspace(outer, inner, rows, dtype, false);
     L.total = at + aligned(x > w ? x : w);
     return L;
 }
@@ -579,7 +579,7 @@ int32_t fnn_rms_norm_backward(const fnn_map* dy, const fnn_map* sum, const float
 
 size_t fnn_linear_e4m3_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
     if (!linear_sizes(rows, inner, outer) || !valid_type(dtype)) return 0;
-    return scaled_gemm_workspace(rows, outer, inner, dtype);
+    return scaled_gemm_workspace(rows, outer, inner, dtype, true);
 }
 
 int32_t fnn_linear_e4m3(const fnn_scaled* x, const fnn_scaled* w, const void* bias, int32_t act, const fnn_map* residual,
@@ -597,7 +597,7 @@ int32_t fnn_linear_e4m3(const fnn_scaled* x, const fnn_scaled* w, const void* bi
         if (m->dtype != y->dtype) return FNN_E_DTYPE;
     }
     if (act < FNN_ACT_NONE || act > FNN_ACT_SILU) return FNN_E_RANGE;
-    FNN_CHECK(check_workspace(workspace, workspace_bytes, scaled_gemm_workspace(rows, outer, inner, y->dtype)));
+    FNN_CHECK(check_workspace(workspace, workspace_bytes, scaled_gemm_workspace(rows, outer, inner, y->dtype, true)));
     ScaledGemmArgs a;
     memset(&a, 0, sizeof(a));
     a.g.a = x->data;
@@ -624,7 +624,7 @@ int32_t fnn_linear_e4m3(const fnn_scaled* x, const fnn_scaled* w, const void* bi
     a.sb_block = scale_block_of(w);
     a.shift_a = x->block_rows == 1 ? 0 : 7;
     a.shift_b = w->block_rows == 1 ? 0 : 7;
-    return done(launch_scaled_gemm(a, y->dtype, TK_LINEAR_E4M3, (hipStream_t)stream));
+    return done(launch_scaled_gemm(a, y->dtype, true, TK_LINEAR_E4M3, (hipStream_t)stream));
 }
 
 size_t fnn_linear_e4m3_backward_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
@@ -699,7 +699,7 @@ int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_
         a.sb_row = scale_block_of(w);
         a.sb_block = scale_row_of(w);
         a.shift_b = 7;
-        if (launch_scaled_gemm(a, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+        if (launch_scaled_gemm(a, x->dtype, false, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
     }
     if (dw) {
         a.g.a = ws + L.q_across;
@@ -717,7 +717,7 @@ int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_
         a.sb_row = 1;
         a.sb_block = inner;
         a.shift_b = 0;
-        if (launch_scaled_gemm(a, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
+        if (launch_scaled_gemm(a, x->dtype, false, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
     }
     return FNN_OK;
 }

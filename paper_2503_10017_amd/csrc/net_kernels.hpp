@@ -187,7 +187,8 @@ struct ScaledGemmArgs {
     int64_t sa_row, sa_block, sb_row, sb_block;     // strides of the scales
     int32_t shift_a, shift_b;                       // log2 of the rows that share a scale: 0 or 7
 };
-size_t scaled_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype);
-hipError_t launch_scaled_gemm(ScaledGemmArgs a, int dtype, int trace_kind, hipStream_t s);
+// `partial` is a workspace of these bytes: for the shares of a split product, with `copies` also for copies of operands that do not start on 16-byte boundaries.
+size_t scaled_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, bool copies);
+hipError_t launch_scaled_gemm(ScaledGemmArgs a, int dtype, bool copies, int trace_kind, hipStream_t s);
 
 }  // namespace fnn

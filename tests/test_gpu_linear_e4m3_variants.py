@@ -26,7 +26,7 @@ def launches(call):
 
 
 # size, what its product runs as, and whether its sum is cut into shares; fp32 has no large tile
-CASES = [((1, 300, 50), FEW, False), ((16, 5000, 33), FEW, False), ((17, 300, 520), FEW_32, False), ((32, 1000, 40), FEW_32, False), ((33, 200, 520), SMALL, False), ((100, 6000, 130), SMALL, True),
+CASES = [((200, 272, 300), SMALL, False), ((2100, 8320, 1100), MIDDLE, True), ((1, 300, 50), FEW, False), ((16, 5000, 33), FEW, False), ((17, 300, 520), FEW_32, False), ((32, 1000, 40), FEW_32, False), ((33, 200, 520), SMALL, False), ((100, 6000, 130), SMALL, True),
          ((700, 777, 600), SMALL, False), ((3000, 260, 2100), MIDDLE, False), ((2100, 8300, 1100), MIDDLE, True), ((4000, 1100, 4000), LARGE, False), ((2048, 20100, 2300), LARGE, True)]
 
 
@@ -45,9 +45,11 @@ def test_each_way_is_exact_on_few_digits(size, way, shares, tiles, kind):
     assert torch.equal(got[0], want)
     if kind != "f32" or way != LARGE:
         assert ran[0] == way and len(ran) == 1 + shares, ran
-    if way > FEW_32:
-        ran = launches(lambda: got.append(fnn.fnn_linear_e4m3(placed(x, sx, 1, 1, 3), placed(w, sw, 3, 2, 0, True), dtype=TYPES[kind])[0]))
-        assert torch.equal(got[1], want) and ran[0] == THROUGH_REGISTERS
+    for where in ((1, 1, 3), (3, 2, 0, True)):
+        ran = launches(lambda: got.append(fnn.fnn_linear_e4m3(placed(x, sx, *where), placed(w, sw, *where), dtype=TYPES[kind])[0]))
+        assert torch.equal(got.pop(), want)
+        if way > FEW_32:     # copied to aligned rows where k is no multiple of 16, and otherwise through registers
+            assert ran[0] == (0 if k % 16 else THROUGH_REGISTERS) and len(ran) == 1 + (k % 16 > 0) + shares, ran
 
 
 @pytest.mark.parametrize("size,way,shares", [c for c in CASES if c[1] in (SMALL, MIDDLE)] + [((4000, 330, 4000), LARGE, False)])

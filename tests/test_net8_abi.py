@@ -73,11 +73,14 @@ def test_rms_norm_backward_refusals(lib):  # noqa: F811
 def test_linear_e4m3_refusals(lib):  # noqa: F811
     x, w, y = scaled(n=100, d=300), scaled(n=32, d=300, high=128), matrix(n=100, d=32, data=0x30000)
     need = lib.fnn_linear_e4m3_workspace_bytes(100, 64000, 32, 1)
-    assert need > 0 and lib.fnn_linear_e4m3_workspace_bytes(100, 300, 32, 1) == 0
+    # copies of rows that are no whole runs of 16 bytes, unless there are so few that any alignment does
+    assert need > 0 and lib.fnn_linear_e4m3_workspace_bytes(100, 304, 32, 1) == 0 and lib.fnn_linear_e4m3_workspace_bytes(16, 301, 32, 1) == 0
+    copies = lib.fnn_linear_e4m3_workspace_bytes(100, 300, 32, 1)
+    assert 132 * 304 <= copies <= 132 * 304 + 512
     for sizes in ((-1, 64, 32, 1), (100, -1, 32, 1), (100, 64, 2 ** 31, 1), (100, 64000, 32, 3)):
         assert lib.fnn_linear_e4m3_workspace_bytes(*sizes) == 0
 
-    def call(x=x, w=w, y=y, act=0, residual=None, pre=None, ws=None, ws_bytes=0):
+    def call(x=x, w=w, y=y, act=0, residual=None, pre=None, ws=0x200000, ws_bytes=copies):
         return lib.fnn_linear_e4m3(x, w, None, act, residual, y, pre, ws, ws_bytes, None)
 
     assert call(x=None) == NULL and call(w=None) == NULL and call(y=None) == NULL
@@ -92,6 +95,7 @@ def test_linear_e4m3_refusals(lib):  # noqa: F811
     assert call(residual=matrix(n=100, d=32, dtype=0)) == DTYPE and call(pre=matrix(n=100, d=32, dtype=2)) == DTYPE and call(y=matrix(n=100, d=32, dtype=3)) == DTYPE
     assert call(act=-1) == RANGE and call(act=4) == RANGE
     long = dict(x=scaled(n=100, d=64000), w=scaled(n=32, d=64000, high=128))
+    assert call(ws=None) == WORKSPACE and call(ws=0x200010) == WORKSPACE and call(ws_bytes=copies - 1) == WORKSPACE
     assert call(**long) == WORKSPACE and call(**long, ws=0x100001, ws_bytes=need) == WORKSPACE and call(**long, ws=0x100000, ws_bytes=need - 1) == WORKSPACE
     assert call(x=scaled(n=0, d=300, data=0, scale=0, scale_block=4), y=matrix(n=0, d=32, data=0)) == OK
 
