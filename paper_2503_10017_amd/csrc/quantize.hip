@@ -22,7 +22,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const void* x, int64
     const int count = row < n ? d - at : 0;
     float v[N];
     load_elems<DT, N>((const T*)x + (count > 0 ? row * x_stride + at : 0), count, v);
-    const Scale s(block_top<LANES>(v));
+    const Scale s = Scale::of<true>(block_top<LANES>(v));
     if (row >= n) return;
     if (count > 0) store_codes<N>(out.data + row * out.row + at, count, v, s);
     if (lane == 0) out.scale[row * out.scale_row + block * out.scale_block] = s.scale;
@@ -30,36 +30,39 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const void* x, int64
 
 constexpr int TILE_THREADS = 512;
 
-// Of a value in each of 128 columns of every strand of rows (a thread has N columns of one strand): join(x, y) over all strands, for the thread's columns.  First over the wave's
-// strands, then over the waves.  `parts` and `whole`: LDS; the caller has met the others since their last use.
-template <int N, typename Join>
-__device__ __forceinline__ void over_strands(float (&x)[N], float (*parts)[SCALED_BLOCK], float* whole, Join join) {
-    constexpr int LANES = SCALED_BLOCK / N, WAVES = TILE_THREADS / 64;
+// join(x, y) over the wave's strands of rows, for each of the thread's N columns, left in LDS.
+template <int N, typename V, typename Join>
+__device__ __forceinline__ void over_strands(V (&x)[N], V (*parts)[SCALED_BLOCK], Join join) {
+    constexpr int LANES = SCALED_BLOCK / N;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto bits = [](V v) { return __builtin_bit_cast(uint32_t, v); };
+    auto value = [](uint32_t v) { return __builtin_bit_cast(V, v); };
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         if constexpr (LANES == 16) {
-            const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(x[e]), false, false);
-            x[e] = join(__uint_as_float(a[0]), __uint_as_float(a[1]));
+            const auto a = __builtin_amdgcn_permlane16_swap(bits(x[e]), bits(x[e]), false, false);
+            x[e] = join(value(a[0]), value(a[1]));
         }
-        const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[e]), __float_as_uint(x[e]), false, false);
-        x[e] = join(__uint_as_float(b[0]), __uint_as_float(b[1]));
+        const auto b = __builtin_amdgcn_permlane32_swap(bits(x[e]), bits(x[e]), false, false);
+        x[e] = join(value(b[0]), value(b[1]));
     }
-    if (lane < LANES) store_elems<CT_F32, N>(&parts[wave][lane * N], N, x);
-    __syncthreads();
-    if (threadIdx.x < SCALED_BLOCK) {
-        float total = parts[0][threadIdx.x];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) total = join(total, parts[w][threadIdx.x]);
-        whole[threadIdx.x] = total;
-    }
-    __syncthreads();
-    load_elems<CT_F32, N>(&whole[lane % LANES * N], N, x);
+    if (lane < LANES) __builtin_memcpy(&parts[wave][lane * N], x, sizeof(x));
 }
+// ... and over the waves, of one column.
+template <typename V, typename Join>
+__device__ __forceinline__ V over_waves(const V (*parts)[SCALED_BLOCK], int column, Join join) {
+    V total = parts[0][column];
+#pragma unroll
+    for (int w = 1; w < TILE_THREADS / 64; ++w) total = join(total, parts[w][column]);
+    return total;
+}
+__device__ __forceinline__ float plus(float x, float y) { return x + y; }
 
 struct TileRoom {
     __attribute__((aligned(16))) char codes[SCALED_BLOCK * SCALED_BLOCK];
-    float parts[2][TILE_THREADS / 64][SCALED_BLOCK], whole[2][SCALED_BLOCK];
+    float sums[TILE_THREADS / 64][SCALED_BLOCK];
+    uint32_t tops[TILE_THREADS / 64][SCALED_BLOCK];
+    float scale[SCALED_BLOCK], over[SCALED_BLOCK];
 };
 
 // A tile of 128 x 128 a workgroup, 32 values a thread: N neighbouring columns of R rows.  From it come, as wanted, codes by rows, codes across (the matrix transposed, its codes gathered in
@@ -72,27 +75,34 @@ __device__ __forceinline__ void quantize_tile(const QuantizeArgs& a, uint32_t ti
     const uint32_t tiles_c = (uint32_t)scaled_blocks(a.d), tile_r = tile / tiles_c, tile_c = tile % tiles_c;
     const int64_t r0 = (int64_t)tile_r * SCALED_BLOCK + strand * R;
     const int c0 = (int)tile_c * SCALED_BLOCK, at = c0 + run * N, count = a.d - at;
+    // Everything is asked for before anything is used.
+    const bool inside = (int64_t)(tile_r + 1) * SCALED_BLOCK <= a.n && c0 + SCALED_BLOCK <= a.d;
+    auto ask = [&](uint4 (&to)[R], const void* base, int64_t stride) {
+        const T* from = (const T*)base + r0 * stride + at;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            if (inside) __builtin_memcpy(&to[i], from + i * stride, 16);
+            else to[i] = load_run<DT>(from + i * stride, r0 + i < a.n ? count : 0);
+        }
+    };
+    auto values = [&](float (&to)[N], const uint4& of) {
+        T raw[N];
+        __builtin_memcpy(raw, &of, 16);
+#pragma unroll
+        for (int e = 0; e < N; ++e) to[e] = (float)raw[e];
+    };
+    uint4 asked[R], pre[R];
+    ask(asked, a.x, a.x_stride);
+    if (SLOPE && a.act != ACT_NONE) ask(pre, a.pre, a.pre_stride);
     float v[R][N];
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const bool there = r0 + i < a.n && count > 0;
-        load_elems<DT, N>((const T*)a.x + (there ? (r0 + i) * a.x_stride + at : 0), there ? count : 0, v[i]);
-    }
+    for (int i = 0; i < R; ++i) values(v[i], asked[i]);
     if constexpr (SLOPE) {
         if (a.act != ACT_NONE) {
-            uint4 pre[R];
 #pragma unroll
             for (int i = 0; i < R; ++i) {
-                const bool there = r0 + i < a.n && count > 0;
-                pre[i] = load_run<DT>((const T*)a.pre + (there ? (r0 + i) * a.pre_stride + at : 0), there ? count : 0);
-            }
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                T raw[N];
                 float p[N];
-                __builtin_memcpy(raw, &pre[i], 16);
-#pragma unroll
-                for (int e = 0; e < N; ++e) p[e] = (float)raw[e];
+                values(p, pre[i]);
                 times_slope<DT != CT_F32>(v[i], p, a.act);
             }
         }
@@ -104,76 +114,76 @@ __device__ __forceinline__ void quantize_tile(const QuantizeArgs& a, uint32_t ti
 #pragma unroll
                 for (int i = 0; i < R; ++i) sum[e] += v[i][e];
             }
-            over_strands<N>(sum, room.parts[0], room.whole[0], [](float x, float y) { return x + y; });
-            if (strand == 0 && count > 0) store_elems<CT_F32, N>(a.partial + tile_r * (int64_t)a.d + at, count, sum);
+            over_strands<N>(sum, room.sums, plus);
         }
     }
-    float whole = 0.f;
+    uint32_t whole = 0;
     if constexpr (TILES) {
-        float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < R; ++i) top = __builtin_fmaxf(top, top_of<true>(v[i]));
-        top = lanes_max<64>(top);
-        if ((threadIdx.x & 63) == 0) room.whole[0][threadIdx.x >> 6] = top;
+        for (int i = 0; i < R; ++i) whole = larger(whole, top_of<true>(v[i]));
+        whole = lanes_max<64>(whole);
+        if ((threadIdx.x & 63) == 0) room.tops[0][threadIdx.x >> 6] = whole;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < TILE_THREADS / 64; ++w) whole = __builtin_fmaxf(whole, room.whole[0][w]);
-        const Scale s(whole);
+        for (int w = 0; w < TILE_THREADS / 64; ++w) whole = larger(whole, room.tops[0][w]);
+        const float scale = Scale::of<false>(whole).scale;
         if (threadIdx.x == 0) {
-            if (a.rows.data) a.rows.scale[tile_r * a.rows.scale_row + tile_c * a.rows.scale_block] = s.scale;
-            if (a.across.data) a.across.scale[tile_c * a.across.scale_row + tile_r * a.across.scale_block] = s.scale;
+            if (a.rows.data) a.rows.scale[tile_r * a.rows.scale_row + tile_c * a.rows.scale_block] = scale;
+            if (a.across.data) a.across.scale[tile_c * a.across.scale_row + tile_r * a.across.scale_block] = scale;
         }
-    }
-    // DIVIDED: see four_codes
-    auto by_rows = [&](auto divided) {
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const Scale s(TILES ? whole : block_top<LANES>(v[i]));
-            if (r0 + i >= a.n) continue;
-            if (count > 0) store_codes<N, decltype(divided)::value>(a.rows.data + (r0 + i) * a.rows.row + at, count, v[i], s);
-            if (!TILES && run == 0) a.rows.scale[(r0 + i) * a.rows.scale_row + tile_c * a.rows.scale_block] = s.scale;
-        }
-    };
-    // Column c lies at 128 c, the 16-byte runs of its codes exchanged by the thread that had it, so that the writes of one instruction spread over LDS.
-    auto across = [&](auto divided) {
-        float top[N];
-        bool rare = false;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            float column[R];
-#pragma unroll
-            for (int i = 0; i < R; ++i) column[i] = v[i][e];
-            top[e] = TILES ? whole : top_of<false>(column);
-            rare |= top[e] == __builtin_inff();
-        }
-        if (!TILES && rare) {  // infinities do not enter the scale
+    } else {
+        if (a.across.data) {
+            uint32_t top[N];
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 float column[R];
 #pragma unroll
                 for (int i = 0; i < R; ++i) column[i] = v[i][e];
-                top[e] = top_of<true>(column);
+                top[e] = top_of<false>(column);
+                if (__any(top[e] >= INFINITE)) top[e] = top_of<true>(column);  // what is not finite is rare, and does not enter the scale
+            }
+            over_strands<N>(top, room.tops, larger);
+        }
+        __syncthreads();
+    }
+    auto encode = [&](auto divided) {  // see four_codes
+        constexpr bool DIVIDED = decltype(divided)::value;
+        // two waves join the columns' largest and two their sums, the others begin with the rows
+        if (!TILES && a.across.data && threadIdx.x < SCALED_BLOCK) {
+            const Scale s = Scale::of<DIVIDED>(over_waves(room.tops, threadIdx.x, larger));
+            room.scale[threadIdx.x] = s.scale;
+            room.over[threadIdx.x] = s.over;
+            if (c0 + threadIdx.x < a.d) a.across.scale[(c0 + threadIdx.x) * a.across.scale_row + tile_r * a.across.scale_block] = s.scale;
+        }
+        if constexpr (SLOPE) {
+            const int column = threadIdx.x - SCALED_BLOCK;
+            if (a.partial && column >= 0 && column < SCALED_BLOCK && c0 + column < a.d) a.partial[tile_r * (int64_t)a.d + c0 + column] = over_waves(room.sums, column, plus);
+        }
+        if (a.rows.data) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const Scale s = Scale::of<DIVIDED>(TILES ? whole : block_top<LANES>(v[i]));
+                if (r0 + i >= a.n) continue;
+                if (count > 0) store_codes<N, DIVIDED>(a.rows.data + (r0 + i) * a.rows.row + at, count, v[i], s);
+                if (!TILES && run == 0) a.rows.scale[(r0 + i) * a.rows.scale_row + tile_c * a.rows.scale_block] = s.scale;
             }
         }
-        if constexpr (!TILES) over_strands<N>(top, room.parts[1], room.whole[1], [](float x, float y) { return __builtin_fmaxf(x, y); });
+        if (!a.across.data) return;
+        Scale s = Scale::of<DIVIDED>(whole);
+        if (!TILES) __syncthreads();
+        // Column c lies at 128 c, the 16-byte runs of its codes exchanged by the thread that had it, so that the writes of one instruction spread over LDS.
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const Scale s(top[e]);
+            if (!TILES) s = Scale::kept<DIVIDED>(room.scale[run * N + e], room.over[run * N + e]);
             uint32_t raw[R / 4];
 #pragma unroll
-            for (int i = 0; i < R; i += 4) raw[i / 4] = four_codes<decltype(divided)::value>(v[i][e], v[i + 1][e], v[i + 2][e], v[i + 3][e], s);
+            for (int i = 0; i < R; i += 4) raw[i / 4] = four_codes<DIVIDED>(v[i][e], v[i + 1][e], v[i + 2][e], v[i + 3][e], s);
             const int first = strand * R, slot = ((first >> 4) ^ (run & 7)) * 16 + (first & 15);
             __builtin_memcpy(room.codes + (run * N + e) * SCALED_BLOCK + slot, raw, R);
-            if (!TILES && strand == 0 && e < count) a.across.scale[(at + e) * a.across.scale_row + tile_r * a.across.scale_block] = s.scale;
         }
     };
-    if (SLOPE && DT != CT_F32 && a.act >= ACT_GELU) {
-        if (a.rows.data) by_rows(std::false_type());
-        if (a.across.data) across(std::false_type());
-    } else {
-        if (a.rows.data) by_rows(std::true_type());
-        if (a.across.data) across(std::true_type());
-    }
+    if (SLOPE && DT != CT_F32 && a.act >= ACT_GELU) encode(std::false_type());
+    else encode(std::true_type());
     if (!a.across.data) return;
     __syncthreads();
 #pragma unroll

@@ -15,17 +15,18 @@ namespace {
 // magnitude, and put together in 64 bits.  v is left in these units; `of_v` is what brings it to the norm.  Every thread of the row is here.
 template <int LANES, int CHUNKS, int N>
 __device__ float rare_rstd(float (&v)[CHUNKS][N], float total, int d, float eps, float* slot, float& of_v) {
-    float top = 0.f;
+    uint32_t bits = 0;
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) top = __builtin_fmaxf(top, top_of<false>(v[c]));
-    top = lanes_max<64>(top);
+    for (int c = 0; c < CHUNKS; ++c) bits = larger(bits, top_of<false>(v[c]));
+    bits = lanes_max<64>(bits);
     if constexpr (LANES > 64) {
         __syncthreads();
-        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = top;
+        if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = __uint_as_float(bits);
         __syncthreads();
-        for (int w = 0; w < LANES / 64; ++w) top = __builtin_fmaxf(top, slot[w]);
+        for (int w = 0; w < LANES / 64; ++w) bits = larger(bits, __float_as_uint(slot[w]));
         __syncthreads();
     }
+    const float top = __uint_as_float(bits);
     int exponent = 0;
     if (top > 0.f && top < __builtin_inff()) {
         exponent = ilogbf(top);
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
                 const int at = (c * LANES + lane) * N, count = a.d - at;
-                const Scale s(block_top<BLOCK_LANES>(v[c]));
+                const Scale s = Scale::of<true>(block_top<BLOCK_LANES>(v[c]));
                 if (count <= 0) continue;
                 store_codes<N>(a.codes.data + row * a.codes.row + at, count, v[c], s);
                 if (lane % BLOCK_LANES == 0) a.codes.scale[row * a.codes.scale_row + at / SCALED_BLOCK * a.codes.scale_block] = s.scale;

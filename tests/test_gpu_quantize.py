@@ -105,3 +105,17 @@ def test_offsets_past_32_bits():
     for tiles, transposed in MODES:
         got, want = (fnn.fnn_quantize(t, tiles=tiles, transposed=transposed) for t in (x, x.contiguous()))
         assert torch.equal(got.data.float(), want.data.float()) and torch.equal(got.scale, want.scale)
+
+
+@pytest.mark.parametrize("tiles,transposed", MODES)
+def test_borders_of_codes_at_magnitudes_whose_corrections_leave_fp32(tiles, transposed):
+    """Blocks whose largest magnitude is 21 times a power of two, so that the scale is 3 times one: values of 3 (2 j + 1) times one lie on the border of two codes exactly, also where
+    the products' corrections are below fp32's numbers."""
+    x = torch.empty(256, 384)
+    for i in range(256):
+        for b in range(3):
+            low = -149 + (3 * i + b) % 128
+            j = torch.arange(128) % 64
+            x[i, 128 * b:128 * b + 128] = torch.ldexp(3.0 * (2 * j + 1).double(), torch.tensor(low)).float()
+            x[i, 128 * b] = torch.ldexp(torch.tensor(21.0, dtype=torch.float64), torch.tensor(low + 6 + i % 6)).float()
+    check(x.to(DEV), tiles, transposed)
