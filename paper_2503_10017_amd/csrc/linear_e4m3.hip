@@ -306,7 +306,9 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
         }
     };
     // What was asked for is in its stage, and everyone has left the other one, which is asked for next.  What lies behind k in a row is not zero: it is cleared before anything is read.
-    auto arrive = [&](int into) {
+    // Stores of a tile's results that were begun after what arrives here was asked for are not waited for: loads and stores end in the order in which they began.
+    int behind = 0;
+    auto arrive = [&](int into, auto after_stores) {
         Stage& to = stages[into];
         if constexpr (!DIRECT) {
             opa.put(to.a, held_a);
@@ -314,7 +316,9 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
 #pragma unroll
             for (int i = 0; i < SCALES; ++i) to.scale[i * THREADS + threadIdx.x] = held_scale[i];
         }
-        lds_loads_arrived();
+        if (!DIRECT || !decltype(after_stores)::value || behind == 0) lds_loads_arrived();
+        else if (behind == 2 * BM) lds_loads_left<2 * BM>();
+        else lds_loads_left<4 * BM>();
         meet();
         if (DIRECT && left > 0 && left < SCALED_BLOCK) {
 #pragma unroll
@@ -370,10 +374,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
     begin();
     ask_scales();
     ask_pieces<PIECES>(ask_piece);
-    arrive(0);
+    arrive(0, std::false_type());
     ask_on();
     ask_scales();
-    if constexpr (!DIRECT) ask_piece(std::integral_constant<int, 0>());
+    if constexpr (DIRECT) ask_pieces<PIECES>(ask_piece);
+    else ask_piece(std::integral_constant<int, 0>());
 
     for (int id = blockIdx.x; id < total; id += gridDim.x) {
         const TileAt tile = tile_at(a, id);
@@ -388,7 +393,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
         read_scales();
         // 16 rows of a after the other against all of the wave's columns.  A product is scaled and added while the third after it is formed.
         constexpr int LAG = 3;
-        for (int step = first_step(tile.split + 1) - first_step(tile.split);;) {
+        auto one_step = [&](auto first) {
             f32x4 t[LAG + 1];
             float factor[2];
             auto add = [&](int p) {
@@ -400,7 +405,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
             ask_pieces<BM * BN>([&](auto product) {
                 constexpr int at = decltype(product)::value, i = at / BN, j = at % BN;
                 if constexpr (i == BM - 1 && j == 0) {
-                    arrive(stage ^ 1);
+                    arrive(stage ^ 1, first);
                     ask_on();
                     ask_scales();
                     if constexpr (!DIRECT) ask_piece(std::integral_constant<int, 0>());
@@ -410,7 +415,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
                 t[at % (LAG + 1)] = block_product<WIDE>(fb[j], fa[i & 1]);
                 if constexpr (j == 0) read_rows(i + 1 < BM ? i + 1 : 0);
                 if constexpr (i == BM - 1) read_columns(j);
-                if constexpr (DIRECT && at < PIECES) ask_piece(product);
+                if constexpr (DIRECT && !decltype(first)::value && at < PIECES) ask_piece(product);
                 if constexpr (at >= LAG) add(at - LAG);
                 if constexpr (j == LAG - 1) factor[i & 1] = SHARED ? sa[i & 1] * sb[0][0] : sa[i & 1];
                 if constexpr (!WIDE) __builtin_amdgcn_sched_barrier(0);
@@ -419,8 +424,11 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
             for (int p = BM * BN - LAG; p < BM * BN; ++p) add(p);
             read_scales();
             stage ^= 1;
-            if (--step == 0) break;
-        }
+        };
+        // What follows a tile's first step is asked for before the results of the tile before are stored.
+        one_step(std::true_type());
+        for (int step = first_step(tile.split + 1) - first_step(tile.split); --step > 0;) one_step(std::false_type());
+        if constexpr (DIRECT) ask_pieces<PIECES>(ask_piece);
 
         // Of 16 rows and 64 columns a lane has four columns each in four places of one row.  Exchanged with the lane 16 away they are eight each in two places, 32 columns apart, and with the lane
         // 8 away eight columns each of two rows, 8 apart: eight lanes have a row's 64 columns, whole lines of 16-bit results.
@@ -474,6 +482,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
                 }
             }
         }
+        // at least one store of 16 bytes for each run of eight results, two of shares and where `pre` is kept
+        behind = (int64_t)(tile.m + 1) * TM > a.m || (tile.n + 1) * TN > a.n ? 0 : whole && !a.pre ? 2 * BM : 4 * BM;
     }
     lds_loads_arrived();  // what was asked for last ends before its place is given away
 }
