@@ -677,13 +677,12 @@ int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_
     }
     if (dx && inner > 0 && outer > 0) o.w = {(const uint8_t*)w->data, (uint8_t*)ws + L.w, stride_of(w), L.outer_stride, outer, (int32_t)inner};
     if (launch_gradient_operands(o, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
-    if (dbias && outer > 0 &&
-        launch_column_sums(o.q.partial, scaled_blocks(rows), outer, outer, dbias, nullptr, x->dtype, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess)
-        return FNN_E_HIP;
-    ScaledGemmArgs a;
-    memset(&a, 0, sizeof(a));
-    a.g.partial = (float*)(ws + L.partial);
+    ScaledGemmArgs x_grad, w_grad;
+    memset(&x_grad, 0, sizeof(x_grad));
+    memset(&w_grad, 0, sizeof(w_grad));
+    x_grad.g.partial = w_grad.g.partial = (float*)(ws + L.partial);
     if (dx) {
+        ScaledGemmArgs& a = x_grad;
         a.g.a = ws + L.q;
         a.g.b = ws + L.w;
         a.g.lda = a.g.ldb = L.outer_stride;
@@ -699,9 +698,9 @@ int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_
         a.sb_row = scale_block_of(w);
         a.sb_block = scale_row_of(w);
         a.shift_b = 7;
-        if (launch_scaled_gemm(a, x->dtype, false, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
     }
     if (dw) {
+        ScaledGemmArgs& a = w_grad;
         a.g.a = ws + L.q_across;
         a.g.b = ws + L.x;
         a.g.lda = a.g.ldb = L.rows_stride;
@@ -716,10 +715,8 @@ int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_
         a.scale_b = (float*)(ws + L.x_scale);
         a.sb_row = 1;
         a.sb_block = inner;
-        a.shift_b = 0;
-        if (launch_scaled_gemm(a, x->dtype, false, TK_LINEAR_E4M3_BACKWARD, s) != hipSuccess) return FNN_E_HIP;
     }
-    return FNN_OK;
+    return done(launch_scaled_gradient(x_grad, w_grad, o.q.partial, scaled_blocks(rows), outer, outer > 0 ? dbias : nullptr, x->dtype, TK_LINEAR_E4M3_BACKWARD, s));
 }
 
 }  // extern "C"

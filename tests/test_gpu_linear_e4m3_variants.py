@@ -8,25 +8,29 @@ import torch
 import paper_2503_10017_amd as fnn
 from e4m3_helpers import placed, quantized, scaled_of, spread
 from net_helpers import DEV, TYPES, normal
-from test_gpu_linear_e4m3 import check_forward
+from test_gpu_linear_e4m3 import check_backward, check_forward
 
 pytestmark = pytest.mark.gpu
 
 FEW, FEW_32, SMALL, MIDDLE, LARGE, THROUGH_REGISTERS = 16, 32, 64, 128, 256, 129
 
 
-def launches(call):
+GRADIENT = 65     # both products and the columns' sums in one launch
+
+
+def launches(call, kernels="linear_e4m3_kernels"):
     fnn.fnn_trace_begin(64)
     try:
         call()
         torch.cuda.synchronize()
     finally:
         trace = fnn.fnn_trace_end(64, details=True)
-    return [detail for name, _, detail in trace if name == "linear_e4m3_kernels"]
+    return [detail for name, _, detail in trace if name == kernels]
 
 
 # size, what its product runs as, and whether its sum is cut into shares; fp32 has no large tile
-CASES = [((200, 272, 300), SMALL, False), ((2100, 8320, 1100), MIDDLE, True), ((1, 300, 50), FEW, False), ((16, 5000, 33), FEW, False), ((17, 300, 520), FEW_32, False), ((32, 1000, 40), FEW_32, False), ((33, 200, 520), SMALL, False), ((100, 6000, 130), SMALL, True),
+CASES = [((1, 300, 50), FEW, False), ((16, 5000, 33), FEW, False), ((17, 300, 520), FEW_32, False), ((32, 1000, 40), FEW_32, False), ((33, 200, 520), SMALL, False), ((100, 6000, 130), SMALL, True),
+         ((200, 272, 300), SMALL, False), ((2100, 8320, 1100), MIDDLE, True),
          ((700, 777, 600), SMALL, False), ((3000, 260, 2100), MIDDLE, False), ((2100, 8300, 1100), MIDDLE, True), ((4000, 1100, 4000), LARGE, False), ((2048, 20100, 2300), LARGE, True)]
 
 
@@ -106,3 +110,20 @@ def test_two_streams_at_once():
         torch.cuda.synchronize()
         assert torch.equal(outs[0], want) and torch.equal(outs[1], want2)
         ws.fill_(0x7F)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size,one", [((200, 264, 300), True), ((33, 129, 40), True), ((700, 65, 1001), True), ((6, 264, 300), False), ((100, 70, 9000), False), ((9000, 70, 100), False)])
+def test_a_gradient_in_one_launch_or_product_by_product(size, one, kind):
+    m, k, n = size
+    dtype = TYPES[kind]
+    dy, x, w = normal(1, m, n, dtype=dtype), normal(2, m, k, dtype=dtype), scaled_of(normal(3, n, k, std=1 / math.sqrt(k)), tiles=True)
+    got = []
+    ran = launches(lambda: got.extend(check_backward(dy, x, w, None, "none")), "linear_e4m3_backward_kernels")
+    assert (ran == [0, GRADIENT]) == one, ran
+    parts = (fnn.fnn_linear_e4m3_backward(dy, x, w, want_x=i == 0, want_w=i == 1, want_bias=i == 2)[i] for i in range(3))
+    for part, whole in zip(parts, got):
+        assert torch.equal(part, whole)
+    if one:     # without sums, and twice the same bits
+        again = fnn.fnn_linear_e4m3_backward(dy, x, w, want_bias=False)
+        assert again[2] is None and torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
