@@ -47,8 +47,8 @@ __device__ float rare_rstd(float (&v)[CHUNKS][N], float total, int d, float eps,
 }
 
 // s = x + residual, r = 1 / sqrt(mean(s^2) + eps), y = s r w; the sum is rounded where it is stored, y is of the unrounded one.  Rows are divided as the layer
-// norm's are: a wave a row while its registers hold one.  24576 x 1024 bf16 with a residual, the sum stored and the norm in 8 bits (177 MB): 35-37 us, 4.9 TB/s of the 5.15 that a copy
-// reaches; one row: 3.1-3.6 us, a launch.
+// norm's are: a wave a row while its registers hold one.  24576 x 1024 bf16 with a residual, the sum stored and the norm in 8 bits (177 MB): 33-35 us, what a copy
+// takes (35-37 with loads that waited for each other); one row: 3.1-3.6 us, a launch.
 template <int DT, int WT, int LANES, int CHUNKS>
 __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a) {
     constexpr int N = Elem<DT>::N, THREADS = norm_threads(LANES), ROWS = THREADS / LANES, BLOCK_LANES = SCALED_BLOCK / N;
@@ -67,22 +67,37 @@ __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < a.n; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
         const T* x = (const T*)a.x + row * a.x_stride;
-        float v[CHUNKS][N];
-        float sum = 0.f;
+        // everything is asked for before anything is used
+        uint4 asked[CHUNKS], more[CHUNKS];
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             const int at = (c * LANES + lane) * N;
-            load_elems<DT, N>(x + at, a.d - at, v[c]);
+            asked[c] = load_run<DT>(x + at, a.d - at);
         }
         if (a.residual) {
             const T* residual = (const T*)a.residual + row * a.residual_stride;
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
                 const int at = (c * LANES + lane) * N;
-                float more[N];
-                load_elems<DT, N>(residual + at, a.d - at, more);
+                more[c] = load_run<DT>(residual + at, a.d - at);
+            }
+        }
+        float v[CHUNKS][N];
+        float sum = 0.f;
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[c][e] += more[e];
+        for (int c = 0; c < CHUNKS; ++c) {
+            T raw[N];
+            __builtin_memcpy(raw, &asked[c], 16);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[c][e] = (float)raw[e];
+        }
+        if (a.residual) {
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                T raw[N];
+                __builtin_memcpy(raw, &more[c], 16);
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[c][e] += (float)raw[e];
             }
         }
 #pragma unroll
