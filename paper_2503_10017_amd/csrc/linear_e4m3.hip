@@ -446,14 +446,14 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
         const int n = tile.n * TN + b0 + 32 * ((of >> 3) & 1) + 16 * ((of >> 4) & 1) + 8 * (of >> 5);  // the first of the eight columns
         Eight<DT> bias = {}, residual[2][2] = {};
         auto fetch_residual = [&](int i) {
-            if (!a.residual || !whole || n + 8 > a.n) return;
+            if (!a.residual || !whole || a.n - n < 8) return;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t m = m0 + 16 * i + 8 * h;
                 if (m < a.m) residual[i & 1][h].load(a.residual, m * a.ldr + n, 8);
             }
         };
-        if (a.bias && whole && n + 8 <= a.n) bias.load(a.bias, n, 8);
+        if (a.bias && whole && a.n - n >= 8) bias.load(a.bias, n, 8);
         fetch_residual(0);
 #pragma unroll
         for (int i = 0; i < BM; ++i) {
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
             }
         }
         // at least one store of 16 bytes for each run of eight results, two of shares and where `pre` is kept
-        behind = (int64_t)(tile.m + 1) * TM > a.m || (tile.n + 1) * TN > a.n ? 0 : whole && !a.pre ? 2 * BM : 4 * BM;
+        behind = (int64_t)(tile.m + 1) * TM > a.m || a.n - tile.n * TN < TN ? 0 : whole && !a.pre ? 2 * BM : 4 * BM;
     }
     lds_loads_arrived();  // what was asked for last ends before its place is given away
 }
@@ -791,7 +791,7 @@ size_t scaled_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, bool co
     const Plan p = plan_of(m, n, k, dtype);
     const int64_t tile = std::max(p.tile, 128), stride = round_to(k, 16);
     const size_t partial = p.splits > 1 ? (size_t)p.splits * round_to(m, tile) * round_to(n, tile) * sizeof(float) : 0;
-    return copies && k % 16 ? round_to(partial, 256) + round_to(m * stride, 256) + round_to(n * stride, 256) : partial;
+    return copies && k % 16 ? (size_t)round_to(partial, 256) + (size_t)round_to(m * stride, 256) + (size_t)round_to(n * stride, 256) : partial;
 }
 
 hipError_t launch_scaled_gemm(ScaledGemmArgs a, int dtype, bool copies, int kind, hipStream_t s) {

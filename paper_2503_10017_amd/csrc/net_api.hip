@@ -193,7 +193,7 @@ E4m3BackLayout e4m3_back_layout(int64_t rows, int64_t inner, int64_t outer, int3
     size_t at = 0;
     auto area = [&](size_t& place, int64_t bytes) {
         place = at;
-        at += aligned((size_t)bytes);
+        if (at < SIZE_MAX / 2) at += aligned((size_t)bytes);  // what no memory holds stays that large
     };
     area(L.q, rows * L.outer_stride);
     area(L.q_scale, rows * scaled_blocks(outer) * 4);

@@ -146,7 +146,7 @@ struct TransposeArgs {
 struct GradientOperands {
     QuantizeArgs q, x;
     TransposeArgs w;
-    uint32_t tiles_q, tiles_x;
+    uint32_t tiles_q, tiles_x, first;  // the launch's first tile of all
 };
 hipError_t launch_gradient_operands(GradientOperands a, int dtype, int trace_kind, hipStream_t s);
 

@@ -13,10 +13,10 @@ namespace {
 
 // Blocks of 128 along the rows: 16 bytes a lane, so 16 lanes (fp32: 32) a block, and a block's largest takes no LDS.  24576 x 4096 bf16 (305 MB): 57 us, 5.3 TB/s.
 template <int DT>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const void* x, int64_t x_stride, int64_t n, int32_t d, uint32_t blocks, CodesOut out) {
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const void* x, int64_t x_stride, int64_t n, int32_t d, uint32_t blocks, uint32_t first, CodesOut out) {
     typedef typename Elem<DT>::T T;
     constexpr int N = Elem<DT>::N, LANES = SCALED_BLOCK / N, PER = 256 / LANES;
-    const uint32_t item = blockIdx.x * PER + threadIdx.x / LANES, block = item % blocks;
+    const uint32_t item = (first + blockIdx.x) * PER + threadIdx.x / LANES, block = item % blocks;
     const int64_t row = item / blocks;
     const int lane = threadIdx.x % LANES, at = (int)block * SCALED_BLOCK + lane * N;
     const int count = row < n ? d - at : 0;
@@ -78,7 +78,7 @@ __device__ __forceinline__ void quantize_tile(const QuantizeArgs& a, uint32_t ti
     const int64_t r0 = (int64_t)tile_r * SCALED_BLOCK + strand * R;
     const int c0 = (int)tile_c * SCALED_BLOCK, at = c0 + run * N, count = a.d - at;
     // Everything is asked for before anything is used.
-    const bool inside = (int64_t)(tile_r + 1) * SCALED_BLOCK <= a.n && c0 + SCALED_BLOCK <= a.d;
+    const bool inside = (int64_t)(tile_r + 1) * SCALED_BLOCK <= a.n && a.d - c0 >= SCALED_BLOCK;
     auto ask = [&](uint4 (&to)[R], const void* base, int64_t stride) {
         const T* from = (const T*)base + r0 * stride + at;
 #pragma unroll
@@ -208,9 +208,9 @@ __device__ __forceinline__ void quantize_tile(const QuantizeArgs& a, uint32_t ti
 }
 
 template <int DT, bool TILES>
-__global__ __launch_bounds__(TILE_THREADS) void quantize_tile_kernel(QuantizeArgs a) {
+__global__ __launch_bounds__(TILE_THREADS) void quantize_tile_kernel(QuantizeArgs a, uint32_t first) {
     __shared__ TileRoom room;
-    quantize_tile<DT, TILES, false>(a, blockIdx.x, room);
+    quantize_tile<DT, TILES, false>(a, first + blockIdx.x, room);
 }
 
 // Codes transposed as they are: a tile of 128 x 64 bytes a workgroup, through LDS.
@@ -248,9 +248,21 @@ __device__ __forceinline__ void transpose_tile(const TransposeArgs& a, uint32_t 
 template <int DT>
 __global__ __launch_bounds__(TILE_THREADS) void gradient_operands_kernel(GradientOperands a) {
     __shared__ TileRoom room;
-    if (blockIdx.x < a.tiles_q) quantize_tile<DT, false, true>(a.q, blockIdx.x, room);
-    else if (blockIdx.x < a.tiles_q + a.tiles_x) quantize_tile<DT, false, false>(a.x, blockIdx.x - a.tiles_q, room);
-    else transpose_tile(a.w, blockIdx.x - a.tiles_q - a.tiles_x, room.codes);
+    const uint32_t tile = a.first + blockIdx.x;
+    if (tile < a.tiles_q) quantize_tile<DT, false, true>(a.q, tile, room);
+    else if (tile < a.tiles_q + a.tiles_x) quantize_tile<DT, false, false>(a.x, tile - a.tiles_q, room);
+    else transpose_tile(a.w, tile - a.tiles_q - a.tiles_x, room.codes);
+}
+
+// A launch has fewer than 2^32 threads: long narrow matrices take several.  f(first, grid)
+template <typename F>
+hipError_t in_launches(int64_t groups, F f) {
+    constexpr int64_t MOST = 1 << 22;
+    for (int64_t first = 0; first < groups; first += MOST) {
+        const hipError_t e = f((uint32_t)first, dim3((unsigned)(groups - first < MOST ? groups - first : MOST)));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename F>
@@ -268,7 +280,9 @@ hipError_t launch_quantize_rows(const void* x, int64_t x_stride, int64_t n, int3
         constexpr int per = 256 * Elem<dt.value>::N / SCALED_BLOCK;
         const int64_t blocks = scaled_blocks(d), groups = (n * blocks + per - 1) / per;
         if (n * blocks > (int64_t)UINT32_MAX - per) return hipErrorInvalidValue;  // blocks are counted in 32 bits: no memory holds so many
-        return launch(kind, quantize_rows_kernel<dt.value>, dim3((unsigned)groups), dim3(256), 0, s, x, x_stride, n, d, (uint32_t)blocks, out);
+        return in_launches(groups, [&](uint32_t first, dim3 grid) {
+            return launch(kind, quantize_rows_kernel<dt.value>, grid, dim3(256), 0, s, x, x_stride, n, d, (uint32_t)blocks, first, out);
+        });
     });
 }
 
@@ -276,9 +290,10 @@ hipError_t launch_quantize_tiles(const QuantizeArgs& a, bool tiles, int dtype, i
     if (a.n < 1 || a.d < 1) return hipSuccess;
     const int64_t count = scaled_blocks(a.n) * scaled_blocks(a.d);
     if (count > INT32_MAX) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)count), block(TILE_THREADS);
     return with_type(dtype, [&](auto dt) {
-        return tiles ? launch(kind, quantize_tile_kernel<dt.value, true>, grid, block, 0, s, a) : launch(kind, quantize_tile_kernel<dt.value, false>, grid, block, 0, s, a);
+        return in_launches(count, [&](uint32_t first, dim3 grid) {
+            return launch(kind, tiles ? quantize_tile_kernel<dt.value, true> : quantize_tile_kernel<dt.value, false>, grid, dim3(TILE_THREADS), 0, s, a, first);
+        });
     });
 }
 
@@ -289,7 +304,12 @@ hipError_t launch_gradient_operands(GradientOperands a, int dtype, int kind, hip
     if (count == 0) return hipSuccess;
     a.tiles_q = (uint32_t)q;
     a.tiles_x = (uint32_t)x;
-    return with_type(dtype, [&](auto dt) { return launch(kind, gradient_operands_kernel<dt.value>, dim3((unsigned)count), dim3(TILE_THREADS), 0, s, a); });
+    return with_type(dtype, [&](auto dt) {
+        return in_launches(count, [&](uint32_t first, dim3 grid) {
+            a.first = first;
+            return launch(kind, gradient_operands_kernel<dt.value>, grid, dim3(TILE_THREADS), 0, s, a);
+        });
+    });
 }
 
 }  // namespace fnn

@@ -119,3 +119,28 @@ def test_borders_of_codes_at_magnitudes_whose_corrections_leave_fp32(tiles, tran
             x[i, 128 * b:128 * b + 128] = torch.ldexp(3.0 * (2 * j + 1).double(), torch.tensor(low)).float()
             x[i, 128 * b] = torch.ldexp(torch.tensor(21.0, dtype=torch.float64), torch.tensor(low + 6 + i % 6)).float()
     check(x.to(DEV), tiles, transposed)
+
+
+@pytest.mark.parametrize("tiles,transposed", [(False, False), (True, False), (True, True)])
+def test_the_longest_row(tiles, transposed):
+    """2^31 - 65 columns, as many as a matrix may have: the last block would end at 2^31."""
+    d = 2 ** 31 - 65
+    x = torch.zeros(1, d, dtype=torch.bfloat16, device=DEV)
+    tail = 3 * 128 + 63                             # from a block's first column on
+    x[:, -tail:] = normal(1, 1, tail, dtype=torch.bfloat16)
+    x[0, 5] = 1.0
+    got = fnn.fnn_quantize(x.view(d, 1) if transposed else x, tiles=tiles, transposed=transposed)
+    want, scale = quantized(x[:, -tail:], tiles)
+    assert torch.equal(got.scale[:, -4:], scale) and same(got.data[:, -tail:].double(), want)
+    assert got.data[0, 5].item() == 448 and got.scale[0, 0].item() == torch.tensor(1.0).div(448).item()
+
+
+@pytest.mark.parametrize("tiles", [False, True])
+def test_more_rows_than_one_launch_takes(tiles):
+    n = 2 ** 26 * (16 if tiles else 1) + 77
+    x = torch.full((n, 1), 2.0, dtype=torch.bfloat16, device=DEV)
+    x[-77:] = normal(1, 77, 1, dtype=torch.bfloat16)
+    got = fnn.fnn_quantize(x, tiles=tiles)
+    want, scale = quantized(x[-77:], tiles)
+    assert torch.equal(got.scale[-len(scale):], scale) and same(got.data[-77:].double(), want)
+    assert (got.data[:-77].view(torch.uint8) == 0x7E).all() and (got.scale[:-len(scale)] == torch.tensor(2.0).div(448).to(DEV)).all()
