@@ -52,15 +52,14 @@ def _scaled(s: Optional[FnnScaled], what: str):
                         scale_row, scale_block)
 
 
-def _empty_scaled(n: int, d: int, tiles: bool, device, stream) -> FnnScaled:
-    """Rows of codes on 16-byte boundaries; the scales of a column of blocks next to each other."""
+def _empty_scaled(n: int, d: int, tiles: bool, device, stream):
+    """Rows of codes on 16-byte boundaries, the scales of a column of blocks next to each other; and the struct fnn_scaled that they are."""
     high, blocks = _blocks(n) if tiles else n, _blocks(d)
-    data = _empty((n, d if d % 16 == 0 else (d + 15) // 16 * 16), torch.float8_e4m3fn, device, stream)
-    if d % 16:
-        data = data[:, :d]
-    if high == 1:
-        return FnnScaled(data, _empty((1, blocks), torch.float32, device, stream))
-    return FnnScaled(data, _empty((blocks, high), torch.float32, device, stream).t())
+    stride = d if d % 16 == 0 else (d + 15) // 16 * 16
+    data = _empty((n, stride), torch.float8_e4m3fn, device, stream)
+    scale = _empty((1, blocks) if high == 1 else (blocks, high), torch.float32, device, stream)
+    packed = _pack_scaled(data.data_ptr(), scale.data_ptr(), n, d, 1 if high == n else SCALED_BLOCK, stride, 1, high)
+    return FnnScaled(data if stride == d else data[:, :d], scale if high == 1 else scale.t()), packed
 
 
 def _call(where: str, function, device, others, *args):
@@ -82,8 +81,11 @@ def fnn_quantize(x: torch.Tensor, tiles: bool = False, transposed: bool = False,
     xm = _matrix(x, "x")
     n, d = x.shape
     if out is None:
-        out = _empty_scaled(d, n, tiles, x.device, stream) if transposed else _empty_scaled(n, d, tiles, x.device, stream)
-    _call("fnn_quantize", lib.fnn_quantize, x.device, out, xm, 1 if transposed else 0, _scaled(out, "out"), _stream_ptr(stream, x.device))
+        out, om = _empty_scaled(d, n, tiles, x.device, stream) if transposed else _empty_scaled(n, d, tiles, x.device, stream)
+        others = ()
+    else:
+        om, others = _scaled(out, "out"), out
+    _call("fnn_quantize", lib.fnn_quantize, x.device, others, xm, 1 if transposed else 0, om, _stream_ptr(stream, x.device))
     return out
 
 
@@ -99,13 +101,19 @@ def fnn_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residua
     wt = x.dtype if weight is None else weight.dtype
     if out is None and want_y:
         out = _like(x, stream)
-    if out_scaled is None and want_scaled:
-        out_scaled = _empty_scaled(n, d, False, x.device, stream)
+    others = (weight, residual, out, out_sum)
+    if out_scaled is not None:
+        cm = _scaled(out_scaled, "out_scaled")
+        others += out_scaled
+    elif want_scaled:
+        out_scaled, cm = _empty_scaled(n, d, False, x.device, stream)
+    else:
+        cm = None
     if out_sum is None and residual is not None:
         out_sum = _like(x, stream)
     rstd = _empty(n, torch.float32, x.device, stream) if want_rstd else None
-    _call("fnn_rms_norm", lib.fnn_rms_norm, x.device, (weight, residual, out, out_sum, *(out_scaled or ())), xm, _matrix(residual, "residual"),
-          _vector(weight, d, wt, "weight"), _DTYPES.get(wt, -1), eps, _matrix(out_sum, "out_sum"), _matrix(out, "out"), _scaled(out_scaled, "out_scaled"), _ptr(rstd),
+    _call("fnn_rms_norm", lib.fnn_rms_norm, x.device, others, xm, _matrix(residual, "residual"),
+          _vector(weight, d, wt, "weight"), _DTYPES.get(wt, -1), eps, _matrix(out_sum, "out_sum"), _matrix(out, "out"), cm, _ptr(rstd),
           _stream_ptr(stream, x.device))
     return out, out_scaled, out_sum, rstd
 
