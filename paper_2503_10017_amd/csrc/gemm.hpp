@@ -329,8 +329,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
 // The shares of a split product, added up in the order of k, so that the result does not depend on which workgroup ended first; the epilogue is here then.  Bound
 // by memory: 1024 x 4096 in four shares (67 MB written by the product, still in the caches) 12 us.
 template <int DT>
-__global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs a, int64_t pitch, int64_t share) {
-    const int64_t runs = (a.n + 7) / 8, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__device__ __forceinline__ void gemm_join(const GemmArgs& a, int64_t pitch, int64_t share, unsigned block) {
+    const int64_t runs = (a.n + 7) / 8, at = (int64_t)block * 256 + threadIdx.x;
     if (at >= runs * a.m) return;
     const int64_t m = at / runs;
     const int n = (int)(at - m * runs) * 8;
@@ -342,6 +342,10 @@ __global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs a, int64_t pitc
         for (int e = 0; e < 4; ++e) v[e] += lo[e], v[4 + e] += hi[e];
     }
     finish_run<DT>(a, m, n, a.n - n, v);
+}
+template <int DT>
+__global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs a, int64_t pitch, int64_t share) {
+    gemm_join<DT>(a, pitch, share, blockIdx.x);
 }
 
 }  // namespace fnn

@@ -622,24 +622,23 @@ __global__ __launch_bounds__(256) void gemm_small_e4m3_kernel(ScaledGemmArgs s) 
     gemm_small_e4m3<DT, SHARED, STAGES>(s, blockIdx.x, stages);
 }
 
-// The two products of a small gradient and the sums of its columns in one launch, since each by itself leaves compute units idle: the tiles of the first, those of the second, then 32 columns a
-// workgroup.  (1531 x 777 -> 1001 fp16: 14.7 us for 10.5, 9.1 and 3.7 in launches of their own.)
-struct SmallGradient {
-    ScaledGemmArgs of[2];
-    int32_t first, tiles;  // of the first product and of both
-    const float* partial;  // [groups][columns]
-    void* sums;
+// The sums of the columns of partial ([groups][columns]), beside other work of their launch.
+struct ColumnSums {
+    const float* partial;
+    void* to;
     int64_t groups, columns;
+    unsigned workgroups() const { return to ? (unsigned)((columns + 31) / 32) : 0u; }
 };
 // 32 columns, in the order of column_sums_kernel: 32 strands of groups, then the strands one after the other; a thread has four strands.
 template <int DT>
-__device__ __forceinline__ void sum_columns(const SmallGradient& p, int id, float (*parts)[33]) {
+__device__ __forceinline__ void sum_columns(const ColumnSums& p, int id, float (*parts)[33]) {
     const int lane = threadIdx.x & 31, first = threadIdx.x >> 5;
     const int64_t column = (int64_t)id * 32 + lane;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float sum = 0.f;
         if (column < p.columns)
+#pragma unroll 4
             for (int64_t g = first + 8 * i; g < p.groups; g += 32) sum += p.partial[g * p.columns + column];
         parts[first + 8 * i][lane] = sum;
     }
@@ -647,15 +646,22 @@ __device__ __forceinline__ void sum_columns(const SmallGradient& p, int id, floa
     if (first == 0 && column < p.columns) {
         float sum = parts[0][lane];
         for (int i = 1; i < 32; ++i) sum += parts[i][lane];
-        ((typename Elem<DT>::T*)p.sums)[column] = (typename Elem<DT>::T)sum;
+        ((typename Elem<DT>::T*)p.to)[column] = (typename Elem<DT>::T)sum;
     }
 }
+// The two products of a small gradient and the sums of its columns in one launch, since each by itself leaves compute units idle: the tiles of the first, those of the second, then 32 columns a
+// workgroup.  (1531 x 777 -> 1001 fp16: 14.7 us for 10.5, 9.1 and 3.7 in launches of their own.)
+struct SmallGradient {
+    ScaledGemmArgs of[2];
+    int32_t first, tiles;  // of the first product and of both
+    ColumnSums sums;
+};
 template <int DT>
 __global__ __launch_bounds__(256) void gradient_small_e4m3_kernel(SmallGradient p) {
     constexpr int STAGES = 3;  // so that a compute unit has room for three workgroups: four stages and two of them take 18.2 us at the size above
     __shared__ __attribute__((aligned(128))) SmallStage stages[STAGES];
     const int id = blockIdx.x;
-    if (id >= p.tiles) return sum_columns<DT>(p, id - p.tiles, (float(*)[33])stages);
+    if (id >= p.tiles) return sum_columns<DT>(p.sums, id - p.tiles, (float(*)[33])stages);
     const int which = id >= p.first;
     gemm_small_e4m3<DT, false, STAGES>(p.of[which], id - (which ? p.first : 0), stages);
 }
@@ -704,9 +710,18 @@ bool direct(const void* data, int64_t stride, int64_t rows, int64_t scale_row) {
     return on_runs(data, stride, rows) && stride < ((int64_t)1 << 31) / 256 && scale_row < ((int64_t)1 << 31) / 256;
 }
 
+// gemm_join_kernel with the columns' sums in its first workgroups.  1024 x 4096 in four shares and 4096 columns of 96 groups: 15.5 us for 12.8 and 4.9 in launches of their own; with
+// the sums in the last workgroups 17.7.
+template <int DT>
+__global__ __launch_bounds__(256) void join_and_sum_kernel(GemmArgs a, int64_t pitch, int64_t share, unsigned first, ColumnSums sums) {
+    __shared__ float parts[32][33];
+    if (blockIdx.x >= first) gemm_join<DT>(a, pitch, share, blockIdx.x - first);
+    else sum_columns<DT>(sums, blockIdx.x, parts);
+}
+
 // (The numbers that go with the launches name what ran to a trace: a tile's side, 129 for what goes through registers, 16 or 32 for few rows.)
 template <int DT, bool SHARED>
-hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStream_t s) {
+hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, const ColumnSums& sums, int kind, hipStream_t s) {
     GemmArgs& g = a.g;
     if (!is_direct) p.tile = 128;  // what goes through registers; the workspace has room for its shares, too
     g.tiles_m = (int)(round_to(g.m, p.tile) / p.tile);
@@ -727,7 +742,9 @@ hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, int kind, hipStre
     }
     if (e != hipSuccess || g.splits == 1) return e;
     const int64_t pitch = (int64_t)g.tiles_n * p.tile, share = pitch * g.tiles_m * p.tile, runs = (int64_t)((g.n + 7) / 8) * g.m;
-    return launch(kind, gemm_join_kernel<DT>, dim3((unsigned)((runs + 255) / 256)), dim3(256), 0, s, g, pitch, share);
+    const unsigned joins = (unsigned)((runs + 255) / 256);
+    if (sums.to) return launch(kind, join_and_sum_kernel<DT>, dim3(joins + sums.workgroups()), dim3(256), 0, s, g, pitch, share, sums.workgroups(), sums);
+    return launch(kind, gemm_join_kernel<DT>, dim3(joins), dim3(256), 0, s, g, pitch, share);
 }
 
 // Rows on 16-byte boundaries, zeros behind their ends, of one operand or of both: a thread writes 16 bytes, read from wherever they are.
@@ -794,24 +811,37 @@ size_t scaled_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, bool co
     return copies && k % 16 ? (size_t)round_to(partial, 256) + (size_t)round_to(m * stride, 256) + (size_t)round_to(n * stride, 256) : partial;
 }
 
-hipError_t launch_scaled_gemm(ScaledGemmArgs a, int dtype, bool copies, int kind, hipStream_t s) {
+namespace {
+
+// sums: taken along where the product's shares are joined, and otherwise before it.
+hipError_t run_product(ScaledGemmArgs a, int dtype, bool copies, const ColumnSums& sums, int kind, hipStream_t s) {
     GemmArgs& g = a.g;
-    if (g.m < 1 || g.n < 1) return hipSuccess;
+    const bool some = g.m > 0 && g.n > 0, few = some && few_rows(g.m, g.k);
+    const Plan p = some && !few ? plan_of(g.m, g.n, g.k, dtype) : Plan{SMALL, 1};
+    if (sums.to && p.splits == 1) {
+        const hipError_t e = launch_column_sums(sums.partial, sums.groups, sums.columns, sums.columns, sums.to, nullptr, dtype, kind, s);
+        if (e != hipSuccess) return e;
+    }
+    if (!some) return hipSuccess;
     return with_type(dtype, [&](auto dt) {
         constexpr int DT = dt.value;
-        if (few_rows(g.m, g.k)) return run_few_rows<DT>(a, kind, s);
-        const Plan p = plan_of(g.m, g.n, g.k, dtype);
+        if (few) return run_few_rows<DT>(a, kind, s);
         if (copies && g.k % 16) {
             const hipError_t e = copy_operands(g, (char*)g.partial + round_to((int64_t)scaled_gemm_workspace(g.m, g.n, g.k, dtype, false), 256), kind, s);
             if (e != hipSuccess) return e;
         }
         const bool d = direct(g.a, g.lda, g.m, a.sa_row) && direct(g.b, g.ldb, g.n, a.sb_row);
-        return a.shift_b ? run_tiles<DT, true>(a, d, p, kind, s) : run_tiles<DT, false>(a, d, p, kind, s);
+        return a.shift_b ? run_tiles<DT, true>(a, d, p, sums, kind, s) : run_tiles<DT, false>(a, d, p, sums, kind, s);
     });
 }
 
+}  // namespace
+
+hipError_t launch_scaled_gemm(const ScaledGemmArgs& a, int dtype, int kind, hipStream_t s) { return run_product(a, dtype, true, ColumnSums{}, kind, s); }
+
 hipError_t launch_scaled_gradient(const ScaledGemmArgs& dx, const ScaledGemmArgs& dw, const float* partial, int64_t groups, int64_t columns, void* sums, int dtype, int kind, hipStream_t s) {
     const ScaledGemmArgs* of[2] = {&dx, &dw};
+    const ColumnSums columns_sums = {partial, sums, groups, columns};
     int64_t tiles[2];
     bool small = true;
     for (int i = 0; i < 2 && small; ++i) {
@@ -833,19 +863,12 @@ hipError_t launch_scaled_gradient(const ScaledGemmArgs& dx, const ScaledGemmArgs
         }
         p.first = (int32_t)tiles[0];
         p.tiles = (int32_t)(tiles[0] + tiles[1]);
-        p.partial = partial;
-        p.sums = sums;
-        p.groups = groups;
-        p.columns = sums ? columns : 0;
-        const dim3 grid((unsigned)(p.tiles + (p.columns + 31) / 32));
+        p.sums = columns_sums;
+        const dim3 grid((unsigned)p.tiles + columns_sums.workgroups());
         return with_type(dtype, [&](auto dt) { return launch_detail(kind, SMALL + 1, gradient_small_e4m3_kernel<dt.value>, grid, dim3(256), 0, s, p); });
     }
-    if (sums) {
-        const hipError_t e = launch_column_sums(partial, groups, columns, columns, sums, nullptr, dtype, kind, s);
-        if (e != hipSuccess) return e;
-    }
-    const hipError_t e = launch_scaled_gemm(dx, dtype, false, kind, s);
-    return e == hipSuccess ? launch_scaled_gemm(dw, dtype, false, kind, s) : e;
+    const hipError_t e = run_product(dx, dtype, false, ColumnSums{}, kind, s);
+    return e == hipSuccess ? run_product(dw, dtype, false, columns_sums, kind, s) : e;
 }
 
 }  // namespace fnn

@@ -624,7 +624,7 @@ int32_t fnn_linear_e4m3(const fnn_scaled* x, const fnn_scaled* w, const void* bi
     a.sb_block = scale_block_of(w);
     a.shift_a = x->block_rows == 1 ? 0 : 7;
     a.shift_b = w->block_rows == 1 ? 0 : 7;
-    return done(launch_scaled_gemm(a, y->dtype, true, TK_LINEAR_E4M3, (hipStream_t)stream));
+    return done(launch_scaled_gemm(a, y->dtype, TK_LINEAR_E4M3, (hipStream_t)stream));
 }
 
 size_t fnn_linear_e4m3_backward_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {

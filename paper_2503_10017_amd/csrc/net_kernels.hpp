@@ -189,7 +189,7 @@ struct ScaledGemmArgs {
 };
 // `partial` is a workspace of these bytes: for the shares of a split product, with `copies` also for copies of operands that do not start on 16-byte boundaries.
 size_t scaled_gemm_workspace(int64_t m, int64_t n, int64_t k, int dtype, bool copies);
-hipError_t launch_scaled_gemm(ScaledGemmArgs a, int dtype, bool copies, int trace_kind, hipStream_t s);
+hipError_t launch_scaled_gemm(const ScaledGemmArgs& a, int dtype, int trace_kind, hipStream_t s);  // with a workspace that has room for copies
 // A gradient's two products (either may have no rows or columns) and, unless `sums` is NULL, sums[c] = the sum of column c of partial ([groups][columns]).
 hipError_t launch_scaled_gradient(const ScaledGemmArgs& dx, const ScaledGemmArgs& dw, const float* partial, int64_t groups, int64_t columns, void* sums, int dtype, int trace_kind,
                                   hipStream_t s);

@@ -11,7 +11,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from .binding import _DTYPES, _empty, _ptr, load_library
-from .net import _ACTS, _check, _like, _matrix, _scratch, _stream_ptr, _vector
+from .net import _ACTS, _check, _like, _matrix, _pack_map, _scratch, _stream_ptr, _vector
 
 SCALED_BLOCK = 128
 
@@ -62,6 +62,11 @@ def _empty_scaled(n: int, d: int, tiles: bool, device, stream):
     return FnnScaled(data if stride == d else data[:, :d], scale if high == 1 else scale.t()), packed
 
 
+def _fresh(t: torch.Tensor, n: int, d: int):
+    """The struct fnn_map of an output [n][d] of the call's own, without the checks of _matrix."""
+    return _pack_map(t.data_ptr(), n, d, _DTYPES[t.dtype], d)
+
+
 def _call(where: str, function, device, others, *args):
     """The call, on `device`; the tensors of `others` have to be there too."""
     index = -1 if device.index is None else device.index
@@ -99,9 +104,11 @@ def fnn_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residua
     xm = _matrix(x, "x")
     n, d = x.shape
     wt = x.dtype if weight is None else weight.dtype
+    others = (weight, residual, out, out_sum)
+    ym, sm = _matrix(out, "out"), _matrix(out_sum, "out_sum")
     if out is None and want_y:
         out = _like(x, stream)
-    others = (weight, residual, out, out_sum)
+        ym = _fresh(out, n, d)
     if out_scaled is not None:
         cm = _scaled(out_scaled, "out_scaled")
         others += out_scaled
@@ -111,9 +118,10 @@ def fnn_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residua
         cm = None
     if out_sum is None and residual is not None:
         out_sum = _like(x, stream)
+        sm = _fresh(out_sum, n, d)
     rstd = _empty(n, torch.float32, x.device, stream) if want_rstd else None
     _call("fnn_rms_norm", lib.fnn_rms_norm, x.device, others, xm, _matrix(residual, "residual"),
-          _vector(weight, d, wt, "weight"), _DTYPES.get(wt, -1), eps, _matrix(out_sum, "out_sum"), _matrix(out, "out"), cm, _ptr(rstd),
+          _vector(weight, d, wt, "weight"), _DTYPES.get(wt, -1), eps, sm, ym, cm, _ptr(rstd),
           _stream_ptr(stream, x.device))
     return out, out_scaled, out_sum, rstd
 
@@ -158,13 +166,17 @@ def fnn_linear_e4m3(x: FnnScaled, w: FnnScaled, bias: Optional[torch.Tensor] = N
     rows, inner = x.data.shape
     outer, device = w.data.shape[0], x.data.device
     if out is None:
+        if dtype not in _DTYPES:
+            raise ValueError(f"unsupported dtype {dtype} of the results")
         out = _empty((rows, outer), dtype, device, stream)
-    om = _matrix(out, "out")
+        om = _fresh(out, rows, outer)
+    else:
+        om = _matrix(out, "out")
     pre = _empty((rows, outer), out.dtype, device, stream) if want_pre else None
     if workspace is None:
         workspace = _scratch(lib.fnn_linear_e4m3_workspace_bytes(rows, inner, outer, _DTYPES[out.dtype]), device, stream)
     _call("fnn_linear_e4m3", lib.fnn_linear_e4m3, device, (x.scale, *w, bias, residual, out, workspace), xm, wm, _vector(bias, outer, out.dtype, "bias"), _ACTS[act],
-          _matrix(residual, "residual"), om, _matrix(pre, "pre"), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream, device))
+          _matrix(residual, "residual"), om, None if pre is None else _fresh(pre, rows, outer), _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream, device))
     return out, pre
 
 
