@@ -719,7 +719,7 @@ __global__ __launch_bounds__(256) void join_and_sum_kernel(GemmArgs a, int64_t p
     else sum_columns<DT>(sums, blockIdx.x, parts);
 }
 
-// (The numbers that go with the launches name what ran to a trace: a tile's side, 129 for what goes through registers, 16 or 32 for few rows.)
+// (The numbers that go with the launches name what ran to a trace: a tile's side, 129 for what goes through registers, 65 for a small gradient, 16 or 32 for few rows.)
 template <int DT, bool SHARED>
 hipError_t run_tiles(ScaledGemmArgs a, bool is_direct, Plan p, const ColumnSums& sums, int kind, hipStream_t s) {
     GemmArgs& g = a.g;
