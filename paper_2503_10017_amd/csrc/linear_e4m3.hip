@@ -66,12 +66,12 @@ constexpr int FEW_WAVES = 8;
 // its runs of TURNS blocks before it multiplies the first.  The shares are joined in LDS in the order of the waves.  1 x 1024 -> 4096 bf16 with GELU (4.2 MB): 4.4-4.8 us, most of it a launch
 // and one latency of memory.
 template <int DT, int BLOCKS>
-__global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_e4m3_kernel(ScaledGemmArgs s) {
+__global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_e4m3_kernel(ScaledGemmArgs s, uint32_t first_group) {
     constexpr int TURNS = 2;
     __shared__ f32x4 shares[FEW_WAVES][BLOCKS][64];
     const GemmArgs& a = s.g;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t n0 = (int64_t)(first_group + blockIdx.x) * 16;
     const uint8_t* row_b = (const uint8_t*)a.b + min(n0 + r, (int64_t)a.n - 1) * a.ldb;
     const uint8_t* row_a[BLOCKS];
     const float* scale_a[BLOCKS];
@@ -790,8 +790,11 @@ hipError_t copy_operands(GemmArgs& g, char* room, int kind, hipStream_t s) {
 
 template <int DT>
 hipError_t run_few_rows(const ScaledGemmArgs& a, int kind, hipStream_t s) {
-    const dim3 grid((unsigned)((a.g.n + 15) / 16)), block(FEW_WAVES * 64);
-    return a.g.m <= 16 ? launch_detail(kind, 16, few_rows_e4m3_kernel<DT, 1>, grid, block, 0, s, a) : launch_detail(kind, 32, few_rows_e4m3_kernel<DT, 2>, grid, block, 0, s, a);
+    constexpr int THREADS = FEW_WAVES * 64;
+    return in_launches(((int64_t)a.g.n + 15) / 16, THREADS, [&](uint32_t first, dim3 grid) {
+        return a.g.m <= 16 ? launch_detail(kind, 16, few_rows_e4m3_kernel<DT, 1>, grid, dim3(THREADS), 0, s, a, first)
+                           : launch_detail(kind, 32, few_rows_e4m3_kernel<DT, 2>, grid, dim3(THREADS), 0, s, a, first);
+    });
 }
 
 template <typename F>

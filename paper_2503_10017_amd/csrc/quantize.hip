@@ -254,17 +254,6 @@ __global__ __launch_bounds__(TILE_THREADS) void gradient_operands_kernel(Gradien
     else transpose_tile(a.w, tile - a.tiles_q - a.tiles_x, room.codes);
 }
 
-// A launch has fewer than 2^32 threads: long narrow matrices take several.  f(first, grid)
-template <typename F>
-hipError_t in_launches(int64_t groups, F f) {
-    constexpr int64_t MOST = 1 << 22;
-    for (int64_t first = 0; first < groups; first += MOST) {
-        const hipError_t e = f((uint32_t)first, dim3((unsigned)(groups - first < MOST ? groups - first : MOST)));
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
-}
-
 template <typename F>
 hipError_t with_type(int dtype, F f) {
     if (dtype == FNN_F32) return f(std::integral_constant<int, CT_F32>());
@@ -280,7 +269,7 @@ hipError_t launch_quantize_rows(const void* x, int64_t x_stride, int64_t n, int3
         constexpr int per = 256 * Elem<dt.value>::N / SCALED_BLOCK;
         const int64_t blocks = scaled_blocks(d), groups = (n * blocks + per - 1) / per;
         if (n * blocks > (int64_t)UINT32_MAX - per) return hipErrorInvalidValue;  // blocks are counted in 32 bits: no memory holds so many
-        return in_launches(groups, [&](uint32_t first, dim3 grid) {
+        return in_launches(groups, 256, [&](uint32_t first, dim3 grid) {
             return launch(kind, quantize_rows_kernel<dt.value>, grid, dim3(256), 0, s, x, x_stride, n, d, (uint32_t)blocks, first, out);
         });
     });
@@ -291,7 +280,7 @@ hipError_t launch_quantize_tiles(const QuantizeArgs& a, bool tiles, int dtype, i
     const int64_t count = scaled_blocks(a.n) * scaled_blocks(a.d);
     if (count > INT32_MAX) return hipErrorInvalidValue;
     return with_type(dtype, [&](auto dt) {
-        return in_launches(count, [&](uint32_t first, dim3 grid) {
+        return in_launches(count, TILE_THREADS, [&](uint32_t first, dim3 grid) {
             return launch(kind, tiles ? quantize_tile_kernel<dt.value, true> : quantize_tile_kernel<dt.value, false>, grid, dim3(TILE_THREADS), 0, s, a, first);
         });
     });
@@ -305,7 +294,7 @@ hipError_t launch_gradient_operands(GradientOperands a, int dtype, int kind, hip
     a.tiles_q = (uint32_t)q;
     a.tiles_x = (uint32_t)x;
     return with_type(dtype, [&](auto dt) {
-        return in_launches(count, [&](uint32_t first, dim3 grid) {
+        return in_launches(count, TILE_THREADS, [&](uint32_t first, dim3 grid) {
             a.first = first;
             return launch(kind, gradient_operands_kernel<dt.value>, grid, dim3(TILE_THREADS), 0, s, a);
         });

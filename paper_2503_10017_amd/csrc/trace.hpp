@@ -63,5 +63,16 @@ template <typename Kernel, typename... Args>
 inline hipError_t launch(int kind, Kernel kernel, dim3 grid, dim3 block, size_t lds_bytes, hipStream_t s, Args... args) {
     return launch_detail(kind, 0, kernel, grid, block, lds_bytes, s, args...);
 }
+// Calls f(first, grid) for one launch after the other of `groups` workgroups of `threads` threads: a launch has fewer than 2^32 threads, and one that is asked for more leaves workgroups out without
+// an error.
+template <typename F>
+inline hipError_t in_launches(int64_t groups, int threads, F f) {
+    const int64_t most = ((int64_t)1 << 30) / threads;
+    for (int64_t first = 0; first < groups; first += most) {
+        const hipError_t e = f((uint32_t)first, dim3((unsigned)(groups - first < most ? groups - first : most)));
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 }  // namespace fnn

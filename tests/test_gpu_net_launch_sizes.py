@@ -1,0 +1,29 @@
+"""Sizes at which one launch has no room for all workgroups (a launch has fewer than 2^32 threads)."""
+import pytest
+import torch
+
+import paper_2503_10017_amd as fnn
+from net_helpers import DEV
+
+pytestmark = pytest.mark.gpu
+
+OUTER = 2 ** 27 + 40      # 16 results to a workgroup of 512 threads: 2^32 threads at 2^27
+
+
+def whole(shape, most, dtype):
+    """Whole numbers up to `most` in size; made on the device, the same every time."""
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    return torch.randint(-most, most + 1, shape, generator=gen, device=DEV, dtype=torch.int8).to(dtype)
+
+
+def codes(v, tiles):
+    n = -(-v.shape[0] // 128) if tiles else v.shape[0]
+    return fnn.FnnScaled(v.to(torch.float8_e4m3fn), torch.ones((-(-v.shape[1] // 128), n), device=DEV).t())
+
+
+@pytest.mark.parametrize("rows", [1, 17])
+def test_few_rows_over_many_columns(rows):
+    w, x = whole((OUTER, 16), 2, torch.bfloat16), whole((rows, 16), 2, torch.bfloat16)
+    y = fnn.fnn_linear_e4m3(codes(x, False), codes(w, True))[0]
+    for i in range(rows):
+        assert torch.equal(y[i], (w * x[i]).sum(1))      # sums below 65: exact
