@@ -124,11 +124,11 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, int64_t strip) 
 // The sums of columns over the shares that other launches left: 32 columns a workgroup, 32 threads over the shares of each, added in one fixed order, so that a
 // gradient has the same bits every time.  768 shares of 2048 columns (6.3 MB): 4.5 us, of which 3.5 are a launch.
 template <int WT>
-__global__ __launch_bounds__(1024) void column_sums_kernel(const float* partial, int64_t groups, int64_t width, int64_t first, void* out, void* more) {
+__global__ __launch_bounds__(1024) void column_sums_kernel(const float* partial, int64_t groups, int64_t width, int64_t first, void* out, void* more, uint32_t first_group) {
     typedef typename Elem<WT>::T W;
     __shared__ float part[32][33];
     const int strand = threadIdx.x >> 5;
-    const int64_t column = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
+    const int64_t column = (int64_t)(first_group + blockIdx.x) * 32 + (threadIdx.x & 31);
     float sum = 0.f;
     if (column < width) {
 #pragma unroll 8
@@ -279,7 +279,9 @@ hipError_t launch_slope(const SlopeArgs& a, int dtype, hipStream_t s) {
 
 hipError_t launch_column_sums(const float* partial, int64_t groups, int64_t width, int64_t first, void* out, void* more, int dtype, int kind, hipStream_t s) {
     return with_type(dtype, [&](auto dt) {
-        return launch(kind, column_sums_kernel<dt.value>, dim3((unsigned)((width + 31) / 32)), dim3(1024), 0, s, partial, groups, width, first, out, more);
+        return in_launches((width + 31) / 32, 1024, [&](uint32_t first_group, dim3 grid) {
+            return launch(kind, column_sums_kernel<dt.value>, grid, dim3(1024), 0, s, partial, groups, width, first, out, more, first_group);
+        });
     });
 }
 

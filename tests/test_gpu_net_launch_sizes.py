@@ -7,7 +7,7 @@ from net_helpers import DEV
 
 pytestmark = pytest.mark.gpu
 
-OUTER = 2 ** 27 + 40      # 16 results to a workgroup of 512 threads: 2^32 threads at 2^27
+OUTER = 2 ** 27 + 40      # 16 results to a workgroup of 512 threads, 32 columns to one of 1024: 2^32 threads at 2^27
 
 
 def whole(shape, most, dtype):
@@ -27,3 +27,15 @@ def test_few_rows_over_many_columns(rows):
     y = fnn.fnn_linear_e4m3(codes(x, False), codes(w, True))[0]
     for i in range(rows):
         assert torch.equal(y[i], (w * x[i]).sum(1))      # sums below 65: exact
+
+
+def test_the_bias_gradient_of_many_columns():
+    dy = whole((1, OUTER), 2, torch.bfloat16) * 3.5       # codes and scales of these are exact: a block's largest is 448 times a power of two
+    x, w = whole((1, 16), 2, torch.bfloat16) * 1.75, whole((OUTER, 16), 2, torch.bfloat16)
+    dx, dw, dbias = fnn.fnn_linear_e4m3_backward(dy, x, codes(w, True))
+    assert torch.equal(dbias, dy[0])
+    assert torch.equal(dw, dy.t() * x)                    # 49 / 8 times 0, 1, 2 or 4
+    want = sum((dy[0, i:i + 2 ** 24, None].double() * w[i:i + 2 ** 24]).sum(0) for i in range(0, OUTER, 2 ** 24))
+    assert torch.equal(dx[0], want.bfloat16())            # multiples of 3.5, far fewer than 2^24 of them
+    del dw
+    assert torch.equal(fnn.fnn_linear_backward(dy, x, w, want_x=False, want_w=False)[2], dy[0])
