@@ -755,8 +755,8 @@ struct CopyCodes {
     int64_t stride;
     int32_t width;
 };
-__global__ __launch_bounds__(256) void copy_codes_kernel(CopyCodes a) {
-    const int64_t runs = a.stride / 16, at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / runs;
+__global__ __launch_bounds__(256) void copy_codes_kernel(CopyCodes a, uint32_t first_group) {
+    const int64_t runs = a.stride / 16, at = (int64_t)(first_group + blockIdx.x) * 256 + threadIdx.x, row = at / runs;
     const int e = (int)(at - row * runs) * 16, which = row >= a.rows[0];
     const int64_t of = which ? row - a.rows[0] : row;
     if (of >= a.rows[which]) return;
@@ -784,8 +784,8 @@ hipError_t copy_operands(GemmArgs& g, char* room, int kind, hipStream_t s) {
     }
     if (rows == 0) return hipSuccess;
     const int64_t groups = (rows * (c.stride / 16) + 255) / 256;
-    if (groups > INT32_MAX) return hipErrorInvalidValue;
-    return launch(kind, copy_codes_kernel, dim3((unsigned)groups), dim3(256), 0, s, c);
+    if (groups > INT32_MAX) return hipErrorInvalidValue;  // 8 TB
+    return in_launches(groups, 256, [&](uint32_t first, dim3 grid) { return launch(kind, copy_codes_kernel, grid, dim3(256), 0, s, c, first); });
 }
 
 template <int DT>

@@ -1,4 +1,6 @@
 """Sizes at which one launch has no room for all workgroups (a launch has fewer than 2^32 threads)."""
+import gc
+
 import pytest
 import torch
 
@@ -39,3 +41,25 @@ def test_the_bias_gradient_of_many_columns():
     assert torch.equal(dx[0], want.bfloat16())            # multiples of 3.5, far fewer than 2^24 of them
     del dw
     assert torch.equal(fnn.fnn_linear_backward(dy, x, w, want_x=False, want_w=False)[2], dy[0])
+
+
+def test_copies_of_many_rows():
+    """Rows of 33 codes copied to 16-byte boundaries: three runs of 16 bytes each, of which 2^32 are 64 GB."""
+    rows, inner = 1440 * 10 ** 6, 33
+    gc.collect()
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("needs 130 GB")
+    data = torch.zeros((rows, inner), dtype=torch.uint8, device=DEV).view(torch.float8_e4m3fn)
+    scale = torch.ones((1, rows), device=DEV).t()
+    every = 2 ** 20 - 3                                   # these rows hold something, the first and the last among them
+    some = torch.cat([torch.arange(0, rows, every), torch.tensor([rows - 1])]).to(DEV)
+    v, w = whole((len(some), inner), 2, torch.bfloat16), whole((1, inner), 2, torch.bfloat16)
+    data.view(torch.uint8)[some] = v.to(torch.float8_e4m3fn).view(torch.uint8)
+    y = fnn.fnn_linear_e4m3(fnn.FnnScaled(data, scale), codes(w, True))[0]
+    assert torch.equal(y[some], (v * w).sum(1, keepdim=True))
+    y[some] = 0
+    assert not y.any()
+    del data, scale, y
+    gc.collect()
+    torch.cuda.empty_cache()
