@@ -117,10 +117,11 @@ __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a
         float rstd, of_v;
         if (sum < 0x1p126f && (sum > 0x1p-100f || a.eps > 0x1p-90f)) of_v = rstd = 1.f / sqrtf(sum / (float)a.d + a.eps);
         else rstd = rare_rstd<LANES>(v, sum, a.d, a.eps, slots[turn], of_v);
+        // in this order: s r is at most sqrt(d) in size, while r w leaves fp32's range for weights and rows far from 1
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-            for (int e = 0; e < N; ++e) v[c][e] *= of_v * w[c][e];
+            for (int e = 0; e < N; ++e) v[c][e] = v[c][e] * of_v * w[c][e];
         if (a.y) {
             T* y = (T*)a.y + row * a.y_stride;
 #pragma unroll
