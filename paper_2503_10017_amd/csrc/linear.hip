@@ -18,12 +18,12 @@ constexpr int FEW_WAVES = 8;
 // lane asks for all of its runs of four turns before it multiplies the first; a (its rows are few) comes out of the L2.  The shares are
 // joined in LDS in the order of the waves.  1 x 1024 -> 4096 bf16: 4.4 us, 1.9 TB/s of 8.4 MB; a launch that does nothing is about 3.5 of it.
 template <int DT, int BLOCKS>
-__global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(GemmArgs a) {
+__global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_kernel(GemmArgs a, uint32_t first_group) {
     typedef typename Elem<DT>::T E;
     constexpr int N = Elem<DT>::N, STEP = 4 * N, TURNS = 4;
     __shared__ f32x4 shares[FEW_WAVES][BLOCKS][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t n0 = (int64_t)(first_group + blockIdx.x) * 16;
     const E* row_b = (const E*)a.b + min(n0 + r, (int64_t)a.n - 1) * a.ldb;
     const E* row_a[BLOCKS];
 #pragma unroll
@@ -212,10 +212,12 @@ hipError_t run_gemm(GemmArgs a, bool is_direct, const Plan& p, int kind, hipStre
 
 template <int DT>
 hipError_t run_few_rows(const GemmArgs& a, int kind, hipStream_t s) {
-    const dim3 grid((unsigned)((a.n + 15) / 16)), block(FEW_WAVES * 64);
-    if (a.m <= 16) return launch(kind, few_rows_kernel<DT, 1>, grid, block, 0, s, a);
-    if (a.m <= 32) return launch(kind, few_rows_kernel<DT, 2>, grid, block, 0, s, a);
-    return launch(kind, few_rows_kernel<DT, 4>, grid, block, 0, s, a);
+    constexpr int THREADS = FEW_WAVES * 64;
+    return in_launches(((int64_t)a.n + 15) / 16, THREADS, [&](uint32_t first, dim3 grid) {
+        if (a.m <= 16) return launch(kind, few_rows_kernel<DT, 1>, grid, dim3(THREADS), 0, s, a, first);
+        if (a.m <= 32) return launch(kind, few_rows_kernel<DT, 2>, grid, dim3(THREADS), 0, s, a, first);
+        return launch(kind, few_rows_kernel<DT, 4>, grid, dim3(THREADS), 0, s, a, first);
+    });
 }
 
 template <typename F>

@@ -31,6 +31,14 @@ def test_few_rows_over_many_columns(rows):
         assert torch.equal(y[i], (w * x[i]).sum(1))      # sums below 65: exact
 
 
+@pytest.mark.parametrize("rows", [1, 17])
+def test_few_rows_over_many_columns_in_16_bits(rows):
+    w, x = whole((OUTER, 16), 2, torch.float16), whole((rows, 16), 2, torch.float16)
+    y = fnn.fnn_linear(x, w)[0]
+    for i in range(rows):
+        assert torch.equal(y[i], (w * x[i]).sum(1))
+
+
 def test_the_bias_gradient_of_many_columns():
     dy = whole((1, OUTER), 2, torch.bfloat16) * 3.5       # codes and scales of these are exact: a block's largest is 448 times a power of two
     x, w = whole((1, 16), 2, torch.bfloat16) * 1.75, whole((OUTER, 16), 2, torch.bfloat16)
