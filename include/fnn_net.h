@@ -23,6 +23,8 @@
  *    rows on 16-byte boundaries are faster.  A matrix of no elements needs no pointer.  Elements between the rows are neither read for
  *    their value nor written.  All matrices of a call have one dtype, unless said otherwise.
  *  - Outputs must not overlap inputs or each other; the exceptions are named.
+ *  - A call that would need more workgroups than one launch takes ends in FNN_E_HIP (some 2^24: attention and its gradient where sequences, or
+ *    tiles of 32 or 128 rows or keys, times key heads come to that; fnn_linear with 2^31 - 128 rows or 64 GB of copied operands).
  *  - Results do not depend on the order in which workgroups run: the same call gives the same bits.
  *  - Sums, products, statistics and activations are fp32; outputs are rounded once, to nearest even, to their type.  Infinities and NaN in the inputs
  *    reach the outputs that depend on them, and no others.

@@ -48,9 +48,14 @@ enum TraceKind : int {
 // `detail` is a number the launcher wants reported with the kernel (the launch shape it chose).
 bool trace_next(int kind, int detail, hipEvent_t* start, hipEvent_t* stop);
 
+// A launch has fewer than 2^32 threads in each direction; the runtime takes one of more and leaves workgroups out without an error.
+inline bool launch_fits(dim3 grid, dim3 block) {
+    return (uint64_t)grid.x * block.x <= UINT32_MAX && (uint64_t)grid.y * block.y <= UINT32_MAX && (uint64_t)grid.z * block.z <= UINT32_MAX;
+}
 template <typename Kernel, typename... Args>
 inline hipError_t launch_detail(int kind, int detail, Kernel kernel, dim3 grid, dim3 block, size_t lds_bytes,
                                 hipStream_t s, Args... args) {
+    if (!launch_fits(grid, block)) return hipErrorInvalidConfiguration;
     hipEvent_t e0, e1;
     if (trace_next(kind, detail, &e0, &e1)) {
         hipExtLaunchKernelGGL(kernel, grid, block, lds_bytes, s, e0, e1, 0, args...);
@@ -63,8 +68,7 @@ template <typename Kernel, typename... Args>
 inline hipError_t launch(int kind, Kernel kernel, dim3 grid, dim3 block, size_t lds_bytes, hipStream_t s, Args... args) {
     return launch_detail(kind, 0, kernel, grid, block, lds_bytes, s, args...);
 }
-// Calls f(first, grid) for one launch after the other of `groups` workgroups of `threads` threads: a launch has fewer than 2^32 threads, and one that is asked for more leaves workgroups out without
-// an error.
+// Calls f(first, grid) for one launch after the other of `groups` workgroups of `threads` threads, none of which has too many.
 template <typename F>
 inline hipError_t in_launches(int64_t groups, int threads, F f) {
     const int64_t most = ((int64_t)1 << 30) / threads;

@@ -39,6 +39,25 @@ def test_few_rows_over_many_columns_in_16_bits(rows):
         assert torch.equal(y[i], (w * x[i]).sum(1))
 
 
+def test_a_launch_of_too_many_workgroups_is_refused():
+    """A workgroup of 256 threads for each of 2^24 sequences and more: an error instead of rows that nothing has written."""
+    batch = 2 ** 24 + 100
+    q = torch.zeros((batch, 1, 8), dtype=torch.float16, device=DEV)
+    starts = torch.arange(batch + 1, dtype=torch.int32, device=DEV)
+    with pytest.raises(fnn.FnnError):
+        fnn.fnn_attention(q, q, q, starts, starts)
+    with pytest.raises(fnn.FnnError):
+        fnn.fnn_attention_backward(q, q, q, q, q, torch.zeros((batch, 1), device=DEV), starts, starts)
+
+
+def test_as_many_rows_as_a_matrix_may_have():
+    rows = 2 ** 31 - 65
+    data, scale = torch.zeros((rows, 16), dtype=torch.uint8, device=DEV), torch.ones((1, rows), device=DEV).t()
+    data[-5:, 3] = 0x38                                   # 1
+    y = fnn.fnn_linear_e4m3(fnn.FnnScaled(data.view(torch.float8_e4m3fn), scale), codes(torch.ones((1, 16), device=DEV), True))[0]
+    assert (y[-5:] == 1).all() and not y[:-5].any()
+
+
 def test_the_bias_gradient_of_many_columns():
     dy = whole((1, OUTER), 2, torch.bfloat16) * 3.5       # codes and scales of these are exact: a block's largest is 448 times a power of two
     x, w = whole((1, 16), 2, torch.bfloat16) * 1.75, whole((OUTER, 16), 2, torch.bfloat16)
