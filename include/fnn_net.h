@@ -197,7 +197,7 @@ int32_t fnn_rms_norm_backward(const fnn_map* dy, const fnn_map* sum, const float
  * fnn_linear of operands in 8 bits: p = x w^T + bias, y = act(p) + residual for x [rows][inner], w [outer][inner], y, pre and residual [rows][outer] and bias
  * [outer], the latter four of one dtype, which may be any.  The products of a block of 128 are summed first, then multiplied by the product of the two scales (fp32, so this has to be a number that
  * fp32 has), and added to the fp32 sum over the blocks.  16-bit results take the matrix instructions for 8 bits, which cut each of eight products at 2^-13 of the largest of the eight before they
- * add them: an error of some 10^-5 of the sum's size, below what the result is rounded by.  FNN_F32 results take exact products and fp32 sums, at half the rate or less.
+ * add them: an error of some 10^-5 of the sum's size (where the terms cancel: of theirs), below what the result is rounded by.  FNN_F32 results take exact products and fp32 sums, at half the rate or less.
  * The workspace is for few tiles with a long `inner`, whose products are split and joined in a fixed order, and for aligned copies of operands with an `inner` that is no multiple of 16;
  * fnn_linear_e4m3_workspace_bytes may return 0, and returns 0 for invalid sizes.  dtype: that of y.  y may be the residual itself (same rows).
  * Errors: FNN_E_NULL, FNN_E_SHAPE, FNN_E_DTYPE, FNN_E_RANGE (act), FNN_E_WORKSPACE.
@@ -210,8 +210,9 @@ int32_t fnn_linear_e4m3(const fnn_scaled* x, const fnn_scaled* w, const void* bi
  * The gradient of that layer, in 8 bits too, from dy, x as it was before its quantising, the layer's w (block_rows == 128: its transpose has the same codes and scales) and pre.  With
  * q = dy * act'(pre) (act == FNN_ACT_NONE: q = dy, and pre is not looked at) and Q(.) a matrix as fnn_quantize gives it, a scale for each block of 128 of a row:
  *   dx = Q(q) w,  dw = Q(q^T) Q(x^T)^T,  dbias = sum over the rows of q
- * dy, x, pre, dx, dw and dbias are of one dtype, dx [rows][inner], dw [outer][inner] and dbias [outer] may each be NULL: not wanted.  q is quantised, and summed, as it is in fp32.  The residual's
- * gradient is dy itself.  Products as in fnn_linear_e4m3.
+ * dy, x, pre, dx, dw and dbias are of one dtype, dx [rows][inner], dw [outer][inner] and dbias [outer] may each be NULL: not wanted.  q is quantised, and summed, as it is in fp32.  With
+ * GELU and SiLU q is off by what their slopes are (16-bit types: up to 4e-6 of dy), and in 16-bit types its quotient by the scale may be off by another two units in fp32's last place: a code
+ * next to the border of two may be its neighbour there.  All other codes are fnn_quantize's to the bit.  The residual's gradient is dy itself.  Products as in fnn_linear_e4m3.
  */
 size_t fnn_linear_e4m3_backward_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype);
 int32_t fnn_linear_e4m3_backward(const fnn_map* dy, const fnn_map* x, const fnn_scaled* w, const fnn_map* pre, int32_t act,

@@ -136,3 +136,18 @@ def test_infinities_in_pre(act, kind):
     assert torch.isnan(got[0][~r]).all() and torch.equal(got[0][r], clean[0][r])
     assert torch.isnan(got[1][~c]).all() and torch.equal(got[1][c], clean[1][c])
     assert torch.isnan(got[2][~c]).all() and torch.equal(got[2][c], clean[2][c])
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("m,k,n", [(6, 264, 300), (200, 264, 300), (531, 777, 401), (100, 70, 9000), (3000, 2100, 2300), (6000, 1700, 2900)])
+def test_gradient_is_made_of_the_other_operators(m, k, n, act, kind):
+    """Without an activation, or with one whose slope is 0 or 1, q is not rounded on the way: its codes are those of fnn_quantize, and the products those of fnn_linear_e4m3, to the bit."""
+    dtype = TYPES[kind]
+    x, dy, pre = normal(1, m, k, dtype=dtype), normal(3, m, n, dtype=dtype), normal(4, m, n, dtype=dtype)
+    w = scaled_of(normal(2, n, k, std=1 / math.sqrt(k)), tiles=True)
+    dx, dw, _ = fnn.fnn_linear_e4m3_backward(dy, x, w, None if act == "none" else pre, act=act)
+    q = dy if act == "none" else torch.where(pre > 0, dy, torch.zeros_like(dy))
+    across = fnn.FnnScaled(w.data.view(torch.uint8).t().contiguous().view(torch.float8_e4m3fn), w.scale.t())
+    assert torch.equal(dx, fnn.fnn_linear_e4m3(fnn.fnn_quantize(q), across, dtype=dtype)[0])
+    assert torch.equal(dw, fnn.fnn_linear_e4m3(fnn.fnn_quantize(q, transposed=True), fnn.fnn_quantize(x, transposed=True), dtype=dtype)[0])
