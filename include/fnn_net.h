@@ -149,7 +149,7 @@ int32_t fnn_attention_backward(const fnn_heads* dout, const fnn_heads* q, const 
  * bytes apart, and an fp32 scale for each block of FNN_SCALED_BLOCK columns, of one row (block_rows == 1) or of a tile of 128 rows (block_rows == 128):
  *   element (r, k) = e4m3(data[r * row_stride + k]) * scale[(r / block_rows) * scale_row + (k / 128) * scale_block]
  * The last block of a row, and the last tile of rows, may be short.  scale_row and scale_block may have any values of at least 1; scales of one column of blocks next to each
- * other (scale_row == 1) and rows of codes on 16-byte boundaries are faster.  The strides of what there is one of are not looked at.
+ * other (scale_row == 1) and rows of codes on 16-byte boundaries are faster.  The strides of what there is one of, or none, are not looked at.
  */
 #define FNN_SCALED_BLOCK 128
 typedef struct {

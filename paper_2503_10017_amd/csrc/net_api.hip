@@ -161,22 +161,22 @@ int32_t attention_args(const fnn_heads* q, const fnn_heads* k, const fnn_heads* 
     return FNN_OK;
 }
 
-// Shape, then pointers, of a matrix in 8 bits; the strides of what there is one of are not looked at.
+// Shape, then pointers, of a matrix in 8 bits; the strides of what there is one of, and those of no scales, are not looked at.
 int32_t check_scaled(const fnn_scaled* m) {
     if (!m) return FNN_E_NULL;
     // columns are counted in 32 bits, up to the end of a block
     if (m->n < 0 || m->n > MAX_SLOTS || m->d < 0 || m->d > MAX_SLOTS || (m->block_rows != 1 && m->block_rows != SCALED_BLOCK)) return FNN_E_SHAPE;
     const int64_t high = m->block_rows == 1 ? m->n : scaled_blocks(m->n), blocks = scaled_blocks(m->d);
     if (m->n > 1 && (m->row_stride < m->d || m->row_stride > INT64_MAX / 8 / m->n)) return FNN_E_SHAPE;
-    if (high > 1 && (m->scale_row < 1 || m->scale_row > INT64_MAX / 16 / high)) return FNN_E_SHAPE;
-    if (blocks > 1 && (m->scale_block < 1 || m->scale_block > INT64_MAX / 16 / blocks)) return FNN_E_SHAPE;
+    if (high > 1 && blocks > 0 && (m->scale_row < 1 || m->scale_row > INT64_MAX / 16 / high)) return FNN_E_SHAPE;
+    if (blocks > 1 && high > 0 && (m->scale_block < 1 || m->scale_block > INT64_MAX / 16 / blocks)) return FNN_E_SHAPE;
     if (m->n > 0 && m->d > 0 && (!m->data || !m->scale)) return FNN_E_NULL;
     return FNN_OK;
 }
 int64_t stride_of(const fnn_scaled* m) { return m->n > 1 ? m->row_stride : m->d; }
 // A stride that is not looked at is 0: a product reads the scale of the first row, or block, in place of those behind the last.
-int64_t scale_row_of(const fnn_scaled* m) { return (m->block_rows == 1 ? m->n : scaled_blocks(m->n)) > 1 ? m->scale_row : 0; }
-int64_t scale_block_of(const fnn_scaled* m) { return m->d > SCALED_BLOCK ? m->scale_block : 0; }
+int64_t scale_row_of(const fnn_scaled* m) { return m->d > 0 && (m->block_rows == 1 ? m->n : scaled_blocks(m->n)) > 1 ? m->scale_row : 0; }
+int64_t scale_block_of(const fnn_scaled* m) { return m->n > 0 && m->d > SCALED_BLOCK ? m->scale_block : 0; }
 CodesOut codes_of(const fnn_scaled* m) {
     return {(uint8_t*)const_cast<void*>(m->data), const_cast<float*>(m->scale), stride_of(m), scale_row_of(m), scale_block_of(m)};
 }

@@ -151,3 +151,22 @@ def test_gradient_is_made_of_the_other_operators(m, k, n, act, kind):
     across = fnn.FnnScaled(w.data.view(torch.uint8).t().contiguous().view(torch.float8_e4m3fn), w.scale.t())
     assert torch.equal(dx, fnn.fnn_linear_e4m3(fnn.fnn_quantize(q), across, dtype=dtype)[0])
     assert torch.equal(dw, fnn.fnn_linear_e4m3(fnn.fnn_quantize(q, transposed=True), fnn.fnn_quantize(x, transposed=True), dtype=dtype)[0])
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16"])
+def test_sums_of_nothing_in_tiles(kind):
+    """No rows, no outputs or no inputs, with the other sizes beyond few rows: zeros where something is asked for, whatever the memory held."""
+    def zeros(*s):
+        return torch.zeros(s, device=DEV, dtype=TYPES[kind])
+
+    def weights(n, k):
+        return fnn.fnn_quantize(zeros(n, k), tiles=True)
+
+    for act in ("none", "gelu"):
+        dx, dw, dbias = fnn.fnn_linear_e4m3_backward(zeros(0, 300), zeros(0, 264), weights(300, 264), zeros(0, 300), act=act)
+        assert dx.shape == (0, 264) and dw.shape == (300, 264) and not dw.any() and dbias.shape == (300,) and not dbias.any()
+        out = torch.full((300, 264), 7.0, device=DEV, dtype=TYPES[kind])
+        dx, dw, dbias = fnn.fnn_linear_e4m3_backward(zeros(300, 0), zeros(300, 264), weights(0, 264), zeros(300, 0), act=act, out=out)
+        assert dx is out and not out.any() and dw.shape == (0, 264) and dbias.shape == (0,)
+        dx, dw, dbias = fnn.fnn_linear_e4m3_backward(zeros(300, 264) + 1, zeros(300, 0), weights(264, 0), zeros(300, 264), act=act)
+        assert dx.shape == (300, 0) and dw.shape == (264, 0) and (dbias == (300 if act == "none" else 150)).all()
