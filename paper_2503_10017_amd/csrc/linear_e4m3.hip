@@ -63,8 +63,8 @@ bool few_rows(int64_t m, int64_t k) { return m <= 16 || (m <= 32 && m * k <= 983
 constexpr int FEW_WAVES = 8;
 
 // Few rows of a: the time is that of reading b once.  A workgroup takes 16 rows of b, its waves share the blocks of k between them, and a lane asks for all of
-// its runs of TURNS blocks before it multiplies the first.  The shares are joined in LDS in the order of the waves.  1 x 1024 -> 4096 bf16 with GELU (4.2 MB): 4.4-4.8 us, most of it a launch
-// and one latency of memory.
+// its runs of TURNS blocks before it multiplies the first, but for the partial run of a row whose length is no multiple of 16, whose codes come one by one (load_run).  The shares are joined in LDS in
+// the order of the waves.  1 x 1024 -> 4096 bf16 (4.2 MB): 4.1 us, with GELU 4.2-4.9, most of it a launch and one latency of memory; 1 x 1023 -> 4096 5.2.
 template <int DT, int BLOCKS>
 __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_e4m3_kernel(ScaledGemmArgs s, uint32_t first_group) {
     constexpr int TURNS = 2;
@@ -135,7 +135,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void few_rows_e4m3_kernel(ScaledGem
 
 // ---- tiles ----
 
-// finish_run of fewer than eight results, one after the other: there is one such place in a row at most, and in line they would be most of the kernel's code.
+// finish_run of fewer than eight results, one after the other: there is one such place in a row at most, and in line they would be most of the kernel's code.  Each result waits for its bias, its residual
+// and the store before it, which shows in large tiles: 24576 x 1024 -> 4095 bf16 194 us, with bias and residual 332, where 4096 columns take 122 and 200; 1531 x 777 -> 1007 fp32 with residual 16.9, 1008 13.0.
 template <int DT>
 __device__ __forceinline__ void finish_few(const GemmArgs& a, int64_t m, int n, int count, float (&v)[8]) {
     typedef typename Elem<DT>::T E;
@@ -184,10 +185,12 @@ __device__ __forceinline__ void ask_pieces(F f) {
 // waves meet, then it reads that step's first operands beside these products and asks for the step after, of the next tile where this one ends; so neither the meeting nor a tile's end stops
 // the products for long.  SHARED: a wave's columns have one scale a step (weights in tiles).
 //
-// What bounds it is the number of instructions: a wave issues one in four cycles, and 32 products a step come with 128 multiply-adds of their results, 24 reads of LDS and 18 loads.  bf16 results in tiles
-// of 256 x 256: 1.6 us a step with two waves a SIMD (2.7 PFLOP/s on 256 compute units), 6 us a tile's end, 12 with GELU.  24576 x 4096 -> 6144 553 us (2.24 PFLOP/s; a library product with
-// one scale for everything 2.93), 24576 x 1024 -> 4096 with GELU 171 (38 of them GELU).  Tiles of 128 x 128: 708 and 197; products of 32 x 32 x 64 instead of 16 x 16 x 128: 2 to 5 % longer; one
-// workgroup a tile, with scales loaded where they are used: 3261 (first form), staged 591, as one sequence of steps 531 to 566.
+// What bounds it is the issue of instructions, and power: a wave issues one in four cycles, and 32 products a step come with 128 multiply-adds of their results, 24 reads of LDS and 18 loads.  At
+// 24576 x 4096 -> 6144 bf16 an instruction is issued in 69 to 74 % of the slots, the matrix cores are busy 53 % of the cycles and LDS 24 %, without conflicts, at 2.0 of 2.6 GHz.  Tiles of 256 x 256 take
+// 1.6 us a step with two waves a SIMD (2.7 PFLOP/s on 256 compute units), 6 us a tile's end, 12 with GELU.  24576 x 4096 -> 6144 520 to 550 us one call after the other (2.3 PFLOP/s; a library
+// product with one scale for everything 2.93), 540 to 630 with the card idle before it; 24576 x 1024 -> 4096 122, with GELU 156 to 165 (170 to 190); fp32 results, in tiles of 128, 1148 and 234.  Tiles of
+// 128 x 128 for bf16: 708 and, with GELU, 197; products of 32 x 32 x 64 instead of 16 x 16 x 128: 2 to 5 % longer; one workgroup a tile, with scales loaded where they are used: 3261 (first form),
+// staged 591, as one sequence of steps 531 to 566.
 template <int DT, int TM, int TN, int WAVES_M, int WAVES_N, bool SHARED, bool DIRECT>
 __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 64)) void gemm_e4m3_kernel(ScaledGemmArgs s) {
     constexpr int THREADS = WAVES_M * WAVES_N * 64, BM = TM / WAVES_M / 16, BN = TN / WAVES_N / 16, SCALES = (TM + TN) / THREADS;
@@ -444,6 +447,8 @@ __global__ __launch_bounds__(WAVES_M* WAVES_N * 64, 512 / (WAVES_M * WAVES_N * 6
         asm volatile("" : "+v"(of));  // what follows from it is formed here, not before the loop and kept
         const int64_t m0 = (int64_t)tile.m * TM + a0 + (of & 7);
         const int n = tile.n * TN + b0 + 32 * ((of >> 3) & 1) + 16 * ((of >> 4) & 1) + 8 * (of >> 5);  // the first of the eight columns
+        // A run of the residual is unpacked, and so waited for, where it is loaded, since each is under a branch of its own: with bias and residual 24576 x 1024 -> 4096 bf16 takes 200 us instead of 122
+        // (39 of the difference are the residual's bytes), 24576 x 4096 -> 1024 142 instead of 124 with the bias.
         Eight<DT> bias = {}, residual[2][2] = {};
         auto fetch_residual = [&](int i) {
             if (!a.residual || !whole || a.n - n < 8) return;

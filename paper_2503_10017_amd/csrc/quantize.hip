@@ -11,7 +11,7 @@ namespace fnn {
 
 namespace {
 
-// Blocks of 128 along the rows: 16 bytes a lane, so 16 lanes (fp32: 32) a block, and a block's largest takes no LDS.  24576 x 4096 bf16 (305 MB): 57 us, 5.3 TB/s.
+// Blocks of 128 along the rows: 16 bytes a lane, so 16 lanes (fp32: 32) a block, and a block's largest takes no LDS.  24576 x 4096 bf16 (305 MB): 55-59 us, 5.2 to 5.5 TB/s.
 template <int DT>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const void* x, int64_t x_stride, int64_t n, int32_t d, uint32_t blocks, uint32_t first, CodesOut out) {
     typedef typename Elem<DT>::T T;
@@ -67,8 +67,9 @@ struct TileRoom {
 
 // A tile of 128 x 128 a workgroup, 32 values a thread: N neighbouring columns of R rows.  From it come, as wanted, codes by rows, codes across (the matrix transposed, its codes gathered in
 // LDS so that 16 of a row leave together), with TILES one scale for the whole of it, and the columns' sums.  With SLOPE the values are dy * act'(pre).  A column's scale is formed by one
-// thread, not by the 16 that use it, and the joins over rows share the workgroup's three meetings.  12289 x 1021 fp16 across (38 MB): 14-15.5 us, of which 7.3 are the bytes and the rest a launch of
-// 776 workgroups, each of which waits for its loads, joins, encodes and stores once.
+// thread, not by the 16 that use it, and the joins over rows share the workgroup's three meetings.  Inside a matrix the time is the bytes': 12288 x 1024 fp16 across (38 MB) 9.4 us, 24576 x 4096 bf16
+// (305 MB) in tiles 57 and across 56 us, fp32 (503 MB) 90 and 98.  A tile at an edge takes longer, and a launch of few generations of workgroups as long as those do: 12289 x 1024 10.9 us, and
+// 12289 x 1016 12.0, whose rows are asked for under a branch each; 12289 x 1021 14.0, whose partial runs are read element by element and waited for one after the other.
 template <int DT, bool TILES, bool SLOPE>
 __device__ __forceinline__ void quantize_tile(const QuantizeArgs& a, uint32_t tile, TileRoom& room) {
     typedef typename Elem<DT>::T T;
@@ -77,7 +78,7 @@ __device__ __forceinline__ void quantize_tile(const QuantizeArgs& a, uint32_t ti
     const uint32_t tiles_c = (uint32_t)scaled_blocks(a.d), tile_r = tile / tiles_c, tile_c = tile % tiles_c;
     const int64_t r0 = (int64_t)tile_r * SCALED_BLOCK + strand * R;
     const int c0 = (int)tile_c * SCALED_BLOCK, at = c0 + run * N, count = a.d - at;
-    // Everything is asked for before anything is used.
+    // Everything is asked for before anything is used, but for partial runs of 16 bytes (load_run).
     const bool inside = (int64_t)(tile_r + 1) * SCALED_BLOCK <= a.n && a.d - c0 >= SCALED_BLOCK;
     auto ask = [&](uint4 (&to)[R], const void* base, int64_t stride) {
         const T* from = (const T*)base + r0 * stride + at;

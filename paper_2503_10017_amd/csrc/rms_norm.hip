@@ -48,7 +48,8 @@ __device__ float rare_rstd(float (&v)[CHUNKS][N], float total, int d, float eps,
 
 // s = x + residual, r = 1 / sqrt(mean(s^2) + eps), y = s r w; the sum is rounded where it is stored, y is of the unrounded one.  Rows are divided as the layer
 // norm's are: a wave a row while its registers hold one.  24576 x 1024 bf16 with a residual, the sum stored and the norm in 8 bits (177 MB): 33-35 us, what a copy
-// takes (35-37 with loads that waited for each other); one row: 3.1-3.6 us, a launch.
+// takes (35-37 with loads that waited for each other); fp32 (328 MB) 61 us; one row: 3.1-3.6 us, a launch.  16-bit rows that end in a partial run of 16 bytes wait for its elements one after the other:
+// 24576 x 1021 bf16 50 us (fp32 64).
 template <int DT, int WT, int LANES, int CHUNKS>
 __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a) {
     constexpr int N = Elem<DT>::N, THREADS = norm_threads(LANES), ROWS = THREADS / LANES, BLOCK_LANES = SCALED_BLOCK / N;
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; row < a.n; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
         const T* x = (const T*)a.x + row * a.x_stride;
-        // everything is asked for before anything is used
+        // everything is asked for before anything is used, but for partial runs of 16 bytes (load_run)
         uint4 asked[CHUNKS], more[CHUNKS];
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
@@ -145,8 +146,8 @@ __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_kernel(RmsArgs a
 }
 
 // With g = dy w, h = s r:  dx = r (g - h mean(g h)) + dsum,  dw = sum dy h.  One pass over dy, s and dsum; in registers the columns' sums over the workgroup's
-// rows, which end as one row of `partial`.  24576 x 1024 bf16 with dsum (201 MB): 36-41 us, 5.2 TB/s, and 4.6 to join the columns' sums; 6151 x 1021 fp32, whose rows start on 4-byte
-// boundaries (75 MB): 17 us, 4.4 TB/s, and 3.9.
+// rows, which end as one row of `partial`.  24576 x 1024 bf16 with dsum (201 MB): 36-41 us, 5.2 TB/s, and 4 to 4.7 to join the columns' sums; fp32 (403 MB) 74 and 4.1.  6151 x 1021 fp32, whose rows start on 4-byte
+// boundaries (75 MB): 17 us, 4.4 TB/s, and 3.9; 6151 x 1024 16.5.  Partial runs of 16-bit types are waited for as above, and with them the row asked for ahead: 24576 x 1021 bf16 60 us.
 template <int DT, int WT, int LANES, int CHUNKS>
 __global__ __launch_bounds__(norm_threads(LANES)) void rms_norm_backward_kernel(RmsBackArgs a) {
     constexpr int N = Elem<DT>::N, THREADS = norm_threads(LANES), ROWS = THREADS / LANES;
